@@ -336,6 +336,88 @@ int hsd_gemm_bf16(const void *A, int R, int K, const void *W, int N, float *out,
 /* Synchronises `stream` and returns DEVICE_TIMEOUT if a kernel using `workspace` gave up a bounded wait. */
 int hsd_gemm_status(void *workspace, void *stream);
 
+/* ---------------------------------------------------------------------------------------
+ * Operators of one decoding step of a drafter that the caller runs (Algorithm 1's M_0, or any level below the target,
+ * outside of hsd_create): new keys and values into a paged cache, attention of one new token over it, projections with
+ * 4-bit weights, and what the tokens' probabilities were.  They chain: hsd_gemm_w4 or hsd_gemm_bf16 gives fp32 rows of q, k
+ * and v, hsd_kv_append takes them and gives queries in the cache's type, hsd_paged_attention gives what the next projection
+ * takes, and the last projection's logits go to hsd_draft_sample, hsd_verify_level and hsd_token_logprobs.  All are
+ * asynchronous on `stream`, hold no state between calls, and may be captured into graphs; calls that share a workspace, an
+ * output or pages must not overlap on the GPU.
+ *
+ * The cache: two pools of pages of page_size tokens.  A head's row of head_dim values stands at
+ * head * head_stride + page * page_stride + token in page * token_stride elements of each pool; the engine's own layout
+ * [head][page][token][head_dim] and [page][token][head][head_dim] are two of the possible orders.  Sequence b's token at
+ * position p lies in page page_table[b * pages_per_seq + p / page_size].
+ *   k, v     device, 16-byte aligned; the three strides in bytes are multiples of 16
+ *   dtype    HSD_F32 or HSD_BF16 */
+typedef struct {
+  void *k, *v;
+  int32_t dtype, n_pages, page_size;
+  int64_t head_stride, page_stride, token_stride;
+} hsd_kv_pool;
+
+/* New rows of q, k and v: rotary embedding of q and k by the row's position (half-split pairing, as the engine's;
+ * products and sum in fp32, one rounding to the pool's type), k and v into their pages, q to q_out.
+ *   qkv         device [rows, n_q_heads + 2 n_kv_heads, head_dim] (queries, keys, values), rows row_stride elements apart,
+ *               HSD_F32 or HSD_BF16, 16-byte aligned, row_stride in bytes a multiple of 16; n_q_heads may be 0
+ *   row_starts  device [batch + 1] int32, not descending: rows row_starts[b] .. row_starts[b+1]-1 are sequence b's next tokens, at
+ *               positions kv_lens[b], kv_lens[b] + 1, ...; NULL: rows == batch, row b is sequence b's one token
+ *   kv_lens     device [batch] int32: tokens the cache holds of each sequence before the call (not changed by it)
+ *   page_table  device [batch, pages_per_seq] int32
+ *   rope        device fp32 [n_positions, 2, head_dim / 2], 16-byte aligned: cosine, then sine of every pair at each position
+ *   q_out       device [rows, n_q_heads, head_dim] in the pool's type, 16-byte aligned (may be NULL when n_q_heads is 0)
+ * Skipped, with nothing of them written anywhere: rows in front of row_starts[0] or from row_starts[batch] on, sequences with a negative
+ * kv_lens, positions past the table or the sequence's pages, and pages that are not in [0, n_pages).  Two rows never share a
+ * place unless page tables name a page twice; then either row's values stay.  qkv must not overlap the pools or q_out.
+ * Errors: INVALID_ARG, UNSUPPORTED (head_dim not in {32, 64, 128}), TOO_LARGE (over 65536 heads, 2^31 - 256 positions), CUDA. */
+int hsd_kv_append(const void *qkv, int qkv_dtype, int rows, long long row_stride, int n_q_heads, int n_kv_heads, int head_dim,
+                  const int32_t *row_starts, const int32_t *kv_lens, int batch, const int32_t *page_table, int pages_per_seq,
+                  const float *rope, int n_positions, const hsd_kv_pool *pool, void *q_out, void *stream);
+
+/* Attention of one new token per sequence: out[b, h] = sum_j softmax_j(scale q[b, h] . k_j) v_j over the keys at positions
+ * j < kv_lens[b] of head h * n_kv_heads / n_q_heads (the new token's own key is among them once it has been appended: pass
+ * the lengths after the append).  Softmax and both sums in fp32, rounded once.
+ *   q, out     device [batch, n_q_heads, head_dim] in the pool's type, 16-byte aligned; n_q_heads a multiple of n_kv_heads
+ *   kv_lens    device [batch] int32, of any mixture; read by the kernels only, so a captured call follows their changes.
+ *              0 or less: zeros.  More than the page table has room for: its room
+ *   page_table device [batch, pages_per_seq] int32; keys on a page that is not in [0, n_pages) count as absent.  Memory of
+ *              the pages behind a sequence's last key is not used, whatever it holds
+ *   scale      finite
+ *   workspace  device, 16-byte aligned, at least hsd_paged_attention_workspace_bytes(...) (0 = bad sizes); contents on entry are
+ *              ignored, on exit unspecified
+ * Results do not depend on earlier calls; how a sequence's keys are divided, and so the order of its fp32 sums, follows
+ * the lengths of the whole batch.
+ * Errors: INVALID_ARG, UNSUPPORTED (head_dim not in {32, 64, 128}), TOO_LARGE (batch over 4096, over 65536 query heads,
+ * batch * pages_per_seq * page_size over 2^33), WORKSPACE_TOO_SMALL, CUDA. */
+size_t hsd_paged_attention_workspace_bytes(int n_q_heads, int n_kv_heads, int head_dim);
+int hsd_paged_attention(const void *q, int batch, int n_q_heads, int n_kv_heads, int head_dim, const hsd_kv_pool *pool,
+                        const int32_t *page_table, int pages_per_seq, const int32_t *kv_lens, float scale, void *workspace,
+                        size_t workspace_bytes, void *out, void *stream);
+
+/* hsd_gemm_bf16 with 4-bit weights, for few rows: out[r, n] = sum_k A[r, k] (codes[n, k] - 8) scales[n, k / group].  Products exact,
+ * sums in fp32 in a fixed order.
+ *   A       device bf16 [R, K] row-major, 16-byte aligned, 1 <= R <= 64
+ *   codes   device [N, K / 2] bytes, 16-byte aligned: k even in the low four bits, k odd in the high ones
+ *   scales  device bf16 [N, K / group]
+ *   group   32, 64 or 128; K a multiple of it
+ *   out     device fp32 [R, N]
+ * Errors: INVALID_ARG, TOO_LARGE (K over 2^28), CUDA. */
+int hsd_gemm_w4(const void *A, int R, int K, const void *codes, const void *scales, int N, int group, float *out, void *stream);
+
+/* What given tokens' probabilities were under softmax(logits[r, :]), and what else was likely: out_logprobs[r] = log p(tokens[r]),
+ * out_entropy[r] = -sum_x p(x) log p(x), out_ranks[r] = number of tokens in front of tokens[r], and the `top` first tokens with their log
+ * probabilities.  Order: larger logit first, the lower id among equals (+0 and -0 are equal).  fp32 sums, relative to the row's maximum.
+ *   logits  device [rows, vocab] row-major, HSD_F32 or HSD_BF16
+ *   tokens  device [rows] int32; outside of [0, vocab) (hsd_verify_level pads with -1): log probability NaN, rank -1
+ *   top     0 .. min(32, vocab); 0: the last two arrays are not written and may be NULL
+ *   out_logprobs, out_entropy  device fp32 [rows];  out_ranks  device int32 [rows]
+ *   out_top_tokens  device int32 [rows, top];  out_top_logprobs  device fp32 [rows, top]
+ * -inf is a logit of probability 0; a row of nothing else has every log probability -inf and entropy 0.  A row with a NaN or +inf has no
+ * distribution: NaN, NaN, rank -1, top tokens -1 with NaN.  Errors: INVALID_ARG, TOO_LARGE (vocab over 2^31 - 256), CUDA. */
+int hsd_token_logprobs(const void *logits, int dtype, int rows, int vocab, const int32_t *tokens, int top, float *out_logprobs,
+                       float *out_entropy, int32_t *out_ranks, int32_t *out_top_tokens, float *out_top_logprobs, void *stream);
+
 /* Measurement aid: one read-only pass over `bytes` (a multiple of 16 is read) of device memory at `buffer` (16-byte
  * aligned) with plain vector loads on every SM, nothing written (`sink`, a device word or NULL, is written only if a
  * checksum happens to match a constant).  Timed with events around it, bytes / time is the HBM rate a weight-streaming

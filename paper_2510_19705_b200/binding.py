@@ -51,7 +51,8 @@ def _host_calls():
         spec.loader.exec_module(mod)
         mod.init(*(ctypes.cast(f, ctypes.c_void_p).value for f in
                    (lib.hsd_draft_sample, lib.hsd_verify_workspace_bytes, lib.hsd_verify_level, lib.hsd_gemm_workspace_bytes,
-                    lib.hsd_gemm_bf16, lib.hsd_gemm_status, lib.hsd_strerror)), HsdError)
+                    lib.hsd_gemm_bf16, lib.hsd_gemm_status, lib.hsd_strerror, lib.hsd_kv_append, lib.hsd_paged_attention_workspace_bytes,
+                    lib.hsd_paged_attention, lib.hsd_gemm_w4, lib.hsd_token_logprobs)), HsdError)
         _host = mod
     return _host
 
@@ -141,6 +142,11 @@ class _ModelDesc(ctypes.Structure):
                 ("lm_head", ctypes.c_void_p), ("layer_weights", ctypes.POINTER(ctypes.c_void_p))]
 
 
+class _KvPool(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("dtype", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("head_stride", ctypes.c_int64), ("page_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64)]
+
+
 class LevelStats(ctypes.Structure):
     _fields_ = [("calls", ctypes.c_int64), ("rows", ctypes.c_int64), ("drafted", ctypes.c_int64),
                 ("tested", ctypes.c_int64), ("accepted", ctypes.c_int64), ("emitted", ctypes.c_int64),
@@ -206,6 +212,16 @@ def _declare_engine(lib):
     lib.hsd_gemm_bf16.argtypes = [vp, i32, i32, vp, i32, vp, vp, sz, vp]
     lib.hsd_gemm_status.restype = i32
     lib.hsd_gemm_status.argtypes = [vp, vp]
+    lib.hsd_kv_append.restype = i32
+    lib.hsd_kv_append.argtypes = [vp, i32, i32, c.c_longlong, i32, i32, i32, vp, vp, i32, vp, i32, vp, i32, c.POINTER(_KvPool), vp, vp]
+    lib.hsd_paged_attention_workspace_bytes.restype = sz
+    lib.hsd_paged_attention_workspace_bytes.argtypes = [i32, i32, i32]
+    lib.hsd_paged_attention.restype = i32
+    lib.hsd_paged_attention.argtypes = [vp, i32, i32, i32, i32, c.POINTER(_KvPool), vp, i32, vp, c.c_float, vp, sz, vp, vp]
+    lib.hsd_gemm_w4.restype = i32
+    lib.hsd_gemm_w4.argtypes = [vp, i32, i32, vp, vp, i32, i32, vp, vp]
+    lib.hsd_token_logprobs.restype = i32
+    lib.hsd_token_logprobs.argtypes = [vp, i32, i32, i32, vp, i32, vp, vp, vp, vp, vp, vp]
 
 
 def _model_desc(cfg, weights, max_batch, max_seq, page_size):
@@ -468,3 +484,56 @@ def hsd_gemm_workspace_bytes(R, N, K):
 def hsd_gemm_bf16(A, W, out=None, workspace=None, check=True):
     """A bf16 [R, K], W bf16 [N, K] (CUDA) -> fp32 [R, N] = A @ W^T on the tensor cores."""
     return (_host or _host_calls()).gemm_bf16(A, W, out, workspace, check)
+
+
+# ------------------------------------------------------------------- operators of a caller's own drafter
+def rope_table(n_positions, head_dim, theta=10000.0, device="cuda"):
+    """Cosine and sine of every position and pair, fp32 [n_positions, 2, head_dim / 2], from angles in 64 bits: hsd_kv_append's table."""
+    freq = float(theta) ** (-torch.arange(0, head_dim, 2, dtype=torch.float64, device=device) / head_dim)
+    angle = torch.arange(n_positions, dtype=torch.float64, device=device)[:, None] * freq
+    return torch.stack((angle.cos(), angle.sin()), dim=1).to(torch.float32)
+
+
+def w4_pack(W, group=128):
+    """Weights [N, K] -> (codes uint8 [N, K / 2], scales bf16 [N, K / group]) for hsd_gemm_w4: per group the scale is the largest
+    magnitude / 7 rounded to bf16, the code the nearest whole number of scales (ties to even) within -8 .. 7, plus 8.  A group with an
+    infinity or a NaN has the scale NaN."""
+    N, K = W.shape
+    if group not in (32, 64, 128) or K % group:
+        raise HsdError("w4_pack: K = %d is not a whole number of groups of 32, 64 or 128 (got %d)" % (K, group))
+    w = W.detach().to(torch.float32).reshape(N, K // group, group)
+    scales = (w.abs().amax(dim=2) / 7).to(torch.bfloat16)
+    scales = torch.where(torch.isfinite(scales), scales, torch.full_like(scales, float("nan")))
+    c = torch.round(w / scales.to(torch.float32)[:, :, None]).clamp(-8, 7)
+    c = (torch.where(torch.isfinite(c), c, torch.zeros_like(c)) + 8).to(torch.uint8).view(N, K)
+    return (c[:, 0::2] | (c[:, 1::2] << 4)).contiguous(), scales.contiguous()
+
+
+def hsd_kv_append(qkv, k_pool, v_pool, page_table, kv_lens, rope, row_starts=None, q_out=None):
+    """New rows qkv [rows, n_q + 2 n_kv, head_dim] (fp32/bf16; rows may lie apart) into the pools [n_kv, n_pages, page, head_dim]
+    (fp32/bf16, any order in memory with head_dim innermost), queries and keys rotated by their positions -> queries
+    [rows, n_q, head_dim] in the pools' type.  page_table int32 [batch, pages], kv_lens int32 [batch] (lengths before the call), rope from
+    rope_table(), row_starts int32 [batch + 1] or None (row b is sequence b's one token).  Rows that have no place are skipped
+    and their queries are not written (include/hsd.h)."""
+    return (_host or _host_calls()).kv_append(qkv, k_pool, v_pool, page_table, kv_lens, rope, row_starts, q_out)
+
+
+def hsd_paged_attention_workspace_bytes(n_q_heads, n_kv_heads, head_dim):
+    return int(library().hsd_paged_attention_workspace_bytes(n_q_heads, n_kv_heads, head_dim))
+
+
+def hsd_paged_attention(q, k_pool, v_pool, page_table, kv_lens, scale=None, workspace=None, out=None):
+    """Attention of one token per sequence, q [batch, n_q, head_dim], over the keys at positions below kv_lens int32 [batch] of the
+    pools (as hsd_kv_append's) -> [batch, n_q, head_dim] in their type.  scale None: head_dim ** -0.5."""
+    return (_host or _host_calls()).paged_attention(q, k_pool, v_pool, page_table, kv_lens, scale, workspace, out)
+
+
+def hsd_gemm_w4(A, codes, scales, out=None):
+    """A bf16 [R, K] (R <= 64), codes uint8 [N, K / 2] and scales bf16 [N, K / group] from w4_pack -> fp32 [R, N]."""
+    return (_host or _host_calls()).gemm_w4(A, codes, scales, out)
+
+
+def hsd_token_logprobs(logits, tokens, top=0):
+    """logits [..., vocab] (fp32/bf16), tokens int32 [...] -> (log probabilities fp32 [...], entropies fp32 [...], ranks int32 [...], top
+    tokens int32 [..., top], their log probabilities fp32 [..., top])."""
+    return (_host or _host_calls()).token_logprobs(logits, tokens, top)

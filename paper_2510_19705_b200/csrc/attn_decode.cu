@@ -1,0 +1,537 @@
+// Attention of one new token per sequence over the caller's paged cache (hsd_paged_attention).
+//   o = sum_j w_j v_j / sum_j w_j,  w_j = exp(scale q.k_j - m),  m = max_j scale q.k_j   over the sequence's keys j
+// Bound by memory: every key and value is read once, for all query heads of its group.  The tiles (16 or 8 keys of one sequence
+// and head) of the whole batch stand in one line, which is divided evenly over the warps, whatever the lengths are: the grid
+// does not depend on them, and they are read on the device.  A warp streams its stretch through a ring of its own in shared memory
+// (cp.async, no barrier between warps), across the borders of sequences and heads.  Where a stretch ends inside a sequence, the warp
+// leaves (m, sum, o) in the workspace and attn_join_kernel adds the parts of a sequence in order.
+// bf16: both products on mma.sync with the group's queries as the 16 rows of a tile (at 4 to 16 queries a key the tensor pipe is
+// far from its limit); weights as bf16 high and low parts, so that only the final rounding is one of 8 bits.
+// fp32: the products in fp32, four lanes a key for the scores, a lane a few columns for the output.
+#include <math.h>
+
+#include "paged.cuh"
+
+namespace hsd {
+namespace {
+
+constexpr int kWarps = 8, kThreads = kWarps * 32;
+constexpr int kGrid = kMeasuredSMs;            // CTAs at most: fixed, as the workspace's size depends on it
+constexpr int kMinTiles = 4;                   // tiles a warp at least: fewer parts to join
+constexpr int kMaxBatch = 4096;                // its tiles' prefix sums lie in shared memory
+constexpr int kJoinWarps = 8;
+
+struct DecodeArgs {
+  const void *q;
+  void *out;
+  const int32_t *page_table, *kv_lens;
+  float *parts;
+  PoolView pool;
+  float scale;                                 // times log2(e)
+  int batch, nq, nkv, pages_per_seq;
+  int group, chunk, chunks;                    // query heads of a key head; of them at once; times
+};
+
+template <typename T> struct Form;
+template <> struct Form<__nv_bfloat16> { static constexpr int KEYS = 16, HEADS = 16; };
+template <> struct Form<float> { static constexpr int KEYS = 8, HEADS = 8; };
+template <typename T, int HD> struct Ring {
+  static constexpr int ROW = HD * (int)sizeof(T), HALF = Form<T>::KEYS * ROW, STAGE = 2 * HALF;    // keys, then values
+  static constexpr int STAGES = (sizeof(T) == 4 ? 16384 : 24576) / STAGE, BYTES = STAGE * STAGES;  // (fp32 has its queries beside it)
+};
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ void copy16(u32 to, const void *from, bool there) {       // zeros where there is nothing to read
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void mma(float *c, const u32 *a, u32 b0, u32 b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void ldsm4(u32 *r, u32 at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void ldsm4t(u32 *r, u32 at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+// Byte of 16-byte piece c of row r of a tile: permuted so that the pieces a quarter warp reads together lie in different banks.
+template <typename T, int HD> __device__ __forceinline__ u32 piece(int r, int c) {
+  if constexpr (sizeof(T) == 4) return r * (HD * 4) + ((c ^ ((r & 1) << 2)) << 4);
+  else if constexpr (HD == 32) return r * 64 + ((c ^ ((r >> 1) & 3)) << 4);
+  else return r * (HD * 2) + ((c ^ (r & 7)) << 4);
+}
+
+// The line of tiles: sequence b has as many for each of `items` (key head, chunk of query heads); before[b]: tiles of the
+// sequences in front of b, per item.
+struct Line {
+  const int *before;
+  int batch, items;
+  long long per;                               // tiles of a warp
+};
+// Lengths within the page table's room, and the prefix sums; all threads of the CTA.
+template <int KEYS, int THREADS>
+__device__ __forceinline__ Line make_line(const int32_t *kv_lens, int batch, long long room, int items, int *before, int *warp_sum) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int carry = 0;
+  for (int b0 = 0; b0 < batch; b0 += THREADS) {
+    const int b = b0 + threadIdx.x;
+    int n = 0;
+    if (b < batch) n = (int)((min((long long)max(kv_lens[b], 0), room) + KEYS - 1) / KEYS);
+    int upto = n;
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+      if (lane >= o) upto += x;
+    }
+    if (lane == 31) warp_sum[warp] = upto;
+    __syncthreads();
+    int front = carry;
+    for (int w = 0; w < THREADS / 32; ++w) {
+      if (w < warp) front += warp_sum[w];
+      carry += warp_sum[w];
+    }
+    if (b < batch) before[b + 1] = front + upto;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) before[0] = 0;
+  __syncthreads();
+  Line l;
+  l.before = before; l.batch = batch; l.items = items;
+  const long long total = (long long)carry * items, warps = kGrid * kWarps;
+  l.per = max((total + warps - 1) / warps, (long long)kMinTiles);
+  return l;
+}
+
+// A place on the line.
+struct Place {
+  int b, item, tile, tiles;                    // tiles: of the sequence
+  __device__ __forceinline__ void find(const Line &l, long long at) {
+    const int per_item = (int)(at / l.items);  // before[b] <= per_item < before[b + 1]
+    int lo = 0, hi = l.batch - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (l.before[mid] <= per_item) lo = mid;
+      else hi = mid - 1;
+    }
+    b = lo;
+    tiles = l.before[b + 1] - l.before[b];
+    const long long rest = at - (long long)l.before[b] * l.items;
+    item = (int)(rest / tiles);
+    tile = (int)(rest % tiles);
+  }
+  __device__ __forceinline__ void next(const Line &l) {
+    if (++tile < tiles) return;
+    tile = 0;
+    if (++item < l.items) return;
+    item = 0;
+    do ++b;
+    while (b < l.batch && l.before[b + 1] == l.before[b]);
+    if (b < l.batch) tiles = l.before[b + 1] - l.before[b];
+  }
+};
+
+// Part of a warp's stretch: slot 0 where it begins inside a sequence, slot 1 where it begins with one and ends inside it.
+template <int HD> __device__ __forceinline__ float *part_at(float *parts, int chunk, int warp, int slot) {
+  return parts + ((size_t)warp * 2 + slot) * chunk * (HD + 2);         // per head: o [HD]; behind all of them m and sum
+}
+
+// ---------------------------------------------------------------------------- tiles into a warp's ring
+template <typename T, int HD> struct Feeder {
+  using R = Ring<T, HD>;
+  static constexpr int KEYS = Form<T>::KEYS;
+  const DecodeArgs &a;
+  const Line &line;
+  u32 ring;                                    // shared memory
+  u32 *masks;                                  // per stage: keys of its tile that are there
+  Place at;                                    // tile whose rows are looked up next
+  long long left;                              // tiles not looked up yet
+  long long row;                               // of key `lane` of the tile that is copied next: its place in the pools, -1 without one
+  int lane;
+  __device__ __forceinline__ void look_up() {
+    row = -1;
+    if (left <= 0) return;
+    --left;
+    const int key = at.tile * KEYS + lane;
+    if (lane < KEYS && key < min((long long)a.kv_lens[at.b], (long long)a.pages_per_seq * a.pool.page)) {
+      const int pg = a.page_table[(size_t)at.b * a.pages_per_seq + key / a.pool.page];
+      if (pg >= 0 && pg < a.pool.n_pages)
+        row = pg * a.pool.page_bytes + (key % a.pool.page) * a.pool.token_bytes + (long long)(at.item / a.chunks) * a.pool.head_bytes;
+    }
+    at.next(line);
+  }
+  __device__ __forceinline__ void copy(int stage) {
+    const u32 to = ring + stage * R::STAGE;
+    const u32 there = __ballot_sync(0xFFFFFFFFu, row >= 0);
+    constexpr int PIECES = R::ROW / 16, AT_ONCE = 32 / PIECES;         // rows that the warp copies at once
+    const int c = lane % PIECES;
+#pragma unroll
+    for (int i = 0; i < KEYS / AT_ONCE; ++i) {
+      const int r = i * AT_ONCE + lane / PIECES;
+      const long long off = __shfl_sync(0xFFFFFFFFu, row, r);
+      const bool ok = off >= 0;
+      const long long from = ok ? off + c * 16 : 0;
+      copy16(to + piece<T, HD>(r, c), a.pool.k + from, ok);
+      copy16(to + R::HALF + piece<T, HD>(r, c), a.pool.v + from, ok);
+    }
+    if (lane == 0) masks[stage] = there;
+  }
+};
+
+// ---------------------------------------------------------------------------- bf16
+template <int HD> struct Bf16Tile {
+  using T = __nv_bfloat16;
+  u32 qf[HD / 16][4];
+  float o[HD / 8][4], m[2], l[2];
+  int lane;
+
+  // Rows of the tile: the chunk's query heads; rows without one are zeros.
+  __device__ __forceinline__ void begin(const DecodeArgs &a, int b, int item) {
+    const int h = item / a.chunks, c = item % a.chunks, heads = min(a.chunk, a.group - c * a.chunk);
+    const T *q = static_cast<const T *>(a.q) + ((size_t)b * a.nq + (size_t)h * a.group + c * a.chunk) * HD;
+    const int r = lane >> 2, col = (lane & 3) * 2;
+#pragma unroll
+    for (int k = 0; k < HD / 16; ++k)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const int row = r + (x & 1) * 8;
+        qf[k][x] = row < heads ? __ldg(reinterpret_cast<const u32 *>(q + row * HD + k * 16 + col + (x >> 1) * 8)) : 0u;
+      }
+#pragma unroll
+    for (int n = 0; n < HD / 8; ++n)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) o[n][x] = 0.f;
+    m[0] = m[1] = -INFINITY;
+    l[0] = l[1] = 0.f;
+  }
+  __device__ __forceinline__ void tile(const DecodeArgs &a, u32 at, u32 there) {
+    float s[2][4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) s[0][x] = s[1][x] = 0.f;
+    const int kr = (lane & 7) + ((lane >> 4) << 3), kc = (lane >> 3) & 1;
+#pragma unroll
+    for (int k = 0; k < HD / 16; ++k) {
+      u32 f[4];
+      ldsm4(f, at + piece<T, HD>(kr, 2 * k + kc));
+      mma(s[0], qf[k], f[0], f[1]);
+      mma(s[1], qf[k], f[2], f[3]);
+    }
+    const int col = (lane & 3) * 2;
+    float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        s[n][x] = (there >> (n * 8 + col + (x & 1))) & 1 ? s[n][x] * a.scale : -INFINITY;
+        mx[x >> 1] = fmaxf(mx[x >> 1], s[n][x]);
+      }
+    u32 hi[4], lo[4];
+    float f[2];
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      mx[y] = fmaxf(mx[y], __shfl_xor_sync(0xFFFFFFFFu, mx[y], 1));
+      mx[y] = fmaxf(mx[y], __shfl_xor_sync(0xFFFFFFFFu, mx[y], 2));
+      const float n = fmaxf(m[y], mx[y]);
+      f[y] = n > -INFINITY ? ex2(m[y] - n) : 1.f;
+      m[y] = n;
+      const float ref = n > -INFINITY ? n : 0.f;
+      l[y] *= f[y];
+#pragma unroll
+      for (int n2 = 0; n2 < 2; ++n2) {
+        const float p0 = ex2(s[n2][2 * y] - ref), p1 = ex2(s[n2][2 * y + 1] - ref);
+        l[y] += p0 + p1;
+        const __nv_bfloat162 h2 = __floats2bfloat162_rn(p0, p1);
+        const __nv_bfloat162 l2 = __floats2bfloat162_rn(p0 - __low2float(h2), p1 - __high2float(h2));
+        hi[n2 * 2 + y] = *reinterpret_cast<const u32 *>(&h2);
+        lo[n2 * 2 + y] = *reinterpret_cast<const u32 *>(&l2);
+      }
+    }
+    if (__any_sync(0xFFFFFFFFu, f[0] != 1.f || f[1] != 1.f)) {
+#pragma unroll
+      for (int n = 0; n < HD / 8; ++n) {
+        o[n][0] *= f[0]; o[n][1] *= f[0];
+        o[n][2] *= f[1]; o[n][3] *= f[1];
+      }
+    }
+    const u32 v = at + Ring<T, HD>::HALF;
+    const int vr = lane & 15, vc = lane >> 4;
+#pragma unroll
+    for (int n = 0; n < HD / 16; ++n) {
+      u32 b[4];
+      ldsm4t(b, v + piece<T, HD>(vr, 2 * n + vc));
+      mma(o[2 * n], hi, b[0], b[1]);
+      mma(o[2 * n + 1], hi, b[2], b[3]);
+      mma(o[2 * n], lo, b[0], b[1]);
+      mma(o[2 * n + 1], lo, b[2], b[3]);
+    }
+  }
+  __device__ __forceinline__ void end(const DecodeArgs &a, int b, int item, bool whole, float *part) {
+    const int h = item / a.chunks, c = item % a.chunks, heads = min(a.chunk, a.group - c * a.chunk), col = (lane & 3) * 2;
+    T *out = static_cast<T *>(a.out) + ((size_t)b * a.nq + (size_t)h * a.group + c * a.chunk) * HD;
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      l[y] += __shfl_xor_sync(0xFFFFFFFFu, l[y], 1);
+      l[y] += __shfl_xor_sync(0xFFFFFFFFu, l[y], 2);
+      const int row = (lane >> 2) + 8 * y;
+      if (row >= heads) continue;
+      if (whole) {
+        const float inv = l[y] != 0.f ? 1.f / l[y] : 0.f;
+#pragma unroll
+        for (int n = 0; n < HD / 8; ++n)
+          *reinterpret_cast<__nv_bfloat162 *>(out + row * HD + n * 8 + col) = __floats2bfloat162_rn(o[n][2 * y] * inv, o[n][2 * y + 1] * inv);
+      } else {
+#pragma unroll
+        for (int n = 0; n < HD / 8; ++n) *reinterpret_cast<float2 *>(part + row * HD + n * 8 + col) = make_float2(o[n][2 * y], o[n][2 * y + 1]);
+        if ((lane & 3) == 0) *reinterpret_cast<float2 *>(part + a.chunk * HD + row * 2) = make_float2(m[y], l[y]);
+      }
+    }
+  }
+};
+
+// ---------------------------------------------------------------------------- fp32
+template <int HD> struct Fp32Tile {
+  using T = float;
+  static constexpr int KEYS = 8, HEADS = Form<float>::HEADS, COLS = HD / 32;
+  float o[HEADS][COLS], m[HEADS], l[HEADS];
+  float *q;                                    // the warp's queries in shared memory [HEADS][HD]
+  int lane, heads;
+
+  __device__ __forceinline__ void begin(const DecodeArgs &a, int b, int item) {
+    const int h = item / a.chunks, c = item % a.chunks;
+    heads = min(a.chunk, a.group - c * a.chunk);
+    const float *from = static_cast<const float *>(a.q) + ((size_t)b * a.nq + (size_t)h * a.group + c * a.chunk) * HD;
+    __syncwarp();
+    for (int i = lane; i < heads * HD; i += 32) q[i] = from[i];
+    __syncwarp();
+#pragma unroll
+    for (int g = 0; g < HEADS; ++g) {
+      m[g] = -INFINITY;
+      l[g] = 0.f;
+#pragma unroll
+      for (int e = 0; e < COLS; ++e) o[g][e] = 0.f;
+    }
+  }
+  __device__ __forceinline__ void tile(const DecodeArgs &a, u32 at, u32 there) {
+    const unsigned char *k = static_cast<const unsigned char *>(__cvta_shared_to_generic(at)), *v = k + Ring<T, HD>::HALF;
+    const int key = lane >> 2, j = lane & 3;
+    float s[HEADS];
+#pragma unroll
+    for (int g = 0; g < HEADS; ++g) s[g] = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < HD / 16; ++i) {
+      const float4 x = *reinterpret_cast<const float4 *>(k + piece<T, HD>(key, i * 4 + j));
+#pragma unroll
+      for (int g = 0; g < HEADS; ++g)
+        if (g < heads) {
+          const float4 y = *reinterpret_cast<const float4 *>(q + g * HD + (i * 4 + j) * 4);
+          s[g] = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, s[g]))));
+        }
+    }
+    const bool here = (there >> key) & 1;
+#pragma unroll
+    for (int g = 0; g < HEADS; ++g)
+      if (g < heads) {
+        float x = s[g];
+        x += __shfl_xor_sync(0xFFFFFFFFu, x, 1);
+        x += __shfl_xor_sync(0xFFFFFFFFu, x, 2);
+        x = here ? x * a.scale : -INFINITY;
+        float mx = x;
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, d));
+        const float n = fmaxf(m[g], mx), f = n > -INFINITY ? ex2(m[g] - n) : 1.f;
+        m[g] = n;
+        s[g] = ex2(x - (n > -INFINITY ? n : 0.f));
+        l[g] = fmaf(l[g], f, s[g]);            // of this lane's keys: added up at the end
+#pragma unroll
+        for (int e = 0; e < COLS; ++e) o[g][e] *= f;
+      }
+#pragma unroll
+    for (int kk = 0; kk < KEYS; ++kk) {
+      float x[COLS];
+      const unsigned char *row = v + piece<T, HD>(kk, lane * COLS / 4) + (lane * COLS % 4) * 4;
+      if constexpr (COLS == 4) { const float4 y = *reinterpret_cast<const float4 *>(row); x[0] = y.x; x[1] = y.y; x[2] = y.z; x[3] = y.w; }
+      else if constexpr (COLS == 2) { const float2 y = *reinterpret_cast<const float2 *>(row); x[0] = y.x; x[1] = y.y; }
+      else x[0] = *reinterpret_cast<const float *>(row);
+#pragma unroll
+      for (int g = 0; g < HEADS; ++g)
+        if (g < heads) {
+          const float p = __shfl_sync(0xFFFFFFFFu, s[g], kk * 4);
+#pragma unroll
+          for (int e = 0; e < COLS; ++e) o[g][e] = fmaf(p, x[e], o[g][e]);
+        }
+    }
+  }
+  __device__ __forceinline__ void end(const DecodeArgs &a, int b, int item, bool whole, float *part) {
+    const int h = item / a.chunks, c = item % a.chunks;
+    float *out = static_cast<float *>(a.out) + ((size_t)b * a.nq + (size_t)h * a.group + c * a.chunk) * HD;
+#pragma unroll
+    for (int g = 0; g < HEADS; ++g)
+      if (g < heads) {
+        float sum = l[g];
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
+        const float inv = !whole ? 1.f : sum != 0.f ? 1.f / sum : 0.f;
+        float *to = (whole ? out : part) + g * HD + lane * COLS;
+#pragma unroll
+        for (int e = 0; e < COLS; ++e) to[e] = o[g][e] * inv;
+        if (!whole && lane == 0) *reinterpret_cast<float2 *>(part + a.chunk * HD + g * 2) = make_float2(m[g], sum);
+      }
+  }
+};
+
+template <typename T, int HD> struct TileOf { using type = Bf16Tile<HD>; };
+template <int HD> struct TileOf<float, HD> { using type = Fp32Tile<HD>; };
+template <typename T, int HD> constexpr int kQueryBytes = sizeof(T) == 4 ? Form<T>::HEADS * HD * 4 : 0;     // a warp's, in shared memory
+template <typename T, int HD> constexpr int smem_bytes(int batch) {
+  return kWarps * (Ring<T, HD>::BYTES + kQueryBytes<T, HD>) + kWarps * Ring<T, HD>::STAGES * 4 + kWarps * 4 + (batch + 1) * 4;
+}
+
+template <typename T, int HD>
+__global__ void __launch_bounds__(kThreads, 1)
+attn_decode_kernel(DecodeArgs a) {
+  using R = Ring<T, HD>;
+  constexpr int S = R::STAGES;
+  extern __shared__ __align__(128) unsigned char smem[];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  unsigned char *rest = smem + kWarps * (R::BYTES + kQueryBytes<T, HD>);
+  u32 *masks = reinterpret_cast<u32 *>(rest) + warp * S;
+  int *warp_sum = reinterpret_cast<int *>(rest) + kWarps * S, *before = warp_sum + kWarps;
+  const Line line = make_line<Form<T>::KEYS, kThreads>(a.kv_lens, a.batch, (long long)a.pages_per_seq * a.pool.page, a.nkv * a.chunks, before, warp_sum);
+
+  // sequences without a key: zeros
+  for (int b = blockIdx.x; b < a.batch; b += gridDim.x)
+    if (before[b + 1] == before[b])
+      for (int i = threadIdx.x; i < a.nq * HD; i += kThreads) static_cast<T *>(a.out)[(size_t)b * a.nq * HD + i] = T(0.f);
+
+  const int me = blockIdx.x * kWarps + warp;
+  const long long total = (long long)before[a.batch] * line.items, from = me * line.per, n = min(line.per, total - from);
+  if (n <= 0) return;
+  typename TileOf<T, HD>::type t;
+  t.lane = lane;
+  if constexpr (sizeof(T) == 4) t.q = reinterpret_cast<float *>(smem + kWarps * R::BYTES) + warp * Form<T>::HEADS * HD;
+  Place at;
+  at.find(line, from);
+  Feeder<T, HD> feed = {a, line, (u32)__cvta_generic_to_shared(smem) + warp * R::BYTES, masks, at, n, -1, lane};
+  feed.look_up();
+#pragma unroll
+  for (int i = 0; i < S - 1; ++i) {
+    if (i < n) { feed.copy(i); feed.look_up(); }
+    copies_end();
+  }
+  int stage = 0, fill = S - 1, first = at.tile;
+  t.begin(a, at.b, at.item);
+  for (long long i = 0; i < n; ++i) {
+    copies_wait<S - 2>();
+    __syncwarp();
+    if (i + S - 1 < n) { feed.copy(fill); feed.look_up(); }
+    copies_end();
+    t.tile(a, feed.ring + stage * R::STAGE, masks[stage]);
+    if (++stage == S) stage = 0;
+    if (++fill == S) fill = 0;
+    const bool last = at.tile + 1 == at.tiles;
+    if (last || i + 1 == n) t.end(a, at.b, at.item, first == 0 && last, part_at<HD>(a.parts, a.chunk, me, first > 0 ? 0 : 1));
+    if (i + 1 < n) {
+      at.next(line);
+      if (last) { first = 0; t.begin(a, at.b, at.item); }
+    }
+  }
+}
+
+// One CTA a query head of a sequence: adds its parts, if it has any.  Warps take parts in turn and add them in order, then the warps'
+// sums are added in order.
+template <typename T, int HD>
+__global__ void __launch_bounds__(kJoinWarps * 32)
+attn_join_kernel(DecodeArgs a) {
+  constexpr int COLS = HD / 32;
+  extern __shared__ int before[];
+  __shared__ int warp_sum[kJoinWarps];
+  __shared__ float sh_o[kJoinWarps][HD], sh_l[kJoinWarps];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const Line line = make_line<Form<T>::KEYS, kJoinWarps * 32>(a.kv_lens, a.batch, (long long)a.pages_per_seq * a.pool.page, a.nkv * a.chunks, before, warp_sum);
+  for (long long x = blockIdx.x; x < (long long)a.batch * a.nq; x += gridDim.x) {
+    const int b = (int)(x / a.nq), hq = (int)(x % a.nq), h = hq / a.group, c = hq % a.group / a.chunk, g = hq % a.group % a.chunk;
+    const int tiles = before[b + 1] - before[b];
+    if (tiles == 0) continue;
+    const long long from = (long long)before[b] * line.items + (long long)(h * a.chunks + c) * tiles;
+    const int w0 = (int)(from / line.per), w1 = (int)((from + tiles - 1) / line.per);
+    if (w0 == w1) continue;                    // one warp had all of it
+    float m = -INFINITY;
+    auto stat = [&](int w) { return *reinterpret_cast<const float2 *>(part_at<HD>(a.parts, a.chunk, w, w * line.per > from ? 0 : 1) + a.chunk * HD + g * 2); };
+    for (int w = w0 + lane; w <= w1; w += 32) m = fmaxf(m, stat(w).x);
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+    const float ref = m > -INFINITY ? m : 0.f;
+    float o[COLS], l = 0.f;
+#pragma unroll
+    for (int e = 0; e < COLS; ++e) o[e] = 0.f;
+#pragma unroll 4
+    for (int w = w0 + warp; w <= w1; w += kJoinWarps) {
+      const float *p = part_at<HD>(a.parts, a.chunk, w, w * line.per > from ? 0 : 1) + g * HD + lane * COLS;
+      const float2 ml = stat(w);
+      const float f = ex2(ml.x - ref);
+      l = fmaf(ml.y, f, l);
+#pragma unroll
+      for (int e = 0; e < COLS; ++e) o[e] = fmaf(p[e], f, o[e]);
+    }
+#pragma unroll
+    for (int e = 0; e < COLS; ++e) sh_o[warp][lane * COLS + e] = o[e];
+    if (lane == 0) sh_l[warp] = l;
+    __syncthreads();
+    for (int i = threadIdx.x; i < HD; i += kJoinWarps * 32) {
+      float sum = 0.f, all = 0.f;
+      for (int w = 0; w < kJoinWarps; ++w) { sum += sh_o[w][i]; all += sh_l[w]; }
+      const float y = all != 0.f ? sum / all : 0.f;
+      if constexpr (sizeof(T) == 4) static_cast<float *>(a.out)[((size_t)b * a.nq + hq) * HD + i] = y;
+      else static_cast<__nv_bfloat16 *>(a.out)[((size_t)b * a.nq + hq) * HD + i] = __float2bfloat16_rn(y);
+    }
+    __syncthreads();
+  }
+}
+
+template <typename T, int HD> int run(const DecodeArgs &a, cudaStream_t s) {
+  static std::atomic<u64> done{0};
+  const int status = hsd_smem_limit((const void *)attn_decode_kernel<T, HD>, smem_bytes<T, HD>(kMaxBatch), done);
+  if (status) return status;
+  attn_decode_kernel<T, HD><<<kGrid, kThreads, smem_bytes<T, HD>(a.batch), s>>>(a);
+  const long long heads = (long long)a.batch * a.nq;
+  attn_join_kernel<T, HD><<<(unsigned)(heads < 8 * kGrid ? heads : 8 * kGrid), kJoinWarps * 32, (a.batch + 1) * 4, s>>>(a);
+  hsd_count_launches(2);
+  return hsd_launch_status();
+}
+template <typename T> int run_hd(const DecodeArgs &a, int hd, cudaStream_t s) {
+  return hd == 32 ? run<T, 32>(a, s) : hd == 64 ? run<T, 64>(a, s) : run<T, 128>(a, s);
+}
+
+}  // namespace
+}  // namespace hsd
+
+extern "C" size_t hsd_paged_attention_workspace_bytes(int n_q_heads, int n_kv_heads, int head_dim) {
+  if (n_q_heads <= 0 || n_kv_heads <= 0 || n_q_heads % n_kv_heads || (head_dim != 32 && head_dim != 64 && head_dim != 128)) return 0;
+  const int group = n_q_heads / n_kv_heads, chunk = group < 16 ? group : 16;
+  return (size_t)hsd::kGrid * hsd::kWarps * 2 * chunk * (head_dim + 2) * sizeof(float);
+}
+
+extern "C" int hsd_paged_attention(const void *q, int batch, int n_q_heads, int n_kv_heads, int head_dim, const hsd_kv_pool *pool,
+                                   const int32_t *page_table, int pages_per_seq, const int32_t *kv_lens, float scale, void *workspace,
+                                   size_t workspace_bytes, void *out, void *stream) {
+  using namespace hsd;
+  if (!q || !page_table || !kv_lens || !out || !workspace || batch <= 0 || n_q_heads <= 0 || n_kv_heads <= 0 || n_q_heads % n_kv_heads) return HSD_E_INVALID_ARG;
+  if (!(scale == scale) || isinf(scale)) return HSD_E_INVALID_ARG;
+  DecodeArgs a = {};
+  const int status = pool_view(pool, n_kv_heads, head_dim, pages_per_seq, a.pool);
+  if (status) return status;
+  if (batch > kMaxBatch || (long long)pages_per_seq * pool->page_size > (1ll << 33) / batch || n_q_heads > 65536) return HSD_E_TOO_LARGE;
+  if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out) | reinterpret_cast<uintptr_t>(workspace)) & 15) return HSD_E_INVALID_ARG;
+  if (workspace_bytes < hsd_paged_attention_workspace_bytes(n_q_heads, n_kv_heads, head_dim)) return HSD_E_WORKSPACE_TOO_SMALL;
+  a.q = q; a.out = out; a.page_table = page_table; a.kv_lens = kv_lens; a.parts = static_cast<float *>(workspace);
+  a.scale = scale * 1.4426950408889634f;
+  a.batch = batch; a.nq = n_q_heads; a.nkv = n_kv_heads; a.pages_per_seq = pages_per_seq;
+  a.group = n_q_heads / n_kv_heads;
+  const int most = pool->dtype == HSD_F32 ? Form<float>::HEADS : Form<__nv_bfloat16>::HEADS;
+  a.chunks = ceil_div(a.group, most);
+  a.chunk = ceil_div(a.group, a.chunks);
+  return pool->dtype == HSD_F32 ? run_hd<float>(a, head_dim, (cudaStream_t)stream) : run_hd<__nv_bfloat16>(a, head_dim, (cudaStream_t)stream);
+}

@@ -1,0 +1,357 @@
+// Log probabilities of given tokens, with entropy, rank and the top alternatives of every row (hsd_token_logprobs).
+//   m = max l, S = sum exp(l - m), T = sum exp(l - m) (l - m):  log p(x) = (l_x - m) - log S,  H = log S - T / S
+// (both terms of H are >= 0: nothing cancels).  One read of the row: every thread keeps its own running (m, S, T), rescaled when
+// its maximum grows, its count of tokens in front of the given one, and its maximum; the triples are merged at the end.
+// The top tokens need no second read either, but for a few threads' shares of the row: the k-th largest of the maxima of
+// groups of threads bounds the k-th largest token from below, so only threads whose own maximum reaches it can hold one of the k.
+// Their shares (out of L2 or L1, a warp together on each) give the candidates, usually little more than k; a candidate's place is
+// the number of candidates in front of it.  Order: larger logit first, lower id among equals, so the result does not
+// depend on the order in which candidates were found.
+// Rows with more candidates than fit (masses of equal logits: a mask's -inf) take select_slow().
+#include <math.h>
+
+#include "common.cuh"
+
+namespace hsd {
+namespace {
+
+constexpr int kMaxTop = 32;
+constexpr int kCand = 1024;            // candidates that fit
+constexpr float kLog2e = 1.4426950408889634f;
+
+struct LogprobArgs {
+  const void *logits;
+  const int32_t *tokens;
+  float *logprob, *entropy;
+  int32_t *rank, *top_id;
+  float *top_lp;
+  int V, top;
+};
+
+template <typename T> struct Vec;      // 16 bytes of logits
+template <> struct Vec<__nv_bfloat16> {
+  static constexpr int N = 8;
+  __device__ static void unpack(const uint4 &v, float *f) {
+    f[0] = __uint_as_float(v.x << 16); f[1] = __uint_as_float(v.x & 0xFFFF0000u);
+    f[2] = __uint_as_float(v.y << 16); f[3] = __uint_as_float(v.y & 0xFFFF0000u);
+    f[4] = __uint_as_float(v.z << 16); f[5] = __uint_as_float(v.z & 0xFFFF0000u);
+    f[6] = __uint_as_float(v.w << 16); f[7] = __uint_as_float(v.w & 0xFFFF0000u);
+  }
+};
+template <> struct Vec<float> {
+  static constexpr int N = 4;
+  __device__ static void unpack(const uint4 &v, float *f) {
+    f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y); f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
+  }
+};
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// A float as a whole number of the same order (-0 as +0), and a token's place in a row's order.
+__device__ __forceinline__ u32 ordered(float x) {
+  const u32 b = __float_as_uint(x + 0.f);
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float unordered(u32 o) { return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o); }
+__device__ __forceinline__ u64 key_of(float x, int id) { return ((u64)ordered(x) << 32) | (u32)~id; }
+
+// A CTA's part [lo, hi) of a row, in 16-byte pieces of the row's memory: piece i holds ids first + i * N .., of which those outside
+// the part are not read.
+template <typename T> struct Part {
+  static constexpr int N = Vec<T>::N;
+  const T *row;
+  int lo, hi, first, pieces;
+  __device__ Part(const T *row_, int lo_, int hi_) : row(row_), lo(lo_), hi(hi_) {
+    const int off = (int)((reinterpret_cast<uintptr_t>(row + lo) & 15) / sizeof(T));
+    first = lo - off;
+    pieces = hi > lo ? (hi - first + N - 1) / N : 0;
+  }
+  __device__ __forceinline__ bool whole(int i) const { return first + i * N >= lo && first + (i + 1) * N <= hi; }
+  // f: -inf where there is no token
+  __device__ __forceinline__ void read(int i, float *f) const {
+    if (whole(i)) {
+      Vec<T>::unpack(__ldg(reinterpret_cast<const uint4 *>(row + first + (ptrdiff_t)i * N)), f);
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const int id = first + i * N + e;
+        f[e] = id >= lo && id < hi ? to_f32(row[id]) : -INFINITY;
+      }
+    }
+  }
+  __device__ __forceinline__ bool has(int i, int e) const {
+    const int id = first + i * N + e;
+    return id >= lo && id < hi;
+  }
+};
+
+// Running sums of a thread relative to its own maximum (never below the lowest finite value, so that -inf tokens weigh 0).
+struct Sums {
+  float m = -3.402823466e38f, s = 0.f, t = 0.f;
+  __device__ __forceinline__ void raise(float m2) {
+    const float d = fmaxf(m - m2, -200.f), f = ex2(d * kLog2e);
+    t = f * fmaf(s, d, t);
+    s *= f;
+    m = m2;
+  }
+  __device__ __forceinline__ void add(float x) {
+    const float d = x - m, e = ex2(d * kLog2e);
+    s += e;
+    t = fmaf(e, fmaxf(d, -200.f), t);
+  }
+  __device__ __forceinline__ void merge(float m2, float s2, float t2) {
+    Sums o;
+    o.m = m2; o.s = s2; o.t = t2;
+    const float n = fmaxf(m, m2);
+    if (n > m) raise(n);
+    if (n > o.m) o.raise(n);
+    s += o.s;
+    t += o.t;
+  }
+};
+
+template <int THREADS> struct Shared {
+  float group_max[128];
+  float m[THREADS / 32], s[THREADS / 32], t[THREADS / 32];
+  int front[THREADS / 32];
+  u64 cand[kCand];
+  u64 list[kMaxTop];                   // the top tokens in order
+  float bound;
+  int n_cand, warp_n[THREADS / 32];
+};
+
+// The k-th largest value of a part whose candidates did not fit, by bisection on ordered(): counts of the tokens above a value,
+// each one pass.  Then the tokens above it (fewer than k) and, in ascending order until there are k, those equal to it.
+template <typename T, int THREADS>
+__device__ void select_slow(const Part<T> &p, int k, float bound, float top, Shared<THREADS> &sh) {
+  constexpr int N = Vec<T>::N;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  u32 lo = ordered(bound), hi = ordered(top);                          // at least k tokens >= lo; fewer than k > hi
+  u32 v = lo;
+  for (int step = 0; step < 34 && lo < hi; ++step) {
+    int n = 0;
+    const float at = unordered(v);
+    for (int i = threadIdx.x; i < p.pieces; i += THREADS) {
+      float f[N];
+      p.read(i, f);
+#pragma unroll
+      for (int e = 0; e < N; ++e) n += f[e] > at && p.has(i, e);
+    }
+    for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(0xFFFFFFFFu, n, o);
+    __syncthreads();
+    if (lane == 0) sh.warp_n[warp] = n;
+    __syncthreads();
+    int all = 0;
+    for (int w = 0; w < THREADS / 32; ++w) all += sh.warp_n[w];
+    if (all < k) hi = v;
+    else lo = v + 1;
+    v = lo + (hi - lo) / 2;
+  }
+  const float kth = unordered(lo);
+  __syncthreads();
+  if (threadIdx.x == 0) sh.n_cand = 0;
+  __syncthreads();
+  for (int i = threadIdx.x; i < p.pieces; i += THREADS) {
+    float f[N];
+    p.read(i, f);
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (f[e] > kth && p.has(i, e)) sh.cand[atomicAdd(&sh.n_cand, 1)] = key_of(f[e], p.first + i * N + e);
+  }
+  __syncthreads();
+  int got = sh.n_cand;
+  __syncthreads();
+  for (int i0 = 0; i0 < p.pieces && got < k; i0 += THREADS) {
+    const int i = i0 + threadIdx.x;
+    float f[N];
+    int n = 0;
+    if (i < p.pieces) {
+      p.read(i, f);
+#pragma unroll
+      for (int e = 0; e < N; ++e) n += f[e] == kth && p.has(i, e);
+    }
+    int upto = n;
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+      if (lane >= o) upto += x;
+    }
+    if (lane == 31) sh.warp_n[warp] = upto;
+    __syncthreads();
+    int at = got + upto - n, all = 0;
+    for (int w = 0; w < THREADS / 32; ++w) {
+      if (w < warp) at += sh.warp_n[w];
+      all += sh.warp_n[w];
+    }
+    if (n > 0) {
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (f[e] == kth && p.has(i, e)) {
+          if (at < k) sh.cand[at] = key_of(f[e], p.first + i * N + e);
+          ++at;
+        }
+    }
+    got = min(k, got + all);
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) sh.n_cand = got;
+  __syncthreads();
+}
+
+// The part's k first tokens (fewer if it has fewer; the rest of the list is 0, which no token's key is) into sh.list.
+template <typename T, int THREADS>
+__device__ void select_top(const Part<T> &p, int k, float mine, Shared<THREADS> &sh) {
+  constexpr int N = Vec<T>::N, GROUPS = 128, LANES = THREADS / GROUPS;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  float g = mine;
+#pragma unroll
+  for (int o = 1; o < LANES; o <<= 1) g = fmaxf(g, __shfl_xor_sync(0xFFFFFFFFu, g, o));
+  if (threadIdx.x % LANES == 0) sh.group_max[threadIdx.x / LANES] = g;
+  if (threadIdx.x == 0) sh.n_cand = 0;
+  __syncthreads();
+  if (threadIdx.x < GROUPS) {
+    const float x = sh.group_max[threadIdx.x];
+    int above = 0, same = 0;
+#pragma unroll 8
+    for (int i = 0; i < GROUPS / 4; ++i) {
+      const float4 y = reinterpret_cast<const float4 *>(sh.group_max)[i];
+      above += (y.x > x) + (y.y > x) + (y.z > x) + (y.w > x);
+      same += (y.x == x) + (y.y == x) + (y.z == x) + (y.w == x);
+    }
+    if (above < k && above + same >= k) sh.bound = x;
+  }
+  __syncthreads();
+  const float bound = sh.bound;
+  // each flagged thread's pieces are read by its whole warp
+  for (u32 flagged = __ballot_sync(0xFFFFFFFFu, mine >= bound && (int)threadIdx.x < p.pieces); flagged; flagged &= flagged - 1) {
+    const int owner = warp * 32 + __ffs(flagged) - 1;
+    for (int i = owner + lane * THREADS; i < p.pieces; i += 32 * THREADS) {
+      float f[N];
+      p.read(i, f);
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (f[e] >= bound && p.has(i, e)) {
+          const int at = atomicAdd(&sh.n_cand, 1);
+          if (at < kCand) sh.cand[at] = key_of(f[e], p.first + i * N + e);
+        }
+    }
+  }
+  __syncthreads();
+  if (sh.n_cand > kCand) {
+    float top = -INFINITY;
+    for (int i = 0; i < GROUPS; ++i) top = fmaxf(top, sh.group_max[i]);
+    select_slow<T, THREADS>(p, k, bound, top, sh);
+  }
+  const int n = sh.n_cand;
+  if (threadIdx.x < kMaxTop && (int)threadIdx.x >= n) sh.list[threadIdx.x] = 0;
+  for (int c = threadIdx.x; c < n; c += THREADS) {
+    const u64 x = sh.cand[c];
+    int place = 0;
+    for (int i = 0; i < n; ++i) place += sh.cand[i] > x;
+    if (place < k) sh.list[place] = x;
+  }
+  __syncthreads();
+}
+
+// One CTA a row.
+template <typename T, int THREADS>
+__global__ void __launch_bounds__(THREADS)
+logprobs_kernel(LogprobArgs a) {
+  constexpr int N = Vec<T>::N, U = 4;
+  __shared__ __align__(16) Shared<THREADS> sh;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const long long r = blockIdx.x;
+  const T *row = static_cast<const T *>(a.logits) + (size_t)r * a.V;
+  const Part<T> p(row, 0, a.V);
+  const int tok = a.tokens[r];
+  const bool given = tok >= 0 && tok < a.V;
+  const float xt = given ? to_f32(row[tok]) : 0.f;
+
+  Sums z;
+  float mine = -INFINITY;
+  int front = 0;
+  for (int i0 = threadIdx.x; i0 < p.pieces; i0 += THREADS * U) {
+    float f[U][N];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (i0 + u * THREADS < p.pieces) {
+        p.read(i0 + u * THREADS, f[u]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) f[u][e] = -INFINITY;
+      }
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < N; ++e) mx = fmaxf(mx, f[u][e]);
+    mine = fmaxf(mine, mx);
+    if (mx > z.m) z.raise(mx);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int id0 = p.first + (i0 + u * THREADS) * N;
+      if (i0 + u * THREADS >= p.pieces) continue;
+      const bool before = id0 + N <= tok;
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        z.add(f[u][e]);
+        front += before ? f[u][e] >= xt && id0 + e >= p.lo : f[u][e] > xt || (f[u][e] == xt && id0 + e < tok && id0 + e >= p.lo);
+      }
+    }
+  }
+  for (int o = 16; o > 0; o >>= 1) {
+    const float m2 = __shfl_xor_sync(0xFFFFFFFFu, z.m, o), s2 = __shfl_xor_sync(0xFFFFFFFFu, z.s, o), t2 = __shfl_xor_sync(0xFFFFFFFFu, z.t, o);
+    z.merge(m2, s2, t2);
+    front += __shfl_xor_sync(0xFFFFFFFFu, front, o);
+  }
+  if (lane == 0) { sh.m[warp] = z.m; sh.s[warp] = z.s; sh.t[warp] = z.t; sh.front[warp] = front; }
+  __syncthreads();
+  Sums all;
+  front = 0;
+  for (int w = 0; w < THREADS / 32; ++w) { all.merge(sh.m[w], sh.s[w], sh.t[w]); front += sh.front[w]; }
+  const bool none = !(all.s == all.s) || all.m == INFINITY;           // a NaN or +inf: no distribution
+  const float log_s = logf(all.s);
+  if (threadIdx.x == 0) {
+    a.logprob[r] = none || !given ? NAN : all.s > 0.f ? xt - all.m - log_s : -INFINITY;
+    a.entropy[r] = none ? NAN : all.s > 0.f ? log_s - all.t / all.s : 0.f;
+    a.rank[r] = none || !given ? -1 : front;
+  }
+  if (a.top == 0) return;
+  if (none) {
+    if ((int)threadIdx.x < a.top) { a.top_id[r * a.top + threadIdx.x] = -1; a.top_lp[r * a.top + threadIdx.x] = NAN; }
+    return;
+  }
+  select_top<T, THREADS>(p, a.top, mine, sh);
+  if ((int)threadIdx.x < a.top) {
+    const u64 x = sh.list[threadIdx.x];
+    const float l = unordered((u32)(x >> 32));
+    a.top_id[r * a.top + threadIdx.x] = (int)~(u32)x;
+    a.top_lp[r * a.top + threadIdx.x] = all.s > 0.f ? l - all.m - log_s : -INFINITY;
+  }
+}
+
+template <typename T> int run(const LogprobArgs &a, int rows, cudaStream_t s) {
+  if (a.V <= 4096) logprobs_kernel<T, 128><<<rows, 128, 0, s>>>(a);
+  else logprobs_kernel<T, 512><<<rows, 512, 0, s>>>(a);
+  hsd_count_launches(1);
+  return hsd_launch_status();
+}
+
+}  // namespace
+}  // namespace hsd
+
+extern "C" int hsd_token_logprobs(const void *logits, int dtype, int rows, int vocab, const int32_t *tokens, int top, float *out_logprobs,
+                                  float *out_entropy, int32_t *out_ranks, int32_t *out_top_tokens, float *out_top_logprobs, void *stream) {
+  using namespace hsd;
+  if (!logits || !tokens || !out_logprobs || !out_entropy || !out_ranks || rows <= 0 || vocab <= 0) return HSD_E_INVALID_ARG;
+  if (dtype != HSD_F32 && dtype != HSD_BF16) return HSD_E_INVALID_ARG;
+  if (top < 0 || top > kMaxTop || top > vocab || (top > 0 && (!out_top_tokens || !out_top_logprobs))) return HSD_E_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(logits) % (dtype == HSD_F32 ? 4 : 2)) return HSD_E_INVALID_ARG;
+  if (vocab > 0x7FFFFF00) return HSD_E_TOO_LARGE;
+  LogprobArgs a = {logits, tokens, out_logprobs, out_entropy, out_ranks, out_top_tokens, out_top_logprobs, vocab, top};
+  return dtype == HSD_F32 ? run<float>(a, rows, (cudaStream_t)stream) : run<__nv_bfloat16>(a, rows, (cudaStream_t)stream);
+}
