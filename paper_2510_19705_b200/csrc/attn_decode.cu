@@ -68,21 +68,20 @@ template <typename T, int HD> __device__ __forceinline__ u32 piece(int r, int c)
 }
 
 // The line of tiles: sequence b has as many for each of `items` (key head, chunk of query heads); before[b]: tiles of the
-// sequences in front of b, per item.
+// sequences in front of b, per item; lens[b]: keys.
 struct Line {
-  const int *before;
+  const int *before, *lens;
   int batch, items;
   long long per;                               // tiles of a warp
 };
-// Lengths within the page table's room, and the prefix sums; all threads of the CTA.
+// Lengths within the page table's room, and the prefix sums; all threads of the CTA.  lens may be null.
 template <int KEYS, int THREADS>
-__device__ __forceinline__ Line make_line(const int32_t *kv_lens, int batch, long long room, int items, int *before, int *warp_sum) {
+__device__ __forceinline__ Line make_line(const int32_t *kv_lens, int batch, long long room, int items, int *before, int *lens, int *warp_sum) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int carry = 0;
   for (int b0 = 0; b0 < batch; b0 += THREADS) {
     const int b = b0 + threadIdx.x;
-    int n = 0;
-    if (b < batch) n = (int)((min((long long)max(kv_lens[b], 0), room) + KEYS - 1) / KEYS);
+    const int len = b < batch ? (int)min((long long)max(kv_lens[b], 0), room) : 0, n = (len + KEYS - 1) / KEYS;
     int upto = n;
     for (int o = 1; o < 32; o <<= 1) {
       const int x = __shfl_up_sync(0xFFFFFFFFu, upto, o);
@@ -95,13 +94,16 @@ __device__ __forceinline__ Line make_line(const int32_t *kv_lens, int batch, lon
       if (w < warp) front += warp_sum[w];
       carry += warp_sum[w];
     }
-    if (b < batch) before[b + 1] = front + upto;
+    if (b < batch) {
+      before[b + 1] = front + upto;
+      if (lens) lens[b] = len;
+    }
     __syncthreads();
   }
   if (threadIdx.x == 0) before[0] = 0;
   __syncthreads();
   Line l;
-  l.before = before; l.batch = batch; l.items = items;
+  l.before = before; l.lens = lens; l.batch = batch; l.items = items;
   const long long total = (long long)carry * items, warps = kGrid * kWarps;
   l.per = max((total + warps - 1) / warps, (long long)kMinTiles);
   return l;
@@ -125,7 +127,9 @@ struct Place {
     tile = (int)(rest % tiles);
   }
   __device__ __forceinline__ void next(const Line &l) {
-    if (++tile < tiles) return;
+    if (++tile == tiles) next_item(l);
+  }
+  __device__ __forceinline__ void next_item(const Line &l) {           // b == batch behind the last
     tile = 0;
     if (++item < l.items) return;
     item = 0;
@@ -141,6 +145,8 @@ template <int HD> __device__ __forceinline__ float *part_at(float *parts, int ch
 }
 
 // ---------------------------------------------------------------------------- tiles into a warp's ring
+// Pages are looked up 32 at a time, a lane one: those of the window that the tiles come from, and, loaded a window ahead, those of the
+// next one (the sequence's next 32 pages, or the first of the item behind it).
 template <typename T, int HD> struct Feeder {
   using R = Ring<T, HD>;
   static constexpr int KEYS = Form<T>::KEYS;
@@ -148,23 +154,36 @@ template <typename T, int HD> struct Feeder {
   const Line &line;
   u32 ring;                                    // shared memory
   u32 *masks;                                  // per stage: keys of its tile that are there
-  Place at;                                    // tile whose rows are looked up next
-  long long left;                              // tiles not looked up yet
-  long long row;                               // of key `lane` of the tile that is copied next: its place in the pools, -1 without one
   int lane;
-  __device__ __forceinline__ void look_up() {
-    row = -1;
-    if (left <= 0) return;
-    --left;
-    const int key = at.tile * KEYS + lane;
-    if (lane < KEYS && key < min((long long)a.kv_lens[at.b], (long long)a.pages_per_seq * a.pool.page)) {
-      const int pg = a.page_table[(size_t)at.b * a.pages_per_seq + key / a.pool.page];
-      if (pg >= 0 && pg < a.pool.n_pages)
-        row = pg * a.pool.page_bytes + (key % a.pool.page) * a.pool.token_bytes + (long long)(at.item / a.chunks) * a.pool.head_bytes;
-    }
-    at.next(line);
+  Place at, ahead;                             // tile that is copied next; item of the next window
+  int base, ahead_base;                        // first page of the windows
+  int pages, ahead_pages;                      // the lane's
+
+  __device__ __forceinline__ int load(const Place &p, int from) const {
+    const int i = from + lane;
+    return p.b < line.batch && (long long)i * a.pool.page < line.lens[p.b] ? a.page_table[(size_t)p.b * a.pages_per_seq + i] : -1;
+  }
+  __device__ __forceinline__ void window_behind() {                    // of the one in `ahead`
+    if (((long long)ahead_base + 32) * a.pool.page < line.lens[ahead.b]) ahead_base += 32;
+    else { ahead.next_item(line); ahead_base = 0; }
+    ahead_pages = load(ahead, ahead_base);
+  }
+  __device__ __forceinline__ void begin(const Place &from) {
+    at = ahead = from;
+    base = ahead_base = from.tile * KEYS / a.pool.page / 32 * 32;
+    pages = load(at, base);
+    window_behind();
   }
   __device__ __forceinline__ void copy(int stage) {
+    const int key = at.tile * KEYS + lane, pg = key / a.pool.page;
+    int rel = pg - base;
+    // a tile has at most 16 pages, so they lie in this window and the next
+    int id = __shfl_sync(0xFFFFFFFFu, pages, rel & 31);
+    const int other = __shfl_sync(0xFFFFFFFFu, ahead_pages, rel & 31);
+    if (rel >= 32) id = other;
+    long long row = -1;                        // of key `lane`: its place in the pools, -1 without one
+    if (lane < KEYS && key < line.lens[at.b] && id >= 0 && id < a.pool.n_pages)
+      row = id * a.pool.page_bytes + (key - pg * a.pool.page) * a.pool.token_bytes + (at.item / a.chunks) * a.pool.head_bytes;
     const u32 to = ring + stage * R::STAGE;
     const u32 there = __ballot_sync(0xFFFFFFFFu, row >= 0);
     constexpr int PIECES = R::ROW / 16, AT_ONCE = 32 / PIECES;         // rows that the warp copies at once
@@ -179,6 +198,21 @@ template <typename T, int HD> struct Feeder {
       copy16(to + R::HALF + piece<T, HD>(r, c), a.pool.v + from, ok);
     }
     if (lane == 0) masks[stage] = there;
+    at.next(line);
+    if (at.tile == 0) {
+      if (at.b >= line.batch) return;          // the line's end
+      shift();
+      const int h = at.item / a.chunks, q0 = h * a.group + at.item % a.chunks * a.chunk;     // the next item's queries into L1
+      const unsigned char *q = static_cast<const unsigned char *>(a.q) + ((size_t)at.b * a.nq + q0) * HD * sizeof(T);
+      if (lane * 128 < min(a.chunk, h * a.group + a.group - q0) * HD * (int)sizeof(T)) asm volatile("prefetch.global.L1 [%0];" ::"l"(q + lane * 128));
+    } else if ((long long)at.tile * KEYS >= ((long long)base + 32) * a.pool.page) {
+      shift();
+    }
+  }
+  __device__ __forceinline__ void shift() {
+    base = ahead_base;
+    pages = ahead_pages;
+    if (ahead.b < line.batch) window_behind();
   }
 };
 
@@ -387,7 +421,7 @@ template <typename T, int HD> struct TileOf { using type = Bf16Tile<HD>; };
 template <int HD> struct TileOf<float, HD> { using type = Fp32Tile<HD>; };
 template <typename T, int HD> constexpr int kQueryBytes = sizeof(T) == 4 ? Form<T>::HEADS * HD * 4 : 0;     // a warp's, in shared memory
 template <typename T, int HD> constexpr int smem_bytes(int batch) {
-  return kWarps * (Ring<T, HD>::BYTES + kQueryBytes<T, HD>) + kWarps * Ring<T, HD>::STAGES * 4 + kWarps * 4 + (batch + 1) * 4;
+  return kWarps * (Ring<T, HD>::BYTES + kQueryBytes<T, HD>) + kWarps * Ring<T, HD>::STAGES * 4 + kWarps * 4 + (2 * batch + 1) * 4;
 }
 
 template <typename T, int HD>
@@ -399,15 +433,17 @@ attn_decode_kernel(DecodeArgs a) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   unsigned char *rest = smem + kWarps * (R::BYTES + kQueryBytes<T, HD>);
   u32 *masks = reinterpret_cast<u32 *>(rest) + warp * S;
-  int *warp_sum = reinterpret_cast<int *>(rest) + kWarps * S, *before = warp_sum + kWarps;
-  const Line line = make_line<Form<T>::KEYS, kThreads>(a.kv_lens, a.batch, (long long)a.pages_per_seq * a.pool.page, a.nkv * a.chunks, before, warp_sum);
+  int *warp_sum = reinterpret_cast<int *>(rest) + kWarps * S, *before = warp_sum + kWarps, *lens = before + a.batch + 1;
+  chain_wait();
+  chain_next();                                // (behind the wait: the join reads the lengths ahead of its own)
+  const Line line = make_line<Form<T>::KEYS, kThreads>(a.kv_lens, a.batch, (long long)a.pages_per_seq * a.pool.page, a.nkv * a.chunks, before, lens, warp_sum);
 
   // sequences without a key: zeros
   for (int b = blockIdx.x; b < a.batch; b += gridDim.x)
     if (before[b + 1] == before[b])
       for (int i = threadIdx.x; i < a.nq * HD; i += kThreads) static_cast<T *>(a.out)[(size_t)b * a.nq * HD + i] = T(0.f);
 
-  const int me = blockIdx.x * kWarps + warp;
+  const int me = warp * kGrid + blockIdx.x;    // few stretches lie on as many SMs
   const long long total = (long long)before[a.batch] * line.items, from = me * line.per, n = min(line.per, total - from);
   if (n <= 0) return;
   typename TileOf<T, HD>::type t;
@@ -415,11 +451,11 @@ attn_decode_kernel(DecodeArgs a) {
   if constexpr (sizeof(T) == 4) t.q = reinterpret_cast<float *>(smem + kWarps * R::BYTES) + warp * Form<T>::HEADS * HD;
   Place at;
   at.find(line, from);
-  Feeder<T, HD> feed = {a, line, (u32)__cvta_generic_to_shared(smem) + warp * R::BYTES, masks, at, n, -1, lane};
-  feed.look_up();
+  Feeder<T, HD> feed = {a, line, (u32)__cvta_generic_to_shared(smem) + warp * R::BYTES, masks, lane};
+  feed.begin(at);
 #pragma unroll
   for (int i = 0; i < S - 1; ++i) {
-    if (i < n) { feed.copy(i); feed.look_up(); }
+    if (i < n) feed.copy(i);
     copies_end();
   }
   int stage = 0, fill = S - 1, first = at.tile;
@@ -427,7 +463,7 @@ attn_decode_kernel(DecodeArgs a) {
   for (long long i = 0; i < n; ++i) {
     copies_wait<S - 2>();
     __syncwarp();
-    if (i + S - 1 < n) { feed.copy(fill); feed.look_up(); }
+    if (i + S - 1 < n) feed.copy(fill);
     copies_end();
     t.tile(a, feed.ring + stage * R::STAGE, masks[stage]);
     if (++stage == S) stage = 0;
@@ -449,9 +485,11 @@ attn_join_kernel(DecodeArgs a) {
   constexpr int COLS = HD / 32;
   extern __shared__ int before[];
   __shared__ int warp_sum[kJoinWarps];
-  __shared__ float sh_o[kJoinWarps][HD], sh_l[kJoinWarps];
+  __shared__ float sh_o[kJoinWarps][HD], sh_m[kJoinWarps], sh_l[kJoinWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const Line line = make_line<Form<T>::KEYS, kJoinWarps * 32>(a.kv_lens, a.batch, (long long)a.pages_per_seq * a.pool.page, a.nkv * a.chunks, before, warp_sum);
+  const Line line = make_line<Form<T>::KEYS, kJoinWarps * 32>(a.kv_lens, a.batch, (long long)a.pages_per_seq * a.pool.page, a.nkv * a.chunks, before, nullptr, warp_sum);
+  chain_wait();
+  chain_next();
   for (long long x = blockIdx.x; x < (long long)a.batch * a.nq; x += gridDim.x) {
     const int b = (int)(x / a.nq), hq = (int)(x % a.nq), h = hq / a.group, c = hq % a.group / a.chunk, g = hq % a.group % a.chunk;
     const int tiles = before[b + 1] - before[b];
@@ -459,30 +497,34 @@ attn_join_kernel(DecodeArgs a) {
     const long long from = (long long)before[b] * line.items + (long long)(h * a.chunks + c) * tiles;
     const int w0 = (int)(from / line.per), w1 = (int)((from + tiles - 1) / line.per);
     if (w0 == w1) continue;                    // one warp had all of it
-    float m = -INFINITY;
-    auto stat = [&](int w) { return *reinterpret_cast<const float2 *>(part_at<HD>(a.parts, a.chunk, w, w * line.per > from ? 0 : 1) + a.chunk * HD + g * 2); };
-    for (int w = w0 + lane; w <= w1; w += 32) m = fmaxf(m, stat(w).x);
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-    const float ref = m > -INFINITY ? m : 0.f;
-    float o[COLS], l = 0.f;
+    float o[COLS], l = 0.f, m = -INFINITY;
 #pragma unroll
     for (int e = 0; e < COLS; ++e) o[e] = 0.f;
 #pragma unroll 4
     for (int w = w0 + warp; w <= w1; w += kJoinWarps) {
-      const float *p = part_at<HD>(a.parts, a.chunk, w, w * line.per > from ? 0 : 1) + g * HD + lane * COLS;
-      const float2 ml = stat(w);
-      const float f = ex2(ml.x - ref);
-      l = fmaf(ml.y, f, l);
+      const float *p = part_at<HD>(a.parts, a.chunk, w, w * line.per > from ? 0 : 1);
+      const float2 ml = *reinterpret_cast<const float2 *>(p + a.chunk * HD + g * 2);
+      const float n = fmaxf(m, ml.x), ref = n > -INFINITY ? n : 0.f, f = ex2(m - ref), f2 = ex2(ml.x - ref);
+      m = n;
+      l = fmaf(l, f, ml.y * f2);
 #pragma unroll
-      for (int e = 0; e < COLS; ++e) o[e] = fmaf(p[e], f, o[e]);
+      for (int e = 0; e < COLS; ++e) o[e] = fmaf(o[e], f, p[g * HD + lane * COLS + e] * f2);
     }
 #pragma unroll
     for (int e = 0; e < COLS; ++e) sh_o[warp][lane * COLS + e] = o[e];
-    if (lane == 0) sh_l[warp] = l;
+    if (lane == 0) { sh_m[warp] = m; sh_l[warp] = l; }
     __syncthreads();
     for (int i = threadIdx.x; i < HD; i += kJoinWarps * 32) {
-      float sum = 0.f, all = 0.f;
-      for (int w = 0; w < kJoinWarps; ++w) { sum += sh_o[w][i]; all += sh_l[w]; }
+      float top = -INFINITY, sum = 0.f, all = 0.f;
+#pragma unroll
+      for (int w = 0; w < kJoinWarps; ++w) top = fmaxf(top, sh_m[w]);
+      const float ref = top > -INFINITY ? top : 0.f;
+#pragma unroll
+      for (int w = 0; w < kJoinWarps; ++w) {
+        const float f = ex2(sh_m[w] - ref);
+        sum = fmaf(sh_o[w][i], f, sum);
+        all = fmaf(sh_l[w], f, all);
+      }
       const float y = all != 0.f ? sum / all : 0.f;
       if constexpr (sizeof(T) == 4) static_cast<float *>(a.out)[((size_t)b * a.nq + hq) * HD + i] = y;
       else static_cast<__nv_bfloat16 *>(a.out)[((size_t)b * a.nq + hq) * HD + i] = __float2bfloat16_rn(y);
@@ -495,9 +537,9 @@ template <typename T, int HD> int run(const DecodeArgs &a, cudaStream_t s) {
   static std::atomic<u64> done{0};
   const int status = hsd_smem_limit((const void *)attn_decode_kernel<T, HD>, smem_bytes<T, HD>(kMaxBatch), done);
   if (status) return status;
-  attn_decode_kernel<T, HD><<<kGrid, kThreads, smem_bytes<T, HD>(a.batch), s>>>(a);
+  HSD_CUDA_OK(hsd_launch(attn_decode_kernel<T, HD>, dim3(kGrid), kThreads, smem_bytes<T, HD>(a.batch), s, 0, true, a));
   const long long heads = (long long)a.batch * a.nq;
-  attn_join_kernel<T, HD><<<(unsigned)(heads < 8 * kGrid ? heads : 8 * kGrid), kJoinWarps * 32, (a.batch + 1) * 4, s>>>(a);
+  HSD_CUDA_OK(hsd_launch(attn_join_kernel<T, HD>, dim3((unsigned)(heads < 8 * kGrid ? heads : 8 * kGrid)), kJoinWarps * 32, (a.batch + 1) * 4, s, 0, true, a));
   hsd_count_launches(2);
   return hsd_launch_status();
 }
