@@ -1,6 +1,6 @@
 // Attention of one new token per sequence over the caller's paged cache (hsd_paged_attention).
 //   o = sum_j w_j v_j / sum_j w_j,  w_j = exp(scale q.k_j - m),  m = max_j scale q.k_j   over the sequence's keys j
-// Bound by memory: every key and value is read once, for all query heads of its group.  The tiles (16 or 8 keys of one sequence
+// Bound by memory: every key and value is read once, for all query heads of its group.  The tiles (8 to 32 keys of one sequence
 // and head) of the whole batch stand in one line, which is divided evenly over the warps, whatever the lengths are: the grid
 // does not depend on them, and they are read on the device.  A warp streams its stretch through a ring of its own in shared memory
 // (cp.async, no barrier between warps), across the borders of sequences and heads.  Where a stretch ends inside a sequence, the parts
@@ -8,7 +8,8 @@
 // attn_join_kernel adds those in order.
 // bf16: both products on mma.sync with the group's queries as the 16 rows of a tile (at 4 to 16 queries a key the tensor pipe is
 // far from its limit); weights as bf16 high and low parts, so that only the final rounding is one of 8 bits.
-// fp32: the products in fp32, four lanes a key for the scores, a lane a few columns for the output.
+// fp32: both products on mma.sync in TF32, each factor as two TF32 parts (x = high + low to 2^-21) and the three products of them that
+// count: the same tile of 8 queries for any group, where products in fp32 read every query again from shared memory for each key.
 #include <math.h>
 
 #include "paged.cuh"
@@ -19,7 +20,7 @@ namespace {
 constexpr int kWarps = 8, kThreads = kWarps * 32;
 constexpr int kGrid = kMeasuredSMs;            // CTAs at most: fixed, as the workspace's size depends on it
 constexpr int kMaxBatch = 4096;                // its tiles' prefix sums lie in shared memory
-constexpr int kJoinWarps = 8;
+constexpr int kJoinWarps = 16;
 
 struct DecodeArgs {
   const void *q;
@@ -29,16 +30,17 @@ struct DecodeArgs {
   int4 *joins;                                 // per CTA: the item that it begins inside of, if it is the second with a part of it
   PoolView pool;
   float scale;                                 // times log2(e)
-  int batch, nq, nkv, pages_per_seq;
+  int batch, nq, nkv, pages_per_seq, page_shift;        // log2 of the page size, or -1
   int group, chunk, chunks;                    // query heads of a key head; of them at once; times
 };
 
-template <typename T> struct Form;
-template <> struct Form<__nv_bfloat16> { static constexpr int KEYS = 16, HEADS = 16; };        // query heads at once, at most
-template <> struct Form<float> { static constexpr int KEYS = 8, HEADS = 8; };
+// Keys of a tile (8 KB of keys and values, 4 KB for heads of 32) and query heads of one pass over them at most.
+template <typename T, int HD> struct Form {
+  static constexpr int KEYS = (HD == 128 ? 16 : 32) / ((int)sizeof(T) / 2), HEADS = sizeof(T) == 4 ? 8 : 16;
+};
 template <typename T, int HD> struct Ring {
-  static constexpr int ROW = HD * (int)sizeof(T), HALF = Form<T>::KEYS * ROW, STAGE = 2 * HALF;    // keys, then values
-  static constexpr int STAGES = (sizeof(T) == 4 ? 16384 : 24576) / STAGE, BYTES = STAGE * STAGES;  // (fp32 has its queries beside it)
+  static constexpr int ROW = HD * (int)sizeof(T), HALF = Form<T, HD>::KEYS * ROW, STAGE = 2 * HALF;    // keys, then values
+  static constexpr int STAGES = 24576 / STAGE, BYTES = STAGE * STAGES;
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -55,6 +57,21 @@ __device__ __forceinline__ void mma(float *c, const u32 *a, u32 b0, u32 b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void mma_tf32(float *c, const u32 *a, u32 b0, u32 b1) {
+  asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// x = high + low to 2^-21: high cut off, what is left rounded, to the 11 bits of TF32 (four operations; the conversion has a quarter of
+// their rate).
+__device__ __forceinline__ void split(float x, u32 &high, u32 &low) {
+  high = __float_as_uint(x) & 0xFFFFE000u;
+  low = (__float_as_uint(x - __uint_as_float(high)) + 0x1000u) & 0xFFFFE000u;
+}
+__device__ __forceinline__ float4 lds4(u32 at) {
+  float4 v;
+  asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+  return v;
+}
 __device__ __forceinline__ void ldsm4(u32 *r, u32 at) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
 }
@@ -63,21 +80,24 @@ __device__ __forceinline__ void ldsm4t(u32 *r, u32 at) {
 }
 // Byte of 16-byte piece c of row r of a tile: permuted so that the pieces a quarter warp reads together lie in different banks.
 template <typename T, int HD> __device__ __forceinline__ u32 piece(int r, int c) {
-  if constexpr (sizeof(T) == 4) return r * (HD * 4) + ((c ^ ((r & 1) << 2)) << 4);
+  if constexpr (sizeof(T) == 4) return r * (HD * 4) + ((c ^ ((r & 1) << 2) ^ (r & 6)) << 4);
   else if constexpr (HD == 32) return r * 64 + ((c ^ ((r >> 1) & 3)) << 4);
   else return r * (HD * 2) + ((c ^ (r & 7)) << 4);
 }
 
 // The line of tiles: sequence b has as many for each of `items` (key head, chunk of query heads); before[b]: tiles of the
 // sequences in front of b, per item; lens[b]: keys.
+__device__ __forceinline__ long long divide(long long a, long long b) {          // (32 bits do nearly always, in a fourth of the time)
+  return ((a | b) >> 31) == 0 ? (long long)((u32)a / (u32)b) : a / b;
+}
 struct Line {
   const int *before, *lens;
   int batch, items, stretches;
-  long long per;                               // tiles of a stretch
+  long long total, per;                        // tiles; of a stretch
   // Stretches [first(c), first(c + 1)) are CTA c's: few of them lie on as many SMs, and no CTA without one stands between others.
   __device__ __forceinline__ int first(int cta) const { return stretches < kGrid ? min(cta, stretches) : cta * stretches / kGrid; }
   __device__ __forceinline__ int cta_of(long long tile) const {
-    const int i = (int)(tile / per);
+    const int i = (int)divide(tile, per);
     return stretches < kGrid ? i : ((i + 1) * kGrid - 1) / stretches;
   }
 };
@@ -86,7 +106,21 @@ template <int KEYS, int THREADS>
 __device__ __forceinline__ Line make_line(const int32_t *kv_lens, int batch, long long room, int items, int *before, int *lens, int *warp_sum) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int carry = 0;
-  for (int b0 = 0; b0 < batch; b0 += THREADS) {
+  if (batch <= 32) {                           // every warp for itself: all of them write the same
+    const int len = lane < batch ? (int)min((long long)max(kv_lens[lane], 0), room) : 0, n = (len + KEYS - 1) / KEYS;
+    int upto = n;
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+      if (lane >= o) upto += x;
+    }
+    carry = __shfl_sync(0xFFFFFFFFu, upto, 31);
+    if (lane < batch) {
+      before[lane + 1] = upto;
+      lens[lane] = len;
+    }
+    if (lane == 0) before[0] = 0;
+    __syncwarp();
+  } else for (int b0 = 0; b0 < batch; b0 += THREADS) {
     const int b = b0 + threadIdx.x;
     const int len = b < batch ? (int)min((long long)max(kv_lens[b], 0), room) : 0, n = (len + KEYS - 1) / KEYS;
     int upto = n;
@@ -105,15 +139,15 @@ __device__ __forceinline__ Line make_line(const int32_t *kv_lens, int batch, lon
       before[b + 1] = front + upto;
       lens[b] = len;
     }
+    if (threadIdx.x == 0) before[0] = 0;
     __syncthreads();
   }
-  if (threadIdx.x == 0) before[0] = 0;
-  __syncthreads();
   Line l;
   l.before = before; l.lens = lens; l.batch = batch; l.items = items;
   const long long total = (long long)carry * items, warps = kGrid * kWarps;
-  l.per = max((total + warps - 1) / warps, 1ll);
-  l.stretches = (int)((total + l.per - 1) / l.per);
+  l.total = total;
+  l.per = max(divide(total + warps - 1, warps), 1ll);
+  l.stretches = (int)divide(total + l.per - 1, l.per);
   return l;
 }
 
@@ -121,7 +155,7 @@ __device__ __forceinline__ Line make_line(const int32_t *kv_lens, int batch, lon
 struct Place {
   int b, item, tile, tiles;                    // tiles: of the sequence
   __device__ __forceinline__ void find(const Line &l, long long at) {
-    const int per_item = (int)(at / l.items);  // before[b] <= per_item < before[b + 1]
+    const int per_item = (int)divide(at, l.items);  // before[b] <= per_item < before[b + 1]
     int lo = 0, hi = l.batch - 1;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
@@ -131,8 +165,8 @@ struct Place {
     b = lo;
     tiles = l.before[b + 1] - l.before[b];
     const long long rest = at - (long long)l.before[b] * l.items;
-    item = (int)(rest / tiles);
-    tile = (int)(rest % tiles);
+    item = (int)divide(rest, tiles);
+    tile = (int)(rest - (long long)item * tiles);
   }
   __device__ __forceinline__ void next(const Line &l) {
     if (++tile == tiles) next_item(l);
@@ -157,7 +191,7 @@ template <int HD> __device__ __forceinline__ float *cta_part(float *parts, int c
 // next one (the sequence's next 32 pages, or the first of the item behind it).
 template <typename T, int HD> struct Feeder {
   using R = Ring<T, HD>;
-  static constexpr int KEYS = Form<T>::KEYS;
+  static constexpr int KEYS = Form<T, HD>::KEYS, PIECES = R::ROW / 16, AT_ONCE = 32 / PIECES;          // rows that the warp copies at once
   const DecodeArgs &a;
   const Line &line;
   u32 ring;                                    // shared memory
@@ -166,7 +200,14 @@ template <typename T, int HD> struct Feeder {
   Place at, ahead;                             // tile that is copied next; item of the next window
   int base, ahead_base;                        // first page of the windows
   int pages, ahead_pages;                      // the lane's
+  int len;                                     // of the sequence
+  long long head, mine;                        // the head's place in the pools; the lane's in the rows that are copied at once
 
+  __device__ __forceinline__ int page_of(int key) const { return a.page_shift >= 0 ? key >> a.page_shift : key / a.pool.page; }
+  __device__ __forceinline__ void item_begins() {
+    len = line.lens[at.b];
+    head = (at.item / a.chunks) * a.pool.head_bytes;
+  }
   __device__ __forceinline__ int load(const Place &p, int from) const {
     const int i = from + lane;
     return p.b < line.batch && (long long)i * a.pool.page < line.lens[p.b] ? a.page_table[(size_t)p.b * a.pages_per_seq + i] : -1;
@@ -178,38 +219,61 @@ template <typename T, int HD> struct Feeder {
   }
   __device__ __forceinline__ void begin(const Place &from) {
     at = ahead = from;
-    base = ahead_base = from.tile * KEYS / a.pool.page / 32 * 32;
+    base = ahead_base = page_of(from.tile * KEYS) / 32 * 32;
     pages = load(at, base);
     window_behind();
+    mine = lane / PIECES * a.pool.token_bytes + lane % PIECES * 16;
+    item_begins();
   }
-  __device__ __forceinline__ void copy(int stage) {
-    const int key = at.tile * KEYS + lane, pg = key / a.pool.page;
-    int rel = pg - base;
-    // a tile has at most 16 pages, so they lie in this window and the next
+  // Place in the pools of a key of the tile, -1 without one.
+  __device__ __forceinline__ long long place(int key, bool wanted) const {
+    const int pg = page_of(key), rel = pg - base;
+    // a tile has at most 32 pages, so they lie in this window and the next
     int id = __shfl_sync(0xFFFFFFFFu, pages, rel & 31);
     const int other = __shfl_sync(0xFFFFFFFFu, ahead_pages, rel & 31);
     if (rel >= 32) id = other;
-    long long row = -1;                        // of key `lane`: its place in the pools, -1 without one
-    if (lane < KEYS && key < line.lens[at.b] && id >= 0 && id < a.pool.n_pages)
-      row = id * a.pool.page_bytes + (key - pg * a.pool.page) * a.pool.token_bytes + (at.item / a.chunks) * a.pool.head_bytes;
+    return wanted && key < len && id >= 0 && id < a.pool.n_pages ? id * a.pool.page_bytes + (key - pg * a.pool.page) * a.pool.token_bytes + head : -1;
+  }
+  __device__ __forceinline__ void copy(int stage) {
     const u32 to = ring + stage * R::STAGE;
-    const u32 there = __ballot_sync(0xFFFFFFFFu, row >= 0);
-    constexpr int PIECES = R::ROW / 16, AT_ONCE = 32 / PIECES;         // rows that the warp copies at once
-    const int c = lane % PIECES;
+    const int key0 = at.tile * KEYS, rest = len - key0, c = lane % PIECES;
+    u32 there;
+    if (a.pool.page % 8 == 0) {                // eight keys in one page: lane b has the place of the b-th eight
+      const long long p = place(key0 + 8 * (lane & 3), lane < KEYS / 8);
+      there = 0;
 #pragma unroll
-    for (int i = 0; i < KEYS / AT_ONCE; ++i) {
-      const int r = i * AT_ONCE + lane / PIECES;
-      const long long off = __shfl_sync(0xFFFFFFFFu, row, r);
-      const bool ok = off >= 0;
-      const long long from = ok ? off + c * 16 : 0;
-      copy16(to + piece<T, HD>(r, c), a.pool.k + from, ok);
-      copy16(to + R::HALF + piece<T, HD>(r, c), a.pool.v + from, ok);
+      for (int b = 0; b < KEYS / 8; ++b) {
+        const long long block = __shfl_sync(0xFFFFFFFFu, p, b);
+        there |= block >= 0 ? 0xFFu << (8 * b) : 0u;
+#pragma unroll
+        for (int i = 0; i < 8 / AT_ONCE; ++i) {
+          const int r = b * 8 + i * AT_ONCE + lane / PIECES;
+          const bool ok = block >= 0 && r < rest;
+          const long long from = ok ? block + i * AT_ONCE * a.pool.token_bytes + mine : 0;
+          copy16(to + piece<T, HD>(r, c), a.pool.k + from, ok);
+          copy16(to + R::HALF + piece<T, HD>(r, c), a.pool.v + from, ok);
+        }
+      }
+      if (rest < 32) there &= (1u << rest) - 1;
+    } else {                                   // lane i has the place of key i
+      const long long p = place(key0 + lane, lane < KEYS);
+      there = __ballot_sync(0xFFFFFFFFu, p >= 0);
+#pragma unroll
+      for (int i = 0; i < KEYS / AT_ONCE; ++i) {
+        const int r = i * AT_ONCE + lane / PIECES;
+        const long long row = __shfl_sync(0xFFFFFFFFu, p, r);
+        const bool ok = row >= 0;
+        const long long from = ok ? row + c * 16 : 0;
+        copy16(to + piece<T, HD>(r, c), a.pool.k + from, ok);
+        copy16(to + R::HALF + piece<T, HD>(r, c), a.pool.v + from, ok);
+      }
     }
     if (lane == 0) masks[stage] = there;
     at.next(line);
     if (at.tile == 0) {
       if (at.b >= line.batch) return;          // the line's end
       shift();
+      item_begins();
       const int h = at.item / a.chunks, q0 = h * a.group + at.item % a.chunks * a.chunk;     // the next item's queries into L1
       const unsigned char *q = static_cast<const unsigned char *>(a.q) + ((size_t)at.b * a.nq + q0) * HD * sizeof(T);
       if (lane * 128 < min(a.chunk, h * a.group + a.group - q0) * HD * (int)sizeof(T)) asm volatile("prefetch.global.L1 [%0];" ::"l"(q + lane * 128));
@@ -252,48 +316,59 @@ template <int HD, int H> struct Bf16Tile {     // H: 8 or 16 rows with queries
     l[0] = l[1] = 0.f;
   }
   __device__ __forceinline__ void tile(const DecodeArgs &a, u32 at, u32 there) {
-    float s[2][4];
+    constexpr int KB = Form<T, HD>::KEYS / 16;                         // blocks of 16 keys
+    float s[2 * KB][4];
 #pragma unroll
-    for (int x = 0; x < 4; ++x) s[0][x] = s[1][x] = 0.f;
+    for (int n = 0; n < 2 * KB; ++n)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) s[n][x] = 0.f;
     const int kr = (lane & 7) + ((lane >> 4) << 3), kc = (lane >> 3) & 1;
 #pragma unroll
-    for (int k = 0; k < HD / 16; ++k) {
-      u32 f[4];
-      ldsm4(f, at + piece<T, HD>(kr, 2 * k + kc));
-      mma(s[0], qf[k], f[0], f[1]);
-      mma(s[1], qf[k], f[2], f[3]);
-    }
+    for (int k = 0; k < HD / 16; ++k)
+#pragma unroll
+      for (int b = 0; b < KB; ++b) {
+        u32 f[4];
+        ldsm4(f, at + piece<T, HD>(b * 16 + kr, 2 * k + kc));
+        mma(s[2 * b], qf[k], f[0], f[1]);
+        mma(s[2 * b + 1], qf[k], f[2], f[3]);
+      }
     const int col = (lane & 3) * 2;
     float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-    for (int n = 0; n < 2; ++n)
+    for (int n = 0; n < 2 * KB; ++n)
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
+      for (int x = 0; x < 2 * YS; ++x) {
         s[n][x] = (there >> (n * 8 + col + (x & 1))) & 1 ? s[n][x] * a.scale : -INFINITY;
         mx[x >> 1] = fmaxf(mx[x >> 1], s[n][x]);
       }
-    u32 hi[4] = {0, 0, 0, 0}, lo[4] = {0, 0, 0, 0};
+    u32 hi[KB][4], lo[KB][4];
     float f[2] = {1.f, 1.f};
+    bool grown = false;
 #pragma unroll
-    for (int y = 0; y < YS; ++y) {
+    for (int y = 0; y < 2; ++y) {
+      if (y >= YS) {
+#pragma unroll
+        for (int b = 0; b < KB; ++b) hi[b][y] = hi[b][2 + y] = lo[b][y] = lo[b][2 + y] = 0;
+        continue;
+      }
       mx[y] = fmaxf(mx[y], __shfl_xor_sync(0xFFFFFFFFu, mx[y], 1));
       mx[y] = fmaxf(mx[y], __shfl_xor_sync(0xFFFFFFFFu, mx[y], 2));
-      const float n = fmaxf(m[y], mx[y]);
-      f[y] = n > -INFINITY ? ex2(m[y] - n) : 1.f;
+      const float n = fmaxf(m[y], mx[y]), ref = n > -INFINITY ? n : 0.f;
+      f[y] = ex2(m[y] - ref);
+      grown |= n > m[y];
       m[y] = n;
-      const float ref = n > -INFINITY ? n : 0.f;
       l[y] *= f[y];
 #pragma unroll
-      for (int n2 = 0; n2 < 2; ++n2) {
+      for (int n2 = 0; n2 < 2 * KB; ++n2) {
         const float p0 = ex2(s[n2][2 * y] - ref), p1 = ex2(s[n2][2 * y + 1] - ref);
         l[y] += p0 + p1;
         const __nv_bfloat162 h2 = __floats2bfloat162_rn(p0, p1);
         const __nv_bfloat162 l2 = __floats2bfloat162_rn(p0 - __low2float(h2), p1 - __high2float(h2));
-        hi[n2 * 2 + y] = *reinterpret_cast<const u32 *>(&h2);
-        lo[n2 * 2 + y] = *reinterpret_cast<const u32 *>(&l2);
+        hi[n2 / 2][n2 % 2 * 2 + y] = *reinterpret_cast<const u32 *>(&h2);
+        lo[n2 / 2][n2 % 2 * 2 + y] = *reinterpret_cast<const u32 *>(&l2);
       }
     }
-    if (__any_sync(0xFFFFFFFFu, f[0] != 1.f || f[1] != 1.f)) {
+    if (__any_sync(0xFFFFFFFFu, grown)) {
 #pragma unroll
       for (int n = 0; n < HD / 8; ++n) {
         o[n][0] *= f[0]; o[n][1] *= f[0];
@@ -303,14 +378,16 @@ template <int HD, int H> struct Bf16Tile {     // H: 8 or 16 rows with queries
     const u32 v = at + Ring<T, HD>::HALF;
     const int vr = lane & 15, vc = lane >> 4;
 #pragma unroll
-    for (int n = 0; n < HD / 16; ++n) {
-      u32 b[4];
-      ldsm4t(b, v + piece<T, HD>(vr, 2 * n + vc));
-      mma(o[2 * n], hi, b[0], b[1]);
-      mma(o[2 * n + 1], hi, b[2], b[3]);
-      mma(o[2 * n], lo, b[0], b[1]);
-      mma(o[2 * n + 1], lo, b[2], b[3]);
-    }
+    for (int b = 0; b < KB; ++b)
+#pragma unroll
+      for (int n = 0; n < HD / 16; ++n) {
+        u32 x[4];
+        ldsm4t(x, v + piece<T, HD>(b * 16 + vr, 2 * n + vc));
+        mma(o[2 * n], hi[b], x[0], x[1]);
+        mma(o[2 * n + 1], hi[b], x[2], x[3]);
+        mma(o[2 * n], lo[b], x[0], x[1]);
+        mma(o[2 * n + 1], lo[b], x[2], x[3]);
+      }
   }
   __device__ __forceinline__ void end(const DecodeArgs &a, int b, int item, bool whole, float *part) {
     const int h = item / a.chunks, c = item % a.chunks, heads = min(a.chunk, a.group - c * a.chunk), col = (lane & 3) * 2;
@@ -336,103 +413,127 @@ template <int HD, int H> struct Bf16Tile {     // H: 8 or 16 rows with queries
 };
 
 // ---------------------------------------------------------------------------- fp32
-template <int HD, int H> struct Fp32Tile {     // H: queries at once; those past the chunk's are zeros
+// A lane's four values of a 16-byte piece are its k = j and j + 4 of two steps (keys) or its columns of four tiles (values): any order
+// of k will do that both factors have, and of columns that the output is written in.
+template <int HD> struct Fp32Tile {
   using T = float;
-  static constexpr int KEYS = 8, HEADS = H, COLS = HD / 32;
-  float o[HEADS][COLS], m[HEADS], l[HEADS];
-  float *q;                                    // the warp's queries in shared memory [HEADS][HD]
-  int lane, heads;
+  u32 qh[HD / 8][2], ql[HD / 8][2];            // rows 8 to 15 of the tile are zeros
+  float o[HD / 8][4], m, l;
+  int lane;
 
   __device__ __forceinline__ void begin(const DecodeArgs &a, int b, int item) {
-    const int h = item / a.chunks, c = item % a.chunks;
-    heads = min(a.chunk, a.group - c * a.chunk);
-    const float *from = static_cast<const float *>(a.q) + ((size_t)b * a.nq + (size_t)h * a.group + c * a.chunk) * HD;
-    __syncwarp();
-    for (int i = lane; i < H * HD; i += 32) q[i] = i < heads * HD ? from[i] : 0.f;
-    __syncwarp();
-#pragma unroll
-    for (int g = 0; g < HEADS; ++g) {
-      m[g] = -INFINITY;
-      l[g] = 0.f;
-#pragma unroll
-      for (int e = 0; e < COLS; ++e) o[g][e] = 0.f;
-    }
-  }
-  __device__ __forceinline__ void tile(const DecodeArgs &a, u32 at, u32 there) {
-    const unsigned char *k = static_cast<const unsigned char *>(__cvta_shared_to_generic(at)), *v = k + Ring<T, HD>::HALF;
-    const int key = lane >> 2, j = lane & 3;
-    float s[HEADS];
-#pragma unroll
-    for (int g = 0; g < HEADS; ++g) s[g] = 0.f;
+    const int h = item / a.chunks, c = item % a.chunks, heads = min(a.chunk, a.group - c * a.chunk), r = lane >> 2, j = lane & 3;
+    const float *q = static_cast<const float *>(a.q) + ((size_t)b * a.nq + (size_t)h * a.group + c * a.chunk + r) * HD;
 #pragma unroll
     for (int i = 0; i < HD / 16; ++i) {
-      const float4 x = *reinterpret_cast<const float4 *>(k + piece<T, HD>(key, i * 4 + j));
+      const float4 x = r < heads ? __ldg(reinterpret_cast<const float4 *>(q + i * 16 + j * 4)) : make_float4(0.f, 0.f, 0.f, 0.f);
+      split(x.x, qh[2 * i][0], ql[2 * i][0]);
+      split(x.y, qh[2 * i][1], ql[2 * i][1]);
+      split(x.z, qh[2 * i + 1][0], ql[2 * i + 1][0]);
+      split(x.w, qh[2 * i + 1][1], ql[2 * i + 1][1]);
+    }
 #pragma unroll
-      for (int g = 0; g < H; ++g) {
-        const float4 y = *reinterpret_cast<const float4 *>(q + g * HD + (i * 4 + j) * 4);
-        s[g] = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, s[g]))));
+    for (int n = 0; n < HD / 8; ++n)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) o[n][x] = 0.f;
+    m = -INFINITY;
+    l = 0.f;
+  }
+  __device__ __forceinline__ void tile(const DecodeArgs &a, u32 at, u32 there) {
+    constexpr int KB = Form<T, HD>::KEYS / 8;                          // blocks of 8 keys
+    const int r = lane >> 2, j = lane & 3;
+    float p[KB][2], mx = -INFINITY;
+#pragma unroll
+    for (int b = 0; b < KB; ++b) {
+      float s[2][4], t[2][4], u[2][4];         // high x high, high x low, low x high
+#pragma unroll
+      for (int x = 0; x < 4; ++x) s[0][x] = s[1][x] = t[0][x] = t[1][x] = u[0][x] = u[1][x] = 0.f;
+#pragma unroll
+      for (int i = 0; i < HD / 16; ++i) {
+        const float4 k = lds4(at + piece<T, HD>(b * 8 + r, i * 4 + j));
+        const float x[4] = {k.x, k.y, k.z, k.w};
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          u32 h0, l0, h1, l1;
+          split(x[2 * y], h0, l0);
+          split(x[2 * y + 1], h1, l1);
+          const u32 hi[4] = {qh[2 * i + y][0], 0, qh[2 * i + y][1], 0}, lo[4] = {ql[2 * i + y][0], 0, ql[2 * i + y][1], 0};
+          mma_tf32(s[y], hi, h0, h1);
+          mma_tf32(t[y], hi, l0, l1);
+          mma_tf32(u[y], lo, h0, h1);
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        p[b][x] = (there >> (b * 8 + 2 * j + x)) & 1 ? (((t[0][x] + t[1][x]) + (u[0][x] + u[1][x])) + (s[0][x] + s[1][x])) * a.scale : -INFINITY;
+        mx = fmaxf(mx, p[b][x]);
       }
     }
-    const bool here = (there >> key) & 1;
-    float f[H], mx[H];
+    mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 1));
+    mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 2));
+    const float n = fmaxf(m, mx), ref = n > -INFINITY ? n : 0.f, f = ex2(m - ref);
+    const bool grown = n > m;
+    m = n;
+    l *= f;
+    if (__any_sync(0xFFFFFFFFu, grown)) {
 #pragma unroll
-    for (int d = 1; d < 4; d <<= 1)
-#pragma unroll
-      for (int g = 0; g < H; ++g) s[g] += __shfl_xor_sync(0xFFFFFFFFu, s[g], d);
-#pragma unroll
-    for (int g = 0; g < H; ++g) mx[g] = s[g] = here ? s[g] * a.scale : -INFINITY;
-#pragma unroll
-    for (int d = 4; d < 32; d <<= 1)
-#pragma unroll
-      for (int g = 0; g < H; ++g) mx[g] = fmaxf(mx[g], __shfl_xor_sync(0xFFFFFFFFu, mx[g], d));
-#pragma unroll
-    for (int g = 0; g < H; ++g) {
-      const float n = fmaxf(m[g], mx[g]), ref = n > -INFINITY ? n : 0.f;
-      f[g] = ex2(m[g] - ref);
-      m[g] = n;
-      s[g] = ex2(s[g] - ref);
-      l[g] = fmaf(l[g], f[g], s[g]);           // of this lane's keys: added up at the end
-#pragma unroll
-      for (int e = 0; e < COLS; ++e) o[g][e] *= f[g];
+      for (int i = 0; i < HD / 8; ++i) { o[i][0] *= f; o[i][1] *= f; }
     }
+    const u32 v = at + Ring<T, HD>::HALF;
 #pragma unroll
-    for (int kk = 0; kk < KEYS; ++kk) {
-      float x[COLS];
-      const unsigned char *row = v + piece<T, HD>(kk, lane * COLS / 4) + (lane * COLS % 4) * 4;
-      if constexpr (COLS == 4) { const float4 y = *reinterpret_cast<const float4 *>(row); x[0] = y.x; x[1] = y.y; x[2] = y.z; x[3] = y.w; }
-      else if constexpr (COLS == 2) { const float2 y = *reinterpret_cast<const float2 *>(row); x[0] = y.x; x[1] = y.y; }
-      else x[0] = *reinterpret_cast<const float *>(row);
+    for (int b = 0; b < KB; ++b) {
+      const float p0 = ex2(p[b][0] - ref), p1 = ex2(p[b][1] - ref);
+      l += p0 + p1;
+      u32 hi[4] = {0, 0, 0, 0}, lo[4] = {0, 0, 0, 0};                  // k = j: key 2 j; k = j + 4: key 2 j + 1
+      split(p0, hi[0], lo[0]);
+      split(p1, hi[2], lo[2]);
 #pragma unroll
-      for (int g = 0; g < H; ++g) {
-        const float p = __shfl_sync(0xFFFFFFFFu, s[g], kk * 4);
+      for (int i = 0; i < HD / 32; ++i) {
+        const float4 v0 = lds4(v + piece<T, HD>(b * 8 + 2 * j, i * 8 + r)), v1 = lds4(v + piece<T, HD>(b * 8 + 2 * j + 1, i * 8 + r));
+        const float x[4] = {v0.x, v0.y, v0.z, v0.w}, y[4] = {v1.x, v1.y, v1.z, v1.w};
+        u32 h0[4], l0[4], h1[4], l1[4];
 #pragma unroll
-        for (int e = 0; e < COLS; ++e) o[g][e] = fmaf(p, x[e], o[g][e]);
+        for (int c = 0; c < 4; ++c) {
+          split(x[c], h0[c], l0[c]);
+          split(y[c], h1[c], l1[c]);
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) mma_tf32(o[4 * i + c], hi, h0[c], h1[c]);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) mma_tf32(o[4 * i + c], hi, l0[c], l1[c]);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) mma_tf32(o[4 * i + c], lo, h0[c], h1[c]);
       }
     }
   }
   __device__ __forceinline__ void end(const DecodeArgs &a, int b, int item, bool whole, float *part) {
-    const int h = item / a.chunks, c = item % a.chunks;
-    float *out = static_cast<float *>(a.out) + ((size_t)b * a.nq + (size_t)h * a.group + c * a.chunk) * HD;
+    const int h = item / a.chunks, c = item % a.chunks, r = lane >> 2, j = lane & 3;
+    l += __shfl_xor_sync(0xFFFFFFFFu, l, 1);
+    l += __shfl_xor_sync(0xFFFFFFFFu, l, 2);
+    if (r >= min(a.chunk, a.group - c * a.chunk)) return;
+    float *to = (whole ? static_cast<float *>(a.out) + ((size_t)b * a.nq + (size_t)h * a.group + c * a.chunk) * HD : part) + r * HD;
+    const float inv = !whole ? 1.f : l != 0.f ? 1.f / l : 0.f;
 #pragma unroll
-    for (int g = 0; g < HEADS; ++g)
-      if (g < heads) {
-        float sum = l[g];
+    for (int i = 0; i < HD / 32; ++i)
 #pragma unroll
-        for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
-        const float inv = !whole ? 1.f : sum != 0.f ? 1.f / sum : 0.f;
-        float *to = (whole ? out : part) + g * HD + lane * COLS;
+      for (int x = 0; x < 2; ++x)              // column n of tile 4 i + c stands for 32 i + 4 n + c
 #pragma unroll
-        for (int e = 0; e < COLS; ++e) to[e] = o[g][e] * inv;
-        if (!whole && lane == 0) *reinterpret_cast<float2 *>(part + a.chunk * HD + g * 2) = make_float2(m[g], sum);
-      }
+        for (int y = 0; y < 2; ++y)
+          *reinterpret_cast<float2 *>(to + i * 32 + j * 8 + x * 4 + y * 2) = make_float2(o[4 * i + 2 * y][x] * inv, o[4 * i + 2 * y + 1][x] * inv);
+    if (!whole && j == 0) *reinterpret_cast<float2 *>(part + a.chunk * HD + r * 2) = make_float2(m, l);
   }
 };
 
 template <typename T, int HD, int H> struct TileOf { using type = Bf16Tile<HD, H>; };
-template <int HD, int H> struct TileOf<float, HD, H> { using type = Fp32Tile<HD, H>; };
-template <typename T, int HD, int H> constexpr int kQueryBytes = sizeof(T) == 4 ? H * HD * 4 : 0;          // a warp's, in shared memory
-template <typename T, int HD, int H> constexpr int smem_bytes(int batch) {
-  return kWarps * (Ring<T, HD>::BYTES + kQueryBytes<T, HD, H>) + kWarps * Ring<T, HD>::STAGES * 4 + kWarps * 4 + (2 * batch + 1) * 4;
+template <int HD> struct TileOf<float, HD, 8> { using type = Fp32Tile<HD>; };
+template <typename T, int HD> constexpr int smem_bytes(int batch) {
+  return kWarps * Ring<T, HD>::BYTES + kWarps * Ring<T, HD>::STAGES * 4 + kWarps * 4 + (2 * batch + 1) * 4;
+}
+
+__device__ __forceinline__ void store4(float *to, float4 v) { *reinterpret_cast<float4 *>(to) = v; }
+__device__ __forceinline__ void store4(__nv_bfloat16 *to, float4 v) {
+  reinterpret_cast<__nv_bfloat162 *>(to)[0] = __floats2bfloat162_rn(v.x, v.y);
+  reinterpret_cast<__nv_bfloat162 *>(to)[1] = __floats2bfloat162_rn(v.z, v.w);
 }
 
 // What a warp's stretch leaves to its CTA.
@@ -448,12 +549,12 @@ attn_decode_kernel(DecodeArgs a) {
   __shared__ int left[kWarps];                 // kHead, kEnd, kThrough
   __shared__ int2 left_item[kWarps];           // sequence and item of the part that runs on
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, cta = blockIdx.x;
-  unsigned char *rest = smem + kWarps * (R::BYTES + kQueryBytes<T, HD, H>);
+  unsigned char *rest = smem + kWarps * R::BYTES;
   u32 *masks = reinterpret_cast<u32 *>(rest) + warp * S;
   int *warp_sum = reinterpret_cast<int *>(rest) + kWarps * S, *before = warp_sum + kWarps, *lens = before + a.batch + 1;
   chain_wait();
   chain_next();
-  const Line line = make_line<Form<T>::KEYS, kThreads>(a.kv_lens, a.batch, (long long)a.pages_per_seq * a.pool.page, a.nkv * a.chunks, before, lens, warp_sum);
+  const Line line = make_line<Form<T, HD>::KEYS, kThreads>(a.kv_lens, a.batch, (long long)a.pages_per_seq * a.pool.page, a.nkv * a.chunks, before, lens, warp_sum);
 
   // sequences without a key: zeros
   for (int b = cta; b < a.batch; b += kGrid)
@@ -461,33 +562,31 @@ attn_decode_kernel(DecodeArgs a) {
       for (int i = threadIdx.x; i < a.nq * HD; i += kThreads) static_cast<T *>(a.out)[(size_t)b * a.nq * HD + i] = T(0.f);
 
   const int s0 = line.first(cta), n_warps = line.first(cta + 1) - s0, me = s0 + warp;
-  const long long total = (long long)before[a.batch] * line.items;
   int left_here = 0;
   if (warp < n_warps) {
-    const long long from = me * line.per, n = min(line.per, total - from);
+    const long long from = me * line.per, n = min(line.per, line.total - from);
     typename TileOf<T, HD, H>::type t;
     t.lane = lane;
-    if constexpr (sizeof(T) == 4) t.q = reinterpret_cast<float *>(smem + kWarps * R::BYTES) + warp * H * HD;
     Place at;
     at.find(line, from);
     Feeder<T, HD> feed = {a, line, (u32)__cvta_generic_to_shared(smem) + warp * R::BYTES, masks, lane};
     feed.begin(at);
-#pragma unroll
-    for (int i = 0; i < S - 1; ++i) {
-      if (i < n) feed.copy(i);
+    int stage = 0, fill = 0, first = at.tile;
+    const Place start = at;
+#pragma unroll 1
+    for (; fill < S - 1; ++fill) {             // (not unrolled: short calls wait for their instructions)
+      if (fill < n) feed.copy(fill);
       copies_end();
     }
-    int stage = 0, fill = S - 1, first = at.tile;
-    const Place start = at;
     t.begin(a, at.b, at.item);
     for (long long i = 0; i < n; ++i) {
       copies_wait<S - 2>();
       __syncwarp();
       if (i + S - 1 < n) feed.copy(fill);
       copies_end();
+      if (++fill == S) fill = 0;
       t.tile(a, feed.ring + stage * R::STAGE, masks[stage]);
       if (++stage == S) stage = 0;
-      if (++fill == S) fill = 0;
       const bool last = at.tile + 1 == at.tiles;
       if (last || i + 1 == n) {
         float *part = nullptr;
@@ -520,47 +619,68 @@ attn_decode_kernel(DecodeArgs a) {
   if (lane == 0) left[warp] = left_here;
   __syncthreads();
 
-  // Runs of parts of one item: from warp w0 (whose part runs on, or the first) to the one that ends it, or to the CTA's last.
-  for (int w0 = 0; w0 < n_warps; ++w0) {
-    const bool outside = w0 == 0 && (left[0] & (kHead | kThrough));       // it began in front of this CTA
-    for (int turn = outside ? 0 : 1; turn < 2; ++turn) {
-      if (turn == 1 && (!(left[w0] & kEnd) || (left[w0] & kThrough))) continue;
-      int w1 = w0;
-      bool ended = turn == 0 && (left[w0] & kHead);
-      while (!ended && w1 + 1 < n_warps) {
-        ++w1;
-        ended = left[w1] & kHead;
-      }
-      const bool whole = turn == 1 && ended;
-      const int2 it = turn == 1 ? left_item[w0] : make_int2(0, 0);
-      const int heads = min(a.chunk, a.group - it.y % a.chunks * a.chunk);
-      float *to = cta_part<HD>(a.parts, a.chunk, cta, turn);
-      for (int i = threadIdx.x; i < (turn == 1 ? heads : a.chunk) * HD; i += kThreads) {
-        const int g = i / HD;
-        float m = -INFINITY, l = 0.f, o = 0.f;
-        for (int w = w0; w <= w1; ++w) {
+  // Runs of parts of one item: from the first warp, if it begins inside of an item (run 0), or one whose part begins there and runs on,
+  // to the warp that ends it, or to the CTA's last.
+  u32 heads_of = 0, ends = 0, through = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    heads_of |= (left[w] & kHead) ? 1u << w : 0u;
+    ends |= (left[w] & kEnd) ? 1u << w : 0u;
+    through |= (left[w] & kThrough) ? 1u << w : 0u;
+  }
+  u32 runs = (ends & ~through) << 1 | ((heads_of | through) & 1u);     // bit 0: run 0, bit w + 1: from warp w
+  // a run for each warp, or for two, four or all of them where there are few
+  const int n_runs = __popc(runs), share = n_runs == 1 ? kWarps : n_runs == 2 ? kWarps / 2 : n_runs <= 4 ? kWarps / 4 : 1;
+  const int thread = threadIdx.x % (share * 32);
+  for (int r = 0; runs; ++r, runs &= runs - 1) {
+    if (r % (kWarps / share) != warp / share) continue;
+    const int run = __ffs(runs) - 1, w0 = max(run - 1, 0);
+    const u32 behind = heads_of & ~(run == 0 ? 0u : (2u << w0) - 1);   // warps that may end it
+    const bool ended = behind != 0, whole = run > 0 && ended;
+    const int w1 = ended ? __ffs(behind) - 1 : n_warps - 1;
+    const int2 it = run > 0 ? left_item[w0] : make_int2(0, 0);
+    float *to = cta_part<HD>(a.parts, a.chunk, cta, run > 0);
+    const int heads = run > 0 ? min(a.chunk, a.group - it.y % a.chunks * a.chunk) : a.chunk;
+    for (int i = thread * 4; i < heads * HD; i += share * 128) {
+      const int g = i / HD, stat = a.chunk * HD + 2 * g;
+      float2 ml[kWarps];
+      float4 o[kWarps];
+      float m = -INFINITY, l = 0.f;
+      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        ml[w] = make_float2(-INFINITY, 0.f);
+        o[w] = sum;
+        if (w >= w0 && w <= w1) {
           const float *p = ended && w == w1 ? part_at<HD>(a.parts, a.chunk, s0 + w) : reinterpret_cast<const float *>(smem + w * R::BYTES);
-          const float m2 = p[a.chunk * HD + 2 * g], n = fmaxf(m, m2), ref = n > -INFINITY ? n : 0.f, f = ex2(m - ref), f2 = ex2(m2 - ref);
-          m = n;
-          l = fmaf(l, f, p[a.chunk * HD + 2 * g + 1] * f2);
-          o = fmaf(o, f, p[i] * f2);
+          ml[w] = *reinterpret_cast<const float2 *>(p + stat);
+          o[w] = make_float4(p[i], p[i + 1], p[i + 2], p[i + 3]);
         }
-        if (whole) {
-          const float y = l != 0.f ? o / l : 0.f;
-          const size_t at = ((size_t)it.x * a.nq + (size_t)(it.y / a.chunks) * a.group + it.y % a.chunks * a.chunk) * HD + i;
-          if constexpr (sizeof(T) == 4) static_cast<float *>(a.out)[at] = y;
-          else static_cast<__nv_bfloat16 *>(a.out)[at] = __float2bfloat16_rn(y);
-        } else {
-          to[i] = o;
-          if (i % HD == 0) { to[a.chunk * HD + 2 * g] = m; to[a.chunk * HD + 2 * g + 1] = l; }
-        }
+        m = fmaxf(m, ml[w].x);
+      }
+      const float ref = m > -INFINITY ? m : 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float f = ex2(ml[w].x - ref);
+        l = fmaf(ml[w].y, f, l);
+        sum.x = fmaf(o[w].x, f, sum.x); sum.y = fmaf(o[w].y, f, sum.y); sum.z = fmaf(o[w].z, f, sum.z); sum.w = fmaf(o[w].w, f, sum.w);
+      }
+      if (whole) {
+        const float inv = l != 0.f ? 1.f / l : 0.f;
+        store4(static_cast<T *>(a.out) + ((size_t)it.x * a.nq + (size_t)(it.y / a.chunks) * a.group + it.y % a.chunks * a.chunk) * HD + i,
+               make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
+      } else {
+        *reinterpret_cast<float2 *>(to + i) = make_float2(sum.x, sum.y);
+        *reinterpret_cast<float2 *>(to + i + 2) = make_float2(sum.z, sum.w);
+        if (i % HD == 0) *reinterpret_cast<float2 *>(to + stat) = make_float2(m, l);
       }
     }
   }
 }
 
-// Adds the CTAs' parts of the item that CTA blockIdx.x told of, a CTA a query head.  Warps take parts in turn and add them in order,
-// then the warps' sums are added in order.
+// Adds the CTAs' parts of the item that CTA blockIdx.x told of, a CTA a query head.  Warps take parts in turn, each at most kPerWarp, whose
+// loads wait for nothing but the item's description, and add them in order; then the warps' sums are added in order.
+constexpr int kPerWarp = (kGrid + kJoinWarps - 1) / kJoinWarps;
 template <typename T, int HD>
 __global__ void __launch_bounds__(kJoinWarps * 32)
 attn_join_kernel(DecodeArgs a) {
@@ -571,21 +691,36 @@ attn_join_kernel(DecodeArgs a) {
   chain_next();
   const int4 it = a.joins[blockIdx.x];         // first row of the output, heads, CTAs
   if (g >= it.y) return;
-  float o[COLS], l = 0.f, m = -INFINITY;
+  auto part = [&](int c) -> const float * { return cta_part<HD>(a.parts, a.chunk, c, c == it.z ? 1 : 0); };
+  const int mine = it.z + warp + lane * kJoinWarps;                    // the lane's part's statistics
+  const bool there = lane < kPerWarp && mine <= it.w;
+  const float2 ml = there ? *reinterpret_cast<const float2 *>(part(mine) + a.chunk * HD + g * 2) : make_float2(-INFINITY, 0.f);
+  float x[kPerWarp][COLS];
+#pragma unroll
+  for (int k = 0; k < kPerWarp; ++k) {
+    const int c = it.z + warp + k * kJoinWarps;
+#pragma unroll
+    for (int e = 0; e < COLS; ++e) x[k][e] = 0.f;
+    if (c <= it.w) {
+#pragma unroll
+      for (int e = 0; e < COLS; ++e) x[k][e] = part(c)[g * HD + e * 32 + lane];
+    }
+  }
+  float m = ml.x;
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+  const float f = ex2(ml.x - (m > -INFINITY ? m : 0.f));
+  float l = ml.y * f, o[COLS];
+  for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, d);
 #pragma unroll
   for (int e = 0; e < COLS; ++e) o[e] = 0.f;
-#pragma unroll 4
-  for (int c = it.z + warp; c <= it.w; c += kJoinWarps) {
-    const float *p = cta_part<HD>(a.parts, a.chunk, c, c == it.z ? 1 : 0);
-    const float2 ml = *reinterpret_cast<const float2 *>(p + a.chunk * HD + g * 2);
-    const float n = fmaxf(m, ml.x), ref = n > -INFINITY ? n : 0.f, f = ex2(m - ref), f2 = ex2(ml.x - ref);
-    m = n;
-    l = fmaf(l, f, ml.y * f2);
 #pragma unroll
-    for (int e = 0; e < COLS; ++e) o[e] = fmaf(o[e], f, p[g * HD + lane * COLS + e] * f2);
+  for (int k = 0; k < kPerWarp; ++k) {
+    const float f2 = __shfl_sync(0xFFFFFFFFu, f, k);
+#pragma unroll
+    for (int e = 0; e < COLS; ++e) o[e] = fmaf(x[k][e], f2, o[e]);
   }
 #pragma unroll
-  for (int e = 0; e < COLS; ++e) sh_o[warp][lane * COLS + e] = o[e];
+  for (int e = 0; e < COLS; ++e) sh_o[warp][e * 32 + lane] = o[e];
   if (lane == 0) { sh_m[warp] = m; sh_l[warp] = l; }
   __syncthreads();
   for (int i = threadIdx.x; i < HD; i += kJoinWarps * 32) {
@@ -595,9 +730,9 @@ attn_join_kernel(DecodeArgs a) {
     const float ref = top > -INFINITY ? top : 0.f;
 #pragma unroll
     for (int w = 0; w < kJoinWarps; ++w) {
-      const float f = ex2(sh_m[w] - ref);
-      sum = fmaf(sh_o[w][i], f, sum);
-      all = fmaf(sh_l[w], f, all);
+      const float f2 = ex2(sh_m[w] - ref);
+      sum = fmaf(sh_o[w][i], f2, sum);
+      all = fmaf(sh_l[w], f2, all);
     }
     const float y = all != 0.f ? sum / all : 0.f;
     const size_t at = ((size_t)it.x + g) * HD + i;
@@ -608,16 +743,16 @@ attn_join_kernel(DecodeArgs a) {
 
 template <typename T, int HD, int H> int run(const DecodeArgs &a, cudaStream_t s) {
   static std::atomic<u64> done{0};
-  const int status = hsd_smem_limit((const void *)attn_decode_kernel<T, HD, H>, smem_bytes<T, HD, H>(kMaxBatch), done);
+  const int status = hsd_smem_limit((const void *)attn_decode_kernel<T, HD, H>, smem_bytes<T, HD>(kMaxBatch), done);
   if (status) return status;
-  HSD_CUDA_OK(hsd_launch(attn_decode_kernel<T, HD, H>, dim3(kGrid), kThreads, smem_bytes<T, HD, H>(a.batch), s, 0, true, a));
+  HSD_CUDA_OK(hsd_launch(attn_decode_kernel<T, HD, H>, dim3(kGrid), kThreads, smem_bytes<T, HD>(a.batch), s, 0, true, a));
   HSD_CUDA_OK(hsd_launch(attn_join_kernel<T, HD>, dim3(kGrid, a.chunk), kJoinWarps * 32, 0, s, 0, true, a));
   hsd_count_launches(2);
   return hsd_launch_status();
 }
 template <typename T, int HD> int run_heads(const DecodeArgs &a, cudaStream_t s) {
-  if constexpr (sizeof(T) == 2) return a.chunk <= 8 ? run<T, HD, 8>(a, s) : run<T, HD, 16>(a, s);
-  else return a.chunk == 1 ? run<T, HD, 1>(a, s) : a.chunk == 2 ? run<T, HD, 2>(a, s) : a.chunk <= 4 ? run<T, HD, 4>(a, s) : run<T, HD, 8>(a, s);
+  if constexpr (sizeof(T) == 2) if (a.chunk > 8) return run<T, HD, 16>(a, s);
+  return run<T, HD, 8>(a, s);
 }
 template <typename T> int run_hd(const DecodeArgs &a, int hd, cudaStream_t s) {
   return hd == 32 ? run_heads<T, 32>(a, s) : hd == 64 ? run_heads<T, 64>(a, s) : run_heads<T, 128>(a, s);
@@ -649,7 +784,10 @@ extern "C" int hsd_paged_attention(const void *q, int batch, int n_q_heads, int 
   a.scale = scale * 1.4426950408889634f;
   a.batch = batch; a.nq = n_q_heads; a.nkv = n_kv_heads; a.pages_per_seq = pages_per_seq;
   a.group = n_q_heads / n_kv_heads;
-  const int most = pool->dtype == HSD_F32 ? Form<float>::HEADS : Form<__nv_bfloat16>::HEADS;
+  a.page_shift = -1;
+  for (int i = 0; i < 31; ++i)
+    if (pool->page_size == 1 << i) a.page_shift = i;
+  const int most = pool->dtype == HSD_F32 ? Form<float, 128>::HEADS : Form<__nv_bfloat16, 128>::HEADS;
   a.chunks = ceil_div(a.group, most);
   a.chunk = ceil_div(a.group, a.chunks);
   return pool->dtype == HSD_F32 ? run_hd<float>(a, head_dim, (cudaStream_t)stream) : run_hd<__nv_bfloat16>(a, head_dim, (cudaStream_t)stream);
