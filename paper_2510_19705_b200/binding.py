@@ -52,7 +52,7 @@ def _host_calls():
         mod.init(*(ctypes.cast(f, ctypes.c_void_p).value for f in
                    (lib.hsd_draft_sample, lib.hsd_verify_workspace_bytes, lib.hsd_verify_level, lib.hsd_gemm_workspace_bytes,
                     lib.hsd_gemm_bf16, lib.hsd_gemm_status, lib.hsd_strerror, lib.hsd_kv_append, lib.hsd_paged_attention_workspace_bytes,
-                    lib.hsd_paged_attention, lib.hsd_gemm_w4, lib.hsd_token_logprobs)), HsdError)
+                    lib.hsd_paged_attention, lib.hsd_gemm_w4_workspace_bytes, lib.hsd_gemm_w4, lib.hsd_token_logprobs)), HsdError)
         _host = mod
     return _host
 
@@ -218,8 +218,10 @@ def _declare_engine(lib):
     lib.hsd_paged_attention_workspace_bytes.argtypes = [i32, i32, i32]
     lib.hsd_paged_attention.restype = i32
     lib.hsd_paged_attention.argtypes = [vp, i32, i32, i32, i32, c.POINTER(_KvPool), vp, i32, vp, c.c_float, vp, sz, vp, vp]
+    lib.hsd_gemm_w4_workspace_bytes.restype = sz
+    lib.hsd_gemm_w4_workspace_bytes.argtypes = [i32, i32, i32, i32]
     lib.hsd_gemm_w4.restype = i32
-    lib.hsd_gemm_w4.argtypes = [vp, i32, i32, vp, vp, i32, i32, vp, vp]
+    lib.hsd_gemm_w4.argtypes = [vp, i32, i32, vp, vp, i32, i32, vp, vp, sz, vp]
     lib.hsd_token_logprobs.restype = i32
     lib.hsd_token_logprobs.argtypes = [vp, i32, i32, i32, vp, i32, vp, vp, vp, vp, vp, vp]
 
@@ -528,9 +530,13 @@ def hsd_paged_attention(q, k_pool, v_pool, page_table, kv_lens, scale=None, work
     return (_host or _host_calls()).paged_attention(q, k_pool, v_pool, page_table, kv_lens, scale, workspace, out)
 
 
-def hsd_gemm_w4(A, codes, scales, out=None):
+def hsd_gemm_w4_workspace_bytes(R, N, K, group):
+    return int(library().hsd_gemm_w4_workspace_bytes(R, N, K, group))
+
+
+def hsd_gemm_w4(A, codes, scales, out=None, workspace=None):
     """A bf16 [R, K] (R <= 64), codes uint8 [N, K / 2] and scales bf16 [N, K / group] from w4_pack -> fp32 [R, N]."""
-    return (_host or _host_calls()).gemm_w4(A, codes, scales, out)
+    return (_host or _host_calls()).gemm_w4(A, codes, scales, out, workspace)
 
 
 def hsd_token_logprobs(logits, tokens, top=0):

@@ -1,41 +1,38 @@
 // Few-row products with 4-bit weights and group scales (hsd_gemm_w4): out[r, n] = sum_k A[r, k] (c[n, k] - 8) s[n, k / group].
-// Bound by memory (half a byte a weight) up to some 16 rows; the weights never leave registers: a lane loads 32 codes of a weight row
-// and makes bf16 pairs of them (0x4300 | c is 128 + c in bf16, less 136: exact), which are its operands of mma.sync with 16
-// weight rows as the tile's rows and the activations as its columns.  The order of k inside a product is free, so it is the
-// order in which the codes lie in a word: pairs (0,4), (1,5), (2,6), (3,7), the activations permuted alike.
-// A group's products are summed in the tensor core's fp32, then scaled and added in fp32: no rounding to fewer bits anywhere.
-// A CTA has 16 weight rows; its warps divide k (chunk by chunk in turn, so that together they read long pieces of a row), and
-// where the matrix has few rows a cluster divides it once more.  Partial sums are added in a fixed order.
+// Bound by memory: half a byte a weight.  What stands between that and the products is making bf16 of the codes, eleven operations
+// for the eight codes of a word: c less 8 is made from the bits (0x4300 | c is 128 + c in bf16, less 136: exact), a pair at a time, and
+// the pairs are (0,4), (1,5), (2,6), (3,7) of a word; the order of k inside a product is free, so the activations are put in the same.
+// A group's products are summed in the tensor cores' fp32, then scaled and added in fp32: no rounding to fewer bits anywhere.
+// w4_kernel: 128 weight rows a tile, a thread one row.  Codes come by TMA, the pairs go from registers into tensor memory, from where
+// tcgen05.mma takes them as its operand A (the activations, at most 64 rows, are B); a thread reads its row's sums of a group
+// back and scales them.  The tiles' steps (256 of k) stand in one line that is divided evenly over warpgroups, three on an SM (two
+// for more than 16 rows), which wait for nothing but their own loads; where a stretch ends inside a tile its sums go to the workspace
+// and w4_join_kernel adds them in order.
+// w4_small_kernel: see there.
 #include <cooperative_groups.h>
 
-#include "common.cuh"
+#include "gemm_tc.cuh"
+#include "tc_ptx.cuh"
 
 namespace hsd {
 namespace {
 
+using namespace ptx;
+
 constexpr int kWarps = 8, kThreads = kWarps * 32;
+constexpr int kChunk = 128;            // k of a warp's step in w4_small_kernel: 16 bytes of codes a lane
 
 struct W4Args {
   const __nv_bfloat16 *a;
   const uint8_t *codes;
   const __nv_bfloat16 *scales;
   float *out;
-  int R, K, N, groups, steps;          // groups of a row; steps of k
+  int R, K, N, groups;                 // groups of a row
 };
 
 __device__ __forceinline__ void mma(float *c, const u32 *a, u32 b0, u32 b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ void copy16(u32 to, const void *from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory"); }
-__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-// 16-byte pieces of row r of a stage are permuted by this: reads of 4 bytes by 8 rows x 4 lanes, and of 16 by 2 rows x 4, meet no bank twice.
-__device__ __forceinline__ int swizzle(int r) { return (r & 1) << 2 | (r >> 1 & 3); }
-template <int GW> __device__ __forceinline__ void load_words(u32 *w, u32 at) {
-  if constexpr (GW == 4) asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
-  else if constexpr (GW == 2) asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at) : "memory");
-  else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(at) : "memory");
 }
 // Codes i and i + 4 of a word, less 8, as two bf16.
 template <int I> __device__ __forceinline__ u32 pair(u32 word) {
@@ -44,111 +41,68 @@ template <int I> __device__ __forceinline__ u32 pair(u32 word) {
   return *reinterpret_cast<const u32 *>(&y);
 }
 
-// GW: words of a lane in a group (group = 32 GW); RT: tiles of 8 activation rows.
-// A CTA has 128 weight rows, 16 a warp, and [k_lo, k_hi) of k.  A warp's codes come through a ring of its own (cp.async, kStep of k a
-// stage: 128 bytes of each of 16 rows); the activations of kBlock of k are staged once for all warps, in the order of the fragments
-// and twice buffered, the next block's on their way in registers.
-constexpr int kStep = 256, kStages = 4, kRowsCta = kWarps * 16;
-template <int RT> constexpr int kBlock = RT >= 4 ? 256 : 1024 / RT;    // of k, at most 16 KB of activations
-template <int RT> constexpr int kActBytes = RT * 8 * kBlock<RT> * 2;
-template <int RT> constexpr int kSmem = kWarps * kStages * 2048 + 2 * kActBytes<RT>;
-
-template <int GW, int RT>
+// ---------------------------------------------------------------------------- small products
+// The codes never leave registers: a lane loads 32 of a weight row, and their pairs are its operands of mma.sync with 16 weight rows
+// as the tile's rows and up to eight activations as its columns.  A CTA has 16 weight rows; its warps divide k (chunk by chunk in turn, so that
+// together they read long pieces of a row), and where the matrix has few rows a cluster divides it once more.
+// GW: words of a lane in a group (group = 32 GW); RT: tiles of 8 activation rows; MT: tiles of 16 weight rows.
+template <int GW, int RT, int MT>
 __global__ void __launch_bounds__(kThreads)
-gemm_w4_kernel(W4Args p) {
-  constexpr int GROUPS = kStep / (32 * GW), WORDS = kStep / 32;        // groups and words of a step
-  constexpr int BLOCK = kBlock<RT>, PIECES = kActBytes<RT> / 16 / kThreads;
-  extern __shared__ __align__(128) unsigned char smem[];
+w4_small_kernel(W4Args p) {
+  constexpr int GROUPS = 4 / GW;       // of a chunk
+  __shared__ __align__(16) float sums[kWarps][MT * 16][RT * 8];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j = lane & 3, lr = lane >> 2;
-  const int parts = gridDim.y, part = blockIdx.y, n0 = blockIdx.x * kRowsCta + warp * 16;
-  const int k_lo = (int)((long long)p.steps * part / parts) * kStep, k_hi = min((int)((long long)p.steps * (part + 1) / parts) * kStep, p.K);
-  const u32 ring = (u32)__cvta_generic_to_shared(smem) + warp * kStages * 2048;
-  unsigned char *act = smem + kWarps * kStages * 2048;
+  const int parts = gridDim.y, part = blockIdx.y, n0 = blockIdx.x * MT * 16;
+  float acc[MT][RT][4];
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) acc[m][t][x] = 0.f;
 
-  // codes: lane i has piece i % 8 of rows i / 8, i / 8 + 4, ..; rows past the last are read as the last and not stored
-  const uint8_t *from[4];
+  const int chunks = (p.K + kChunk - 1) / kChunk;
+  for (int c = part * kWarps + warp; c < chunks; c += parts * kWarps) {
+    u32 word[MT][2][4];
+    float scale[MT][2][GROUPS];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) from[i] = p.codes + (size_t)min(n0 + i * 4 + (lane >> 3), p.N - 1) * (p.K / 2) + (lane & 7) * 16;
-  auto copy = [&](int k, int stage) {
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = i * 4 + (lane >> 3), c = lane & 7;
-      if (k + c * 32 < k_hi) copy16(ring + stage * 2048 + r * 128 + ((c ^ swizzle(r)) << 4), from[i] + k / 2);
-    }
-  };
-  // activations: piece i of a block is k8 = i % (BLOCK / 8) of row i / (BLOCK / 8)
-  uint4 next[PIECES];
-  auto fetch = [&](int k) {
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-      const int x = i * kThreads + threadIdx.x, r = x / (BLOCK / 8), at = k + x % (BLOCK / 8) * 8;
-      next[i] = r < p.R && at < k_hi ? __ldg(reinterpret_cast<const uint4 *>(p.a + (size_t)r * p.K + at)) : make_uint4(0, 0, 0, 0);
-    }
-  };
-  auto put = [&](int buffer) {
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-      const int x = i * kThreads + threadIdx.x, r = x / (BLOCK / 8), k8 = x % (BLOCK / 8), q = k8 % 16;
-      const int w = (q / (4 * GW)) * GW + q % GW, jj = q / GW % 4;     // the lane's word and quarter of a chunk of 128
-      const uint4 v = next[i];
-      *reinterpret_cast<uint4 *>(act + buffer * kActBytes<RT> + ((((k8 / 16) * 4 + w) * RT * 8 + r) * 4 + jj) * 16) =
-          make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
-    }
-  };
-
-  float acc[RT][4];
-#pragma unroll
-  for (int t = 0; t < RT; ++t)
-#pragma unroll
-    for (int x = 0; x < 4; ++x) acc[t][x] = 0.f;
-  fetch(k_lo);
-#pragma unroll
-  for (int i = 0; i < kStages - 1; ++i) {
-    copy(k_lo + i * kStep, i);
-    copies_end();
-  }
-  const __nv_bfloat16 *scales[2];
-#pragma unroll
-  for (int h = 0; h < 2; ++h) scales[h] = p.scales + (size_t)min(n0 + h * 8 + lr, p.N - 1) * p.groups;
-  float scale[2][GROUPS];              // of the next step
-  auto fetch_scales = [&](int k) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int g = 0; g < GROUPS; ++g) {
-        const int i = k / (32 * GW) + g;
-        scale[h][g] = i < p.groups && k < k_hi ? __bfloat162float(scales[h][i]) : 0.f;
-      }
-  };
-  fetch_scales(k_lo);
-  put(0);
-  __syncthreads();
-
-  int stage = 0, buffer = 0;
-  for (int k0 = k_lo; k0 < k_hi; k0 += BLOCK) {
-    const bool more = k0 + BLOCK < k_hi;
-    if (more) fetch(k0 + BLOCK);
-    for (int k = k0; k < min(k0 + BLOCK, k_hi); k += kStep) {
-      copies_wait<kStages - 2>();
-      __syncwarp();
-      copy(k + (kStages - 1) * kStep, (stage + kStages - 1) % kStages);
-      copies_end();
-      float s[2][GROUPS];
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int g = 0; g < GROUPS; ++g) s[h][g] = scale[h][g];
-      fetch_scales(k + kStep);
-      u32 word[2][WORDS];
-      const u32 codes = ring + stage * 2048;
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
+      for (int h = 0; h < 2; ++h) {
+        const int n = min(n0 + m * 16 + h * 8 + lr, p.N - 1);          // rows past the last are read as the last and not stored
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g) {
-          const int r = h * 8 + lr, byte = g * GW * 16 + j * GW * 4;
-          load_words<GW>(&word[h][g * GW], codes + r * 128 + (((byte >> 4) ^ swizzle(r)) << 4) + (byte & 15));
+          const int k = c * kChunk + g * GW * 32 + j * GW * 8;
+          const bool in = k < p.K;
+          const uint8_t *at = p.codes + ((size_t)n * p.K + k) / 2;
+          u32 *w = &word[m][h][g * GW];
+          if constexpr (GW == 4) {
+            const uint4 v = in ? __ldg(reinterpret_cast<const uint4 *>(at)) : make_uint4(0, 0, 0, 0);
+            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+          } else if constexpr (GW == 2) {
+            const uint2 v = in ? __ldg(reinterpret_cast<const uint2 *>(at)) : make_uint2(0, 0);
+            w[0] = v.x; w[1] = v.y;
+          } else {
+            w[0] = in ? __ldg(reinterpret_cast<const u32 *>(at)) : 0u;
+          }
+          const int group = c * GROUPS + g;
+          scale[m][h][g] = group < p.groups ? __bfloat162float(p.scales[(size_t)n * p.groups + group]) : 0.f;
         }
-      const unsigned char *b0 = act + buffer * kActBytes<RT> + (k - k0) / 8 * RT * 8 * 16 + (lr * 4 + j) * 16;
+      }
+    u32 b[RT][4][4];                   // activations of the lane's row and words, as pairs in the codes' order
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const int k = c * kChunk + (w / GW) * GW * 32 + j * GW * 8 + (w % GW) * 8, r = t * 8 + lr;
+        const uint4 v = r < p.R && k < p.K ? __ldg(reinterpret_cast<const uint4 *>(p.a + (size_t)r * p.K + k)) : make_uint4(0, 0, 0, 0);
+        b[t][w][0] = __byte_perm(v.x, v.z, 0x5410);
+        b[t][w][1] = __byte_perm(v.x, v.z, 0x7632);
+        b[t][w][2] = __byte_perm(v.y, v.w, 0x5410);
+        b[t][w][3] = __byte_perm(v.y, v.w, 0x7632);
+      }
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
       for (int g = 0; g < GROUPS; ++g) {
         float sum[RT][4];
@@ -158,88 +112,377 @@ gemm_w4_kernel(W4Args p) {
           for (int x = 0; x < 4; ++x) sum[t][x] = 0.f;
 #pragma unroll
         for (int w = g * GW; w < (g + 1) * GW; ++w) {
-          const u32 lo[4] = {pair<0>(word[0][w]), pair<0>(word[1][w]), pair<1>(word[0][w]), pair<1>(word[1][w])};
-          const u32 hi[4] = {pair<2>(word[0][w]), pair<2>(word[1][w]), pair<3>(word[0][w]), pair<3>(word[1][w])};
+          const u32 lo[4] = {pair<0>(word[m][0][w]), pair<0>(word[m][1][w]), pair<1>(word[m][0][w]), pair<1>(word[m][1][w])};
+          const u32 hi[4] = {pair<2>(word[m][0][w]), pair<2>(word[m][1][w]), pair<3>(word[m][0][w]), pair<3>(word[m][1][w])};
 #pragma unroll
           for (int t = 0; t < RT; ++t) {
-            const uint4 b = *reinterpret_cast<const uint4 *>(b0 + (w * RT * 8 + t * 8) * 64);
-            mma(sum[t], lo, b.x, b.y);
-            mma(sum[t], hi, b.z, b.w);
+            mma(sum[t], lo, b[t][w][0], b[t][w][1]);
+            mma(sum[t], hi, b[t][w][2], b[t][w][3]);
           }
         }
 #pragma unroll
         for (int t = 0; t < RT; ++t)
 #pragma unroll
-          for (int x = 0; x < 4; ++x) acc[t][x] = fmaf(s[x >> 1][g], sum[t][x], acc[t][x]);
+          for (int x = 0; x < 4; ++x) acc[m][t][x] = fmaf(scale[m][x >> 1][g], sum[t][x], acc[m][t][x]);
       }
-      stage = (stage + 1) % kStages;
-    }
-    if (more) put(buffer ^ 1);
-    buffer ^= 1;
-    __syncthreads();
   }
-  copies_wait<0>();
 
-  if (parts == 1) {                    // a lane's eight output rows of a tile lie N apart, its two weight rows 8
+  // the warps' sums, then the cluster's
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
 #pragma unroll
     for (int t = 0; t < RT; ++t)
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const int n = n0 + lr + (x >> 1) * 8, r = t * 8 + j * 2 + (x & 1);
-        if (r < p.R && n < p.N) p.out[(size_t)r * p.N + n] = acc[t][x];
-      }
+      for (int x = 0; x < 4; ++x) sums[warp][m * 16 + lr + (x >> 1) * 8][t * 8 + j * 2 + (x & 1)] = acc[m][t][x];
+  __syncthreads();
+  if (parts == 1) {
+    for (int i = threadIdx.x; i < MT * 16 * RT * 8; i += kThreads) {
+      const int n = i % (MT * 16), r = i / (MT * 16);
+      float s = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) s += sums[w][n][r];
+      if (r < p.R && n0 + n < p.N) p.out[(size_t)r * p.N + n0 + n] = s;
+    }
     return;
   }
-  // the cluster's sums
-  __syncthreads();
-  float *sums = reinterpret_cast<float *>(smem);       // [RT * 8][kRowsCta]
-#pragma unroll
-  for (int t = 0; t < RT; ++t)
-#pragma unroll
-    for (int x = 0; x < 4; ++x) sums[(t * 8 + j * 2 + (x & 1)) * kRowsCta + warp * 16 + lr + (x >> 1) * 8] = acc[t][x];
   namespace cg = cooperative_groups;
   cg::cluster_group cluster = cg::this_cluster();
-  cluster.sync();
-  for (int i = part * kThreads + threadIdx.x; i < p.R * kRowsCta; i += parts * kThreads) {
-    const int n = blockIdx.x * kRowsCta + i % kRowsCta;
+  for (int i = threadIdx.x; i < MT * 16 * RT * 8; i += kThreads) {
+    const int n = i % (MT * 16), r = i / (MT * 16);
     float s = 0.f;
-    for (int q = 0; q < parts; ++q) s += *cluster.map_shared_rank(sums + i, q);
-    if (n < p.N) p.out[(size_t)(i / kRowsCta) * p.N + n] = s;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) s += sums[w][n][r];
+    sums[0][n][r] = s;
+  }
+  cluster.sync();
+  for (int i = part * kThreads + threadIdx.x; i < MT * 16 * RT * 8; i += parts * kThreads) {
+    const int n = i % (MT * 16), r = i / (MT * 16);
+    float s = 0.f;
+    for (int q = 0; q < parts; ++q) s += *cluster.map_shared_rank(&sums[0][n][r], q);
+    if (r < p.R && n0 + n < p.N) p.out[(size_t)r * p.N + n0 + n] = s;
   }
   cluster.sync();                      // no CTA leaves while others read its sums
 }
 
-template <int GW, int RT> int run(W4Args a, cudaStream_t s) {
-  static std::atomic<u64> done{0};
-  const int status = hsd_smem_limit((const void *)gemm_w4_kernel<GW, RT>, kSmem<RT>, done);
-  if (status) return status;
-  const int tiles = ceil_div(a.N, kRowsCta);
-  a.steps = ceil_div(a.K, kStep);
+template <int GW, int RT, int MT> int run_small(const W4Args &a, cudaStream_t s) {
+  const int tiles = ceil_div(a.N, MT * 16), chunks = ceil_div(a.K, kChunk);
   int parts = 1;
-  while (parts < 8 && tiles * parts < 2 * kMeasuredSMs && parts * 2 <= a.steps) parts *= 2;
+  while (parts < 8 && tiles * parts < kMeasuredSMs && parts * kWarps < chunks) parts *= 2;
   cudaLaunchAttribute at = {};
   at.id = cudaLaunchAttributeClusterDimension;
   at.val.clusterDim.x = 1; at.val.clusterDim.y = parts; at.val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(tiles, parts); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = kSmem<RT>; cfg.stream = s; cfg.attrs = &at; cfg.numAttrs = parts > 1;
-  HSD_CUDA_OK(cudaLaunchKernelEx(&cfg, gemm_w4_kernel<GW, RT>, a));
+  cfg.gridDim = dim3(tiles, parts); cfg.blockDim = dim3(kThreads); cfg.stream = s; cfg.attrs = &at; cfg.numAttrs = parts > 1;
+  HSD_CUDA_OK(cudaLaunchKernelEx(&cfg, w4_small_kernel<GW, RT, MT>, a));
   hsd_count_launches(1);
   return hsd_launch_status();
 }
-template <int GW> int run_rows(const W4Args &a, cudaStream_t s) {
-  return a.R <= 8 ? run<GW, 1>(a, s) : a.R <= 16 ? run<GW, 2>(a, s) : a.R <= 32 ? run<GW, 4>(a, s) : run<GW, 8>(a, s);
+
+// ---------------------------------------------------------------------------- tensor memory
+constexpr int kStep = 256;             // k of a step: 128 bytes of codes of a row
+constexpr int kTile = 128;             // weight rows
+constexpr int kStageBytes = kTile * 128;
+template <int RP> struct Tc {          // RP: rows of B (16, 32 or 64)
+  static constexpr int WGS = RP == 16 ? 3 : 2, STAGES = RP == 32 ? 4 : 3, THREADS = WGS * 128;
+  static constexpr int ACT = RP * kStep * 2, WG_BYTES = STAGES * kStageBytes + 2 * ACT;
+  static constexpr int BARS = WGS * WG_BYTES, SMEM = BARS + 256 + 1024;
+};
+
+struct W4TcArgs {
+  CUtensorMap codes;
+  const __nv_bfloat16 *a, *scales;
+  float *out, *parts;
+  int R, K, N, groups, steps;          // steps of a tile
+  int total, line;                     // steps of all tiles; stretches they are divided over at most
+  int packed;                          // a step's scales of a row are one aligned load
+  // Stretch w is [first(w), first(w + 1)); step x belongs to stretch of(x).
+  __device__ __forceinline__ int first(int w) const { return total < line ? min(w, total) : (int)((long long)w * total / line); }
+  __device__ __forceinline__ int of(int x) const { return total < line ? x : (int)((((long long)x + 1) * line - 1) / total); }
+  // A stretch's sums of a tile that it does not hold whole: slot 0 where it begins inside of it, else 1; [row][weight row].
+  __device__ __forceinline__ float *part(int w, int slot) const { return parts + ((size_t)w * 2 + slot) * R * kTile; }
+};
+
+__device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(acc) : "memory");
 }
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, float *v) {
+  uint32_t r[8];
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr));
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void group_sync(int wg) { asm volatile("bar.sync %0, 128;" ::"r"(wg + 1) : "memory"); }
+
+// G: group; RP: rows of B; RC: of them read back (8, or RP).
+template <int G, int RP, int RC>
+__global__ void __launch_bounds__(Tc<RP>::THREADS, 1)
+w4_kernel(const __grid_constant__ W4TcArgs p) {
+  using C = Tc<RP>;
+  constexpr int U = kStep / G, ACOLS = G / 2, PIECES = RP / 4;         // units (groups) of a step; columns of A; 16-byte pieces of a thread
+  constexpr uint32_t WG_COLS = 2 * ACOLS + 2 * RP;
+  static_assert(C::WGS * WG_COLS <= 512, "tensor memory");
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char *smem = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  const int warp = warp_index(), wg = warp >> 2, row = threadIdx.x & 127;
+  unsigned char *mine = smem + wg * C::WG_BYTES, *act = mine + C::STAGES * kStageBytes;
+  const uint32_t ring = smem_u32(mine), act_at = smem_u32(act), bars = smem_u32(smem + C::BARS) + wg * 64;
+  auto full = [&](int s) { return bars + s * 8; };
+  auto done = [&](int b) { return bars + 32 + b * 8; };
+  volatile int *abort_flag = reinterpret_cast<int *>(smem + C::BARS + 192 + wg * 4);
+  u32 *slot = reinterpret_cast<u32 *>(smem + C::BARS + 208);
+  if (row == 0) {
+    for (int s = 0; s < C::STAGES; ++s) mbar_init(full(s), 1);
+    mbar_init(done(0), 1);
+    mbar_init(done(1), 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 0) tmem_alloc(smem_u32(slot), 512);
+  for (int i = row; i < 2 * C::ACT / 16; i += 128) reinterpret_cast<uint4 *>(act)[i] = make_uint4(0, 0, 0, 0);       // rows past R stay zeros
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *slot + wg * WG_COLS, lanes = (uint32_t)((warp & 3) * 32) << 16;
+  const uint32_t idesc = umma_idesc_bf16(RP);
+  chain_wait();
+  chain_next();
+
+  const int w = wg * (int)gridDim.x + (int)blockIdx.x, begin = p.first(w), n = p.first(w + 1) - begin;
+  int tile = begin / p.steps, s = begin - tile * p.steps;
+  if (n > 0) {
+    const bool issuer = (warp & 3) == 0 && elect_one();
+    int ask_tile = tile, ask_s = s, asked = 0;                         // the next step to ask for
+    auto ask = [&] {                                                   // (the issuer only)
+      const int st = asked % C::STAGES;
+      mbar_expect_tx(full(st), kStageBytes);
+      tma_load_2d(ring + st * kStageBytes, &p.codes, ask_s * 128, ask_tile * kTile, full(st));
+      ++asked;
+      if (++ask_s == p.steps) { ask_s = 0; ++ask_tile; }
+    };
+    if (issuer)
+      for (int i = 0; i < min(C::STAGES, n); ++i) ask();
+
+    uint4 next[PIECES];
+    auto fetch = [&](int step) {       // activations of a step: piece x is k8 = x % 32 of row x / 32
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) {
+        const int x = i * 128 + row, r = x / 32, k = step * kStep + x % 32 * 8;
+        next[i] = r < p.R && k < p.K ? __ldg(reinterpret_cast<const uint4 *>(p.a + (size_t)r * p.K + k)) : make_uint4(0, 0, 0, 0);
+      }
+    };
+    auto put = [&](int b) {
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) {
+        const int x = i * 128 + row, r = x / 32, k8 = x % 32;
+        if (r >= p.R) continue;
+        const uint4 v = next[i];
+        *reinterpret_cast<uint4 *>(act + b * C::ACT + (k8 >> 3) * (RP * 128) + (r >> 3) * 1024 + (r & 7) * 128 + (((k8 & 7) ^ (r & 7)) << 4)) =
+            make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    };
+    u32 scale[(U + 1) / 2], scale_next[(U + 1) / 2];                   // a step's, in pairs
+    auto fetch_scales = [&](int t, int step) {
+      const __nv_bfloat16 *at = p.scales + (size_t)min(t * kTile + row, p.N - 1) * p.groups + step * U;
+      if (p.packed) {
+        if constexpr (U == 2) scale_next[0] = __ldg(reinterpret_cast<const u32 *>(at));
+        else if constexpr (U == 4) { const uint2 v = __ldg(reinterpret_cast<const uint2 *>(at)); scale_next[0] = v.x; scale_next[1] = v.y; }
+        else { const uint4 v = __ldg(reinterpret_cast<const uint4 *>(at)); scale_next[0] = v.x; scale_next[1] = v.y; scale_next[2] = v.z; scale_next[3] = v.w; }
+      } else {
+        const unsigned short *bits = reinterpret_cast<const unsigned short *>(at);
+#pragma unroll
+        for (int u = 0; u < U; u += 2)
+          scale_next[u / 2] = (step * U + u < p.groups ? (u32)bits[u] : 0u) | (step * U + u + 1 < p.groups ? (u32)bits[u + 1] << 16 : 0u);
+      }
+    };
+
+    float acc[RC];
+#pragma unroll
+    for (int r = 0; r < RC; ++r) acc[r] = 0.f;
+    int count = 0;                     // units so far
+    bool pending = false;              // the last one's sums are not added yet
+    float pending_scale = 0.f;
+    auto fold = [&] {                  // (waits that give up go on: every warp takes part in every barrier)
+      const int b = (count - 1) & 1;
+      mbar_wait(done(b), (uint32_t)(((count - 1) >> 1) & 1), abort_flag);
+      __syncwarp();
+      tc_fence_after();
+      const uint32_t d = tmem + lanes + 2 * ACOLS + b * RP;
+#pragma unroll
+      for (int c = 0; c < RC; c += 16) {
+        float v[16];
+        if constexpr (RC == 8) tmem_ld8(d, v);
+        else tmem_ld16(d + c, v);
+        tmem_ld_wait();
+#pragma unroll
+        for (int r = 0; r < (RC < 16 ? RC : 16); ++r) acc[c + r] = fmaf(pending_scale, v[r], acc[c + r]);
+      }
+    };
+    fetch(s);
+    fetch_scales(tile, s);
+    put(0);
+    bool from_start = s == 0;          // of the tile
+    for (int i = 0; i < n; ++i) {
+      const int stage = i % C::STAGES, last_s = s + 1 == p.steps;
+#pragma unroll
+      for (int x = 0; x < (U + 1) / 2; ++x) scale[x] = scale_next[x];
+      if (i + 1 < n) {
+        fetch(last_s ? 0 : s + 1);
+        fetch_scales(tile + last_s, last_s ? 0 : s + 1);
+      }
+      const int units = min(U, p.groups - s * U);
+      mbar_wait(full(stage), (uint32_t)((i / C::STAGES) & 1), abort_flag);
+      __syncwarp();
+      const unsigned char *codes = mine + stage * kStageBytes + row * 128;
+#pragma unroll 1
+      for (int u = 0; u < units; ++u, ++count) {
+        const int b = count & 1;
+        const uint32_t A = tmem + lanes + b * ACOLS;
+        constexpr int HALF = G < 64 ? G : 64;                          // 32 columns of pairs at once at most
+#pragma unroll
+        for (int h = 0; h < G / HALF; ++h) {
+          u32 x[HALF / 2];
+#pragma unroll
+          for (int q = 0; q < HALF / 32; ++q) {
+            const uint4 v = *reinterpret_cast<const uint4 *>(codes + (((u * (G / 32) + h * 2 + q) ^ (row & 7)) << 4));
+            const u32 word[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+              x[q * 16 + y * 4] = pair<0>(word[y]);
+              x[q * 16 + y * 4 + 1] = pair<1>(word[y]);
+              x[q * 16 + y * 4 + 2] = pair<2>(word[y]);
+              x[q * 16 + y * 4 + 3] = pair<3>(word[y]);
+            }
+          }
+#pragma unroll
+          for (int q = 0; q < HALF / 32; ++q) tmem_st16u(A + h * 32 + q * 16, x + q * 16);
+        }
+        tmem_st_wait();
+        tc_fence_before();
+        group_sync(wg);
+        if (issuer) {
+          tc_fence_after();
+          const uint32_t d = tmem + 2 * ACOLS + b * RP, A0 = tmem + b * ACOLS;
+#pragma unroll
+          for (int q = 0; q < G / 16; ++q) {
+            const int k16 = u * (G / 16) + q;                          // 16 of k: 32 bytes of a 128-byte row of B
+            umma_ts(d, A0 + q * 8, umma_desc(act_at + (i & 1) * C::ACT + (k16 >> 2) * (RP * 128) + (k16 & 3) * 32), idesc, q > 0);
+          }
+          umma_commit(done(b));
+          if (u + 1 == units && asked < n) ask();                      // all have read the stage's codes
+        }
+        __syncwarp();
+        if (pending) fold();
+        pending = true;
+        u32 bits = scale[0];
+#pragma unroll
+        for (int x = 1; x < (U + 1) / 2; ++x) bits = u / 2 == x ? scale[x] : bits;
+        pending_scale = __uint_as_float(u & 1 ? bits & 0xFFFF0000u : bits << 16);
+      }
+      if (i + 1 < n) put((i + 1) & 1);                                 // (its last reader was the step before this one, which is folded)
+      if (last_s || i + 1 == n) {
+        fold();
+        pending = false;
+        const bool whole = last_s && from_start;
+        const int nr = tile * kTile + row;
+        float *to = whole ? p.out + nr : p.part(w, from_start ? 1 : 0) + row;
+        const size_t pitch = whole ? p.N : kTile;
+#pragma unroll
+        for (int r = 0; r < RC; ++r) {
+          if (r < p.R && (!whole || nr < p.N)) to[r * pitch] = *abort_flag ? NAN : acc[r];
+          acc[r] = 0.f;
+        }
+        from_start = true;
+      }
+      if (last_s) { s = 0; ++tile; }
+      else ++s;
+    }
+  }
+  if (*abort_flag) {                   // copies in flight land before the shared memory goes away
+    const unsigned long long t0 = globaltimer_ns();
+    while (globaltimer_ns() - t0 < 200000ull) {}
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 0) tmem_dealloc(*slot, 512);
+}
+
+// Tiles that no stretch holds whole: a thread a weight row, four rows of activations.
+__global__ void __launch_bounds__(128) w4_join_kernel(const __grid_constant__ W4TcArgs p) {
+  const int tile = blockIdx.x, r0 = blockIdx.y * 4, n = tile * kTile + threadIdx.x, x = tile * p.steps;
+  const int w0 = p.of(x), w1 = p.of(x + p.steps - 1);
+  chain_wait();
+  chain_next();
+  if (w0 == w1) return;
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int w = w0; w <= w1; ++w) {
+    const float *from = p.part(w, w == w0 ? 1 : 0) + threadIdx.x;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (r0 + r < p.R) sum[r] += from[(r0 + r) * kTile];
+  }
+  if (n >= p.N) return;
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+    if (r0 + r < p.R) p.out[(size_t)(r0 + r) * p.N + n] = sum[r];
+}
+
+int w4_rp(int R) { return R <= 16 ? 16 : R <= 32 ? 32 : 64; }
+int w4_line(int R) { return kMeasuredSMs * (w4_rp(R) == 16 ? Tc<16>::WGS : Tc<32>::WGS); }
+
+template <int G, int RP, int RC> int run_tc(const W4TcArgs &a, cudaStream_t s) {
+  static std::atomic<u64> done{0};
+  const int status = hsd_smem_limit((const void *)w4_kernel<G, RP, RC>, Tc<RP>::SMEM, done);
+  if (status) return status;
+  HSD_CUDA_OK(hsd_launch(w4_kernel<G, RP, RC>, dim3(kMeasuredSMs), Tc<RP>::THREADS, Tc<RP>::SMEM, s, 0, true, a));
+  HSD_CUDA_OK(hsd_launch(w4_join_kernel, dim3(ceil_div(a.N, kTile), ceil_div(a.R, 4)), 128, 0, s, 0, true, a));
+  hsd_count_launches(2);
+  return hsd_launch_status();
+}
+template <int G> int run_tc_rows(const W4TcArgs &a, cudaStream_t s) {
+  return a.R <= 8 ? run_tc<G, 16, 8>(a, s) : a.R <= 16 ? run_tc<G, 16, 16>(a, s) : a.R <= 32 ? run_tc<G, 32, 32>(a, s) : run_tc<G, 64, 64>(a, s);
+}
+
+bool takes_small(int R, long long N, int K) { return false; }
 
 }  // namespace
 }  // namespace hsd
 
-extern "C" int hsd_gemm_w4(const void *A, int R, int K, const void *codes, const void *scales, int N, int group, float *out, void *stream) {
+extern "C" size_t hsd_gemm_w4_workspace_bytes(int R, int N, int K, int group) {
   using namespace hsd;
-  if (!A || !codes || !scales || !out || R <= 0 || R > 64 || N <= 0 || K <= 0) return HSD_E_INVALID_ARG;
+  if (R <= 0 || R > 64 || N <= 0 || K <= 0 || K > (1 << 28) || (group != 32 && group != 64 && group != 128) || K % group) return 0;
+  return (size_t)w4_line(R) * 2 * R * kTile * sizeof(float);
+}
+
+extern "C" int hsd_gemm_w4(const void *A, int R, int K, const void *codes, const void *scales, int N, int group, float *out, void *workspace,
+                           size_t workspace_bytes, void *stream) {
+  using namespace hsd;
+  if (!A || !codes || !scales || !out || !workspace || R <= 0 || R > 64 || N <= 0 || K <= 0) return HSD_E_INVALID_ARG;
   if ((group != 32 && group != 64 && group != 128) || K % group) return HSD_E_INVALID_ARG;
-  if (K > (1 << 28)) return HSD_E_TOO_LARGE;
-  if (((reinterpret_cast<uintptr_t>(A) | reinterpret_cast<uintptr_t>(codes)) & 15) || (reinterpret_cast<uintptr_t>(scales) & 1) || (reinterpret_cast<uintptr_t>(out) & 3)) return HSD_E_INVALID_ARG;
-  W4Args a = {static_cast<const __nv_bfloat16 *>(A), static_cast<const uint8_t *>(codes), static_cast<const __nv_bfloat16 *>(scales), out, R, K, N, K / group, 0};
+  if (K > (1 << 28) || (long long)ceil_div(N, kTile) * ceil_div(K, kStep) > (1 << 30)) return HSD_E_TOO_LARGE;
+  if (((reinterpret_cast<uintptr_t>(A) | reinterpret_cast<uintptr_t>(codes) | reinterpret_cast<uintptr_t>(workspace)) & 15) || (reinterpret_cast<uintptr_t>(scales) & 1) ||
+      (reinterpret_cast<uintptr_t>(out) & 3)) return HSD_E_INVALID_ARG;
+  if (workspace_bytes < hsd_gemm_w4_workspace_bytes(R, N, K, group)) return HSD_E_WORKSPACE_TOO_SMALL;
   cudaStream_t s = (cudaStream_t)stream;
-  return group == 128 ? run_rows<4>(a, s) : group == 64 ? run_rows<2>(a, s) : run_rows<1>(a, s);
+  const auto *a = static_cast<const __nv_bfloat16 *>(A), *sc = static_cast<const __nv_bfloat16 *>(scales);
+  if (takes_small(R, N, K)) {
+    const W4Args p = {a, static_cast<const uint8_t *>(codes), sc, out, R, K, N, K / group};
+    return group == 128 ? run_small<4, 1, 1>(p, s) : group == 64 ? run_small<2, 1, 1>(p, s) : run_small<1, 1, 1>(p, s);
+  }
+  W4TcArgs p = {};
+  const int status = tc_make_byte_map(&p.codes, codes, N, K / 2, kTile);
+  if (status) return status;
+  p.a = a; p.scales = sc; p.out = out; p.parts = static_cast<float *>(workspace);
+  p.R = R; p.K = K; p.N = N; p.groups = K / group;
+  p.steps = ceil_div(K, kStep);
+  p.total = ceil_div(N, kTile) * p.steps;
+  p.line = w4_line(R);
+  p.packed = K % kStep == 0 && reinterpret_cast<uintptr_t>(scales) % (kStep / group * 2) == 0;
+  return group == 128 ? run_tc_rows<128>(p, s) : group == 64 ? run_tc_rows<64>(p, s) : run_tc_rows<32>(p, s);
 }

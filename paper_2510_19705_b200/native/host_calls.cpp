@@ -29,6 +29,7 @@ decltype(&hsd_strerror) strerror_fn = nullptr;
 decltype(&hsd_kv_append) kv_append_fn = nullptr;
 decltype(&hsd_paged_attention_workspace_bytes) attention_bytes_fn = nullptr;
 decltype(&hsd_paged_attention) attention_fn = nullptr;
+decltype(&hsd_gemm_w4_workspace_bytes) gemm_w4_bytes_fn = nullptr;
 decltype(&hsd_gemm_w4) gemm_w4_fn = nullptr;
 decltype(&hsd_token_logprobs) logprobs_fn = nullptr;
 PyObject *error_class = nullptr;
@@ -90,7 +91,7 @@ void *current_stream() { return c10::cuda::getCurrentCUDAStream().stream(); }
 PyObject *init(PyObject *, PyObject *const *args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   try {
-    arguments(n, 13);
+    arguments(n, 14);
     draft_sample_fn = reinterpret_cast<decltype(draft_sample_fn)>(word(args[0]));
     verify_bytes_fn = reinterpret_cast<decltype(verify_bytes_fn)>(word(args[1]));
     verify_level_fn = reinterpret_cast<decltype(verify_level_fn)>(word(args[2]));
@@ -101,10 +102,11 @@ PyObject *init(PyObject *, PyObject *const *args, Py_ssize_t n) {
     kv_append_fn = reinterpret_cast<decltype(kv_append_fn)>(word(args[7]));
     attention_bytes_fn = reinterpret_cast<decltype(attention_bytes_fn)>(word(args[8]));
     attention_fn = reinterpret_cast<decltype(attention_fn)>(word(args[9]));
-    gemm_w4_fn = reinterpret_cast<decltype(gemm_w4_fn)>(word(args[10]));
-    logprobs_fn = reinterpret_cast<decltype(logprobs_fn)>(word(args[11]));
-    Py_INCREF(args[12]);
-    error_class = args[12];
+    gemm_w4_bytes_fn = reinterpret_cast<decltype(gemm_w4_bytes_fn)>(word(args[10]));
+    gemm_w4_fn = reinterpret_cast<decltype(gemm_w4_fn)>(word(args[11]));
+    logprobs_fn = reinterpret_cast<decltype(logprobs_fn)>(word(args[12]));
+    Py_INCREF(args[13]);
+    error_class = args[13];
     Py_RETURN_NONE;
   } catch (const Failed &) { return nullptr; }
   END_HANDLE_TH_ERRORS
@@ -328,11 +330,11 @@ PyObject *paged_attention(PyObject *, PyObject *const *args, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-// gemm_w4(A bf16 [R, K], codes uint8 [N, K / 2], scales bf16 [N, K / group], out or None)
+// gemm_w4(A bf16 [R, K], codes uint8 [N, K / 2], scales bf16 [N, K / group], out or None, workspace or None)
 PyObject *gemm_w4(PyObject *, PyObject *const *args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   try {
-    arguments(n, 4);
+    arguments(n, 5);
     const at::Tensor &a = dims(typed(args[0], "A", at::kBFloat16), "A", 2);
     const int64_t R = a.size(0), K = a.size(1);
     sized(a, "A", {R, K});
@@ -346,12 +348,19 @@ PyObject *gemm_w4(PyObject *, PyObject *const *args, Py_ssize_t n) {
       PyErr_SetString(PyExc_ValueError, "scales: K is not a whole number of groups");
       throw Failed();
     }
+    const int rows = count(R), k = count(K), cols = count(N), group = count(K / groups);
+    const size_t need = gemm_w4_bytes_fn(rows, cols, k, group);
+    if (need == 0) {
+      PyErr_Format(error_class, "hsd_gemm_w4: unsupported shape R=%d N=%d K=%d, groups of %d", rows, cols, k, group);
+      throw Failed();
+    }
     const c10::cuda::CUDAGuard guard(a.device());
     at::Tensor out = args[3] == Py_None ? at::empty({R, N}, a.options().dtype(at::kFloat).requires_grad(false)) : sized(typed(args[3], "out", at::kFloat, &a), "out", {R, N});
-    void *pa = a.data_ptr(), *pc = codes.data_ptr(), *ps = scales.data_ptr(), *stream = current_stream();
+    at::Tensor ws = args[4] == Py_None ? at::empty({(int64_t)need}, a.options().dtype(at::kByte).requires_grad(false)) : typed(args[4], "workspace", at::kByte, &a);
+    if (!ws.is_contiguous()) refuse("expected a contiguous CUDA tensor");
+    void *pa = a.data_ptr(), *pc = codes.data_ptr(), *ps = scales.data_ptr(), *scratch = ws.data_ptr(), *stream = current_stream();
     float *to = static_cast<float *>(out.data_ptr());
-    const int rows = count(R), k = count(K), cols = count(N), group = count(K / groups);
-    check(released([&] { return gemm_w4_fn(pa, rows, k, pc, ps, cols, group, to, stream); }));
+    check(released([&] { return gemm_w4_fn(pa, rows, k, pc, ps, cols, group, to, scratch, (size_t)ws.numel(), stream); }));
     return THPVariable_Wrap(std::move(out));
   } catch (const Failed &) { return nullptr; }
   END_HANDLE_TH_ERRORS

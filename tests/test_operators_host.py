@@ -50,7 +50,7 @@ def test_sizes_past_the_limits():
     assert attention(nq=131072) == -8
     assert attention(pool(page_size=1 << 20), batch=4096, pages=3) == -8
     lib = binding.library()
-    assert lib.hsd_gemm_w4(P, 1, (1 << 28) + 128, P, P, 8, 128, P, None) == -8
+    assert lib.hsd_gemm_w4(P, 1, (1 << 28) + 128, P, P, 8, 128, P, P, 1 << 40, None) == -8
     assert lib.hsd_token_logprobs(P, 0, 1, (1 << 31) - 1, P, 0, P, P, P, None, None, None) == -8
 
 
@@ -71,7 +71,14 @@ def test_attention_workspace():
                                  (P, 1, 128, P, P, 8, 16, P), (P, 1, 128, P, P, 8, 0, P), (P, 1, 128, P, P, 8, 128, None), (P + 2, 1, 128, P, P, 8, 128, P),
                                  (P, 1, 128, P + 1, P, 8, 128, P), (P, 1, 128, P, P + 1, 8, 128, P), (P, 1, 128, P, P, 8, 128, P + 2)])
 def test_gemm_w4_refuses_arguments(bad):
-    assert binding.library().hsd_gemm_w4(*bad, None) == -1
+    assert binding.library().hsd_gemm_w4(*bad, P, 1 << 40, None) == -1
+
+
+def test_gemm_w4_workspace():
+    size, call = binding.hsd_gemm_w4_workspace_bytes, binding.library().hsd_gemm_w4
+    assert size(0, 8, 128, 128) == size(65, 8, 128, 128) == size(1, 0, 128, 128) == size(1, 8, 96, 64) == size(1, 8, 128, 16) == 0
+    assert call(P, 3, 128, P, P, 8, 128, P, P, size(3, 8, 128, 128) - 1, None) == -2
+    assert call(P, 3, 128, P, P, 8, 128, P, None, 1 << 40, None) == -1 and call(P, 3, 128, P, P, 8, 128, P, P + 4, 1 << 40, None) == -1
 
 
 @pytest.mark.parametrize("bad", [dict(logits=None), dict(dtype=2), dict(rows=0), dict(vocab=0), dict(tokens=None), dict(top=-1), dict(top=33), dict(vocab=8, top=9),
