@@ -6,7 +6,7 @@
 // w4_kernel: 128 weight rows a tile, a thread one row.  Codes come by TMA, the pairs go from registers into tensor memory, from where
 // tcgen05.mma takes them as its operand A (the activations, at most 64 rows, are B); a thread reads its row's sums of a group
 // back and scales them.  The tiles' steps (256 of k) stand in one line that is divided evenly over warpgroups, three on an SM (two
-// for more than 16 rows), which wait for nothing but their own loads; where a stretch ends inside a tile its sums go to the workspace
+// for more than 16 rows), each with a warp of its own that asks for codes and issues products; where a stretch ends inside a tile its sums go to the workspace
 // and w4_join_kernel adds them in order.
 // w4_small_kernel: see there.
 #include <cooperative_groups.h>
@@ -28,15 +28,20 @@ struct W4Args {
   const __nv_bfloat16 *scales;
   float *out;
   int R, K, N, groups;                 // groups of a row
+  u32 bits;                            // kCodeBits
 };
 
 __device__ __forceinline__ void mma(float *c, const u32 *a, u32 b0, u32 b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// Codes i and i + 4 of a word, less 8, as two bf16.
-template <int I> __device__ __forceinline__ u32 pair(u32 word) {
-  const u32 x = ((word >> (4 * I)) & 0x000F000Fu) | 0x43004300u, bias = 0x43084308u;
+// Codes i and i + 4 of a word, less 8, as two bf16.  `bits` is 0x43004300 out of the arguments: as a constant it and the mask do not fit
+// one instruction.
+constexpr u32 kCodeBits = 0x43004300u;
+template <int I> __device__ __forceinline__ u32 pair(u32 word, u32 bits) {
+  u32 x;
+  asm("lop3.b32 %0, %1, 0x000F000F, %2, 0xEA;" : "=r"(x) : "r"(I ? word >> (4 * I) : word), "r"(bits));
+  const u32 bias = 0x43084308u;
   const __nv_bfloat162 y = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&x), *reinterpret_cast<const __nv_bfloat162 *>(&bias));
   return *reinterpret_cast<const u32 *>(&y);
 }
@@ -112,8 +117,8 @@ w4_small_kernel(W4Args p) {
           for (int x = 0; x < 4; ++x) sum[t][x] = 0.f;
 #pragma unroll
         for (int w = g * GW; w < (g + 1) * GW; ++w) {
-          const u32 lo[4] = {pair<0>(word[m][0][w]), pair<0>(word[m][1][w]), pair<1>(word[m][0][w]), pair<1>(word[m][1][w])};
-          const u32 hi[4] = {pair<2>(word[m][0][w]), pair<2>(word[m][1][w]), pair<3>(word[m][0][w]), pair<3>(word[m][1][w])};
+          const u32 lo[4] = {pair<0>(word[m][0][w], p.bits), pair<0>(word[m][1][w], p.bits), pair<1>(word[m][0][w], p.bits), pair<1>(word[m][1][w], p.bits)};
+          const u32 hi[4] = {pair<2>(word[m][0][w], p.bits), pair<2>(word[m][1][w], p.bits), pair<3>(word[m][0][w], p.bits), pair<3>(word[m][1][w], p.bits)};
 #pragma unroll
           for (int t = 0; t < RT; ++t) {
             mma(sum[t], lo, b[t][w][0], b[t][w][1]);
@@ -183,7 +188,7 @@ constexpr int kStep = 256;             // k of a step: 128 bytes of codes of a r
 constexpr int kTile = 128;             // weight rows
 constexpr int kStageBytes = kTile * 128;
 template <int RP> struct Tc {          // RP: rows of B (16, 32 or 64)
-  static constexpr int WGS = RP == 16 ? 3 : 2, STAGES = RP == 32 ? 4 : 3, THREADS = WGS * 128;
+  static constexpr int WGS = RP == 16 ? 3 : 2, STAGES = RP == 32 ? 4 : 3, WORKERS = WGS * 4, THREADS = WGS * 160;
   static constexpr int ACT = RP * kStep * 2, WG_BYTES = STAGES * kStageBytes + 2 * ACT;
   static constexpr int BARS = WGS * WG_BYTES, SMEM = BARS + 256 + 1024;
 };
@@ -195,6 +200,7 @@ struct W4TcArgs {
   int R, K, N, groups, steps;          // steps of a tile
   int total, line;                     // steps of all tiles; stretches they are divided over at most
   int packed;                          // a step's scales of a row are one aligned load
+  u32 bits;                            // kCodeBits
   // Stretch w is [first(w), first(w + 1)); step x belongs to stretch of(x).
   __device__ __forceinline__ int first(int w) const { return total < line ? min(w, total) : (int)((long long)w * total / line); }
   __device__ __forceinline__ int of(int x) const { return total < line ? x : (int)((((long long)x + 1) * line - 1) / total); }
@@ -214,7 +220,6 @@ __device__ __forceinline__ void tmem_ld8(uint32_t taddr, float *v) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
 }
-__device__ __forceinline__ void group_sync(int wg) { asm volatile("bar.sync %0, 128;" ::"r"(wg + 1) : "memory"); }
 
 // G: group; RP: rows of B; RC: of them read back (8, or RP).
 template <int G, int RP, int RC>
@@ -226,22 +231,27 @@ w4_kernel(const __grid_constant__ W4TcArgs p) {
   static_assert(C::WGS * WG_COLS <= 512, "tensor memory");
   extern __shared__ unsigned char smem_raw[];
   unsigned char *smem = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  const int warp = warp_index(), wg = warp >> 2, row = threadIdx.x & 127;
+  const int warp = warp_index(), lane = threadIdx.x & 31, row = threadIdx.x & 127;
+  const bool worker = warp < C::WORKERS;
+  const int wg = worker ? warp >> 2 : warp - C::WORKERS;
   unsigned char *mine = smem + wg * C::WG_BYTES, *act = mine + C::STAGES * kStageBytes;
   const uint32_t ring = smem_u32(mine), act_at = smem_u32(act), bars = smem_u32(smem + C::BARS) + wg * 64;
   auto full = [&](int s) { return bars + s * 8; };
   auto done = [&](int b) { return bars + 32 + b * 8; };
+  auto ready = [&](int b) { return bars + 48 + b * 8; };
   volatile int *abort_flag = reinterpret_cast<int *>(smem + C::BARS + 192 + wg * 4);
   u32 *slot = reinterpret_cast<u32 *>(smem + C::BARS + 208);
-  if (row == 0) {
+  if (worker && row == 0) {
     for (int s = 0; s < C::STAGES; ++s) mbar_init(full(s), 1);
+    mbar_init(ready(0), 4);
+    mbar_init(ready(1), 4);
     mbar_init(done(0), 1);
     mbar_init(done(1), 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 0) tmem_alloc(smem_u32(slot), 512);
-  for (int i = row; i < 2 * C::ACT / 16; i += 128) reinterpret_cast<uint4 *>(act)[i] = make_uint4(0, 0, 0, 0);       // rows past R stay zeros
+  for (int i = row; worker && i < 2 * C::ACT / 16; i += 128) reinterpret_cast<uint4 *>(act)[i] = make_uint4(0, 0, 0, 0);     // rows past R stay zeros
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -252,9 +262,10 @@ w4_kernel(const __grid_constant__ W4TcArgs p) {
 
   const int w = wg * (int)gridDim.x + (int)blockIdx.x, begin = p.first(w), n = p.first(w + 1) - begin;
   int tile = begin / p.steps, s = begin - tile * p.steps;
-  if (n > 0) {
-    const bool issuer = (warp & 3) == 0 && elect_one();
-    int ask_tile = tile, ask_s = s, asked = 0;                         // the next step to ask for
+  if (n > 0 && !worker) {
+    // ---------------------------------------------------------------- codes, products
+    const bool issuer = elect_one();
+    int ask_tile = tile, ask_s = s, asked = 0, count = 0;              // the next step to ask for; units so far
     auto ask = [&] {                                                   // (the issuer only)
       const int st = asked % C::STAGES;
       mbar_expect_tx(full(st), kStageBytes);
@@ -264,7 +275,29 @@ w4_kernel(const __grid_constant__ W4TcArgs p) {
     };
     if (issuer)
       for (int i = 0; i < min(C::STAGES, n); ++i) ask();
-
+    for (int i = 0; i < n; ++i) {
+      const int units = min(U, p.groups - s * U);
+#pragma unroll 1
+      for (int u = 0; u < units; ++u, ++count) {
+        const int b = count & 1;
+        mbar_wait_warp(ready(b), (uint32_t)((count >> 1) & 1), abort_flag);    // (waits that give up go on, here and in the workers)
+        tc_fence_after();
+        if (issuer) {
+          const uint32_t d = tmem + 2 * ACOLS + b * RP, A0 = tmem + b * ACOLS;
+#pragma unroll
+          for (int q = 0; q < G / 16; ++q) {
+            const int k16 = u * (G / 16) + q;                          // 16 of k: 32 bytes of a 128-byte row of B
+            umma_ts(d, A0 + q * 8, umma_desc(act_at + (i & 1) * C::ACT + (k16 >> 2) * (RP * 128) + (k16 & 3) * 32), idesc, q > 0);
+          }
+          umma_commit(done(b));
+          if (u + 1 == units && asked < n) ask();                      // all have read the stage's codes
+        }
+        __syncwarp();
+      }
+      if (++s == p.steps) s = 0;
+    }
+  } else if (n > 0) {
+    // ---------------------------------------------------------------- codes -> pairs -> tensor memory -> sums
     uint4 next[PIECES];
     auto fetch = [&](int step) {       // activations of a step: piece x is k8 = x % 32 of row x / 32
 #pragma unroll
@@ -305,7 +338,7 @@ w4_kernel(const __grid_constant__ W4TcArgs p) {
     int count = 0;                     // units so far
     bool pending = false;              // the last one's sums are not added yet
     float pending_scale = 0.f;
-    auto fold = [&] {                  // (waits that give up go on: every warp takes part in every barrier)
+    auto fold = [&] {
       const int b = (count - 1) & 1;
       mbar_wait(done(b), (uint32_t)(((count - 1) >> 1) & 1), abort_flag);
       __syncwarp();
@@ -351,10 +384,10 @@ w4_kernel(const __grid_constant__ W4TcArgs p) {
             const u32 word[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
             for (int y = 0; y < 4; ++y) {
-              x[q * 16 + y * 4] = pair<0>(word[y]);
-              x[q * 16 + y * 4 + 1] = pair<1>(word[y]);
-              x[q * 16 + y * 4 + 2] = pair<2>(word[y]);
-              x[q * 16 + y * 4 + 3] = pair<3>(word[y]);
+              x[q * 16 + y * 4] = pair<0>(word[y], p.bits);
+              x[q * 16 + y * 4 + 1] = pair<1>(word[y], p.bits);
+              x[q * 16 + y * 4 + 2] = pair<2>(word[y], p.bits);
+              x[q * 16 + y * 4 + 3] = pair<3>(word[y], p.bits);
             }
           }
 #pragma unroll
@@ -362,19 +395,8 @@ w4_kernel(const __grid_constant__ W4TcArgs p) {
         }
         tmem_st_wait();
         tc_fence_before();
-        group_sync(wg);
-        if (issuer) {
-          tc_fence_after();
-          const uint32_t d = tmem + 2 * ACOLS + b * RP, A0 = tmem + b * ACOLS;
-#pragma unroll
-          for (int q = 0; q < G / 16; ++q) {
-            const int k16 = u * (G / 16) + q;                          // 16 of k: 32 bytes of a 128-byte row of B
-            umma_ts(d, A0 + q * 8, umma_desc(act_at + (i & 1) * C::ACT + (k16 >> 2) * (RP * 128) + (k16 & 3) * 32), idesc, q > 0);
-          }
-          umma_commit(done(b));
-          if (u + 1 == units && asked < n) ask();                      // all have read the stage's codes
-        }
         __syncwarp();
+        if (lane == 0) mbar_arrive(ready(b));
         if (pending) fold();
         pending = true;
         u32 bits = scale[0];
@@ -472,7 +494,7 @@ extern "C" int hsd_gemm_w4(const void *A, int R, int K, const void *codes, const
   cudaStream_t s = (cudaStream_t)stream;
   const auto *a = static_cast<const __nv_bfloat16 *>(A), *sc = static_cast<const __nv_bfloat16 *>(scales);
   if (takes_small(R, N, K)) {
-    const W4Args p = {a, static_cast<const uint8_t *>(codes), sc, out, R, K, N, K / group};
+    const W4Args p = {a, static_cast<const uint8_t *>(codes), sc, out, R, K, N, K / group, kCodeBits};
     return group == 128 ? run_small<4, 1, 1>(p, s) : group == 64 ? run_small<2, 1, 1>(p, s) : run_small<1, 1, 1>(p, s);
   }
   W4TcArgs p = {};
@@ -483,6 +505,7 @@ extern "C" int hsd_gemm_w4(const void *A, int R, int K, const void *codes, const
   p.steps = ceil_div(K, kStep);
   p.total = ceil_div(N, kTile) * p.steps;
   p.line = w4_line(R);
+  p.bits = kCodeBits;
   p.packed = K % kStep == 0 && reinterpret_cast<uintptr_t>(scales) % (kStep / group * 2) == 0;
   return group == 128 ? run_tc_rows<128>(p, s) : group == 64 ? run_tc_rows<64>(p, s) : run_tc_rows<32>(p, s);
 }
