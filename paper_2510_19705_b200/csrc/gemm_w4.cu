@@ -4,8 +4,8 @@
 // the pairs are (0,4), (1,5), (2,6), (3,7) of a word; the order of k inside a product is free, so the activations are put in the same.
 // A group's products are summed in the tensor cores' fp32, then scaled and added in fp32: no rounding to fewer bits anywhere.
 // w4_kernel: 128 weight rows a tile, a thread one row.  Codes come by TMA, the pairs go from registers into tensor memory, from where
-// tcgen05.mma takes them as its operand A (the activations, at most 64 rows, are B); a thread reads its row's sums of a group
-// back and scales them.  The tiles' steps (256 of k) stand in one line that is divided evenly over warpgroups, three on an SM (two
+// tcgen05.mma takes them as its operand A (the activations, at most 64 rows, are B, once put in the pairs' order by w4_stage_kernel);
+// a thread reads its row's sums of a group back and scales them.  The tiles' steps (256 of k) stand in one line that is divided evenly over warpgroups, three on an SM (two
 // for more than 16 rows), each with a warp of its own that asks for codes and issues products; where a stretch ends inside a tile its sums go to the workspace
 // and w4_join_kernel adds them in order.
 // w4_small_kernel: see there.
@@ -188,14 +188,15 @@ constexpr int kStep = 256;             // k of a step: 128 bytes of codes of a r
 constexpr int kTile = 128;             // weight rows
 constexpr int kStageBytes = kTile * 128;
 template <int RP> struct Tc {          // RP: rows of B (16, 32 or 64)
-  static constexpr int WGS = RP == 16 ? 3 : 2, STAGES = RP == 32 ? 4 : 3, WORKERS = WGS * 4, THREADS = WGS * 160;
-  static constexpr int ACT = RP * kStep * 2, WG_BYTES = STAGES * kStageBytes + 2 * ACT;
+  static constexpr int WGS = RP == 16 ? 3 : 2, STAGES = RP == 64 ? 2 : 3, WORKERS = WGS * 4, THREADS = WGS * 160;
+  static constexpr int ACT = RP * kStep * 2, STAGE = kStageBytes + ACT, WG_BYTES = STAGES * STAGE;     // codes, activations
   static constexpr int BARS = WGS * WG_BYTES, SMEM = BARS + 256 + 1024;
 };
 
 struct W4TcArgs {
   CUtensorMap codes;
   const __nv_bfloat16 *a, *scales;
+  unsigned char *staged;               // activations of every step as they lie in shared memory
   float *out, *parts;
   int R, K, N, groups, steps;          // steps of a tile
   int total, line;                     // steps of all tiles; stretches they are divided over at most
@@ -221,12 +222,28 @@ __device__ __forceinline__ void tmem_ld8(uint32_t taddr, float *v) {
   for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
 }
 
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+
+// Activations as the products read them: per step and 64 of k, RP rows (those past R zeros) of 128 bytes with the 128-byte swizzle,
+// eight of k in a row in the order 0 4 1 5 2 6 3 7.  A thread has eight of k of a row.
+template <int RP> __global__ void __launch_bounds__(128) w4_stage_kernel(const __grid_constant__ W4TcArgs p) {
+  chain_wait();
+  chain_next();
+  const int x = blockIdx.x * 128 + threadIdx.x, step = x / (RP * 32), r = x / 32 % RP, k8 = x % 32, k = step * kStep + k8 * 8;
+  if (step >= p.steps) return;
+  const uint4 v = r < p.R && k < p.K ? __ldg(reinterpret_cast<const uint4 *>(p.a + (size_t)r * p.K + k)) : make_uint4(0, 0, 0, 0);
+  *reinterpret_cast<uint4 *>(p.staged + (size_t)step * Tc<RP>::ACT + (k8 >> 3) * (RP * 128) + (r >> 3) * 1024 + (r & 7) * 128 + (((k8 & 7) ^ (r & 7)) << 4)) =
+      make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
+}
+
 // G: group; RP: rows of B; RC: of them read back (8, or RP).
 template <int G, int RP, int RC>
 __global__ void __launch_bounds__(Tc<RP>::THREADS, 1)
 w4_kernel(const __grid_constant__ W4TcArgs p) {
   using C = Tc<RP>;
-  constexpr int U = kStep / G, ACOLS = G / 2, PIECES = RP / 4;         // units (groups) of a step; columns of A; 16-byte pieces of a thread
+  constexpr int U = kStep / G, ACOLS = G / 2;         // units (groups) of a step; columns of A
   constexpr uint32_t WG_COLS = 2 * ACOLS + 2 * RP;
   static_assert(C::WGS * WG_COLS <= 512, "tensor memory");
   extern __shared__ unsigned char smem_raw[];
@@ -234,8 +251,8 @@ w4_kernel(const __grid_constant__ W4TcArgs p) {
   const int warp = warp_index(), lane = threadIdx.x & 31, row = threadIdx.x & 127;
   const bool worker = warp < C::WORKERS;
   const int wg = worker ? warp >> 2 : warp - C::WORKERS;
-  unsigned char *mine = smem + wg * C::WG_BYTES, *act = mine + C::STAGES * kStageBytes;
-  const uint32_t ring = smem_u32(mine), act_at = smem_u32(act), bars = smem_u32(smem + C::BARS) + wg * 64;
+  unsigned char *mine = smem + wg * C::WG_BYTES;
+  const uint32_t ring = smem_u32(mine), bars = smem_u32(smem + C::BARS) + wg * 64;
   auto full = [&](int s) { return bars + s * 8; };
   auto done = [&](int b) { return bars + 32 + b * 8; };
   auto ready = [&](int b) { return bars + 48 + b * 8; };
@@ -251,7 +268,6 @@ w4_kernel(const __grid_constant__ W4TcArgs p) {
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 0) tmem_alloc(smem_u32(slot), 512);
-  for (int i = row; worker && i < 2 * C::ACT / 16; i += 128) reinterpret_cast<uint4 *>(act)[i] = make_uint4(0, 0, 0, 0);     // rows past R stay zeros
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -268,8 +284,9 @@ w4_kernel(const __grid_constant__ W4TcArgs p) {
     int ask_tile = tile, ask_s = s, asked = 0, count = 0;              // the next step to ask for; units so far
     auto ask = [&] {                                                   // (the issuer only)
       const int st = asked % C::STAGES;
-      mbar_expect_tx(full(st), kStageBytes);
-      tma_load_2d(ring + st * kStageBytes, &p.codes, ask_s * 128, ask_tile * kTile, full(st));
+      mbar_expect_tx(full(st), C::STAGE);
+      tma_load_2d(ring + st * C::STAGE, &p.codes, ask_s * 128, ask_tile * kTile, full(st));
+      bulk_load(ring + st * C::STAGE + kStageBytes, p.staged + (size_t)ask_s * C::ACT, C::ACT, full(st));
       ++asked;
       if (++ask_s == p.steps) { ask_s = 0; ++ask_tile; }
     };
@@ -277,49 +294,38 @@ w4_kernel(const __grid_constant__ W4TcArgs p) {
       for (int i = 0; i < min(C::STAGES, n); ++i) ask();
     for (int i = 0; i < n; ++i) {
       const int units = min(U, p.groups - s * U);
+      const uint32_t act = ring + i % C::STAGES * C::STAGE + kStageBytes;
+      mbar_wait_warp(full(i % C::STAGES), (uint32_t)((i / C::STAGES) & 1), abort_flag);        // (waits that give up go on, here and in the workers)
 #pragma unroll 1
       for (int u = 0; u < units; ++u, ++count) {
         const int b = count & 1;
-        mbar_wait_warp(ready(b), (uint32_t)((count >> 1) & 1), abort_flag);    // (waits that give up go on, here and in the workers)
+        mbar_wait_warp(ready(b), (uint32_t)((count >> 1) & 1), abort_flag);
         tc_fence_after();
         if (issuer) {
           const uint32_t d = tmem + 2 * ACOLS + b * RP, A0 = tmem + b * ACOLS;
 #pragma unroll
           for (int q = 0; q < G / 16; ++q) {
             const int k16 = u * (G / 16) + q;                          // 16 of k: 32 bytes of a 128-byte row of B
-            umma_ts(d, A0 + q * 8, umma_desc(act_at + (i & 1) * C::ACT + (k16 >> 2) * (RP * 128) + (k16 & 3) * 32), idesc, q > 0);
+            umma_ts(d, A0 + q * 8, umma_desc(act + (k16 >> 2) * (RP * 128) + (k16 & 3) * 32), idesc, q > 0);
           }
           umma_commit(done(b));
-          if (u + 1 == units && asked < n) ask();                      // all have read the stage's codes
         }
         __syncwarp();
+        // The stage of the step before is free when this one's first products are ready behind its last ones' sums.
+        if (u == 0 && i > 0 && i - 1 + C::STAGES < n) {
+          mbar_wait_warp(done((count - 1) & 1), (uint32_t)(((count - 1) >> 1) & 1), abort_flag);
+          if (issuer) ask();
+          __syncwarp();
+        }
       }
       if (++s == p.steps) s = 0;
     }
   } else if (n > 0) {
     // ---------------------------------------------------------------- codes -> pairs -> tensor memory -> sums
-    uint4 next[PIECES];
-    auto fetch = [&](int step) {       // activations of a step: piece x is k8 = x % 32 of row x / 32
-#pragma unroll
-      for (int i = 0; i < PIECES; ++i) {
-        const int x = i * 128 + row, r = x / 32, k = step * kStep + x % 32 * 8;
-        next[i] = r < p.R && k < p.K ? __ldg(reinterpret_cast<const uint4 *>(p.a + (size_t)r * p.K + k)) : make_uint4(0, 0, 0, 0);
-      }
-    };
-    auto put = [&](int b) {
-#pragma unroll
-      for (int i = 0; i < PIECES; ++i) {
-        const int x = i * 128 + row, r = x / 32, k8 = x % 32;
-        if (r >= p.R) continue;
-        const uint4 v = next[i];
-        *reinterpret_cast<uint4 *>(act + b * C::ACT + (k8 >> 3) * (RP * 128) + (r >> 3) * 1024 + (r & 7) * 128 + (((k8 & 7) ^ (r & 7)) << 4)) =
-            make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
-      }
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    };
     u32 scale[(U + 1) / 2], scale_next[(U + 1) / 2];                   // a step's, in pairs
-    auto fetch_scales = [&](int t, int step) {
-      const __nv_bfloat16 *at = p.scales + (size_t)min(t * kTile + row, p.N - 1) * p.groups + step * U;
+    const __nv_bfloat16 *row_scales = p.scales + (size_t)min(tile * kTile + row, p.N - 1) * p.groups;
+    auto fetch_scales = [&](int step) {
+      const __nv_bfloat16 *at = row_scales + step * U;
       if (p.packed) {
         if constexpr (U == 2) scale_next[0] = __ldg(reinterpret_cast<const u32 *>(at));
         else if constexpr (U == 4) { const uint2 v = __ldg(reinterpret_cast<const uint2 *>(at)); scale_next[0] = v.x; scale_next[1] = v.y; }
@@ -354,22 +360,20 @@ w4_kernel(const __grid_constant__ W4TcArgs p) {
         for (int r = 0; r < (RC < 16 ? RC : 16); ++r) acc[c + r] = fmaf(pending_scale, v[r], acc[c + r]);
       }
     };
-    fetch(s);
-    fetch_scales(tile, s);
-    put(0);
+    fetch_scales(s);
     bool from_start = s == 0;          // of the tile
     for (int i = 0; i < n; ++i) {
       const int stage = i % C::STAGES, last_s = s + 1 == p.steps;
 #pragma unroll
       for (int x = 0; x < (U + 1) / 2; ++x) scale[x] = scale_next[x];
       if (i + 1 < n) {
-        fetch(last_s ? 0 : s + 1);
-        fetch_scales(tile + last_s, last_s ? 0 : s + 1);
+        if (last_s) row_scales = p.scales + (size_t)min((tile + 1) * kTile + row, p.N - 1) * p.groups;
+        fetch_scales(last_s ? 0 : s + 1);
       }
       const int units = min(U, p.groups - s * U);
       mbar_wait(full(stage), (uint32_t)((i / C::STAGES) & 1), abort_flag);
       __syncwarp();
-      const unsigned char *codes = mine + stage * kStageBytes + row * 128;
+      const unsigned char *codes = mine + stage * C::STAGE + row * 128;
 #pragma unroll 1
       for (int u = 0; u < units; ++u, ++count) {
         const int b = count & 1;
@@ -404,7 +408,6 @@ w4_kernel(const __grid_constant__ W4TcArgs p) {
         for (int x = 1; x < (U + 1) / 2; ++x) bits = u / 2 == x ? scale[x] : bits;
         pending_scale = __uint_as_float(u & 1 ? bits & 0xFFFF0000u : bits << 16);
       }
-      if (i + 1 < n) put((i + 1) & 1);                                 // (its last reader was the step before this one, which is folded)
       if (last_s || i + 1 == n) {
         fold();
         pending = false;
@@ -462,9 +465,10 @@ template <int G, int RP, int RC> int run_tc(const W4TcArgs &a, cudaStream_t s) {
   static std::atomic<u64> done{0};
   const int status = hsd_smem_limit((const void *)w4_kernel<G, RP, RC>, Tc<RP>::SMEM, done);
   if (status) return status;
+  HSD_CUDA_OK(hsd_launch(w4_stage_kernel<RP>, dim3(ceil_div(a.steps * RP * 32, 128)), 128, 0, s, 0, true, a));
   HSD_CUDA_OK(hsd_launch(w4_kernel<G, RP, RC>, dim3(kMeasuredSMs), Tc<RP>::THREADS, Tc<RP>::SMEM, s, 0, true, a));
   HSD_CUDA_OK(hsd_launch(w4_join_kernel, dim3(ceil_div(a.N, kTile), ceil_div(a.R, 4)), 128, 0, s, 0, true, a));
-  hsd_count_launches(2);
+  hsd_count_launches(3);
   return hsd_launch_status();
 }
 template <int G> int run_tc_rows(const W4TcArgs &a, cudaStream_t s) {
@@ -478,8 +482,8 @@ bool takes_small(int R, long long N, int K) { return false; }
 
 extern "C" size_t hsd_gemm_w4_workspace_bytes(int R, int N, int K, int group) {
   using namespace hsd;
-  if (R <= 0 || R > 64 || N <= 0 || K <= 0 || K > (1 << 28) || (group != 32 && group != 64 && group != 128) || K % group) return 0;
-  return (size_t)w4_line(R) * 2 * R * kTile * sizeof(float);
+  if (R <= 0 || R > 64 || N <= 0 || K <= 0 || K > (1 << 27) || (group != 32 && group != 64 && group != 128) || K % group) return 0;
+  return (size_t)w4_line(R) * 2 * R * kTile * sizeof(float) + (size_t)ceil_div(K, kStep) * w4_rp(R) * kStep * 2;
 }
 
 extern "C" int hsd_gemm_w4(const void *A, int R, int K, const void *codes, const void *scales, int N, int group, float *out, void *workspace,
@@ -487,7 +491,7 @@ extern "C" int hsd_gemm_w4(const void *A, int R, int K, const void *codes, const
   using namespace hsd;
   if (!A || !codes || !scales || !out || !workspace || R <= 0 || R > 64 || N <= 0 || K <= 0) return HSD_E_INVALID_ARG;
   if ((group != 32 && group != 64 && group != 128) || K % group) return HSD_E_INVALID_ARG;
-  if (K > (1 << 28) || (long long)ceil_div(N, kTile) * ceil_div(K, kStep) > (1 << 30)) return HSD_E_TOO_LARGE;
+  if (K > (1 << 27) || (long long)ceil_div(N, kTile) * ceil_div(K, kStep) > (1 << 30)) return HSD_E_TOO_LARGE;
   if (((reinterpret_cast<uintptr_t>(A) | reinterpret_cast<uintptr_t>(codes) | reinterpret_cast<uintptr_t>(workspace)) & 15) || (reinterpret_cast<uintptr_t>(scales) & 1) ||
       (reinterpret_cast<uintptr_t>(out) & 3)) return HSD_E_INVALID_ARG;
   if (workspace_bytes < hsd_gemm_w4_workspace_bytes(R, N, K, group)) return HSD_E_WORKSPACE_TOO_SMALL;
@@ -501,6 +505,7 @@ extern "C" int hsd_gemm_w4(const void *A, int R, int K, const void *codes, const
   const int status = tc_make_byte_map(&p.codes, codes, N, K / 2, kTile);
   if (status) return status;
   p.a = a; p.scales = sc; p.out = out; p.parts = static_cast<float *>(workspace);
+  p.staged = static_cast<unsigned char *>(workspace) + (size_t)w4_line(R) * 2 * R * kTile * sizeof(float);
   p.R = R; p.K = K; p.N = N; p.groups = K / group;
   p.steps = ceil_div(K, kStep);
   p.total = ceil_div(N, kTile) * p.steps;
