@@ -5,7 +5,7 @@
 // A group's products are summed in the tensor cores' fp32, then scaled and added in fp32: no rounding to fewer bits anywhere.
 // w4_kernel: 128 weight rows a tile, a thread one row.  Codes come by TMA, the pairs go from registers into tensor memory, from where
 // tcgen05.mma takes them as its operand A (the activations, at most 64 rows, are B, once put in the pairs' order by w4_stage_kernel);
-// a thread reads its row's sums of a group back and scales them.  The tiles' steps (256 of k) stand in one line that is divided evenly over warpgroups, three on an SM (two
+// a thread reads its row's sums of a group back and scales them.  The tiles' steps (128 of k) stand in one line that is divided evenly over warpgroups, three on an SM (two
 // for more than 16 rows), each with a warp of its own that asks for codes and issues products; where a stretch ends inside a tile its sums go to the workspace
 // and w4_join_kernel adds them in order.
 // w4_small_kernel: see there.
@@ -184,23 +184,23 @@ template <int GW, int RT, int MT> int run_small(const W4Args &a, cudaStream_t s)
 }
 
 // ---------------------------------------------------------------------------- tensor memory
-constexpr int kStep = 256;             // k of a step: 128 bytes of codes of a row
+constexpr int kStep = 128;             // k of a step: 64 bytes of codes of a row
 constexpr int kTile = 128;             // weight rows
-constexpr int kStageBytes = kTile * 128;
+constexpr int kStageBytes = kTile * 64, kScaleBytes = kTile * 16;     // of codes; of the eight groups' scales that a step's are among
 template <int RP> struct Tc {          // RP: rows of B (16, 32 or 64)
-  static constexpr int WGS = RP == 16 ? 3 : 2, STAGES = RP == 64 ? 2 : 3, WORKERS = WGS * 4, THREADS = WGS * 160;
+  static constexpr int WGS = RP == 16 ? 3 : 2, STAGES = RP == 16 ? 5 : RP == 32 ? 6 : 4, WORKERS = WGS * 4, THREADS = WGS * 160;
   static constexpr int ACT = RP * kStep * 2, STAGE = kStageBytes + ACT, WG_BYTES = STAGES * STAGE;     // codes, activations
-  static constexpr int BARS = WGS * WG_BYTES, SMEM = BARS + 256 + 1024;
+  static constexpr int SCALES = WGS * WG_BYTES, BARS = SCALES + WGS * STAGES * kScaleBytes, SMEM = BARS + 512 + 1024;
 };
 
 struct W4TcArgs {
-  CUtensorMap codes;
+  CUtensorMap codes, scale_map;
   const __nv_bfloat16 *a, *scales;
   unsigned char *staged;               // activations of every step as they lie in shared memory
   float *out, *parts;
   int R, K, N, groups, steps;          // steps of a tile
   int total, line;                     // steps of all tiles; stretches they are divided over at most
-  int packed;                          // a step's scales of a row are one aligned load
+  int mapped;                          // the scales have a tensor map
   u32 bits;                            // kCodeBits
   // Stretch w is [first(w), first(w + 1)); step x belongs to stretch of(x).
   __device__ __forceinline__ int first(int w) const { return total < line ? min(w, total) : (int)((long long)w * total / line); }
@@ -231,7 +231,7 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
 template <int RP> __global__ void __launch_bounds__(128) w4_stage_kernel(const __grid_constant__ W4TcArgs p) {
   chain_wait();
   chain_next();
-  const int x = blockIdx.x * 128 + threadIdx.x, step = x / (RP * 32), r = x / 32 % RP, k8 = x % 32, k = step * kStep + k8 * 8;
+  const int x = blockIdx.x * 128 + threadIdx.x, step = x / (RP * (kStep / 8)), r = x / (kStep / 8) % RP, k8 = x % (kStep / 8), k = step * kStep + k8 * 8;
   if (step >= p.steps) return;
   const uint4 v = r < p.R && k < p.K ? __ldg(reinterpret_cast<const uint4 *>(p.a + (size_t)r * p.K + k)) : make_uint4(0, 0, 0, 0);
   *reinterpret_cast<uint4 *>(p.staged + (size_t)step * Tc<RP>::ACT + (k8 >> 3) * (RP * 128) + (r >> 3) * 1024 + (r & 7) * 128 + (((k8 & 7) ^ (r & 7)) << 4)) =
@@ -252,12 +252,13 @@ w4_kernel(const __grid_constant__ W4TcArgs p) {
   const bool worker = warp < C::WORKERS;
   const int wg = worker ? warp >> 2 : warp - C::WORKERS;
   unsigned char *mine = smem + wg * C::WG_BYTES;
-  const uint32_t ring = smem_u32(mine), bars = smem_u32(smem + C::BARS) + wg * 64;
+  unsigned char *scales = smem + C::SCALES + wg * C::STAGES * kScaleBytes;
+  const uint32_t ring = smem_u32(mine), scale_ring = smem_u32(scales), bars = smem_u32(smem + C::BARS) + wg * 128;
   auto full = [&](int s) { return bars + s * 8; };
-  auto done = [&](int b) { return bars + 32 + b * 8; };
-  auto ready = [&](int b) { return bars + 48 + b * 8; };
-  volatile int *abort_flag = reinterpret_cast<int *>(smem + C::BARS + 192 + wg * 4);
-  u32 *slot = reinterpret_cast<u32 *>(smem + C::BARS + 208);
+  auto done = [&](int b) { return bars + 64 + b * 8; };
+  auto ready = [&](int b) { return bars + 80 + b * 8; };
+  volatile int *abort_flag = reinterpret_cast<int *>(smem + C::BARS + 384 + wg * 4);
+  u32 *slot = reinterpret_cast<u32 *>(smem + C::BARS + 400);
   if (worker && row == 0) {
     for (int s = 0; s < C::STAGES; ++s) mbar_init(full(s), 1);
     mbar_init(ready(0), 4);
@@ -284,9 +285,10 @@ w4_kernel(const __grid_constant__ W4TcArgs p) {
     int ask_tile = tile, ask_s = s, asked = 0, count = 0;              // the next step to ask for; units so far
     auto ask = [&] {                                                   // (the issuer only)
       const int st = asked % C::STAGES;
-      mbar_expect_tx(full(st), C::STAGE);
-      tma_load_2d(ring + st * C::STAGE, &p.codes, ask_s * 128, ask_tile * kTile, full(st));
+      mbar_expect_tx(full(st), C::STAGE + (p.mapped ? kScaleBytes : 0));
+      tma_load_2d(ring + st * C::STAGE, &p.codes, ask_s * (kStep / 2), ask_tile * kTile, full(st));
       bulk_load(ring + st * C::STAGE + kStageBytes, p.staged + (size_t)ask_s * C::ACT, C::ACT, full(st));
+      if (p.mapped) tma_load_2d(scale_ring + st * kScaleBytes, &p.scale_map, (ask_s * U & ~7) * 2, ask_tile * kTile, full(st));
       ++asked;
       if (++ask_s == p.steps) { ask_s = 0; ++ask_tile; }
     };
@@ -322,31 +324,15 @@ w4_kernel(const __grid_constant__ W4TcArgs p) {
     }
   } else if (n > 0) {
     // ---------------------------------------------------------------- codes -> pairs -> tensor memory -> sums
-    u32 scale[(U + 1) / 2], scale_next[(U + 1) / 2];                   // a step's, in pairs
-    const __nv_bfloat16 *row_scales = p.scales + (size_t)min(tile * kTile + row, p.N - 1) * p.groups;
-    auto fetch_scales = [&](int step) {
-      const __nv_bfloat16 *at = row_scales + step * U;
-      if (p.packed) {
-        if constexpr (U == 2) scale_next[0] = __ldg(reinterpret_cast<const u32 *>(at));
-        else if constexpr (U == 4) { const uint2 v = __ldg(reinterpret_cast<const uint2 *>(at)); scale_next[0] = v.x; scale_next[1] = v.y; }
-        else { const uint4 v = __ldg(reinterpret_cast<const uint4 *>(at)); scale_next[0] = v.x; scale_next[1] = v.y; scale_next[2] = v.z; scale_next[3] = v.w; }
-      } else {
-        const unsigned short *bits = reinterpret_cast<const unsigned short *>(at);
-#pragma unroll
-        for (int u = 0; u < U; u += 2)
-          scale_next[u / 2] = (step * U + u < p.groups ? (u32)bits[u] : 0u) | (step * U + u + 1 < p.groups ? (u32)bits[u + 1] << 16 : 0u);
-      }
-    };
-
     float acc[RC];
 #pragma unroll
     for (int r = 0; r < RC; ++r) acc[r] = 0.f;
-    int count = 0;                     // units so far
-    bool pending = false;              // the last one's sums are not added yet
-    float pending_scale = 0.f;
+    // Units' sums are added two units later, when their products have long been over: the next two units' pairs are made meanwhile.
+    int count = 0, pending = 0;        // units so far; those whose sums are not added yet
+    float scale0 = 0.f, scale1 = 0.f;  // theirs, the older first
     auto fold = [&] {
-      const int b = (count - 1) & 1;
-      mbar_wait(done(b), (uint32_t)(((count - 1) >> 1) & 1), abort_flag);
+      const int x = count - pending, b = x & 1;
+      mbar_wait(done(b), (uint32_t)((x >> 1) & 1), abort_flag);
       __syncwarp();
       tc_fence_after();
       const uint32_t d = tmem + lanes + 2 * ACOLS + b * RP;
@@ -357,26 +343,25 @@ w4_kernel(const __grid_constant__ W4TcArgs p) {
         else tmem_ld16(d + c, v);
         tmem_ld_wait();
 #pragma unroll
-        for (int r = 0; r < (RC < 16 ? RC : 16); ++r) acc[c + r] = fmaf(pending_scale, v[r], acc[c + r]);
+        for (int r = 0; r < (RC < 16 ? RC : 16); ++r) acc[c + r] = fmaf(scale0, v[r], acc[c + r]);
       }
+      scale0 = scale1;
+      --pending;
     };
-    fetch_scales(s);
+    const unsigned short *row_scales = reinterpret_cast<const unsigned short *>(p.scales) + (size_t)min(tile * kTile + row, p.N - 1) * p.groups;
     bool from_start = s == 0;          // of the tile
     for (int i = 0; i < n; ++i) {
-      const int stage = i % C::STAGES, last_s = s + 1 == p.steps;
-#pragma unroll
-      for (int x = 0; x < (U + 1) / 2; ++x) scale[x] = scale_next[x];
-      if (i + 1 < n) {
-        if (last_s) row_scales = p.scales + (size_t)min((tile + 1) * kTile + row, p.N - 1) * p.groups;
-        fetch_scales(last_s ? 0 : s + 1);
-      }
+      const int stage = i % C::STAGES;
+      const bool last_s = s + 1 == p.steps;
       const int units = min(U, p.groups - s * U);
       mbar_wait(full(stage), (uint32_t)((i / C::STAGES) & 1), abort_flag);
       __syncwarp();
-      const unsigned char *codes = mine + stage * C::STAGE + row * 128;
+      const unsigned char *codes = mine + stage * C::STAGE + row * 64;
+      const unsigned short *stage_scales = reinterpret_cast<const unsigned short *>(scales + stage * kScaleBytes + row * 16) + (s * U & 7);
 #pragma unroll 1
-      for (int u = 0; u < units; ++u, ++count) {
+      for (int u = 0; u < units; ++u) {
         const int b = count & 1;
+        const u32 scale = p.mapped ? stage_scales[u] : row_scales[s * U + u];
         const uint32_t A = tmem + lanes + b * ACOLS;
         constexpr int HALF = G < 64 ? G : 64;                          // 32 columns of pairs at once at most
 #pragma unroll
@@ -384,7 +369,7 @@ w4_kernel(const __grid_constant__ W4TcArgs p) {
           u32 x[HALF / 2];
 #pragma unroll
           for (int q = 0; q < HALF / 32; ++q) {
-            const uint4 v = *reinterpret_cast<const uint4 *>(codes + (((u * (G / 32) + h * 2 + q) ^ (row & 7)) << 4));
+            const uint4 v = *reinterpret_cast<const uint4 *>(codes + (((u * (G / 32) + h * 2 + q) ^ (row >> 1 & 3)) << 4));
             const u32 word[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
             for (int y = 0; y < 4; ++y) {
@@ -394,6 +379,7 @@ w4_kernel(const __grid_constant__ W4TcArgs p) {
               x[q * 16 + y * 4 + 3] = pair<3>(word[y], p.bits);
             }
           }
+          if (h == 0 && pending == 2) fold();                          // (the products that read this half of tensor memory before are over then)
 #pragma unroll
           for (int q = 0; q < HALF / 32; ++q) tmem_st16u(A + h * 32 + q * 16, x + q * 16);
         }
@@ -401,16 +387,12 @@ w4_kernel(const __grid_constant__ W4TcArgs p) {
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(ready(b));
-        if (pending) fold();
-        pending = true;
-        u32 bits = scale[0];
-#pragma unroll
-        for (int x = 1; x < (U + 1) / 2; ++x) bits = u / 2 == x ? scale[x] : bits;
-        pending_scale = __uint_as_float(u & 1 ? bits & 0xFFFF0000u : bits << 16);
+        (pending == 0 ? scale0 : scale1) = __uint_as_float(scale << 16);
+        ++pending;
+        ++count;
       }
       if (last_s || i + 1 == n) {
-        fold();
-        pending = false;
+        while (pending > 0) fold();
         const bool whole = last_s && from_start;
         const int nr = tile * kTile + row;
         float *to = whole ? p.out + nr : p.part(w, from_start ? 1 : 0) + row;
@@ -422,8 +404,13 @@ w4_kernel(const __grid_constant__ W4TcArgs p) {
         }
         from_start = true;
       }
-      if (last_s) { s = 0; ++tile; }
-      else ++s;
+      if (last_s) {
+        s = 0;
+        row_scales += (size_t)(min((tile + 1) * kTile + row, p.N - 1) - min(tile * kTile + row, p.N - 1)) * p.groups;
+        ++tile;
+      } else {
+        ++s;
+      }
     }
   }
   if (*abort_flag) {                   // copies in flight land before the shared memory goes away
@@ -465,7 +452,7 @@ template <int G, int RP, int RC> int run_tc(const W4TcArgs &a, cudaStream_t s) {
   static std::atomic<u64> done{0};
   const int status = hsd_smem_limit((const void *)w4_kernel<G, RP, RC>, Tc<RP>::SMEM, done);
   if (status) return status;
-  HSD_CUDA_OK(hsd_launch(w4_stage_kernel<RP>, dim3(ceil_div(a.steps * RP * 32, 128)), 128, 0, s, 0, true, a));
+  HSD_CUDA_OK(hsd_launch(w4_stage_kernel<RP>, dim3(ceil_div(a.steps * RP * (kStep / 8), 128)), 128, 0, s, 0, true, a));
   HSD_CUDA_OK(hsd_launch(w4_kernel<G, RP, RC>, dim3(kMeasuredSMs), Tc<RP>::THREADS, Tc<RP>::SMEM, s, 0, true, a));
   HSD_CUDA_OK(hsd_launch(w4_join_kernel, dim3(ceil_div(a.N, kTile), ceil_div(a.R, 4)), 128, 0, s, 0, true, a));
   hsd_count_launches(3);
@@ -482,7 +469,7 @@ bool takes_small(int R, long long N, int K) { return false; }
 
 extern "C" size_t hsd_gemm_w4_workspace_bytes(int R, int N, int K, int group) {
   using namespace hsd;
-  if (R <= 0 || R > 64 || N <= 0 || K <= 0 || K > (1 << 27) || (group != 32 && group != 64 && group != 128) || K % group) return 0;
+  if (R <= 0 || R > 64 || N <= 0 || K <= 0 || K > (1 << 26) || (group != 32 && group != 64 && group != 128) || K % group) return 0;
   return (size_t)w4_line(R) * 2 * R * kTile * sizeof(float) + (size_t)ceil_div(K, kStep) * w4_rp(R) * kStep * 2;
 }
 
@@ -491,7 +478,7 @@ extern "C" int hsd_gemm_w4(const void *A, int R, int K, const void *codes, const
   using namespace hsd;
   if (!A || !codes || !scales || !out || !workspace || R <= 0 || R > 64 || N <= 0 || K <= 0) return HSD_E_INVALID_ARG;
   if ((group != 32 && group != 64 && group != 128) || K % group) return HSD_E_INVALID_ARG;
-  if (K > (1 << 27) || (long long)ceil_div(N, kTile) * ceil_div(K, kStep) > (1 << 30)) return HSD_E_TOO_LARGE;
+  if (K > (1 << 26) || (long long)ceil_div(N, kTile) * ceil_div(K, kStep) > (1 << 30)) return HSD_E_TOO_LARGE;
   if (((reinterpret_cast<uintptr_t>(A) | reinterpret_cast<uintptr_t>(codes) | reinterpret_cast<uintptr_t>(workspace)) & 15) || (reinterpret_cast<uintptr_t>(scales) & 1) ||
       (reinterpret_cast<uintptr_t>(out) & 3)) return HSD_E_INVALID_ARG;
   if (workspace_bytes < hsd_gemm_w4_workspace_bytes(R, N, K, group)) return HSD_E_WORKSPACE_TOO_SMALL;
@@ -502,7 +489,7 @@ extern "C" int hsd_gemm_w4(const void *A, int R, int K, const void *codes, const
     return group == 128 ? run_small<4, 1, 1>(p, s) : group == 64 ? run_small<2, 1, 1>(p, s) : run_small<1, 1, 1>(p, s);
   }
   W4TcArgs p = {};
-  const int status = tc_make_byte_map(&p.codes, codes, N, K / 2, kTile);
+  const int status = tc_make_byte_map(&p.codes, codes, N, K / 2, kTile, 64);
   if (status) return status;
   p.a = a; p.scales = sc; p.out = out; p.parts = static_cast<float *>(workspace);
   p.staged = static_cast<unsigned char *>(workspace) + (size_t)w4_line(R) * 2 * R * kTile * sizeof(float);
@@ -511,6 +498,10 @@ extern "C" int hsd_gemm_w4(const void *A, int R, int K, const void *codes, const
   p.total = ceil_div(N, kTile) * p.steps;
   p.line = w4_line(R);
   p.bits = kCodeBits;
-  p.packed = K % kStep == 0 && reinterpret_cast<uintptr_t>(scales) % (kStep / group * 2) == 0;
+  if (p.groups % 8 == 0 && reinterpret_cast<uintptr_t>(scales) % 16 == 0) {
+    const int s2 = tc_make_byte_map(&p.scale_map, scales, N, (long long)p.groups * 2, kTile, 16);
+    if (s2) return s2;
+    p.mapped = 1;
+  }
   return group == 128 ? run_tc_rows<128>(p, s) : group == 64 ? run_tc_rows<64>(p, s) : run_tc_rows<32>(p, s);
 }
