@@ -209,10 +209,13 @@ struct W4TcArgs {
   __device__ __forceinline__ float *part(int w, int slot) const { return parts + ((size_t)w * 2 + slot) * R * kTile; }
 };
 
-__device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t acc) {
+// B: the descriptor's low word (address / 16); the high one says 8-row groups 1024 bytes apart, descriptor version, 128-byte swizzle.
+constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_low, uint32_t idesc, uint32_t acc) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-      ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(acc) : "memory");
+      "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\tmov.b64 db, {%2, %5};\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "r"(b_low), "r"(idesc), "r"(acc), "r"(kDescHigh) : "memory");
 }
 __device__ __forceinline__ void tmem_ld8(uint32_t taddr, float *v) {
   uint32_t r[8];
@@ -281,46 +284,50 @@ w4_kernel(const __grid_constant__ W4TcArgs p) {
   int tile = begin / p.steps, s = begin - tile * p.steps;
   if (n > 0 && !worker) {
     // ---------------------------------------------------------------- codes, products
+    // (Every operation between two units' products counts: the workers wait for this warp, and it shares its issue slots with three of
+    // theirs.  Addresses and descriptors go on by constants.)
     const bool issuer = elect_one();
-    int ask_tile = tile, ask_s = s, asked = 0, count = 0;              // the next step to ask for; units so far
-    auto ask = [&] {                                                   // (the issuer only)
-      const int st = asked % C::STAGES;
-      mbar_expect_tx(full(st), C::STAGE + (p.mapped ? kScaleBytes : 0));
-      tma_load_2d(ring + st * C::STAGE, &p.codes, ask_s * (kStep / 2), ask_tile * kTile, full(st));
-      bulk_load(ring + st * C::STAGE + kStageBytes, p.staged + (size_t)ask_s * C::ACT, C::ACT, full(st));
-      if (p.mapped) tma_load_2d(scale_ring + st * kScaleBytes, &p.scale_map, (ask_s * U & ~7) * 2, ask_tile * kTile, full(st));
-      ++asked;
-      if (++ask_s == p.steps) { ask_s = 0; ++ask_tile; }
+    const uint32_t bytes = C::STAGE + (p.mapped ? kScaleBytes : 0);
+    int ask_s = s, ask_stage = 0, ask_y = tile * kTile;                // the next step to ask for
+    auto ask = [&] {
+      if (issuer) {
+        const uint32_t bar = full(ask_stage), to = ring + ask_stage * C::STAGE;
+        mbar_expect_tx(bar, bytes);
+        tma_load_2d(to, &p.codes, ask_s * (kStep / 2), ask_y, bar);
+        bulk_load(to + kStageBytes, p.staged + (size_t)(uint32_t)ask_s * C::ACT, C::ACT, bar);
+        if (p.mapped) tma_load_2d(scale_ring + ask_stage * kScaleBytes, &p.scale_map, (ask_s * U & ~7) * 2, ask_y, bar);
+      }
+      if (++ask_stage == C::STAGES) ask_stage = 0;
+      if (++ask_s == p.steps) { ask_s = 0; ask_y += kTile; }
     };
-    if (issuer)
-      for (int i = 0; i < min(C::STAGES, n); ++i) ask();
+    for (int i = 0; i < min(C::STAGES, n); ++i) ask();
+    const uint32_t desc0 = ((ring + kStageBytes) & 0x3FFFFu) >> 4 | 1u << 16, desc_end = desc0 + C::STAGES * (C::STAGE >> 4);
+    uint32_t desc = desc0, b = 0, phase = 0;                           // of the unit: which half of tensor memory, its barriers' parity
     for (int i = 0; i < n; ++i) {
       const int units = min(U, p.groups - s * U);
-      const uint32_t act = ring + i % C::STAGES * C::STAGE + kStageBytes;
-      mbar_wait_warp(full(i % C::STAGES), (uint32_t)((i / C::STAGES) & 1), abort_flag);        // (waits that give up go on, here and in the workers)
 #pragma unroll 1
-      for (int u = 0; u < units; ++u, ++count) {
-        const int b = count & 1;
-        mbar_wait_warp(ready(b), (uint32_t)((count >> 1) & 1), abort_flag);
+      for (int u = 0; u < units; ++u) {
+        // (the workers have seen this stage's codes and activations land before they say so; waits that give up go on, here and there)
+        mbar_wait_warp(ready(b), phase, abort_flag);
         tc_fence_after();
         if (issuer) {
-          const uint32_t d = tmem + 2 * ACOLS + b * RP, A0 = tmem + b * ACOLS;
+          const uint32_t d = tmem + 2 * ACOLS + b * RP, A0 = tmem + b * ACOLS, at = desc + (u * (G / 16) >> 2) * (RP * 8) + (u * (G / 16) & 3) * 2;
 #pragma unroll
-          for (int q = 0; q < G / 16; ++q) {
-            const int k16 = u * (G / 16) + q;                          // 16 of k: 32 bytes of a 128-byte row of B
-            umma_ts(d, A0 + q * 8, umma_desc(act + (k16 >> 2) * (RP * 128) + (k16 & 3) * 32), idesc, q > 0);
-          }
+          for (int q = 0; q < G / 16; ++q) umma_ts(d, A0 + q * 8, at + (q >> 2) * (RP * 8) + (q & 3) * 2, idesc, q > 0);        // 16 of k: 32 bytes of a row of B
           umma_commit(done(b));
         }
         __syncwarp();
-        // The stage of the step before is free when this one's first products are ready behind its last ones' sums.
+        // The stage of the step before is free when this one's first products are ready behind its last ones.
         if (u == 0 && i > 0 && i - 1 + C::STAGES < n) {
-          mbar_wait_warp(done((count - 1) & 1), (uint32_t)(((count - 1) >> 1) & 1), abort_flag);
-          if (issuer) ask();
-          __syncwarp();
+          mbar_wait_warp(done(b ^ 1), b ? phase : phase ^ 1, abort_flag);
+          ask();
         }
+        phase ^= b;
+        b ^= 1;
       }
       if (++s == p.steps) s = 0;
+      desc += C::STAGE >> 4;
+      if (desc == desc_end) desc = desc0;
     }
   } else if (n > 0) {
     // ---------------------------------------------------------------- codes -> pairs -> tensor memory -> sums
@@ -350,11 +357,12 @@ w4_kernel(const __grid_constant__ W4TcArgs p) {
     };
     const unsigned short *row_scales = reinterpret_cast<const unsigned short *>(p.scales) + (size_t)min(tile * kTile + row, p.N - 1) * p.groups;
     bool from_start = s == 0;          // of the tile
+    int stage = 0;
+    uint32_t full_phase = 0;
     for (int i = 0; i < n; ++i) {
-      const int stage = i % C::STAGES;
       const bool last_s = s + 1 == p.steps;
       const int units = min(U, p.groups - s * U);
-      mbar_wait(full(stage), (uint32_t)((i / C::STAGES) & 1), abort_flag);
+      mbar_wait(full(stage), full_phase, abort_flag);
       __syncwarp();
       const unsigned char *codes = mine + stage * C::STAGE + row * 64;
       const unsigned short *stage_scales = reinterpret_cast<const unsigned short *>(scales + stage * kScaleBytes + row * 16) + (s * U & 7);
@@ -391,6 +399,7 @@ w4_kernel(const __grid_constant__ W4TcArgs p) {
         ++pending;
         ++count;
       }
+      if (++stage == C::STAGES) { stage = 0; full_phase ^= 1; }
       if (last_s || i + 1 == n) {
         while (pending > 0) fold();
         const bool whole = last_s && from_start;
