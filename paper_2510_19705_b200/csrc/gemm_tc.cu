@@ -447,19 +447,6 @@ int tc_make_map(CUtensorMap *map, const void *base, long long rows, long long co
   return r == CUDA_SUCCESS ? HSD_OK : HSD_E_CUDA;
 }
 
-int tc_make_byte_map(CUtensorMap *map, const void *base, long long rows, long long cols, int box_rows, int box_cols) {
-  const int status = tc_init();
-  if (status) return status;
-  if (((uintptr_t)base & 15) != 0 || cols % 16 != 0 || box_rows < 1 || box_rows > 256 || (box_cols != 16 && box_cols != 64)) return HSD_E_INVALID_ARG;
-  cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-  cuuint64_t strides[1] = {(cuuint64_t)cols};
-  cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows};
-  cuuint32_t estr[2] = {1, 1};
-  CUresult r = g_encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                        box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  return r == CUDA_SUCCESS ? HSD_OK : HSD_E_CUDA;
-}
-
 int tc_npad(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
 
 namespace {

@@ -18,10 +18,6 @@ int tc_init();                     // HSD_OK when the tensor-map encoder is avai
 // 2-D bf16 tensor map over a row-major [rows, cols] matrix, box = [box_rows, 64], 128-byte swizzle.
 int tc_make_map(CUtensorMap *map, const void *base, long long rows, long long cols, int box_rows);
 
-// 2-D byte map over a row-major [rows, cols] matrix (cols a multiple of 16), box = [box_rows, box_cols], zeros outside: 64 columns with
-// the 64-byte swizzle, or 16.
-int tc_make_byte_map(CUtensorMap *map, const void *base, long long rows, long long cols, int box_rows, int box_cols);
-
 int tc_npad(int rows);             // 16, 32, 64, 128 or 256 (rows <= 256)
 
 // Where the q / k / v projection's rows go (GEMM_QKV_T): q rotated -> q; k rotated, v -> their cache pages.

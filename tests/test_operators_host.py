@@ -50,7 +50,7 @@ def test_sizes_past_the_limits():
     assert attention(nq=131072) == -8
     assert attention(pool(page_size=1 << 20), batch=4096, pages=3) == -8
     lib = binding.library()
-    assert lib.hsd_gemm_w4(P, 1, (1 << 26) + 128, P, P, 8, 128, P, P, 1 << 40, None) == -8
+    assert lib.hsd_gemm_w4(P, 1, (1 << 27) + 128, P, P, 8, 128, P, P, 1 << 40, None) == -8
     assert lib.hsd_token_logprobs(P, 0, 1, (1 << 31) - 1, P, 0, P, P, P, None, None, None) == -8
 
 
