@@ -4,9 +4,9 @@
 // the pairs are (0,4), (1,5), (2,6), (3,7) of a word; the order of k inside a product is free, so the activations are put in the same.
 // A group's products are summed in the tensor cores' fp32, then scaled and added in fp32: no rounding to fewer bits anywhere.
 // The codes go from shared memory to registers once, as the operand of mma.sync that has 16 weight rows; the activations are its columns,
-// eight a tile, brought into the order of its fragments by w4_stage_kernel.  w4_kernel: a warp has 16 weight rows, a CTA 256, all at the
-// same k, so that the activations come from L1.  Tiles' steps (256 of k) stand in one line that is divided evenly over the CTAs; where a
-// stretch ends inside a tile its sums go to the workspace and w4_join_kernel adds them in order.  No warp waits for another.
+// eight a tile, brought into the order of its fragments by w4_stage_kernel.  w4_kernel: a warp has 16 weight rows, a CTA 128, all at the
+// same k, and both operands come through one ring (cp.async).  Tiles' steps (256 of k) stand in one line that is divided evenly over
+// the CTAs, two on an SM; where a stretch ends inside a tile its sums go to the workspace and w4_join_kernel adds them in order.
 // (Pairs through tensor memory for tcgen05.mma, 128 rows a warpgroup: 25 us for 9 x 28672 x 4096; its chains of codes, pairs, products
 // and sums wait for one another, and three warpgroups an SM do not cover that.)
 // w4_small_kernel: see there.
@@ -183,8 +183,12 @@ template <int GW, int RT, int MT> int run_small(const W4Args &a, cudaStream_t s)
 
 // ---------------------------------------------------------------------------- large products
 constexpr int kStep = 256;             // k of a step: 128 bytes of codes of a row
-constexpr int kWide = 16, kTile = kWide * 16;                          // warps; weight rows
-constexpr int kStages = 4, kStageBytes = 16 * 128, kSmem = kWide * kStages * kStageBytes;
+constexpr int kWide = 8, kTile = kWide * 16;   // warps; weight rows
+constexpr int kLine = 2 * kMeasuredSMs;         // CTAs, two on an SM
+constexpr int kCodeBytes = kTile * 128;
+template <int RT> struct Ring {                // stages of a step's codes and activations
+  static constexpr int ACT = RT * 8 * kStep * 2, STAGE = kCodeBytes + ACT, STAGES = RT == 8 ? 2 : RT == 4 ? 3 : 4, SMEM = STAGES * STAGE;
+};
 
 struct W4Line {
   const __nv_bfloat16 *a, *scales;
@@ -195,9 +199,9 @@ struct W4Line {
   int total;                           // steps of all tiles
   int eights;                          // a row's scales are whole aligned eights
   u32 bits;                            // kCodeBits
-  // Stretch w (of kMeasuredSMs) is [first(w), first(w + 1)); step x belongs to stretch of(x).
-  __device__ __forceinline__ int first(int w) const { return total < kMeasuredSMs ? min(w, total) : (int)((long long)w * total / kMeasuredSMs); }
-  __device__ __forceinline__ int of(int x) const { return total < kMeasuredSMs ? x : (int)((((long long)x + 1) * kMeasuredSMs - 1) / total); }
+  // Stretch w (of kLine) is [first(w), first(w + 1)); step x belongs to stretch of(x).
+  __device__ __forceinline__ int first(int w) const { return total < kLine ? min(w, total) : (int)((long long)w * total / kLine); }
+  __device__ __forceinline__ int of(int x) const { return total < kLine ? x : (int)((((long long)x + 1) * kLine - 1) / total); }
   // A stretch's sums of a tile that it does not hold whole: slot 0 where it begins inside of it, else 1; [row][weight row].
   __device__ __forceinline__ float *part(int w, int slot) const { return parts + ((size_t)w * 2 + slot) * R * kTile; }
 };
@@ -227,12 +231,14 @@ __global__ void __launch_bounds__(128) w4_stage_kernel(W4Line p, int gw, int rt)
 
 // GW: words of a lane in a group (group = 32 GW); RT: tiles of eight activation rows.
 template <int GW, int RT>
-__global__ void __launch_bounds__(kWide * 32, 1)
+__global__ void __launch_bounds__(kWide * 32, 2)
 w4_kernel(W4Line p) {
   constexpr int U = 8 / GW;            // groups of a step
+  using R = Ring<RT>;
+  constexpr int kStages = R::STAGES;
   extern __shared__ __align__(128) unsigned char smem[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j = lane & 3, lr = lane >> 2;
-  const u32 ring = (u32)__cvta_generic_to_shared(smem) + warp * kStages * kStageBytes;
+  const u32 ring = (u32)__cvta_generic_to_shared(smem);
   chain_wait();
   chain_next();
   const int w = blockIdx.x, begin = p.first(w), n = p.first(w + 1) - begin;
@@ -253,8 +259,13 @@ w4_kernel(W4Line p) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int r = i * 4 + cr;
-        copy16(ring + ask_stage * kStageBytes + r * 128 + ((c ^ swizzle(r)) << 4), from[i] + ask_s * (kStep / 2));
+        copy16(ring + ask_stage * R::STAGE + (warp * 16 + r) * 128 + ((c ^ swizzle(r)) << 4), from[i] + ask_s * (kStep / 2));
       }
+    }
+#pragma unroll
+    for (int i = 0; i < R::ACT / 16 / (kWide * 32); ++i) {
+      const int x = (i * kWide * 32 + threadIdx.x) * 16;
+      copy16(ring + ask_stage * R::STAGE + kCodeBytes + x, p.staged + (size_t)ask_s * R::ACT + x);
     }
     if (++ask_stage == kStages) ask_stage = 0;
     if (++ask_s == p.steps) { ask_s = 0; rows_of(++ask_tile); }
@@ -296,7 +307,7 @@ w4_kernel(W4Line p) {
 #pragma unroll 1
   for (int i = 0; i < n; ++i) {
     copies_wait<kStages - 2>();
-    __syncwarp();
+    __syncthreads();                   // (a step's copies are all warps', and so is the stage that is filled again)
     if (i + kStages - 1 < n) ask();
     copies_end();
     if (p.eights) {
@@ -320,8 +331,8 @@ w4_kernel(W4Line p) {
         now[h] = make_uint4(q[0], q[1], q[2], q[3]);
       }
     }
-    const uint4 *b_at = reinterpret_cast<const uint4 *>(p.staged) + (size_t)s * (8 * RT * 32) + lane;
-    const u32 codes = ring + stage * kStageBytes;
+    const uint4 *b_at = reinterpret_cast<const uint4 *>(smem + stage * R::STAGE + kCodeBytes) + lane;
+    const u32 codes = ring + stage * R::STAGE + warp * 16 * 128;
     u32 word[2][8];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -341,7 +352,7 @@ w4_kernel(W4Line p) {
       for (int q = g * GW; q < (g + 1) * GW; ++q) {
         uint4 b[RT];
 #pragma unroll
-        for (int t = 0; t < RT; ++t) b[t] = __ldg(b_at + (q * RT + t) * 32);
+        for (int t = 0; t < RT; ++t) b[t] = b_at[(q * RT + t) * 32];
         const u32 lo[4] = {pair<0>(word[0][q], p.bits), pair<0>(word[1][q], p.bits), pair<1>(word[0][q], p.bits), pair<1>(word[1][q], p.bits)};
         const u32 hi[4] = {pair<2>(word[0][q], p.bits), pair<2>(word[1][q], p.bits), pair<3>(word[0][q], p.bits), pair<3>(word[1][q], p.bits)};
 #pragma unroll
@@ -411,10 +422,10 @@ __global__ void __launch_bounds__(kTile) w4_join_kernel(W4Line p) {
 
 template <int GW, int RT> int run_line(const W4Line &a, cudaStream_t s) {
   static std::atomic<u64> done{0};
-  const int status = hsd_smem_limit((const void *)w4_kernel<GW, RT>, kSmem, done);
+  const int status = hsd_smem_limit((const void *)w4_kernel<GW, RT>, Ring<RT>::SMEM, done);
   if (status) return status;
   HSD_CUDA_OK(hsd_launch(w4_stage_kernel, dim3(a.steps * RT * 2), 128, 0, s, 0, true, a, GW, RT));
-  HSD_CUDA_OK(hsd_launch(w4_kernel<GW, RT>, dim3(kMeasuredSMs), kWide * 32, kSmem, s, 0, true, a));
+  HSD_CUDA_OK(hsd_launch(w4_kernel<GW, RT>, dim3(kLine), kWide * 32, Ring<RT>::SMEM, s, 0, true, a));
   HSD_CUDA_OK(hsd_launch(w4_join_kernel, dim3(ceil_div(a.N, kTile), ceil_div(a.R, 4)), kTile, 0, s, 0, true, a));
   hsd_count_launches(3);
   return hsd_launch_status();
@@ -432,7 +443,7 @@ bool takes_small(int R, long long N, int K) { return false; }
 extern "C" size_t hsd_gemm_w4_workspace_bytes(int R, int N, int K, int group) {
   using namespace hsd;
   if (R <= 0 || R > 64 || N <= 0 || K <= 0 || K > (1 << 27) || (group != 32 && group != 64 && group != 128) || K % group) return 0;
-  return (size_t)kMeasuredSMs * 2 * R * kTile * sizeof(float) + (size_t)ceil_div(K, kStep) * w4_tiles(R) * 8 * kStep * 2;
+  return (size_t)kLine * 2 * R * kTile * sizeof(float) + (size_t)ceil_div(K, kStep) * w4_tiles(R) * 8 * kStep * 2;
 }
 
 extern "C" int hsd_gemm_w4(const void *A, int R, int K, const void *codes, const void *scales, int N, int group, float *out, void *workspace,
@@ -453,7 +464,7 @@ extern "C" int hsd_gemm_w4(const void *A, int R, int K, const void *codes, const
   W4Line p = {};
   p.codes = static_cast<const uint8_t *>(codes);
   p.a = a; p.scales = sc; p.out = out; p.parts = static_cast<float *>(workspace);
-  p.staged = static_cast<unsigned char *>(workspace) + (size_t)kMeasuredSMs * 2 * R * kTile * sizeof(float);
+  p.staged = static_cast<unsigned char *>(workspace) + (size_t)kLine * 2 * R * kTile * sizeof(float);
   p.R = R; p.K = K; p.N = N; p.groups = K / group;
   p.steps = ceil_div(K, kStep);
   p.total = ceil_div(N, kTile) * p.steps;
