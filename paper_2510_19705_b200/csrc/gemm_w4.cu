@@ -9,7 +9,7 @@
 // the CTAs, two on an SM; where a stretch ends inside a tile its sums go to the workspace and w4_join_kernel adds them in order.
 // (Pairs through tensor memory for tcgen05.mma, 128 rows a warpgroup: 25 us for 9 x 28672 x 4096; its chains of codes, pairs, products
 // and sums wait for one another, and three warpgroups an SM do not cover that.)
-// w4_small_kernel: see there.
+// w4_small_kernel: up to eight rows of most matrices.
 #include <cooperative_groups.h>
 
 #include "common.cuh"
@@ -44,139 +44,107 @@ template <int I> __device__ __forceinline__ u32 pair(u32 word, u32 bits) {
   return *reinterpret_cast<const u32 *>(&y);
 }
 
+// Eight of k in the order of a word's pairs: 0 4 1 5 2 6 3 7.
+__device__ __forceinline__ uint4 pairs_of(const uint4 &v) {
+  return make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
+}
+
 // ---------------------------------------------------------------------------- small products
-// The codes never leave registers: a lane loads 32 of a weight row, and their pairs are its operands of mma.sync with 16 weight rows
-// as the tile's rows and up to eight activations as its columns.  A CTA has 16 weight rows; its warps divide k (chunk by chunk in turn, so that
-// together they read long pieces of a row), and where the matrix has few rows a cluster divides it once more.
-// GW: words of a lane in a group (group = 32 GW); RT: tiles of 8 activation rows; MT: tiles of 16 weight rows.
-template <int GW, int RT, int MT>
+// Up to eight rows.  A CTA has 16 weight rows; its warps divide k (chunk by chunk in turn, so that together they read long pieces of a
+// row), and where the matrix has few rows a cluster divides it once more.  Codes and activations are loaded straight into registers:
+// few of these, so that many warps hide the loads.  GW: words of a lane in a group (group = 32 GW).
+template <int GW>
 __global__ void __launch_bounds__(kThreads)
 w4_small_kernel(W4Args p) {
   constexpr int GROUPS = 4 / GW;       // of a chunk
-  __shared__ __align__(16) float sums[kWarps][MT * 16][RT * 8];
+  __shared__ float sums[kWarps][16][8];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j = lane & 3, lr = lane >> 2;
-  const int parts = gridDim.y, part = blockIdx.y, n0 = blockIdx.x * MT * 16;
-  float acc[MT][RT][4];
-#pragma unroll
-  for (int m = 0; m < MT; ++m)
-#pragma unroll
-    for (int t = 0; t < RT; ++t)
-#pragma unroll
-      for (int x = 0; x < 4; ++x) acc[m][t][x] = 0.f;
+  const int parts = gridDim.y, part = blockIdx.y, n0 = blockIdx.x * 16;
+  float acc[4] = {0.f, 0.f, 0.f, 0.f};
+  chain_wait();
+  chain_next();
 
   const int chunks = (p.K + kChunk - 1) / kChunk;
   for (int c = part * kWarps + warp; c < chunks; c += parts * kWarps) {
-    u32 word[MT][2][4];
-    float scale[MT][2][GROUPS];
+    u32 word[2][4];
+    float scale[2][GROUPS];
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int n = min(n0 + m * 16 + h * 8 + lr, p.N - 1);          // rows past the last are read as the last and not stored
-#pragma unroll
-        for (int g = 0; g < GROUPS; ++g) {
-          const int k = c * kChunk + g * GW * 32 + j * GW * 8;
-          const bool in = k < p.K;
-          const uint8_t *at = p.codes + ((size_t)n * p.K + k) / 2;
-          u32 *w = &word[m][h][g * GW];
-          if constexpr (GW == 4) {
-            const uint4 v = in ? __ldg(reinterpret_cast<const uint4 *>(at)) : make_uint4(0, 0, 0, 0);
-            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-          } else if constexpr (GW == 2) {
-            const uint2 v = in ? __ldg(reinterpret_cast<const uint2 *>(at)) : make_uint2(0, 0);
-            w[0] = v.x; w[1] = v.y;
-          } else {
-            w[0] = in ? __ldg(reinterpret_cast<const u32 *>(at)) : 0u;
-          }
-          const int group = c * GROUPS + g;
-          scale[m][h][g] = group < p.groups ? __bfloat162float(p.scales[(size_t)n * p.groups + group]) : 0.f;
-        }
-      }
-    u32 b[RT][4][4];                   // activations of the lane's row and words, as pairs in the codes' order
-#pragma unroll
-    for (int t = 0; t < RT; ++t)
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const int k = c * kChunk + (w / GW) * GW * 32 + j * GW * 8 + (w % GW) * 8, r = t * 8 + lr;
-        const uint4 v = r < p.R && k < p.K ? __ldg(reinterpret_cast<const uint4 *>(p.a + (size_t)r * p.K + k)) : make_uint4(0, 0, 0, 0);
-        b[t][w][0] = __byte_perm(v.x, v.z, 0x5410);
-        b[t][w][1] = __byte_perm(v.x, v.z, 0x7632);
-        b[t][w][2] = __byte_perm(v.y, v.w, 0x5410);
-        b[t][w][3] = __byte_perm(v.y, v.w, 0x7632);
-      }
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
+    for (int h = 0; h < 2; ++h) {
+      const int n = min(n0 + h * 8 + lr, p.N - 1);                     // rows past the last are read as the last and not stored
 #pragma unroll
       for (int g = 0; g < GROUPS; ++g) {
-        float sum[RT][4];
-#pragma unroll
-        for (int t = 0; t < RT; ++t)
-#pragma unroll
-          for (int x = 0; x < 4; ++x) sum[t][x] = 0.f;
-#pragma unroll
-        for (int w = g * GW; w < (g + 1) * GW; ++w) {
-          const u32 lo[4] = {pair<0>(word[m][0][w], p.bits), pair<0>(word[m][1][w], p.bits), pair<1>(word[m][0][w], p.bits), pair<1>(word[m][1][w], p.bits)};
-          const u32 hi[4] = {pair<2>(word[m][0][w], p.bits), pair<2>(word[m][1][w], p.bits), pair<3>(word[m][0][w], p.bits), pair<3>(word[m][1][w], p.bits)};
-#pragma unroll
-          for (int t = 0; t < RT; ++t) {
-            mma(sum[t], lo, b[t][w][0], b[t][w][1]);
-            mma(sum[t], hi, b[t][w][2], b[t][w][3]);
-          }
+        const int k = c * kChunk + g * GW * 32 + j * GW * 8, group = c * GROUPS + g;
+        const bool in = group < p.groups;
+        const uint8_t *at = p.codes + ((size_t)n * p.K + k) / 2;
+        u32 *w = &word[h][g * GW];
+        if constexpr (GW == 4) {
+          const uint4 v = __ldg(reinterpret_cast<const uint4 *>(at));
+          w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+        } else if constexpr (GW == 2) {
+          const uint2 v = in ? __ldg(reinterpret_cast<const uint2 *>(at)) : make_uint2(0, 0);
+          w[0] = v.x; w[1] = v.y;
+        } else {
+          w[0] = in ? __ldg(reinterpret_cast<const u32 *>(at)) : 0u;
         }
-#pragma unroll
-        for (int t = 0; t < RT; ++t)
-#pragma unroll
-          for (int x = 0; x < 4; ++x) acc[m][t][x] = fmaf(scale[m][x >> 1][g], sum[t][x], acc[m][t][x]);
+        scale[h][g] = in ? __bfloat162float(p.scales[(size_t)n * p.groups + group]) : 0.f;
       }
+    }
+    uint4 b[4];                        // activations of the lane's row and words, as pairs in the codes' order
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const int k = c * kChunk + w / GW * GW * 32 + j * GW * 8 + w % GW * 8;
+      b[w] = lr < p.R && k < p.K ? pairs_of(__ldg(reinterpret_cast<const uint4 *>(p.a + (size_t)lr * p.K + k))) : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) {
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = g * GW; w < (g + 1) * GW; ++w) {
+        const u32 lo[4] = {pair<0>(word[0][w], p.bits), pair<0>(word[1][w], p.bits), pair<1>(word[0][w], p.bits), pair<1>(word[1][w], p.bits)};
+        const u32 hi[4] = {pair<2>(word[0][w], p.bits), pair<2>(word[1][w], p.bits), pair<3>(word[0][w], p.bits), pair<3>(word[1][w], p.bits)};
+        mma(sum, lo, b[w].x, b[w].y);
+        mma(sum, hi, b[w].z, b[w].w);
+      }
+#pragma unroll
+      for (int x = 0; x < 4; ++x) acc[x] = fmaf(scale[x >> 1][g], sum[x], acc[x]);
+    }
   }
 
   // the warps' sums, then the cluster's
 #pragma unroll
-  for (int m = 0; m < MT; ++m)
-#pragma unroll
-    for (int t = 0; t < RT; ++t)
-#pragma unroll
-      for (int x = 0; x < 4; ++x) sums[warp][m * 16 + lr + (x >> 1) * 8][t * 8 + j * 2 + (x & 1)] = acc[m][t][x];
+  for (int x = 0; x < 4; ++x) sums[warp][lr + (x >> 1) * 8][j * 2 + (x & 1)] = acc[x];
   __syncthreads();
-  if (parts == 1) {
-    for (int i = threadIdx.x; i < MT * 16 * RT * 8; i += kThreads) {
-      const int n = i % (MT * 16), r = i / (MT * 16);
-      float s = 0.f;
+  const int n = threadIdx.x & 15, r = threadIdx.x >> 4;                // of the first 128 threads
+  float total = 0.f;
+  if (threadIdx.x < 128)
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) s += sums[w][n][r];
-      if (r < p.R && n0 + n < p.N) p.out[(size_t)r * p.N + n0 + n] = s;
+    for (int w = 0; w < kWarps; ++w) total += sums[w][n][r];
+  if (parts > 1) {
+    namespace cg = cooperative_groups;
+    cg::cluster_group cluster = cg::this_cluster();
+    if (threadIdx.x < 128) sums[0][n][r] = total;                      // (read by this thread alone so far)
+    cluster.sync();
+    if (part == 0 && threadIdx.x < 128) {
+      total = 0.f;
+      for (int q = 0; q < parts; ++q) total += *cluster.map_shared_rank(&sums[0][n][r], q);
     }
-    return;
+    cluster.sync();                    // no CTA leaves while others read its sums
   }
-  namespace cg = cooperative_groups;
-  cg::cluster_group cluster = cg::this_cluster();
-  for (int i = threadIdx.x; i < MT * 16 * RT * 8; i += kThreads) {
-    const int n = i % (MT * 16), r = i / (MT * 16);
-    float s = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) s += sums[w][n][r];
-    sums[0][n][r] = s;
-  }
-  cluster.sync();
-  for (int i = part * kThreads + threadIdx.x; i < MT * 16 * RT * 8; i += parts * kThreads) {
-    const int n = i % (MT * 16), r = i / (MT * 16);
-    float s = 0.f;
-    for (int q = 0; q < parts; ++q) s += *cluster.map_shared_rank(&sums[0][n][r], q);
-    if (r < p.R && n0 + n < p.N) p.out[(size_t)r * p.N + n0 + n] = s;
-  }
-  cluster.sync();                      // no CTA leaves while others read its sums
+  if (part == 0 && threadIdx.x < 128 && r < p.R && n0 + n < p.N) p.out[(size_t)r * p.N + n0 + n] = total;
 }
 
-template <int GW, int RT, int MT> int run_small(const W4Args &a, cudaStream_t s) {
-  const int tiles = ceil_div(a.N, MT * 16), chunks = ceil_div(a.K, kChunk);
+template <int GW> int run_small(const W4Args &a, cudaStream_t s) {
+  const int tiles = ceil_div(a.N, 16), chunks = ceil_div(a.K, kChunk);
   int parts = 1;
   while (parts < 8 && tiles * parts < kMeasuredSMs && parts * kWarps < chunks) parts *= 2;
-  cudaLaunchAttribute at = {};
-  at.id = cudaLaunchAttributeClusterDimension;
-  at.val.clusterDim.x = 1; at.val.clusterDim.y = parts; at.val.clusterDim.z = 1;
+  cudaLaunchAttribute at[2] = {};
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = 1; at[1].val.clusterDim.y = parts; at[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(tiles, parts); cfg.blockDim = dim3(kThreads); cfg.stream = s; cfg.attrs = &at; cfg.numAttrs = parts > 1;
-  HSD_CUDA_OK(cudaLaunchKernelEx(&cfg, w4_small_kernel<GW, RT, MT>, a));
+  cfg.gridDim = dim3(tiles, parts); cfg.blockDim = dim3(kThreads); cfg.stream = s; cfg.attrs = at; cfg.numAttrs = 1 + (parts > 1);
+  HSD_CUDA_OK(cudaLaunchKernelEx(&cfg, w4_small_kernel<GW>, a));
   hsd_count_launches(1);
   return hsd_launch_status();
 }
@@ -225,8 +193,7 @@ __global__ void __launch_bounds__(128) w4_stage_kernel(W4Line p, int gw, int rt)
   const int x = blockIdx.x * 128 + threadIdx.x, lane = x & 31, t = (x >> 5) % rt, word = (x >> 5) / rt % 8, step = (x >> 5) / (rt * 8);
   if (step >= p.steps) return;
   const int r = t * 8 + (lane >> 2), k = step * kStep + word / gw * gw * 32 + (lane & 3) * gw * 8 + word % gw * 8;
-  const uint4 v = r < p.R && k < p.K ? __ldg(reinterpret_cast<const uint4 *>(p.a + (size_t)r * p.K + k)) : make_uint4(0, 0, 0, 0);
-  reinterpret_cast<uint4 *>(p.staged)[x] = make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
+  reinterpret_cast<uint4 *>(p.staged)[x] = r < p.R && k < p.K ? pairs_of(__ldg(reinterpret_cast<const uint4 *>(p.a + (size_t)r * p.K + k))) : make_uint4(0, 0, 0, 0);
 }
 
 // GW: words of a lane in a group (group = 32 GW); RT: tiles of eight activation rows.
@@ -435,7 +402,10 @@ template <int GW> int run_line_rows(const W4Line &a, cudaStream_t s) {
 }
 int w4_tiles(int R) { return R <= 8 ? 1 : R <= 16 ? 2 : R <= 32 ? 4 : 8; }
 
-bool takes_small(int R, long long N, int K) { return false; }
+// Up to eight rows, one launch of loads straight into registers against the ring's three: 4096 x 4096 4.1 us (9.7 by the ring), 14336 x 4096 of
+// 1 / 8 rows 11.5 / 15.3 (13.1 / 15.0), 28672 x 4096 19.7 / 25.2 (22.3 / 22.8); with small groups, whose codes come in smaller pieces,
+// 32000 x 2048 20.6 (15.4).
+bool takes_small(int R, int N, int K, int group) { return R <= 8 && ((long long)N * K <= 60000000 || (group == 128 && R <= 4)); }
 
 }  // namespace
 }  // namespace hsd
@@ -457,9 +427,9 @@ extern "C" int hsd_gemm_w4(const void *A, int R, int K, const void *codes, const
   if (workspace_bytes < hsd_gemm_w4_workspace_bytes(R, N, K, group)) return HSD_E_WORKSPACE_TOO_SMALL;
   cudaStream_t s = (cudaStream_t)stream;
   const auto *a = static_cast<const __nv_bfloat16 *>(A), *sc = static_cast<const __nv_bfloat16 *>(scales);
-  if (takes_small(R, N, K)) {
+  if (takes_small(R, N, K, group)) {
     const W4Args p = {a, static_cast<const uint8_t *>(codes), sc, out, R, K, N, K / group, kCodeBits};
-    return group == 128 ? run_small<4, 1, 1>(p, s) : group == 64 ? run_small<2, 1, 1>(p, s) : run_small<1, 1, 1>(p, s);
+    return group == 128 ? run_small<4>(p, s) : group == 64 ? run_small<2>(p, s) : run_small<1>(p, s);
   }
   W4Line p = {};
   p.codes = static_cast<const uint8_t *>(codes);
