@@ -8,6 +8,11 @@
 // the number of candidates in front of it.  Order: larger logit first, lower id among equals, so the result does not
 // depend on the order in which candidates were found.
 // Rows with more candidates than fit (masses of equal logits: a mask's -inf) take select_slow().
+// A CTA has a row, or (few rows, or long ones) a cluster has one: each CTA finds the sums and the top tokens of its part, the first
+// one adds and merges them out of the others' shared memory.
+// Bound by memory for many rows (and by issue slots not far behind: some seven operations a bf16 logit, of which what can be done two at a
+// time is), by latency for few.
+#include <cooperative_groups.h>
 #include <math.h>
 
 #include "common.cuh"
@@ -28,20 +33,72 @@ struct LogprobArgs {
   int V, top;
 };
 
+__device__ __forceinline__ float max_nan(float a, float b) {           // NaN if either is
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
+}
+__device__ __forceinline__ u32 max_nan2(u32 a, u32 b) {
+  u32 y;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(a), "r"(b));
+  return y;
+}
+
 template <typename T> struct Vec;      // 16 bytes of logits
 template <> struct Vec<__nv_bfloat16> {
   static constexpr int N = 8;
+  static constexpr u32 kNone = 0xFF80FF80u;                            // two -inf
   __device__ static void unpack(const uint4 &v, float *f) {
     f[0] = __uint_as_float(v.x << 16); f[1] = __uint_as_float(v.x & 0xFFFF0000u);
     f[2] = __uint_as_float(v.y << 16); f[3] = __uint_as_float(v.y & 0xFFFF0000u);
     f[4] = __uint_as_float(v.z << 16); f[5] = __uint_as_float(v.z & 0xFFFF0000u);
     f[6] = __uint_as_float(v.w << 16); f[7] = __uint_as_float(v.w & 0xFFFF0000u);
   }
+  __device__ static uint4 pack(const float *f) {
+    uint4 v;
+    v.x = __float_as_uint(f[0]) >> 16 | (__float_as_uint(f[1]) & 0xFFFF0000u); v.y = __float_as_uint(f[2]) >> 16 | (__float_as_uint(f[3]) & 0xFFFF0000u);
+    v.z = __float_as_uint(f[4]) >> 16 | (__float_as_uint(f[5]) & 0xFFFF0000u); v.w = __float_as_uint(f[6]) >> 16 | (__float_as_uint(f[7]) & 0xFFFF0000u);
+    return v;
+  }
+  template <int U> __device__ static float largest(const uint4 *v) {
+    u32 m = kNone;
+#pragma unroll
+    for (int u = 0; u < U; ++u) m = max_nan2(m, max_nan2(max_nan2(v[u].x, v[u].y), max_nan2(v[u].z, v[u].w)));
+    return max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
+  }
+  // How many are larger than x (or equal to it): at most 4 a half per vector, whole numbers in bf16.
+  __device__ static int front(const uint4 &v, float x, bool equal) {
+    const __nv_bfloat162 t = __float2bfloat162_rn(x);
+    const u32 w[4] = {v.x, v.y, v.z, v.w};
+    __nv_bfloat162 n = __float2bfloat162_rn(0.f);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 y = *reinterpret_cast<const __nv_bfloat162 *>(&w[i]);
+      n = __hadd2(n, equal ? __hge2(y, t) : __hgt2(y, t));
+    }
+    return (int)(__low2float(n) + __high2float(n));
+  }
 };
 template <> struct Vec<float> {
   static constexpr int N = 4;
+  static constexpr u32 kNone = 0xFF800000u;
   __device__ static void unpack(const uint4 &v, float *f) {
     f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y); f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
+  }
+  __device__ static uint4 pack(const float *f) { return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])); }
+  template <int U> __device__ static float largest(const uint4 *v) {
+    float m = -INFINITY, f[N];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      unpack(v[u], f);
+      m = max_nan(m, max_nan(max_nan(f[0], f[1]), max_nan(f[2], f[3])));
+    }
+    return m;
+  }
+  __device__ static int front(const uint4 &v, float x, bool equal) {
+    float f[N];
+    unpack(v, f);
+    return equal ? (f[0] >= x) + (f[1] >= x) + (f[2] >= x) + (f[3] >= x) : (f[0] > x) + (f[1] > x) + (f[2] > x) + (f[3] > x);
   }
 };
 
@@ -71,37 +128,33 @@ template <typename T> struct Part {
     pieces = hi > lo ? (hi - first + N - 1) / N : 0;
   }
   __device__ __forceinline__ bool whole(int i) const { return first + i * N >= lo && first + (i + 1) * N <= hi; }
-  // f: -inf where there is no token
-  __device__ __forceinline__ void read(int i, float *f) const {
-    if (whole(i)) {
-      Vec<T>::unpack(__ldg(reinterpret_cast<const uint4 *>(row + first + (ptrdiff_t)i * N)), f);
-    } else {
+  // -inf where there is no token
+  __device__ __forceinline__ uint4 read(int i) const {
+    if (whole(i)) return __ldg(reinterpret_cast<const uint4 *>(row + first + (ptrdiff_t)i * N));
+    float f[N];
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
-        const int id = first + i * N + e;
-        f[e] = id >= lo && id < hi ? to_f32(row[id]) : -INFINITY;
-      }
+    for (int e = 0; e < N; ++e) {
+      const int id = first + i * N + e;
+      f[e] = id >= lo && id < hi ? to_f32(row[id]) : -INFINITY;
     }
+    return Vec<T>::pack(f);
   }
+  __device__ __forceinline__ void read(int i, float *f) const { Vec<T>::unpack(read(i), f); }
   __device__ __forceinline__ bool has(int i, int e) const {
     const int id = first + i * N + e;
     return id >= lo && id < hi;
   }
 };
 
-// Running sums of a thread relative to its own maximum (never below the lowest finite value, so that -inf tokens weigh 0).
+// Running sums of a thread relative to its own maximum m (never below the lowest finite value, so that -inf tokens weigh 0):
+// s = sum 2^y, t = sum 2^y y with y = (l - m) log2(e), cut off at -200, where 2^y is 0.
 struct Sums {
   float m = -3.402823466e38f, s = 0.f, t = 0.f;
   __device__ __forceinline__ void raise(float m2) {
-    const float d = fmaxf(m - m2, -200.f), f = ex2(d * kLog2e);
-    t = f * fmaf(s, d, t);
+    const float y = fmaxf((m - m2) * kLog2e, -200.f), f = ex2(y);
+    t = f * fmaf(s, y, t);
     s *= f;
     m = m2;
-  }
-  __device__ __forceinline__ void add(float x) {
-    const float d = x - m, e = ex2(d * kLog2e);
-    s += e;
-    t = fmaf(e, fmaxf(d, -200.f), t);
   }
   __device__ __forceinline__ void merge(float m2, float s2, float t2) {
     Sums o;
@@ -119,7 +172,9 @@ template <int THREADS> struct Shared {
   float m[THREADS / 32], s[THREADS / 32], t[THREADS / 32];
   int front[THREADS / 32];
   u64 cand[kCand];
-  u64 list[kMaxTop];                   // the top tokens in order
+  u64 list[kMaxTop];                   // the part's top tokens in order
+  u64 top[kMaxTop];                    // the row's
+  float4 sums;                         // the part's m (NaN: of no distribution), s, t; tokens in front
   float bound;
   int n_cand, warp_n[THREADS / 32];
 };
@@ -256,16 +311,18 @@ __device__ void select_top(const Part<T> &p, int k, float mine, Shared<THREADS> 
   __syncthreads();
 }
 
-// One CTA a row.
+// A row's CTAs (blockIdx.y, a cluster where there are several).
 template <typename T, int THREADS>
-__global__ void __launch_bounds__(THREADS)
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS)
 logprobs_kernel(LogprobArgs a) {
   constexpr int N = Vec<T>::N, U = 4;
   __shared__ __align__(16) Shared<THREADS> sh;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, parts = gridDim.y, part = blockIdx.y;
   const long long r = blockIdx.x;
   const T *row = static_cast<const T *>(a.logits) + (size_t)r * a.V;
-  const Part<T> p(row, 0, a.V);
+  const Part<T> p(row, (int)((long long)a.V * part / parts), (int)((long long)a.V * (part + 1) / parts));
+  chain_wait();
+  chain_next();
   const int tok = a.tokens[r];
   const bool given = tok >= 0 && tok < a.V;
   const float xt = given ? to_f32(row[tok]) : 0.f;
@@ -273,72 +330,140 @@ logprobs_kernel(LogprobArgs a) {
   Sums z;
   float mine = -INFINITY;
   int front = 0;
+  float2 s2 = make_float2(0.f, 0.f), t2 = s2;                          // of z, even and odd tokens apart
   for (int i0 = threadIdx.x; i0 < p.pieces; i0 += THREADS * U) {
-    float f[U][N];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (i0 + u * THREADS < p.pieces) {
-        p.read(i0 + u * THREADS, f[u]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < N; ++e) f[u][e] = -INFINITY;
-      }
-    }
-    float mx = -INFINITY;
+    uint4 v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int e = 0; e < N; ++e) mx = fmaxf(mx, f[u][e]);
-    mine = fmaxf(mine, mx);
-    if (mx > z.m) z.raise(mx);
+      v[u] = i0 + u * THREADS < p.pieces ? p.read(i0 + u * THREADS) : make_uint4(Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone);
+    mine = max_nan(mine, Vec<T>::template largest<U>(v));
+    if (mine > z.m) {
+      z.s = s2.x + s2.y; z.t = t2.x + t2.y;
+      z.raise(mine);
+      s2 = make_float2(z.s, 0.f); t2 = make_float2(z.t, 0.f);
+    }
+    const float2 minus = make_float2(-z.m, -z.m), scale = make_float2(kLog2e, kLog2e);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int id0 = p.first + (i0 + u * THREADS) * N;
-      if (i0 + u * THREADS >= p.pieces) continue;
-      const bool before = id0 + N <= tok;
+      float f[N];
+      Vec<T>::unpack(v[u], f);
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
-        z.add(f[u][e]);
-        front += before ? f[u][e] >= xt && id0 + e >= p.lo : f[u][e] > xt || (f[u][e] == xt && id0 + e < tok && id0 + e >= p.lo);
+      for (int e = 0; e < N; e += 2) {
+        float2 y = __fmul2_rn(__fadd2_rn(make_float2(f[e], f[e + 1]), minus), scale);
+        y.x = fmaxf(y.x, -200.f); y.y = fmaxf(y.y, -200.f);
+        const float2 w = make_float2(ex2(y.x), ex2(y.y));
+        s2 = __fadd2_rn(s2, w);
+        t2 = __ffma2_rn(w, y, t2);
+      }
+      if (id0 > tok || id0 + N <= tok) {                               // (places without a token hold -inf)
+        front += Vec<T>::front(v[u], xt, id0 < tok && xt > -INFINITY);
+      } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) front += f[e] > xt || (xt > -INFINITY && f[e] == xt && id0 + e < tok);
       }
     }
   }
+  if (given && xt == -INFINITY) {      // among equals of -inf the lower ids count, and places without a token do not
+    front = 0;
+    for (int i = threadIdx.x; i < p.pieces; i += THREADS) {
+      float f[N];
+      p.read(i, f);
+#pragma unroll
+      for (int e = 0; e < N; ++e) front += p.has(i, e) && (f[e] > xt || p.first + i * N + e < tok);
+    }
+  }
+  z.s = s2.x + s2.y; z.t = t2.x + t2.y;
+  if (!(mine < INFINITY)) z.m = NAN;   // a NaN or +inf: no distribution
+  bool none = __any_sync(0xFFFFFFFFu, !(z.m == z.m));
+#pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
-    const float m2 = __shfl_xor_sync(0xFFFFFFFFu, z.m, o), s2 = __shfl_xor_sync(0xFFFFFFFFu, z.s, o), t2 = __shfl_xor_sync(0xFFFFFFFFu, z.t, o);
-    z.merge(m2, s2, t2);
+    z.merge(__shfl_xor_sync(0xFFFFFFFFu, z.m, o), __shfl_xor_sync(0xFFFFFFFFu, z.s, o), __shfl_xor_sync(0xFFFFFFFFu, z.t, o));
     front += __shfl_xor_sync(0xFFFFFFFFu, front, o);
   }
-  if (lane == 0) { sh.m[warp] = z.m; sh.s[warp] = z.s; sh.t[warp] = z.t; sh.front[warp] = front; }
+  if (lane == 0) { sh.m[warp] = none ? NAN : z.m; sh.s[warp] = z.s; sh.t[warp] = z.t; sh.front[warp] = front; }
   __syncthreads();
   Sums all;
   front = 0;
-  for (int w = 0; w < THREADS / 32; ++w) { all.merge(sh.m[w], sh.s[w], sh.t[w]); front += sh.front[w]; }
-  const bool none = !(all.s == all.s) || all.m == INFINITY;           // a NaN or +inf: no distribution
+  none = false;
+#pragma unroll
+  for (int w = 0; w < THREADS / 32; ++w) {
+    none |= !(sh.m[w] == sh.m[w]);
+    all.merge(sh.m[w], sh.s[w], sh.t[w]);
+    front += sh.front[w];
+  }
+  if (a.top > 0) {
+    if (none) {
+      if (threadIdx.x < kMaxTop) sh.list[threadIdx.x] = 0;
+    } else {
+      select_top<T, THREADS>(p, a.top, mine, sh);
+    }
+  }
+  if (parts > 1) {
+    namespace cg = cooperative_groups;
+    cg::cluster_group cluster = cg::this_cluster();
+    if (threadIdx.x == 0) sh.sums = make_float4(none ? NAN : all.m, all.s, all.t, __int_as_float(front));
+    cluster.sync();
+    if (part == 0) {
+      Sums sum;
+      none = false;
+      front = 0;
+      for (int q = 0; q < parts; ++q) {
+        const float4 x = *cluster.map_shared_rank(&sh.sums, q);
+        none |= !(x.x == x.x);
+        sum.merge(x.x, x.y, x.z);
+        front += __float_as_int(x.w);
+      }
+      all = sum;
+      if (a.top > 0) {                 // the parts' lists are in order: a token's place is the sum of its places in them
+        for (int i = threadIdx.x; i < parts * a.top; i += THREADS) sh.cand[i] = *cluster.map_shared_rank(&sh.list[i % a.top], i / a.top);
+        __syncthreads();
+        for (int i = threadIdx.x; i < parts * a.top; i += THREADS) {
+          const u64 x = sh.cand[i];
+          int place = 0;
+          for (int k = 0; k < parts * a.top; ++k) place += sh.cand[k] > x;
+          if (place < a.top && x != 0) sh.top[place] = x;
+        }
+      }
+    }
+    cluster.sync();                    // no CTA leaves while the first one reads
+    if (part > 0) return;
+  }
+  const u64 *list = parts > 1 ? sh.top : sh.list;
   const float log_s = logf(all.s);
   if (threadIdx.x == 0) {
     a.logprob[r] = none || !given ? NAN : all.s > 0.f ? xt - all.m - log_s : -INFINITY;
-    a.entropy[r] = none ? NAN : all.s > 0.f ? log_s - all.t / all.s : 0.f;
+    a.entropy[r] = none ? NAN : all.s > 0.f ? log_s - 0.6931471805599453f * (all.t / all.s) : 0.f;
     a.rank[r] = none || !given ? -1 : front;
   }
-  if (a.top == 0) return;
-  if (none) {
-    if ((int)threadIdx.x < a.top) { a.top_id[r * a.top + threadIdx.x] = -1; a.top_lp[r * a.top + threadIdx.x] = NAN; }
-    return;
-  }
-  select_top<T, THREADS>(p, a.top, mine, sh);
   if ((int)threadIdx.x < a.top) {
-    const u64 x = sh.list[threadIdx.x];
+    const u64 x = list[threadIdx.x];
     const float l = unordered((u32)(x >> 32));
-    a.top_id[r * a.top + threadIdx.x] = (int)~(u32)x;
-    a.top_lp[r * a.top + threadIdx.x] = all.s > 0.f ? l - all.m - log_s : -INFINITY;
+    a.top_id[r * a.top + threadIdx.x] = none ? -1 : (int)~(u32)x;
+    a.top_lp[r * a.top + threadIdx.x] = none ? NAN : all.s > 0.f ? l - all.m - log_s : -INFINITY;
   }
 }
 
-template <typename T> int run(const LogprobArgs &a, int rows, cudaStream_t s) {
-  if (a.V <= 4096) logprobs_kernel<T, 128><<<rows, 128, 0, s>>>(a);
-  else logprobs_kernel<T, 512><<<rows, 512, 0, s>>>(a);
+template <typename T, int THREADS> int run_threads(const LogprobArgs &a, int rows, int parts, cudaStream_t s) {
+  cudaLaunchAttribute at[2] = {};
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = 1; at[1].val.clusterDim.y = parts; at[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(rows, parts); cfg.blockDim = dim3(THREADS); cfg.stream = s; cfg.attrs = at; cfg.numAttrs = 1 + (parts > 1);
+  HSD_CUDA_OK(cudaLaunchKernelEx(&cfg, logprobs_kernel<T, THREADS>, a));
   hsd_count_launches(1);
   return hsd_launch_status();
+}
+// Rows that do not fill the GPU are divided into parts of 2048 tokens or more, long rows into parts of 16384 until there are four rounds of
+// CTAs (four of 256 threads on an SM).
+template <typename T> int run(const LogprobArgs &a, int rows, cudaStream_t s) {
+  if (a.V <= 4096) return run_threads<T, 128>(a, rows, 1, s);
+  int parts = 1;
+  while (parts < 8 && (long long)rows * parts * 2 <= 4 * kMeasuredSMs && a.V / (parts * 2) >= 2048) parts *= 2;
+  while (parts < 8 && (long long)rows * parts < 16 * kMeasuredSMs && a.V / (parts * 2) >= 16384) parts *= 2;
+  return run_threads<T, 256>(a, rows, parts, s);
 }
 
 }  // namespace
