@@ -169,6 +169,7 @@ struct Sums {
 
 template <int THREADS> struct Shared {
   float group_max[128];
+  int flagged[THREADS], n_flagged;     // threads whose pieces may hold one of the top tokens
   float m[THREADS / 32], s[THREADS / 32], t[THREADS / 32];
   int front[THREADS / 32];
   u64 cand[kCand];
@@ -256,48 +257,70 @@ __device__ void select_slow(const Part<T> &p, int k, float bound, float top, Sha
   __syncthreads();
 }
 
-// The part's k first tokens (fewer if it has fewer; the rest of the list is 0, which no token's key is) into sh.list.
-template <typename T, int THREADS>
-__device__ void select_top(const Part<T> &p, int k, float mine, Shared<THREADS> &sh) {
-  constexpr int N = Vec<T>::N, GROUPS = 128, LANES = THREADS / GROUPS;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+// The part's k first tokens (fewer if it has fewer; the rest of the list is 0, which no token's key is) into sh.list.  v: the thread's
+// pieces, if it has no others (`all_here`).
+template <typename T, int THREADS, int U>
+__device__ void select_top(const Part<T> &p, int k, float mine, const uint4 *v, bool all_here, Shared<THREADS> &sh) {
+  constexpr int N = Vec<T>::N, LANES = THREADS / 128;                  // threads of a group: 128 groups
+  const int lane = threadIdx.x & 31;
   float g = mine;
 #pragma unroll
   for (int o = 1; o < LANES; o <<= 1) g = fmaxf(g, __shfl_xor_sync(0xFFFFFFFFu, g, o));
   if (threadIdx.x % LANES == 0) sh.group_max[threadIdx.x / LANES] = g;
-  if (threadIdx.x == 0) sh.n_cand = 0;
+  if (threadIdx.x == 0) sh.n_cand = sh.n_flagged = 0;
   __syncthreads();
-  if (threadIdx.x < GROUPS) {
-    const float x = sh.group_max[threadIdx.x];
-    int above = 0, same = 0;
-#pragma unroll 8
-    for (int i = 0; i < GROUPS / 4; ++i) {
-      const float4 y = reinterpret_cast<const float4 *>(sh.group_max)[i];
-      above += (y.x > x) + (y.y > x) + (y.z > x) + (y.w > x);
-      same += (y.x == x) + (y.y == x) + (y.z == x) + (y.w == x);
-    }
-    if (above < k && above + same >= k) sh.bound = x;
-  }
-  __syncthreads();
-  const float bound = sh.bound;
-  // each flagged thread's pieces are read by its whole warp
-  for (u32 flagged = __ballot_sync(0xFFFFFFFFu, mine >= bound && (int)threadIdx.x < p.pieces); flagged; flagged &= flagged - 1) {
-    const int owner = warp * 32 + __ffs(flagged) - 1;
-    for (int i = owner + lane * THREADS; i < p.pieces; i += 32 * THREADS) {
-      float f[N];
-      p.read(i, f);
+  // Every warp for itself: the largest value of 16 bits that k of the groups' maxima reach, bit by bit.
+  u32 x[4];
 #pragma unroll
-      for (int e = 0; e < N; ++e)
-        if (f[e] >= bound && p.has(i, e)) {
-          const int at = atomicAdd(&sh.n_cand, 1);
-          if (at < kCand) sh.cand[at] = key_of(f[e], p.first + i * N + e);
-        }
+  for (int i = 0; i < 4; ++i) x[i] = ordered(sh.group_max[i * 32 + lane]) >> 16;
+  u32 reached = 0;
+#pragma unroll
+  for (int bit = 15; bit >= 0; --bit) {
+    const u32 at = reached | 1u << bit;
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) n += __popc(__ballot_sync(0xFFFFFFFFu, x[i] >= at));
+    if (n >= k) reached = at;
+  }
+  const float bound = fmaxf(unordered(max(reached << 16, 0x007FFFFFu)), -INFINITY);      // (0x007FFFFF: -inf)
+  const bool flagged = mine >= bound && (int)threadIdx.x < p.pieces;
+  auto take = [&](const uint4 &x, int i) {
+    float f[N];
+    Vec<T>::unpack(x, f);
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (f[e] >= bound && p.has(i, e)) {
+        const int at = atomicAdd(&sh.n_cand, 1);
+        if (at < kCand) sh.cand[at] = key_of(f[e], p.first + i * N + e);
+      }
+  };
+  if (all_here) {
+    if (flagged)
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if ((int)threadIdx.x + u * THREADS < p.pieces) take(v[u], threadIdx.x + u * THREADS);
+  } else {                             // the flagged threads' pieces once more, by all threads
+    if (flagged) sh.flagged[atomicAdd(&sh.n_flagged, 1)] = threadIdx.x;
+    __syncthreads();
+    const int each = (p.pieces + THREADS - 1) / THREADS, n = sh.n_flagged * each;
+    for (int x0 = threadIdx.x; x0 < n; x0 += THREADS * U) {
+      uint4 y[U];
+      int at[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int x = x0 + u * THREADS;
+        at[u] = x < n ? sh.flagged[x / each] + x % each * THREADS : p.pieces;
+        if (at[u] < p.pieces) y[u] = p.read(at[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (at[u] < p.pieces) take(y[u], at[u]);
     }
   }
   __syncthreads();
   if (sh.n_cand > kCand) {
     float top = -INFINITY;
-    for (int i = 0; i < GROUPS; ++i) top = fmaxf(top, sh.group_max[i]);
+    for (int i = 0; i < 128; ++i) top = fmaxf(top, sh.group_max[i]);
     select_slow<T, THREADS>(p, k, bound, top, sh);
   }
   const int n = sh.n_cand;
@@ -305,6 +328,7 @@ __device__ void select_top(const Part<T> &p, int k, float mine, Shared<THREADS> 
   for (int c = threadIdx.x; c < n; c += THREADS) {
     const u64 x = sh.cand[c];
     int place = 0;
+#pragma unroll 4
     for (int i = 0; i < n; ++i) place += sh.cand[i] > x;
     if (place < k) sh.list[place] = x;
   }
@@ -331,8 +355,8 @@ logprobs_kernel(LogprobArgs a) {
   float mine = -INFINITY;
   int front = 0;
   float2 s2 = make_float2(0.f, 0.f), t2 = s2;                          // of z, even and odd tokens apart
+  uint4 v[U];
   for (int i0 = threadIdx.x; i0 < p.pieces; i0 += THREADS * U) {
-    uint4 v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u)
       v[u] = i0 + u * THREADS < p.pieces ? p.read(i0 + u * THREADS) : make_uint4(Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone);
@@ -396,7 +420,7 @@ logprobs_kernel(LogprobArgs a) {
     if (none) {
       if (threadIdx.x < kMaxTop) sh.list[threadIdx.x] = 0;
     } else {
-      select_top<T, THREADS>(p, a.top, mine, sh);
+      select_top<T, THREADS, U>(p, a.top, mine, v, p.pieces <= THREADS * U, sh);
     }
   }
   if (parts > 1) {
