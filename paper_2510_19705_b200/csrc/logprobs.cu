@@ -66,15 +66,18 @@ template <> struct Vec<__nv_bfloat16> {
     for (int u = 0; u < U; ++u) m = max_nan2(m, max_nan2(max_nan2(v[u].x, v[u].y), max_nan2(v[u].z, v[u].w)));
     return max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
   }
-  // How many are larger than x (or equal to it): at most 4 a half per vector, whole numbers in bf16.
-  __device__ static int front(const uint4 &v, float x, bool equal) {
+  // How many are larger than x (or equal to it): at most 4 U a half, whole numbers in bf16.
+  template <int U> __device__ static int front(const uint4 *v, float x, bool equal) {
     const __nv_bfloat162 t = __float2bfloat162_rn(x);
-    const u32 w[4] = {v.x, v.y, v.z, v.w};
     __nv_bfloat162 n = __float2bfloat162_rn(0.f);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const __nv_bfloat162 y = *reinterpret_cast<const __nv_bfloat162 *>(&w[i]);
-      n = __hadd2(n, equal ? __hge2(y, t) : __hgt2(y, t));
+    for (int u = 0; u < U; ++u) {
+      const u32 w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 y = *reinterpret_cast<const __nv_bfloat162 *>(&w[i]);
+        n = __hadd2(n, equal ? __hge2(y, t) : __hgt2(y, t));
+      }
     }
     return (int)(__low2float(n) + __high2float(n));
   }
@@ -95,10 +98,15 @@ template <> struct Vec<float> {
     }
     return m;
   }
-  __device__ static int front(const uint4 &v, float x, bool equal) {
-    float f[N];
-    unpack(v, f);
-    return equal ? (f[0] >= x) + (f[1] >= x) + (f[2] >= x) + (f[3] >= x) : (f[0] > x) + (f[1] > x) + (f[2] > x) + (f[3] > x);
+  template <int U> __device__ static int front(const uint4 *v, float x, bool equal) {
+    int n = 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float f[N];
+      unpack(v[u], f);
+      n += equal ? (f[0] >= x) + (f[1] >= x) + (f[2] >= x) + (f[3] >= x) : (f[0] > x) + (f[1] > x) + (f[2] > x) + (f[3] > x);
+    }
+    return n;
   }
 };
 
@@ -336,10 +344,11 @@ __device__ void select_top(const Part<T> &p, int k, float mine, const uint4 *v, 
 }
 
 // A row's CTAs (blockIdx.y, a cluster where there are several).
-template <typename T, int THREADS>
+// U: pieces of a thread at once.
+template <typename T, int THREADS, int U>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
 logprobs_kernel(LogprobArgs a) {
-  constexpr int N = Vec<T>::N, U = 4;
+  constexpr int N = Vec<T>::N;
   __shared__ __align__(16) Shared<THREADS> sh;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, parts = gridDim.y, part = blockIdx.y;
   const long long r = blockIdx.x;
@@ -357,6 +366,10 @@ logprobs_kernel(LogprobArgs a) {
   float2 s2 = make_float2(0.f, 0.f), t2 = s2;                          // of z, even and odd tokens apart
   uint4 v[U];
   for (int i0 = threadIdx.x; i0 < p.pieces; i0 += THREADS * U) {
+    if (i0 > 0 && i0 + (U - 1) * THREADS < p.pieces - 1) {             // no piece at an end of the part
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u] = __ldg(reinterpret_cast<const uint4 *>(p.row + p.first + (ptrdiff_t)(i0 + u * THREADS) * N));
+    } else
 #pragma unroll
     for (int u = 0; u < U; ++u)
       v[u] = i0 + u * THREADS < p.pieces ? p.read(i0 + u * THREADS) : make_uint4(Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone);
@@ -366,6 +379,9 @@ logprobs_kernel(LogprobArgs a) {
       z.raise(mine);
       s2 = make_float2(z.s, 0.f); t2 = make_float2(z.t, 0.f);
     }
+    const int id_lo = p.first + i0 * N, id_hi = id_lo + (U - 1) * THREADS * N + N;
+    const bool one_side = id_lo > tok || id_hi <= tok;                 // of the given token, as nearly all are
+    if (one_side) front += Vec<T>::template front<U>(v, xt, id_lo < tok && xt > -INFINITY);
     const float2 minus = make_float2(-z.m, -z.m), scale = make_float2(kLog2e, kLog2e);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -380,8 +396,9 @@ logprobs_kernel(LogprobArgs a) {
         s2 = __fadd2_rn(s2, w);
         t2 = __ffma2_rn(w, y, t2);
       }
+      if (one_side) continue;
       if (id0 > tok || id0 + N <= tok) {                               // (places without a token hold -inf)
-        front += Vec<T>::front(v[u], xt, id0 < tok && xt > -INFINITY);
+        front += Vec<T>::template front<1>(v + u, xt, id0 < tok && xt > -INFINITY);
       } else {
 #pragma unroll
         for (int e = 0; e < N; ++e) front += f[e] > xt || (xt > -INFINITY && f[e] == xt && id0 + e < tok);
@@ -398,29 +415,43 @@ logprobs_kernel(LogprobArgs a) {
     }
   }
   z.s = s2.x + s2.y; z.t = t2.x + t2.y;
-  if (!(mine < INFINITY)) z.m = NAN;   // a NaN or +inf: no distribution
-  bool none = __any_sync(0xFFFFFFFFu, !(z.m == z.m));
+  // the part's maximum, then sums relative to it: one rescaling a thread
+  float m = z.m;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    z.merge(__shfl_xor_sync(0xFFFFFFFFu, z.m, o), __shfl_xor_sync(0xFFFFFFFFu, z.s, o), __shfl_xor_sync(0xFFFFFFFFu, z.t, o));
-    front += __shfl_xor_sync(0xFFFFFFFFu, front, o);
-  }
-  if (lane == 0) { sh.m[warp] = none ? NAN : z.m; sh.s[warp] = z.s; sh.t[warp] = z.t; sh.front[warp] = front; }
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+  if (__any_sync(0xFFFFFFFFu, !(mine < INFINITY))) m = NAN;            // a NaN or +inf: no distribution
+  if (lane == 0) sh.m[warp] = m;
   __syncthreads();
-  Sums all;
-  front = 0;
-  none = false;
+  bool none = false;
+  m = z.m;
 #pragma unroll
   for (int w = 0; w < THREADS / 32; ++w) {
     none |= !(sh.m[w] == sh.m[w]);
-    all.merge(sh.m[w], sh.s[w], sh.t[w]);
-    front += sh.front[w];
+    m = fmaxf(m, sh.m[w]);
   }
-  if (a.top > 0) {
-    if (none) {
-      if (threadIdx.x < kMaxTop) sh.list[threadIdx.x] = 0;
-    } else {
-      select_top<T, THREADS, U>(p, a.top, mine, v, p.pieces <= THREADS * U, sh);
+  if (m > z.m) z.raise(m);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    z.s += __shfl_xor_sync(0xFFFFFFFFu, z.s, o);
+    z.t += __shfl_xor_sync(0xFFFFFFFFu, z.t, o);
+  }
+  front = __reduce_add_sync(0xFFFFFFFFu, front);
+  if (lane == 0) { sh.s[warp] = z.s; sh.t[warp] = z.t; sh.front[warp] = front; }
+  if (a.top > 0 && !none) {
+    select_top<T, THREADS, U>(p, a.top, mine, v, p.pieces <= THREADS * U, sh);
+  } else {
+    if (threadIdx.x < kMaxTop) sh.list[threadIdx.x] = 0;
+    __syncthreads();
+  }
+  Sums all;
+  all.m = m;
+  front = 0;
+  if (warp == 0) {                     // (the rest is the first warp's)
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) {
+      all.s += sh.s[w];
+      all.t += sh.t[w];
+      front += sh.front[w];
     }
   }
   if (parts > 1) {
@@ -429,16 +460,18 @@ logprobs_kernel(LogprobArgs a) {
     if (threadIdx.x == 0) sh.sums = make_float4(none ? NAN : all.m, all.s, all.t, __int_as_float(front));
     cluster.sync();
     if (part == 0) {
-      Sums sum;
-      none = false;
-      front = 0;
-      for (int q = 0; q < parts; ++q) {
-        const float4 x = *cluster.map_shared_rank(&sh.sums, q);
-        none |= !(x.x == x.x);
-        sum.merge(x.x, x.y, x.z);
-        front += __float_as_int(x.w);
+      if (warp == 0) {
+        Sums sum;
+        none = false;
+        front = 0;
+        for (int q = 0; q < parts; ++q) {
+          const float4 x = *cluster.map_shared_rank(&sh.sums, q);
+          none |= !(x.x == x.x);
+          sum.merge(x.x, x.y, x.z);
+          front += __float_as_int(x.w);
+        }
+        all = sum;
       }
-      all = sum;
       if (a.top > 0) {                 // the parts' lists are in order: a token's place is the sum of its places in them
         for (int i = threadIdx.x; i < parts * a.top; i += THREADS) sh.cand[i] = *cluster.map_shared_rank(&sh.list[i % a.top], i / a.top);
         __syncthreads();
@@ -453,6 +486,7 @@ logprobs_kernel(LogprobArgs a) {
     cluster.sync();                    // no CTA leaves while the first one reads
     if (part > 0) return;
   }
+  if (warp > 0) return;
   const u64 *list = parts > 1 ? sh.top : sh.list;
   const float log_s = logf(all.s);
   if (threadIdx.x == 0) {
@@ -468,7 +502,7 @@ logprobs_kernel(LogprobArgs a) {
   }
 }
 
-template <typename T, int THREADS> int run_threads(const LogprobArgs &a, int rows, int parts, cudaStream_t s) {
+template <typename T, int THREADS, int U> int run_threads(const LogprobArgs &a, int rows, int parts, cudaStream_t s) {
   cudaLaunchAttribute at[2] = {};
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
@@ -476,18 +510,17 @@ template <typename T, int THREADS> int run_threads(const LogprobArgs &a, int row
   at[1].val.clusterDim.x = 1; at[1].val.clusterDim.y = parts; at[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(rows, parts); cfg.blockDim = dim3(THREADS); cfg.stream = s; cfg.attrs = at; cfg.numAttrs = 1 + (parts > 1);
-  HSD_CUDA_OK(cudaLaunchKernelEx(&cfg, logprobs_kernel<T, THREADS>, a));
+  HSD_CUDA_OK(cudaLaunchKernelEx(&cfg, logprobs_kernel<T, THREADS, U>, a));
   hsd_count_launches(1);
   return hsd_launch_status();
 }
-// Rows that do not fill the GPU are divided into parts of 2048 tokens or more, long rows into parts of 16384 until there are four rounds of
-// CTAs (four of 256 threads on an SM).
+// Rows that do not fill the GPU are divided into parts of 2048 tokens or more.  Long ones take CTAs of 512 threads with eight pieces at once:
+// 700 x 131072 fp32 85 us (of 256 threads with four 117, divided among four such 111), but 576 x 32000 bf16 30 (17).
 template <typename T> int run(const LogprobArgs &a, int rows, cudaStream_t s) {
-  if (a.V <= 4096) return run_threads<T, 128>(a, rows, 1, s);
+  if (a.V <= 4096) return run_threads<T, 128, 4>(a, rows, 1, s);
   int parts = 1;
   while (parts < 8 && (long long)rows * parts * 2 <= 4 * kMeasuredSMs && a.V / (parts * 2) >= 2048) parts *= 2;
-  while (parts < 8 && (long long)rows * parts < 16 * kMeasuredSMs && a.V / (parts * 2) >= 16384) parts *= 2;
-  return run_threads<T, 256>(a, rows, parts, s);
+  return a.V / parts >= 65536 ? run_threads<T, 512, 8>(a, rows, parts, s) : run_threads<T, 256, 4>(a, rows, parts, s);
 }
 
 }  // namespace
