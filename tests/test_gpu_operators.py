@@ -484,3 +484,88 @@ def test_the_binding_refuses_shapes_and_types(lib):
     for c, s in ((codes[:, :32].contiguous(), scales), (codes, scales[:4])):
         with pytest.raises(ValueError):
             lib.hsd_gemm_w4(A, c, s)
+
+
+# ------------------------------------------------------------------------------------------------ together
+def test_a_drafter_of_ones_own(lib):
+    """Two layers with 4-bit projections decode three sequences of different lengths over a paged cache: prompts in one ragged append,
+    then steps of one token; every step's logits against a plain forward in 64 bits with the same rounding points, its draws by hsd_draft_sample
+    and what they were worth by hsd_token_logprobs, a verification of the drafts at the end."""
+    g = gen(77)
+    d, nq, nkv, hd, ff, V, page, layers, steps = 256, 4, 2, 64, 512, 1000, 16, 2, 5
+    prompts = [37, 1, 20]
+    B = len(prompts)
+
+    def pack(n, k):
+        codes, scales = lib.w4_pack(randn(g, n, k, std=0.06), 64)
+        c = torch.stack((codes & 15, codes >> 4), dim=-1).view(n, k).double() - 8
+        return codes, scales, (c * scales.double().repeat_interleave(64, dim=1)).cpu()
+
+    W = [dict(qkv=pack((nq + 2 * nkv) * hd, d), o=pack(d, nq * hd), up=pack(ff, d), down=pack(d, ff)) for _ in range(layers)]
+    head, embed = pack(V, d), randn(g, V, d, dtype=BF16)
+    rope = lib.rope_table(64, hd)
+    k_pools, v_pools, tables = zip(*(cache(g, B, nkv, hd, page, 4, BF16, spare=2) for _ in range(layers)))
+
+    def norm(x):
+        return x * torch.rsqrt(x.square().mean(dim=-1, keepdim=True) + 1e-5)
+
+    def product(x, w):                                                      # in pieces: at most 64 rows a call
+        x = x.to(BF16).contiguous()
+        return torch.cat([lib.hsd_gemm_w4(p.contiguous(), w[0], w[1]) for p in x.split(64)])
+
+    def attend(l, qkv, lens, starts, i):
+        """Rows' attention: each row as a call of its own length, so that prompts take the decoding path too."""
+        q = lib.hsd_kv_append(qkv.view(-1, nq + 2 * nkv, hd), k_pools[l], v_pools[l], tables[l], ints(lens), rope, None if starts is None else ints(starts))
+        if starts is None:
+            return lib.hsd_paged_attention(q, k_pools[l], v_pools[l], tables[l], ints([n + 1 for n in lens]))
+        seq = [b for b in range(B) for _ in range(starts[b + 1] - starts[b])]
+        upto = [lens[b] + r + 1 for b in range(B) for r in range(starts[b + 1] - starts[b])]
+        return lib.hsd_paged_attention(q, k_pools[l], v_pools[l], tables[l][torch.tensor(seq)].contiguous(), ints(upto))
+
+    def forward(tokens, lens, starts=None):
+        x = embed[tokens].float()
+        for l in range(layers):
+            a = attend(l, product(norm(x), W[l]["qkv"]), lens, starts, l)
+            x = x + product(a.reshape(-1, nq * hd), W[l]["o"])
+            x = x + product(torch.nn.functional.gelu(product(norm(x), W[l]["up"])), W[l]["down"])
+        return product(norm(x), head)
+
+    def plain(tokens):
+        """The last position's logits of one sequence, in 64 bits but for the rounding points."""
+        bf = lambda t: t.float().to(BF16).double()
+        x = embed.cpu()[tokens].double()
+        n = len(tokens)
+        t = rope.cpu().double()[:n]
+        for l in range(layers):
+            qkv = (bf(norm(x)) @ W[l]["qkv"][2].T).view(n, nq + 2 * nkv, hd)
+            lo, hi = qkv[:, :nq + nkv, :hd // 2], qkv[:, :nq + nkv, hd // 2:]
+            c, s = t[:, 0, None], t[:, 1, None]
+            qk = bf(torch.cat((lo * c - hi * s, hi * c + lo * s), dim=-1))
+            q, k, v = qk[:, :nq], qk[:, nq:], bf(qkv[:, nq + nkv:])
+            k, v = (z.repeat_interleave(nq // nkv, dim=1) for z in (k, v))
+            w = torch.einsum("ihd,jhd->hij", q, k) * hd ** -0.5
+            w = torch.softmax(w.masked_fill(torch.ones(n, n).triu(1).bool(), -math.inf), dim=-1)
+            x = x + bf(torch.einsum("hij,jhd->ihd", w, v).reshape(n, nq * hd)) @ W[l]["o"][2].T
+            x = x + bf(torch.nn.functional.gelu(bf(norm(x)) @ W[l]["up"][2].T)) @ W[l]["down"][2].T
+        return bf(norm(x[-1])) @ head[2].T
+
+    text = [torch.randint(0, V, (n,), generator=torch.Generator().manual_seed(n)).tolist() for n in prompts]
+    starts = [0, 37, 38, 58]
+    logits = forward(torch.tensor(sum(text, []), device="cuda"), [0] * B, starts)[torch.tensor([36, 37, 57], device="cuda")]
+    rows, drafts = [], []
+    for step in range(steps):
+        for b in range(B):                                                  # the bf16 forwards' own bound: a few flips of a rounding
+            assert float((logits[b].double().cpu() - plain(text[b])).abs().max()) < 2e-2
+        tokens = lib.hsd_draft_sample(logits.view(B, 1, V), 5, step)[:, 0]
+        check_logprobs(lib, logits, tokens, 8)
+        rows.append(logits.clone())
+        drafts.append(tokens.clone())
+        lens = [len(t) for t in text]
+        for b in range(B):
+            text[b].append(int(tokens[b]))
+        logits = forward(tokens.long(), lens)
+    q = torch.stack(rows, dim=1).contiguous()
+    out, n = lib.hsd_verify_level(1, torch.cat((q, logits[:, None]), dim=1).contiguous(), q, torch.stack(drafts, dim=1).contiguous(), 5, 0)
+    assert n.tolist() == [steps] * B                                        # verified by itself: everything is accepted
+    lp = lib.hsd_token_logprobs(torch.cat((q, logits[:, None]), dim=1).contiguous(), out)[0]
+    assert bool((lp <= 0).all()) and bool(lp.isfinite().all())
