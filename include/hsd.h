@@ -382,7 +382,8 @@ int hsd_kv_append(const void *qkv, int qkv_dtype, int rows, long long row_stride
  *   kv_lens    device [batch] int32, of any mixture; read by the kernels only, so a captured call follows their changes.
  *              0 or less: zeros.  More than the page table has room for: its room
  *   page_table device [batch, pages_per_seq] int32; keys on a page that is not in [0, n_pages) count as absent.  Memory of
- *              the pages behind a sequence's last key is not used, whatever it holds
+ *              the pages behind a sequence's last key is not used, whatever it holds; keys and values that are there and not
+ *              finite may make their heads' outputs NaN
  *   scale      finite
  *   workspace  device, 16-byte aligned, at least hsd_paged_attention_workspace_bytes(...) (0 = bad sizes); contents on entry are
  *              ignored, on exit unspecified

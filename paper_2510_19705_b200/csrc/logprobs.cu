@@ -21,7 +21,7 @@ namespace hsd {
 namespace {
 
 constexpr int kMaxTop = 32;
-constexpr int kCand = 1024;            // candidates that fit
+template <int THREADS> constexpr int kCand = THREADS == 32 ? 256 : 1024;       // candidates that fit
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct LogprobArgs {
@@ -180,7 +180,7 @@ template <int THREADS> struct Shared {
   int flagged[THREADS], n_flagged;     // threads whose pieces may hold one of the top tokens
   float m[THREADS / 32], s[THREADS / 32], t[THREADS / 32];
   int front[THREADS / 32];
-  u64 cand[kCand];
+  u64 cand[kCand<THREADS>];
   u64 list[kMaxTop];                   // the part's top tokens in order
   u64 top[kMaxTop];                    // the row's
   float4 sums;                         // the part's m (NaN: of no distribution), s, t; tokens in front
@@ -269,7 +269,7 @@ __device__ void select_slow(const Part<T> &p, int k, float bound, float top, Sha
 // pieces, if it has no others (`all_here`).
 template <typename T, int THREADS, int U>
 __device__ void select_top(const Part<T> &p, int k, float mine, const uint4 *v, bool all_here, Shared<THREADS> &sh) {
-  constexpr int N = Vec<T>::N, LANES = THREADS / 128;                  // threads of a group: 128 groups
+  constexpr int N = Vec<T>::N, LANES = THREADS > 128 ? THREADS / 128 : 1;                // threads of a group: 128 groups at most
   const int lane = threadIdx.x & 31;
   float g = mine;
 #pragma unroll
@@ -280,7 +280,7 @@ __device__ void select_top(const Part<T> &p, int k, float mine, const uint4 *v, 
   // Every warp for itself: the largest value of 16 bits that k of the groups' maxima reach, bit by bit.
   u32 x[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) x[i] = ordered(sh.group_max[i * 32 + lane]) >> 16;
+  for (int i = 0; i < 4; ++i) x[i] = i * 32 < THREADS ? ordered(sh.group_max[i * 32 + lane]) >> 16 : 0;
   u32 reached = 0;
 #pragma unroll
   for (int bit = 15; bit >= 0; --bit) {
@@ -299,7 +299,7 @@ __device__ void select_top(const Part<T> &p, int k, float mine, const uint4 *v, 
     for (int e = 0; e < N; ++e)
       if (f[e] >= bound && p.has(i, e)) {
         const int at = atomicAdd(&sh.n_cand, 1);
-        if (at < kCand) sh.cand[at] = key_of(f[e], p.first + i * N + e);
+        if (at < kCand<THREADS>) sh.cand[at] = key_of(f[e], p.first + i * N + e);
       }
   };
   if (all_here) {
@@ -326,9 +326,9 @@ __device__ void select_top(const Part<T> &p, int k, float mine, const uint4 *v, 
     }
   }
   __syncthreads();
-  if (sh.n_cand > kCand) {
+  if (sh.n_cand > kCand<THREADS>) {
     float top = -INFINITY;
-    for (int i = 0; i < 128; ++i) top = fmaxf(top, sh.group_max[i]);
+    for (int i = 0; i < min(THREADS, 128); ++i) top = fmaxf(top, sh.group_max[i]);
     select_slow<T, THREADS>(p, k, bound, top, sh);
   }
   const int n = sh.n_cand;
@@ -346,7 +346,7 @@ __device__ void select_top(const Part<T> &p, int k, float mine, const uint4 *v, 
 // A row's CTAs (blockIdx.y, a cluster where there are several).
 // U: pieces of a thread at once.
 template <typename T, int THREADS, int U>
-__global__ void __launch_bounds__(THREADS, 1024 / THREADS)
+__global__ void __launch_bounds__(THREADS, THREADS == 32 ? 24 : 1024 / THREADS)
 logprobs_kernel(LogprobArgs a) {
   constexpr int N = Vec<T>::N;
   __shared__ __align__(16) Shared<THREADS> sh;
@@ -514,9 +514,12 @@ template <typename T, int THREADS, int U> int run_threads(const LogprobArgs &a, 
   hsd_count_launches(1);
   return hsd_launch_status();
 }
+// Many short rows take a warp each if few alternatives are asked for: 3000 x 1461 bf16 with five 10.7 us (by 128 threads 19.6), 600 rows 6.4
+// (7.8), 300 rows 6.4 (5.3), but with 20 as long and with 32 twice as long, as the maxima of 32 lanes bound those badly.
 // Rows that do not fill the GPU are divided into parts of 2048 tokens or more.  Long ones take CTAs of 512 threads with eight pieces at once:
 // 700 x 131072 fp32 85 us (of 256 threads with four 117, divided among four such 111), but 576 x 32000 bf16 30 (17).
 template <typename T> int run(const LogprobArgs &a, int rows, cudaStream_t s) {
+  if (a.V <= 2048 && a.top <= 8 && rows >= 600) return run_threads<T, 32, 4>(a, rows, 1, s);
   if (a.V <= 4096) return run_threads<T, 128, 4>(a, rows, 1, s);
   int parts = 1;
   while (parts < 8 && (long long)rows * parts * 2 <= 4 * kMeasuredSMs && a.V / (parts * 2) >= 2048) parts *= 2;

@@ -6,6 +6,8 @@
 // 9.1; this way 7.1, 4.5 and 4.4.  No arithmetic of the method is here.
 #include <Python.h>
 #include <ATen/ATen.h>
+#include <ATen/EmptyTensor.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -230,6 +232,11 @@ int count(int64_t n) {
   if (n > INT32_MAX) refuse("a size is over 2^31 - 1");
   return (int)n;
 }
+// An output on the current device.  (at::empty without its way through the dispatcher: five of them took longer on the host, 4 us, than a
+// short call's kernel.)
+at::Tensor fresh(at::IntArrayRef sizes, at::ScalarType type) {
+  return at::detail::empty_generic(sizes, c10::cuda::CUDACachingAllocator::get(), c10::DispatchKeySet(c10::DispatchKey::CUDA), type, std::nullopt);
+}
 at::ScalarType cache_type(const at::Tensor &t, const char *name) {
   if (t.scalar_type() != at::kFloat && t.scalar_type() != at::kBFloat16) {
     PyErr_Format(error_class, "%s: unsupported dtype %s", name, c10::toString(t.scalar_type()));
@@ -277,7 +284,7 @@ PyObject *kv_append(PyObject *, PyObject *const *args, Py_ssize_t n) {
     if (args[6] != Py_None) starts = static_cast<const int32_t *>(sized(typed(args[6], "row_starts", at::kInt, &qkv), "row_starts", {batch + 1}).data_ptr());
     const at::ScalarType type = pool.dtype == HSD_F32 ? at::kFloat : at::kBFloat16;
     const c10::cuda::CUDAGuard guard(qkv.device());
-    at::Tensor out = args[7] == Py_None ? at::empty({rows, nq, hd}, qkv.options().dtype(type).requires_grad(false))
+    at::Tensor out = args[7] == Py_None ? fresh({rows, nq, hd}, type)
                                         : sized(typed(args[7], "q_out", type, &qkv), "q_out", {rows, nq, hd});
     void *from = qkv.data_ptr(), *to = out.data_ptr(), *stream = current_stream();
     const int n_rows = count(rows), heads = count(nq), kv_heads = count(nkv), dim = count(hd), n_batch = count(batch), pages = count(table.size(1)), positions = count(rope.size(0));
@@ -316,10 +323,9 @@ PyObject *paged_attention(PyObject *, PyObject *const *args, Py_ssize_t n) {
       throw Failed();
     }
     const c10::cuda::CUDAGuard guard(q.device());
-    const auto options = q.options().requires_grad(false);
-    at::Tensor ws = args[6] == Py_None ? at::empty({(int64_t)need}, options.dtype(at::kByte)) : typed(args[6], "workspace", at::kByte, &q);
+    at::Tensor ws = args[6] == Py_None ? fresh({(int64_t)need}, at::kByte) : typed(args[6], "workspace", at::kByte, &q);
     if (!ws.is_contiguous()) refuse("expected a contiguous CUDA tensor");
-    at::Tensor out = args[7] == Py_None ? at::empty({batch, nq, hd}, options) : sized(typed(args[7], "out", q.scalar_type(), &q), "out", {batch, nq, hd});
+    at::Tensor out = args[7] == Py_None ? fresh({batch, nq, hd}, q.scalar_type()) : sized(typed(args[7], "out", q.scalar_type(), &q), "out", {batch, nq, hd});
     void *from = q.data_ptr(), *to = out.data_ptr(), *scratch = ws.data_ptr(), *stream = current_stream();
     check(released([&] {
       return attention_fn(from, n_batch, heads, kv_heads, dim, &pool, static_cast<const int32_t *>(table.data_ptr()), pages,
@@ -355,8 +361,8 @@ PyObject *gemm_w4(PyObject *, PyObject *const *args, Py_ssize_t n) {
       throw Failed();
     }
     const c10::cuda::CUDAGuard guard(a.device());
-    at::Tensor out = args[3] == Py_None ? at::empty({R, N}, a.options().dtype(at::kFloat).requires_grad(false)) : sized(typed(args[3], "out", at::kFloat, &a), "out", {R, N});
-    at::Tensor ws = args[4] == Py_None ? at::empty({(int64_t)need}, a.options().dtype(at::kByte).requires_grad(false)) : typed(args[4], "workspace", at::kByte, &a);
+    at::Tensor out = args[3] == Py_None ? fresh({R, N}, at::kFloat) : sized(typed(args[3], "out", at::kFloat, &a), "out", {R, N});
+    at::Tensor ws = args[4] == Py_None ? fresh({(int64_t)need}, at::kByte) : typed(args[4], "workspace", at::kByte, &a);
     if (!ws.is_contiguous()) refuse("expected a contiguous CUDA tensor");
     void *pa = a.data_ptr(), *pc = codes.data_ptr(), *ps = scales.data_ptr(), *scratch = ws.data_ptr(), *stream = current_stream();
     float *to = static_cast<float *>(out.data_ptr());
@@ -385,10 +391,9 @@ PyObject *token_logprobs(PyObject *, PyObject *const *args, Py_ssize_t n) {
     if (top < 0) refuse("top: expected 0 or more");
     const int rows = count(tokens.numel()), vocab = count(logits.size(-1)), k = count(top);
     const c10::cuda::CUDAGuard guard(logits.device());
-    const auto f = logits.options().dtype(at::kFloat).requires_grad(false), i = f.dtype(at::kInt);
     std::vector<int64_t> more(lead.begin(), lead.end());
     more.push_back(top);
-    at::Tensor out[5] = {at::empty(lead, f), at::empty(lead, f), at::empty(lead, i), at::empty(more, i), at::empty(more, f)};
+    at::Tensor out[5] = {fresh(lead, at::kFloat), fresh(lead, at::kFloat), fresh(lead, at::kInt), fresh(more, at::kInt), fresh(more, at::kFloat)};
     void *to[5], *stream = current_stream();
     for (int x = 0; x < 5; ++x) to[x] = out[x].data_ptr();
     check(released([&] {

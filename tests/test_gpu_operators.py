@@ -389,6 +389,19 @@ def test_logprobs_of_any_vocabulary(lib, dtype, V, rows):
 
 
 @pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("V", [9, 100, 257, 1461, 2048])
+def test_logprobs_of_many_short_rows(lib, dtype, V):
+    g = gen(V)
+    x = randn(g, 700, V, std=3.0, dtype=dtype)
+    x[::7] = x[::7].round()                       # ties
+    x[3::9, V // 2:] = -float("inf")
+    x[5::50] = 2.0
+    tokens = torch.randint(0, V, (700,), generator=g, device="cuda", dtype=torch.int32)
+    for top in (0, 1, 5, 8):
+        check_logprobs(lib, x, tokens, top)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
 @pytest.mark.parametrize("V", [500, 32000, 70001])
 def test_logprobs_of_ties(lib, dtype, V):
     """Rows with more equal logits than candidates fit: all equal, few values, a mask that leaves three tokens, ties at the far end."""
