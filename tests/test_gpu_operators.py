@@ -582,3 +582,55 @@ def test_a_drafter_of_ones_own(lib):
     assert n.tolist() == [steps] * B                                        # verified by itself: everything is accepted
     lp = lib.hsd_token_logprobs(torch.cat((q, logits[:, None]), dim=1).contiguous(), out)[0]
     assert bool((lp <= 0).all()) and bool(lp.isfinite().all())
+
+
+def _step(lib, s):
+    """A decoding step's four calls on the tensors of `s`, none of which the calls keep."""
+    q = lib.hsd_kv_append(s["qkv"], s["k"], s["v"], s["table"], s["lens"], s["rope"])
+    a = lib.hsd_paged_attention(q, s["k"], s["v"], s["table"], s["upto"])
+    logits = lib.hsd_gemm_w4(a.view(a.shape[0], -1), s["codes"], s["scales"])
+    return (a, logits) + lib.hsd_token_logprobs(logits, s["tokens"], 5)
+
+
+def _step_inputs(lib, seed, batch, N):
+    g = gen(seed)
+    k, v, table = cache(g, batch, 2, 64, 16, 30, BF16)
+    codes, scales = weights(g, N, 256, 64)
+    lens = torch.randint(0, 460, (batch,), generator=g, device="cuda", dtype=torch.int32)
+    return dict(qkv=randn(g, batch, 8, 64), k=k, v=v, table=table, lens=lens, upto=lens + 1, rope=lib.rope_table(480, 64), codes=codes, scales=scales,
+                tokens=torch.randint(0, N, (batch,), generator=g, device="cuda", dtype=torch.int32))
+
+
+@pytest.mark.parametrize("batch,N", [(1, 9000), (12, 2500), (40, 70000)])
+def test_captured_steps_follow_their_inputs(lib, batch, N):
+    s = _step_inputs(lib, batch, batch, N)
+    _step(lib, s)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = _step(lib, s)
+    for seed in (1, 2, 3):
+        other = _step_inputs(lib, seed, batch, N)
+        for name, t in other.items():
+            s[name].copy_(t)
+        graph.replay()
+        graph.replay()
+        want = _step(lib, other)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+        assert torch.equal(s["k"], other["k"]) and torch.equal(s["v"], other["v"])
+
+
+def test_steps_on_two_streams_at_once(lib):
+    sides = [_step_inputs(lib, 5, 9, 40000), _step_inputs(lib, 6, 33, 9000)]
+    want = [_step(lib, s) for s in sides]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in sides], [[], []]
+    for _ in range(20):
+        for i, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                got[i].append(_step(lib, sides[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for out in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(out, want[i]))
