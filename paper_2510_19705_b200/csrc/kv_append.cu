@@ -9,7 +9,7 @@
 namespace hsd {
 namespace {
 
-constexpr int kThreads = 256, kRows = 4;       // rows of a CTA at most (8191 rows of 48 heads of 128: 41 us, of 8 45, of 2 49)
+constexpr int kThreads = 256, kRows = 4;       // rows of a CTA at most (8191 rows of 48 heads of 128: 39 us, of 8 45, of 2 49)
 
 struct AppendArgs {
   const unsigned char *qkv;
@@ -51,6 +51,7 @@ template <typename TI, typename TO, int HD>
 __global__ void __launch_bounds__(kThreads)
 kv_append_kernel(AppendArgs a) {
   constexpr int UNITS = HD / 16, HALF = HD / 2;
+  static_assert(kRows == 4, "rows of a piece are found by three comparisons");
   __shared__ int sh_pos[kRows];                 // -1: the row is skipped
   __shared__ long long sh_at[kRows];            // its place in a head of the pools, in bytes
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -91,7 +92,8 @@ kv_append_kernel(AppendArgs a) {
   __syncthreads();
   const int per_row = (a.nq + 2 * a.nkv) * UNITS;
   for (int u = part * kThreads + threadIdx.x; u < n_rows * per_row; u += a.parts * kThreads) {
-    const int row = u / per_row, h = (u % per_row) / UNITS, i = (u % UNITS) * 8, pos = sh_pos[row];
+    const int row = (u >= per_row) + (u >= 2 * per_row) + (u >= 3 * per_row), x = u - row * per_row;
+    const int h = x / UNITS, i = x % UNITS * 8, pos = sh_pos[row];
     if (pos < 0) continue;
     const unsigned char *src = a.qkv + (size_t)(r0 + row) * a.row_bytes + ((size_t)h * HD + i) * sizeof(TI);
     float lo[8], hi[8];
