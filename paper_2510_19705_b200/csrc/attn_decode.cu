@@ -10,6 +10,8 @@
 // far from its limit); weights as bf16 high and low parts, so that only the final rounding is one of 8 bits.
 // fp32: both products on mma.sync in TF32, each factor as two TF32 parts (x = high + low to 2^-21) and the three products of them that
 // count: the same tile of 8 queries for any group, where products in fp32 read every query again from shared memory for each key.
+// The tensor cores' adders cut off: a chain of products loses up to 2^-23 of its sum a product (1.2e-4 of the output over 20000 keys
+// a sequence when the chain was a stretch).  So no chain is longer than a tile; tiles' products are added in fp32, rounded to nearest.
 #include <math.h>
 
 #include "paged.cuh"
@@ -293,7 +295,7 @@ template <int HD, int H> struct Bf16Tile {     // H: 8 or 16 rows with queries
   using T = __nv_bfloat16;
   static constexpr int YS = H / 8;
   u32 qf[HD / 16][4];
-  float o[HD / 8][4], m[2], l[2];
+  float o[HD / 8][2 * YS], m[2], l[2];
   int lane;
 
   // Rows of the tile: the chunk's query heads; rows without one are zeros.
@@ -311,7 +313,7 @@ template <int HD, int H> struct Bf16Tile {     // H: 8 or 16 rows with queries
 #pragma unroll
     for (int n = 0; n < HD / 8; ++n)
 #pragma unroll
-      for (int x = 0; x < 4; ++x) o[n][x] = 0.f;
+      for (int x = 0; x < 2 * YS; ++x) o[n][x] = 0.f;
     m[0] = m[1] = -INFINITY;
     l[0] = l[1] = 0.f;
   }
@@ -370,24 +372,32 @@ template <int HD, int H> struct Bf16Tile {     // H: 8 or 16 rows with queries
     }
     if (__any_sync(0xFFFFFFFFu, grown)) {
 #pragma unroll
-      for (int n = 0; n < HD / 8; ++n) {
-        o[n][0] *= f[0]; o[n][1] *= f[0];
-        o[n][2] *= f[1]; o[n][3] *= f[1];
-      }
+      for (int n = 0; n < HD / 8; ++n)
+#pragma unroll
+        for (int x = 0; x < 2 * YS; ++x) o[n][x] *= f[x >> 1];
     }
     const u32 v = at + Ring<T, HD>::HALF;
     const int vr = lane & 15, vc = lane >> 4;
 #pragma unroll
-    for (int b = 0; b < KB; ++b)
+    for (int n = 0; n < HD / 16; ++n) {
+      float d[2][4];                           // of this tile alone
 #pragma unroll
-      for (int n = 0; n < HD / 16; ++n) {
+      for (int x = 0; x < 4; ++x) d[0][x] = d[1][x] = 0.f;
+#pragma unroll
+      for (int b = 0; b < KB; ++b) {
         u32 x[4];
         ldsm4t(x, v + piece<T, HD>(b * 16 + vr, 2 * n + vc));
-        mma(o[2 * n], hi[b], x[0], x[1]);
-        mma(o[2 * n + 1], hi[b], x[2], x[3]);
-        mma(o[2 * n], lo[b], x[0], x[1]);
-        mma(o[2 * n + 1], lo[b], x[2], x[3]);
+        mma(d[0], hi[b], x[0], x[1]);
+        mma(d[1], hi[b], x[2], x[3]);
+        mma(d[0], lo[b], x[0], x[1]);
+        mma(d[1], lo[b], x[2], x[3]);
       }
+#pragma unroll
+      for (int x = 0; x < 2 * YS; ++x) {
+        o[2 * n][x] += d[0][x];
+        o[2 * n + 1][x] += d[1][x];
+      }
+    }
   }
   __device__ __forceinline__ void end(const DecodeArgs &a, int b, int item, bool whole, float *part) {
     const int h = item / a.chunks, c = item % a.chunks, heads = min(a.chunk, a.group - c * a.chunk), col = (lane & 3) * 2;
@@ -418,7 +428,7 @@ template <int HD, int H> struct Bf16Tile {     // H: 8 or 16 rows with queries
 template <int HD> struct Fp32Tile {
   using T = float;
   u32 qh[HD / 8][2], ql[HD / 8][2];            // rows 8 to 15 of the tile are zeros
-  float o[HD / 8][4], m, l;
+  float o[HD / 8][2], m, l;
   int lane;
 
   __device__ __forceinline__ void begin(const DecodeArgs &a, int b, int item) {
@@ -435,7 +445,7 @@ template <int HD> struct Fp32Tile {
 #pragma unroll
     for (int n = 0; n < HD / 8; ++n)
 #pragma unroll
-      for (int x = 0; x < 4; ++x) o[n][x] = 0.f;
+      for (int x = 0; x < 2; ++x) o[n][x] = 0.f;
     m = -INFINITY;
     l = 0.f;
   }
@@ -479,16 +489,25 @@ template <int HD> struct Fp32Tile {
 #pragma unroll
       for (int i = 0; i < HD / 8; ++i) { o[i][0] *= f; o[i][1] *= f; }
     }
-    const u32 v = at + Ring<T, HD>::HALF;
+    u32 hi[KB][4], lo[KB][4];                  // k = j: key 2 j; k = j + 4: key 2 j + 1
 #pragma unroll
     for (int b = 0; b < KB; ++b) {
       const float p0 = ex2(p[b][0] - ref), p1 = ex2(p[b][1] - ref);
       l += p0 + p1;
-      u32 hi[4] = {0, 0, 0, 0}, lo[4] = {0, 0, 0, 0};                  // k = j: key 2 j; k = j + 4: key 2 j + 1
-      split(p0, hi[0], lo[0]);
-      split(p1, hi[2], lo[2]);
+      hi[b][1] = hi[b][3] = lo[b][1] = lo[b][3] = 0;
+      split(p0, hi[b][0], lo[b][0]);
+      split(p1, hi[b][2], lo[b][2]);
+    }
+    const u32 v = at + Ring<T, HD>::HALF;
 #pragma unroll
-      for (int i = 0; i < HD / 32; ++i) {
+    for (int i = 0; i < HD / 32; ++i) {
+      float d[4][4];                           // of this tile alone
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) d[c][x] = 0.f;
+#pragma unroll
+      for (int b = 0; b < KB; ++b) {
         const float4 v0 = lds4(v + piece<T, HD>(b * 8 + 2 * j, i * 8 + r)), v1 = lds4(v + piece<T, HD>(b * 8 + 2 * j + 1, i * 8 + r));
         const float x[4] = {v0.x, v0.y, v0.z, v0.w}, y[4] = {v1.x, v1.y, v1.z, v1.w};
         u32 h0[4], l0[4], h1[4], l1[4];
@@ -498,12 +517,16 @@ template <int HD> struct Fp32Tile {
           split(y[c], h1[c], l1[c]);
         }
 #pragma unroll
-        for (int c = 0; c < 4; ++c) mma_tf32(o[4 * i + c], hi, h0[c], h1[c]);
+        for (int c = 0; c < 4; ++c) mma_tf32(d[c], hi[b], h0[c], h1[c]);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) mma_tf32(o[4 * i + c], hi, l0[c], l1[c]);
+        for (int c = 0; c < 4; ++c) mma_tf32(d[c], hi[b], l0[c], l1[c]);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) mma_tf32(o[4 * i + c], lo, h0[c], h1[c]);
+        for (int c = 0; c < 4; ++c) mma_tf32(d[c], lo[b], h0[c], h1[c]);
       }
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) o[4 * i + c][x] += d[c][x];
     }
   }
   __device__ __forceinline__ void end(const DecodeArgs &a, int b, int item, bool whole, float *part) {

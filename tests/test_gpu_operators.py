@@ -201,6 +201,62 @@ def test_attention_follows_lengths_when_replayed_and_on_other_streams(lib):
     assert torch.equal(got, want)
 
 
+def shared_pages(g, batch, nkv, n, hd, dtype, values):
+    """Pools of one text of n keys, and a table by which every sequence has it."""
+    pages = -(-n // 16)
+    k = randn(g, nkv, pages, 16, hd, dtype=dtype)
+    return k, values(nkv, pages, 16, hd).to(dtype), torch.arange(pages, dtype=torch.int32, device="cuda").repeat(batch, 1).contiguous()
+
+
+def shared_attention64(q, k, v, n):
+    out = torch.empty(q.shape, dtype=torch.float64, device="cuda")
+    group = q.shape[1] // k.shape[0]
+    for h in range(k.shape[0]):
+        kh, vh = (x[h].reshape(-1, q.shape[2])[:n].double() for x in (k, v))
+        of = slice(h * group, (h + 1) * group)
+        out[:, of] = torch.softmax(q[:, of].double() @ kh.T * q.shape[2] ** -0.5, dim=-1) @ vh
+    return out
+
+
+def nearest_additions(n):
+    """What n additions in turn, each rounded to nearest, are off relative to their sum of positive terms: roundings of a spread of 2^-24 / sqrt(3)
+    at most, independent of one another; eight deviations."""
+    return 8 / 3 ** 0.5 * n ** 0.5 * 2.0 ** -24
+
+
+# a tile's own products and their sum, what warps and CTAs add, the quotient
+TILE_AND_JOIN = 8 * 2.0 ** -23 + 24 * 2.0 ** -24
+
+
+@pytest.mark.parametrize("hd,nq,nkv,batch,n,keys", [(32, 8, 8, 64, 40000, 16), (64, 8, 8, 64, 20000, 16), (128, 8, 8, 48, 20000, 8), (64, 8, 1, 500, 20000, 16)])
+def test_fp32_attention_adds_long_stretches_in_fp32(lib, hd, nq, nkv, batch, n, keys):
+    """Hundreds of tiles a warp, all weights 1 (so their sum is exact), values about 1: errors that all have one sign would show."""
+    g = gen(hd)
+    k, v, table = shared_pages(g, batch, nkv, n, hd, FP32, lambda *s: 1 + 0.2 * randn(g, *s))
+    q = torch.zeros(batch, nq, hd, device="cuda")
+    got = lib.hsd_paged_attention(q, k, v, table, ints([n] * batch)).double()
+    want = shared_attention64(q, k, v, n)
+    tiles = batch * nkv * n / keys / 1184 + 1
+    assert tiles > 300
+    off = float(((got - want).abs() / want).max())
+    assert off <= TILE_AND_JOIN + nearest_additions(tiles), off
+
+
+@pytest.mark.parametrize("hd,nq,keys", [(128, 8, 16), (64, 8, 32), (128, 72, 16)])
+def test_bf16_attention_adds_long_stretches_in_fp32(lib, hd, nq, keys):
+    """Means of 1 and its neighbour lie about their middle, where a small loss rounds down what should be rounded up."""
+    g, nkv, batch, n = gen(hd + nq), 8, 64, 40000
+    k, v, table = shared_pages(g, batch, nkv, n, hd, BF16, lambda *s: 1 + 2.0 ** -7 * torch.randint(0, 2, s, generator=g, device="cuda"))
+    q = randn(g, batch, nq, hd, dtype=BF16, std=0.3)
+    got = lib.hsd_paged_attention(q, k, v, table, ints([n] * batch)).double()
+    want = shared_attention64(q, k, v, n)
+    # a weight's error counts by the values' difference, 2^-7, alone; its sum: two additions for every 16 keys, in each of four lanes
+    tiles = batch * nkv * n / keys / 1184 + 1
+    bound = TILE_AND_JOIN + nearest_additions(tiles) + nearest_additions(tiles * keys / 8) / 2 + 2.0 ** -7 * 2.0 ** -18
+    assert int((want > 1 + 2.0 ** -8 + 2 * bound).sum()) > 100
+    assert bool(((got - want).abs() <= 2.0 ** -8 + bound * want).all()), float(((got - want).abs() - 2.0 ** -8).max())
+
+
 # ------------------------------------------------------------------------------------------------ append
 def append64(qkv, table, before, rope, starts, nkv, pool_shape):
     """Rows' rotated queries and, by (row): (page, token, keys, values), in 64 bits; rows that are skipped are missing."""
