@@ -377,7 +377,7 @@ int hsd_kv_append(const void *qkv, int qkv_dtype, int rows, long long row_stride
 
 /* Attention of one new token per sequence: out[b, h] = sum_j softmax_j(scale q[b, h] . k_j) v_j over the keys at positions
  * j < kv_lens[b] of head h * n_kv_heads / n_q_heads (the new token's own key is among them once it has been appended: pass
- * the lengths after the append).  Softmax and both sums in fp32, rounded once.
+ * the lengths after the append).  Softmax and both sums in fp32, rounded once; fp32 factors count as multiples of 2^-136.
  *   q, out     device [batch, n_q_heads, head_dim] in the pool's type, 16-byte aligned; n_q_heads a multiple of n_kv_heads
  *   kv_lens    device [batch] int32, of any mixture; read by the kernels only, so a captured call follows their changes.
  *              0 or less: zeros.  More than the page table has room for: its room

@@ -8,8 +8,11 @@
 // attn_join_kernel adds those in order.
 // bf16: both products on mma.sync with the group's queries as the 16 rows of a tile (at 4 to 16 queries a key the tensor pipe is
 // far from its limit); weights as bf16 high and low parts, so that only the final rounding is one of 8 bits.
-// fp32: both products on mma.sync in TF32, each factor as two TF32 parts (x = high + low to 2^-21) and the three products of them that
-// count: the same tile of 8 queries for any group, where products in fp32 read every query again from shared memory for each key.
+// fp32: both products on mma.sync in TF32: keys and values as three TF32 parts, which are all of their bits, queries and weights as two, which are
+// theirs but for a last place, one above the other in the rows of a tile, so that three products take all pairs that count: the same tile
+// of 8 queries for any group, where products in fp32 read every query again from shared memory for each key.  (Keys and values as two
+// parts and no product of the low ones were 20 % less exact than fp32, and no faster: 16 x 8200 keys, 32 heads over 8 of 128, 239 us against
+// 234.)  What lies below TF32's smallest number, 2^-136, is lost.
 // The tensor cores' adders cut off: a chain of products loses up to 2^-23 of its sum a product (1.2e-4 of the output over 20000 keys
 // a sequence when the chain was a stretch).  So no chain is longer than a tile; tiles' products are added in fp32, rounded to nearest.
 #include <math.h>
@@ -63,11 +66,19 @@ __device__ __forceinline__ void mma_tf32(float *c, const u32 *a, u32 b0, u32 b1)
   asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// x = high + low to 2^-21: high cut off, what is left rounded, to the 11 bits of TF32 (four operations; the conversion has a quarter of
-// their rate).
-__device__ __forceinline__ void split(float x, u32 &high, u32 &low) {
-  high = __float_as_uint(x) & 0xFFFFE000u;
-  low = (__float_as_uint(x - __uint_as_float(high)) + 0x1000u) & 0xFFFFE000u;
+// x = part[0] + part[1] + part[2], all of it: the first 11 bits, the next 11, the last two (four operations; NaN stays NaN, as do infinities).
+__device__ __forceinline__ void split3(float x, u32 *part) {
+  part[0] = __float_as_uint(x) & 0xFFFFE000u;
+  const float rest = x - __uint_as_float(part[0]);
+  part[1] = __float_as_uint(rest) & 0xFFFFE000u;
+  part[2] = __float_as_uint(rest - __uint_as_float(part[1]));
+}
+// x = high + mid to a last place: rounded to 11 bits, what is left rounded to 11 bits.  (For few numbers: the conversion has a quarter of the
+// rate.)  What rounding would make infinite is cut off.
+__device__ __forceinline__ void split2(float x, u32 &high, u32 &mid) {
+  asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(high) : "f"(x));
+  if (fabsf(x) > 3.4e38f) high = __float_as_uint(x) & 0xFFFFE000u;
+  asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(mid) : "f"(x - __uint_as_float(high)));
 }
 __device__ __forceinline__ float4 lds4(u32 at) {
   float4 v;
@@ -427,25 +438,23 @@ template <int HD, int H> struct Bf16Tile {     // H: 8 or 16 rows with queries
 // of k will do that both factors have, and of columns that the output is written in.
 template <int HD> struct Fp32Tile {
   using T = float;
-  u32 qh[HD / 8][2], ql[HD / 8][2];            // rows 8 to 15 of the tile are zeros
+  u32 q[HD / 8][4];                            // rows 0 to 7 of the tile: the queries' high parts, rows 8 to 15: the rest
   float o[HD / 8][2], m, l;
   int lane;
 
   __device__ __forceinline__ void begin(const DecodeArgs &a, int b, int item) {
     const int h = item / a.chunks, c = item % a.chunks, heads = min(a.chunk, a.group - c * a.chunk), r = lane >> 2, j = lane & 3;
-    const float *q = static_cast<const float *>(a.q) + ((size_t)b * a.nq + (size_t)h * a.group + c * a.chunk + r) * HD;
+    const float *from = static_cast<const float *>(a.q) + ((size_t)b * a.nq + (size_t)h * a.group + c * a.chunk + r) * HD;
 #pragma unroll
     for (int i = 0; i < HD / 16; ++i) {
-      const float4 x = r < heads ? __ldg(reinterpret_cast<const float4 *>(q + i * 16 + j * 4)) : make_float4(0.f, 0.f, 0.f, 0.f);
-      split(x.x, qh[2 * i][0], ql[2 * i][0]);
-      split(x.y, qh[2 * i][1], ql[2 * i][1]);
-      split(x.z, qh[2 * i + 1][0], ql[2 * i + 1][0]);
-      split(x.w, qh[2 * i + 1][1], ql[2 * i + 1][1]);
+      const float4 x = r < heads ? __ldg(reinterpret_cast<const float4 *>(from + i * 16 + j * 4)) : make_float4(0.f, 0.f, 0.f, 0.f);
+      split2(x.x, q[2 * i][0], q[2 * i][1]);
+      split2(x.y, q[2 * i][2], q[2 * i][3]);
+      split2(x.z, q[2 * i + 1][0], q[2 * i + 1][1]);
+      split2(x.w, q[2 * i + 1][2], q[2 * i + 1][3]);
     }
 #pragma unroll
-    for (int n = 0; n < HD / 8; ++n)
-#pragma unroll
-      for (int x = 0; x < 2; ++x) o[n][x] = 0.f;
+    for (int n = 0; n < HD / 8; ++n) o[n][0] = o[n][1] = 0.f;
     m = -INFINITY;
     l = 0.f;
   }
@@ -455,27 +464,30 @@ template <int HD> struct Fp32Tile {
     float p[KB][2], mx = -INFINITY;
 #pragma unroll
     for (int b = 0; b < KB; ++b) {
-      float s[2][4], t[2][4], u[2][4];         // high x high, high x low, low x high
+      float s[3][2][4];                        // of each part of the keys; two chains of each
 #pragma unroll
-      for (int x = 0; x < 4; ++x) s[0][x] = s[1][x] = t[0][x] = t[1][x] = u[0][x] = u[1][x] = 0.f;
+      for (int e = 0; e < 3; ++e)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) s[e][0][x] = s[e][1][x] = 0.f;
 #pragma unroll
       for (int i = 0; i < HD / 16; ++i) {
         const float4 k = lds4(at + piece<T, HD>(b * 8 + r, i * 4 + j));
         const float x[4] = {k.x, k.y, k.z, k.w};
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
-          u32 h0, l0, h1, l1;
-          split(x[2 * y], h0, l0);
-          split(x[2 * y + 1], h1, l1);
-          const u32 hi[4] = {qh[2 * i + y][0], 0, qh[2 * i + y][1], 0}, lo[4] = {ql[2 * i + y][0], 0, ql[2 * i + y][1], 0};
-          mma_tf32(s[y], hi, h0, h1);
-          mma_tf32(t[y], hi, l0, l1);
-          mma_tf32(u[y], lo, h0, h1);
+          u32 k0[3], k1[3];
+          split3(x[2 * y], k0);
+          split3(x[2 * y + 1], k1);
+#pragma unroll
+          for (int e = 0; e < 3; ++e) mma_tf32(s[e][y], q[2 * i + y], k0[e], k1[e]);
         }
       }
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        p[b][x] = (there >> (b * 8 + 2 * j + x)) & 1 ? (((t[0][x] + t[1][x]) + (u[0][x] + u[1][x])) + (s[0][x] + s[1][x])) * a.scale : -INFINITY;
+        float sum = 0.f;                       // the small ones first
+#pragma unroll
+        for (int e = 2; e >= 0; --e) sum += (s[e][0][2 + x] + s[e][1][2 + x]) + (s[e][0][x] + s[e][1][x]);
+        p[b][x] = (there >> (b * 8 + 2 * j + x)) & 1 ? sum * a.scale : -INFINITY;
         mx = fmaxf(mx, p[b][x]);
       }
     }
@@ -489,14 +501,13 @@ template <int HD> struct Fp32Tile {
 #pragma unroll
       for (int i = 0; i < HD / 8; ++i) { o[i][0] *= f; o[i][1] *= f; }
     }
-    u32 hi[KB][4], lo[KB][4];                  // k = j: key 2 j; k = j + 4: key 2 j + 1
+    u32 w[KB][4];                              // k = j: key 2 j; k = j + 4: key 2 j + 1
 #pragma unroll
     for (int b = 0; b < KB; ++b) {
       const float p0 = ex2(p[b][0] - ref), p1 = ex2(p[b][1] - ref);
       l += p0 + p1;
-      hi[b][1] = hi[b][3] = lo[b][1] = lo[b][3] = 0;
-      split(p0, hi[b][0], lo[b][0]);
-      split(p1, hi[b][2], lo[b][2]);
+      split2(p0, w[b][0], w[b][1]);
+      split2(p1, w[b][2], w[b][3]);
     }
     const u32 v = at + Ring<T, HD>::HALF;
 #pragma unroll
@@ -510,23 +521,21 @@ template <int HD> struct Fp32Tile {
       for (int b = 0; b < KB; ++b) {
         const float4 v0 = lds4(v + piece<T, HD>(b * 8 + 2 * j, i * 8 + r)), v1 = lds4(v + piece<T, HD>(b * 8 + 2 * j + 1, i * 8 + r));
         const float x[4] = {v0.x, v0.y, v0.z, v0.w}, y[4] = {v1.x, v1.y, v1.z, v1.w};
-        u32 h0[4], l0[4], h1[4], l1[4];
+        u32 x3[4][3], y3[4][3];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          split(x[c], h0[c], l0[c]);
-          split(y[c], h1[c], l1[c]);
+          split3(x[c], x3[c]);
+          split3(y[c], y3[c]);
         }
 #pragma unroll
-        for (int c = 0; c < 4; ++c) mma_tf32(d[c], hi[b], h0[c], h1[c]);
+        for (int e = 2; e >= 0; --e)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) mma_tf32(d[c], hi[b], l0[c], l1[c]);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) mma_tf32(d[c], lo[b], h0[c], h1[c]);
+          for (int c = 0; c < 4; ++c) mma_tf32(d[c], w[b], x3[c][e], y3[c][e]);
       }
 #pragma unroll
       for (int c = 0; c < 4; ++c)
 #pragma unroll
-        for (int x = 0; x < 2; ++x) o[4 * i + c][x] += d[c][x];
+        for (int x = 0; x < 2; ++x) o[4 * i + c][x] += d[c][x] + d[c][2 + x];
     }
   }
   __device__ __forceinline__ void end(const DecodeArgs &a, int b, int item, bool whole, float *part) {

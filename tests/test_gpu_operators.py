@@ -257,6 +257,32 @@ def test_bf16_attention_adds_long_stretches_in_fp32(lib, hd, nq, keys):
     assert bool(((got - want).abs() <= 2.0 ** -8 + bound * want).all()), float(((got - want).abs() - 2.0 ** -8).max())
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("hd", [32, 64, 128])
+def test_attention_of_one_key_is_its_value(lib, dtype, hd):
+    g = gen(hd + 1)
+    k, v, table = cache(g, 40, 2, hd, 16, 1, dtype)
+    v[0, table[3, 0], 0, 5], v[1, table[4, 0], 0, 6] = torch.finfo(dtype).max, torch.finfo(dtype).min
+    got = lib.hsd_paged_attention(randn(g, 40, 6, hd, dtype=dtype, std=2.0), k, v, table, ints([1] * 40))
+    want = v[:, table[:, 0].long(), 0].transpose(0, 1)                       # [batch, nkv, hd]
+    assert torch.equal(got.view(40, 2, 3, hd), want[:, :, None].expand(40, 2, 3, hd))
+
+
+def test_fp32_attention_takes_the_largest_queries(lib):
+    """A query whose high part would be rounded to infinity, with keys small enough for finite scores."""
+    g = gen(21)
+    k, v, table = cache(g, 1, 1, 64, 16, 1, FP32)
+    k *= 1e-38
+    q = torch.zeros(1, 2, 64, device="cuda")
+    q[0, 0, 7], q[0, 1, 9] = torch.finfo(FP32).max, torch.finfo(FP32).min
+    got = lib.hsd_paged_attention(q, k, v, table, ints([12]))
+    want, size, most = attention64(q, k, v, table.cpu(), [12], 0.125)
+    # as in check_attention(); and factors are multiples of 2^-136, what TF32 holds below 2^-126: a key's two lower parts lose less than that
+    # each, which counts 2^128 times 0.125 in a score
+    weight = (64 + 4) * 2.0 ** -23 * most + 2.0 ** -21 + 66 * 2.0 ** -24 + 0.125 * 2.0 ** 128 * 2 * 2.0 ** -136
+    assert bool(((got.double().cpu() - want).abs() <= 2.0 ** -24 * want.abs() + 2 * weight * size).all())
+
+
 # ------------------------------------------------------------------------------------------------ append
 def append64(qkv, table, before, rope, starts, nkv, pool_shape):
     """Rows' rotated queries and, by (row): (page, token, keys, values), in 64 bits; rows that are skipped are missing."""
