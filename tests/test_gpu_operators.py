@@ -283,6 +283,39 @@ def test_fp32_attention_takes_the_largest_queries(lib):
     assert bool(((got.double().cpu() - want).abs() <= 2.0 ** -24 * want.abs() + 2 * weight * size).all())
 
 
+@pytest.mark.parametrize("nq", [8, 16])
+def test_bf16_attention_weights_have_24_bits(lib, nq):
+    """Sixteen keys, one of score 0, the others of one score whose weight the first 16 bits miss by 2e-6 and more.  Scores are exact (one product
+    each).  A weight is off by 2^-22 (its exponential) and 2^-23 (the exponent, below 1), which counts by its share of the values' differences, a
+    quarter at most; the tile's products 4 * 2^-23, the weights' sum and the quotient six roundings."""
+    def missed(w):
+        w = w.to(FP32)
+        high = w.to(BF16).to(FP32)
+        return ((w - high - (w - high).to(BF16).to(FP32)) / w).double()
+
+    scores = -torch.arange(1, 180, device="cuda", dtype=torch.float64) / 256
+    w = scores.exp()
+    lo, hi = missed(w * (1 - 4e-7)), missed(w * (1 + 4e-7))
+    safe = torch.where(lo.sign() == hi.sign(), torch.minimum(lo.abs(), hi.abs()), torch.zeros_like(lo))
+    best = int(safe.argmax())
+    assert float(safe[best]) > 2e-6
+    g, batch, hd = gen(nq), 256, 128
+    k, v, table = cache(g, batch, 1, hd, 16, 1, BF16)
+    v.copy_(1 + torch.rand(v.shape, generator=g, device="cuda"))
+    k.zero_()
+    k[:, :, 1:, 0] = scores[best].to(BF16)
+    assert float(k[0, 0, 1, 0]) == float(scores[best])
+    q = torch.zeros(batch, nq, hd, dtype=BF16, device="cuda")
+    q[:, :, 0] = 1
+    got = lib.hsd_paged_attention(q, k, v, table, ints([16] * batch), 1.0).double()
+    share = torch.cat((torch.ones(1, dtype=torch.float64, device="cuda"), w[best].expand(15)))
+    share /= share.sum()
+    want = (v[0, table[:, 0].long()].double() * share[:, None]).sum(dim=1)[:, None].expand(batch, nq, hd)
+    off = (got - want).abs()
+    bound = 2.0 ** -8 + (2.0 ** -22 + 2.0 ** -23) / 4 + (4 * 2.0 ** -23 + 6 * 2.0 ** -24) * want          # want lies in [1, 2]
+    assert bool((off <= bound).all()), (float((off - 2.0 ** -8).max()), int((off > bound).sum()))
+
+
 # ------------------------------------------------------------------------------------------------ append
 def append64(qkv, table, before, rope, starts, nkv, pool_shape):
     """Rows' rotated queries and, by (row): (page, token, keys, values), in 64 bits; rows that are skipped are missing."""
