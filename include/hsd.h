@@ -374,6 +374,10 @@ typedef struct {
 int hsd_kv_append(const void *qkv, int qkv_dtype, int rows, long long row_stride, int n_q_heads, int n_kv_heads, int head_dim,
                   const int32_t *row_starts, const int32_t *kv_lens, int batch, const int32_t *page_table, int pages_per_seq,
                   const float *rope, int n_positions, const hsd_kv_pool *pool, void *q_out, void *stream);
+/* hsd_kv_append, but for the skipped rows' queries: zeros are written to q_out for them. */
+int hsd_kv_append_zeros(const void *qkv, int qkv_dtype, int rows, long long row_stride, int n_q_heads, int n_kv_heads, int head_dim,
+                        const int32_t *row_starts, const int32_t *kv_lens, int batch, const int32_t *page_table, int pages_per_seq,
+                        const float *rope, int n_positions, const hsd_kv_pool *pool, void *q_out, void *stream);
 
 /* Attention of one new token per sequence: out[b, h] = sum_j softmax_j(scale q[b, h] . k_j) v_j over the keys at positions
  * j < kv_lens[b] of head h * n_kv_heads / n_q_heads (the new token's own key is among them once it has been appended: pass

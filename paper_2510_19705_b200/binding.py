@@ -52,7 +52,8 @@ def _host_calls():
         mod.init(*(ctypes.cast(f, ctypes.c_void_p).value for f in
                    (lib.hsd_draft_sample, lib.hsd_verify_workspace_bytes, lib.hsd_verify_level, lib.hsd_gemm_workspace_bytes,
                     lib.hsd_gemm_bf16, lib.hsd_gemm_status, lib.hsd_strerror, lib.hsd_kv_append, lib.hsd_paged_attention_workspace_bytes,
-                    lib.hsd_paged_attention, lib.hsd_gemm_w4_workspace_bytes, lib.hsd_gemm_w4, lib.hsd_token_logprobs)), HsdError)
+                    lib.hsd_paged_attention, lib.hsd_gemm_w4_workspace_bytes, lib.hsd_gemm_w4, lib.hsd_token_logprobs,
+                    lib.hsd_kv_append_zeros)), HsdError)
         _host = mod
     return _host
 
@@ -212,8 +213,9 @@ def _declare_engine(lib):
     lib.hsd_gemm_bf16.argtypes = [vp, i32, i32, vp, i32, vp, vp, sz, vp]
     lib.hsd_gemm_status.restype = i32
     lib.hsd_gemm_status.argtypes = [vp, vp]
-    lib.hsd_kv_append.restype = i32
-    lib.hsd_kv_append.argtypes = [vp, i32, i32, c.c_longlong, i32, i32, i32, vp, vp, i32, vp, i32, vp, i32, c.POINTER(_KvPool), vp, vp]
+    for f in (lib.hsd_kv_append, lib.hsd_kv_append_zeros):
+        f.restype = i32
+        f.argtypes = [vp, i32, i32, c.c_longlong, i32, i32, i32, vp, vp, i32, vp, i32, vp, i32, c.POINTER(_KvPool), vp, vp]
     lib.hsd_paged_attention_workspace_bytes.restype = sz
     lib.hsd_paged_attention_workspace_bytes.argtypes = [i32, i32, i32]
     lib.hsd_paged_attention.restype = i32
@@ -516,7 +518,7 @@ def hsd_kv_append(qkv, k_pool, v_pool, page_table, kv_lens, rope, row_starts=Non
     (fp32/bf16, any order in memory with head_dim innermost), queries and keys rotated by their positions -> queries
     [rows, n_q, head_dim] in the pools' type.  page_table int32 [batch, pages], kv_lens int32 [batch] (lengths before the call), rope from
     rope_table(), row_starts int32 [batch + 1] or None (row b is sequence b's one token).  Rows that have no place are skipped
-    and their queries are not written (include/hsd.h)."""
+    (include/hsd.h): their queries are zeros, or what q_out held if it is given."""
     return (_host or _host_calls()).kv_append(qkv, k_pool, v_pool, page_table, kv_lens, rope, row_starts, q_out)
 
 

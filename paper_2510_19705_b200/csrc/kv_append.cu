@@ -20,6 +20,7 @@ struct AppendArgs {
   PoolView pool;
   int rows, batch, pages_per_seq, n_positions, nq, nkv;
   int cta_rows, parts;                          // rows of a CTA, CTAs that share them
+  bool zeros;                                   // the queries of skipped rows become zeros
 };
 
 template <typename T> __device__ __forceinline__ void load8(const unsigned char *p, float *f);
@@ -94,7 +95,15 @@ kv_append_kernel(AppendArgs a) {
   for (int u = part * kThreads + threadIdx.x; u < n_rows * per_row; u += a.parts * kThreads) {
     const int row = (u >= per_row) + (u >= 2 * per_row) + (u >= 3 * per_row), x = u - row * per_row;
     const int h = x / UNITS, i = x % UNITS * 8, pos = sh_pos[row];
-    if (pos < 0) continue;
+    if (pos < 0) {
+      if (a.zeros && h < a.nq) {
+        const float zero[8] = {};
+        unsigned char *to = a.q_out + (((size_t)(r0 + row) * a.nq + h) * HD + i) * sizeof(TO);
+        store8<TO>(to, zero);
+        store8<TO>(to + HALF * sizeof(TO), zero);
+      }
+      continue;
+    }
     const unsigned char *src = a.qkv + (size_t)(r0 + row) * a.row_bytes + ((size_t)h * HD + i) * sizeof(TI);
     float lo[8], hi[8];
     load8<TI>(src, lo);
@@ -136,13 +145,9 @@ template <typename TI, typename TO> int run(AppendArgs &a, int hd, cudaStream_t 
   return hsd_launch_status();
 }
 
-}  // namespace
-}  // namespace hsd
-
-extern "C" int hsd_kv_append(const void *qkv, int qkv_dtype, int rows, long long row_stride, int n_q_heads, int n_kv_heads, int head_dim,
-                             const int32_t *row_starts, const int32_t *kv_lens, int batch, const int32_t *page_table, int pages_per_seq,
-                             const float *rope, int n_positions, const hsd_kv_pool *pool, void *q_out, void *stream) {
-  using namespace hsd;
+int append(const void *qkv, int qkv_dtype, int rows, long long row_stride, int n_q_heads, int n_kv_heads, int head_dim, const int32_t *row_starts,
+           const int32_t *kv_lens, int batch, const int32_t *page_table, int pages_per_seq, const float *rope, int n_positions,
+           const hsd_kv_pool *pool, void *q_out, bool zeros, cudaStream_t s) {
   if (!qkv || !kv_lens || !page_table || !rope || rows <= 0 || batch <= 0 || n_q_heads < 0 || n_positions <= 0) return HSD_E_INVALID_ARG;
   if ((n_q_heads > 0 && !q_out) || (qkv_dtype != HSD_F32 && qkv_dtype != HSD_BF16) || (!row_starts && rows != batch)) return HSD_E_INVALID_ARG;
   AppendArgs a = {};
@@ -157,7 +162,24 @@ extern "C" int hsd_kv_append(const void *qkv, int qkv_dtype, int rows, long long
   a.row_starts = row_starts; a.kv_lens = kv_lens; a.page_table = page_table; a.rope = rope;
   a.q_out = static_cast<unsigned char *>(q_out);
   a.rows = rows; a.batch = batch; a.pages_per_seq = pages_per_seq; a.n_positions = n_positions; a.nq = n_q_heads; a.nkv = n_kv_heads;
-  cudaStream_t s = (cudaStream_t)stream;
+  a.zeros = zeros;
   if (qkv_dtype == HSD_F32) return pool->dtype == HSD_F32 ? run<float, float>(a, head_dim, s) : run<float, __nv_bfloat16>(a, head_dim, s);
   return pool->dtype == HSD_F32 ? run<__nv_bfloat16, float>(a, head_dim, s) : run<__nv_bfloat16, __nv_bfloat16>(a, head_dim, s);
+}
+
+}  // namespace
+}  // namespace hsd
+
+extern "C" int hsd_kv_append(const void *qkv, int qkv_dtype, int rows, long long row_stride, int n_q_heads, int n_kv_heads, int head_dim,
+                             const int32_t *row_starts, const int32_t *kv_lens, int batch, const int32_t *page_table, int pages_per_seq,
+                             const float *rope, int n_positions, const hsd_kv_pool *pool, void *q_out, void *stream) {
+  return hsd::append(qkv, qkv_dtype, rows, row_stride, n_q_heads, n_kv_heads, head_dim, row_starts, kv_lens, batch, page_table, pages_per_seq, rope,
+                     n_positions, pool, q_out, false, (cudaStream_t)stream);
+}
+
+extern "C" int hsd_kv_append_zeros(const void *qkv, int qkv_dtype, int rows, long long row_stride, int n_q_heads, int n_kv_heads, int head_dim,
+                                   const int32_t *row_starts, const int32_t *kv_lens, int batch, const int32_t *page_table, int pages_per_seq,
+                                   const float *rope, int n_positions, const hsd_kv_pool *pool, void *q_out, void *stream) {
+  return hsd::append(qkv, qkv_dtype, rows, row_stride, n_q_heads, n_kv_heads, head_dim, row_starts, kv_lens, batch, page_table, pages_per_seq, rope,
+                     n_positions, pool, q_out, true, (cudaStream_t)stream);
 }

@@ -28,7 +28,7 @@ decltype(&hsd_gemm_workspace_bytes) gemm_bytes_fn = nullptr;
 decltype(&hsd_gemm_bf16) gemm_fn = nullptr;
 decltype(&hsd_gemm_status) gemm_status_fn = nullptr;
 decltype(&hsd_strerror) strerror_fn = nullptr;
-decltype(&hsd_kv_append) kv_append_fn = nullptr;
+decltype(&hsd_kv_append) kv_append_fn = nullptr, kv_append_zeros_fn = nullptr;
 decltype(&hsd_paged_attention_workspace_bytes) attention_bytes_fn = nullptr;
 decltype(&hsd_paged_attention) attention_fn = nullptr;
 decltype(&hsd_gemm_w4_workspace_bytes) gemm_w4_bytes_fn = nullptr;
@@ -93,7 +93,7 @@ void *current_stream() { return c10::cuda::getCurrentCUDAStream().stream(); }
 PyObject *init(PyObject *, PyObject *const *args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   try {
-    arguments(n, 14);
+    arguments(n, 15);
     draft_sample_fn = reinterpret_cast<decltype(draft_sample_fn)>(word(args[0]));
     verify_bytes_fn = reinterpret_cast<decltype(verify_bytes_fn)>(word(args[1]));
     verify_level_fn = reinterpret_cast<decltype(verify_level_fn)>(word(args[2]));
@@ -107,8 +107,9 @@ PyObject *init(PyObject *, PyObject *const *args, Py_ssize_t n) {
     gemm_w4_bytes_fn = reinterpret_cast<decltype(gemm_w4_bytes_fn)>(word(args[10]));
     gemm_w4_fn = reinterpret_cast<decltype(gemm_w4_fn)>(word(args[11]));
     logprobs_fn = reinterpret_cast<decltype(logprobs_fn)>(word(args[12]));
-    Py_INCREF(args[13]);
-    error_class = args[13];
+    kv_append_zeros_fn = reinterpret_cast<decltype(kv_append_zeros_fn)>(word(args[13]));
+    Py_INCREF(args[14]);
+    error_class = args[14];
     Py_RETURN_NONE;
   } catch (const Failed &) { return nullptr; }
   END_HANDLE_TH_ERRORS
@@ -289,9 +290,10 @@ PyObject *kv_append(PyObject *, PyObject *const *args, Py_ssize_t n) {
     void *from = qkv.data_ptr(), *to = out.data_ptr(), *stream = current_stream();
     const int n_rows = count(rows), heads = count(nq), kv_heads = count(nkv), dim = count(hd), n_batch = count(batch), pages = count(table.size(1)), positions = count(rope.size(0));
     const long long stride = rows > 1 ? qkv.stride(0) : qkv.size(1) * hd;
+    const auto call = args[7] == Py_None ? kv_append_zeros_fn : kv_append_fn;              // (fresh memory holds anything)
     check(released([&] {
-      return kv_append_fn(from, source == at::kFloat ? HSD_F32 : HSD_BF16, n_rows, stride, heads, kv_heads, dim, starts, static_cast<const int32_t *>(lens.data_ptr()),
-                          n_batch, static_cast<const int32_t *>(table.data_ptr()), pages, static_cast<const float *>(rope.data_ptr()), positions, &pool, to, stream);
+      return call(from, source == at::kFloat ? HSD_F32 : HSD_BF16, n_rows, stride, heads, kv_heads, dim, starts, static_cast<const int32_t *>(lens.data_ptr()),
+                  n_batch, static_cast<const int32_t *>(table.data_ptr()), pages, static_cast<const float *>(rope.data_ptr()), positions, &pool, to, stream);
     }));
     return THPVariable_Wrap(std::move(out));
   } catch (const Failed &) { return nullptr; }

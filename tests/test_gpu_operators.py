@@ -403,6 +403,26 @@ def test_append_rows_that_lie_apart_and_far_positions(lib):
     assert len(check_append(lib, qkv, k, v, table, before, lib.rope_table(131072, 64))) == 5
 
 
+@pytest.mark.parametrize("rows,starts", [(30, [2, 8, 13, 16, 25]), (1300, [5, 8, 13, 16, 1290]), (4, None)])
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_append_gives_zeros_for_queries_of_skipped_rows(lib, dtype, rows, starts):
+    g = gen(rows)
+    k, v, table = cache(g, 4, 1, 64, 16, 2, dtype)
+    table[1, 1], table[2, 0] = -1, k.shape[1]
+    before, rope, qkv = [28, 14, 0, -1 if starts is None else 18], lib.rope_table(30, 64), randn(g, rows, 5, 64)
+    edges = list(range(5)) if starts is None else starts
+    found = append64(qkv, table.cpu(), before, rope, edges, 1, (k.shape[1], 16))
+    skipped = [r for r in range(rows) if r not in found]
+    assert found and skipped
+    into = torch.full((rows, 3, 64), 7.0, dtype=dtype, device="cuda")
+    lib.hsd_kv_append(qkv, k, v, table, ints(before), rope, None if starts is None else ints(starts), into)
+    for _ in range(3):
+        dirt = torch.full((rows, 3, 64), float("nan"), dtype=dtype, device="cuda")          # what the next tensor of this size is made of
+        del dirt
+        q = lib.hsd_kv_append(qkv, k, v, table, ints(before), rope, None if starts is None else ints(starts))
+        assert bool((q[skipped] == 0).all()) and torch.equal(q[sorted(found)], into[sorted(found)])
+
+
 # ------------------------------------------------------------------------------------------------ 4-bit products
 def check_w4(lib, A, codes, scales, **more):
     got = lib.hsd_gemm_w4(A, codes, scales, **more)

@@ -138,3 +138,12 @@ def test_rope_table():
     a = 69999 * 10000.0 ** (-2 * 5 / 64)
     assert float(t[69999, 0, 5]) == pytest.approx(float(torch.tensor(a, dtype=torch.float64).cos()), abs=2 ** -24)
     assert float(t[69999, 1, 5]) == pytest.approx(float(torch.tensor(a, dtype=torch.float64).sin()), abs=2 ** -24)
+
+
+def test_append_with_zeros_refuses_what_append_refuses():
+    def call(**k):
+        d = dict(qkv=P, dtype=0, rows=2, row_stride=8 * 64, nq=4, nkv=2, hd=64, starts=None, lens=P, batch=2, table=P, pages=3, rope=P, positions=64)
+        d.update(k)
+        return binding.library().hsd_kv_append_zeros(*d.values(), ctypes.byref(pool()), P, None)
+
+    assert call(qkv=None) == call(rows=3) == call(rope=P + 4) == -1 and call(hd=48) == -6
