@@ -379,13 +379,14 @@ logprobs_kernel(LogprobArgs a) {
       z.raise(mine);
       s2 = make_float2(z.s, 0.f); t2 = make_float2(z.t, 0.f);
     }
-    const int id_lo = p.first + i0 * N, id_hi = id_lo + (U - 1) * THREADS * N + N;
-    const bool one_side = id_lo > tok || id_hi <= tok;                 // of the given token, as nearly all are
-    if (one_side) front += Vec<T>::template front<U>(v, xt, id_lo < tok && xt > -INFINITY);
+    // The given token's place behind the first of these.  (Ids past the row's end would not fit 32 bits in the largest vocabularies.)
+    const int at = (given ? tok : -1) - (p.first + i0 * N);
+    const bool one_side = at < 0 || at >= (U - 1) * THREADS * N + N;   // of the given token, as nearly all are
+    if (one_side) front += Vec<T>::template front<U>(v, xt, at > 0 && xt > -INFINITY);
     const float2 minus = make_float2(-z.m, -z.m), scale = make_float2(kLog2e, kLog2e);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int id0 = p.first + (i0 + u * THREADS) * N;
+      const int u0 = u * THREADS * N;
       float f[N];
       Vec<T>::unpack(v[u], f);
 #pragma unroll
@@ -397,11 +398,11 @@ logprobs_kernel(LogprobArgs a) {
         t2 = __ffma2_rn(w, y, t2);
       }
       if (one_side) continue;
-      if (id0 > tok || id0 + N <= tok) {                               // (places without a token hold -inf)
-        front += Vec<T>::template front<1>(v + u, xt, id0 < tok && xt > -INFINITY);
+      if (u0 > at || u0 + N <= at) {                                   // (places without a token hold -inf)
+        front += Vec<T>::template front<1>(v + u, xt, u0 < at && xt > -INFINITY);
       } else {
 #pragma unroll
-        for (int e = 0; e < N; ++e) front += f[e] > xt || (xt > -INFINITY && f[e] == xt && id0 + e < tok);
+        for (int e = 0; e < N; ++e) front += f[e] > xt || (xt > -INFINITY && f[e] == xt && u0 + e < at);
       }
     }
   }
