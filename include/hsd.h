@@ -409,7 +409,7 @@ int hsd_paged_attention(const void *q, int batch, int n_q_heads, int n_kv_heads,
  *   out     device fp32 [R, N]
  *   workspace  device, 16-byte aligned, at least hsd_gemm_w4_workspace_bytes(...) (0 = bad sizes); contents on entry are
  *           ignored, on exit unspecified
- * Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, TOO_LARGE (K over 2^27, 2^45 weights), CUDA. */
+ * Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, TOO_LARGE (N over 2^31 - 256, K over 2^27, 2^45 weights), CUDA. */
 size_t hsd_gemm_w4_workspace_bytes(int R, int N, int K, int group);
 int hsd_gemm_w4(const void *A, int R, int K, const void *codes, const void *scales, int N, int group, float *out, void *workspace,
                 size_t workspace_bytes, void *stream);

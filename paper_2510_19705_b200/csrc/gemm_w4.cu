@@ -421,7 +421,7 @@ extern "C" int hsd_gemm_w4(const void *A, int R, int K, const void *codes, const
   using namespace hsd;
   if (!A || !codes || !scales || !out || !workspace || R <= 0 || R > 64 || N <= 0 || K <= 0) return HSD_E_INVALID_ARG;
   if ((group != 32 && group != 64 && group != 128) || K % group) return HSD_E_INVALID_ARG;
-  if (K > (1 << 27) || (long long)ceil_div(N, kTile) * ceil_div(K, kStep) > (1 << 30)) return HSD_E_TOO_LARGE;
+  if (N > 0x7FFFFF00 || K > (1 << 27) || (long long)ceil_div(N, kTile) * ceil_div(K, kStep) > (1 << 30)) return HSD_E_TOO_LARGE;
   if (((reinterpret_cast<uintptr_t>(A) | reinterpret_cast<uintptr_t>(codes) | reinterpret_cast<uintptr_t>(workspace)) & 15) || (reinterpret_cast<uintptr_t>(scales) & 1) ||
       (reinterpret_cast<uintptr_t>(out) & 3)) return HSD_E_INVALID_ARG;
   if (workspace_bytes < hsd_gemm_w4_workspace_bytes(R, N, K, group)) return HSD_E_WORKSPACE_TOO_SMALL;

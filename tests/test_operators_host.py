@@ -147,3 +147,11 @@ def test_append_with_zeros_refuses_what_append_refuses():
         return binding.library().hsd_kv_append_zeros(*d.values(), ctypes.byref(pool()), P, None)
 
     assert call(qkv=None) == call(rows=3) == call(rope=P + 4) == -1 and call(hd=48) == -6
+
+
+def test_gemm_w4_refuses_rows_past_32_bits():
+    """Tiles of 128 weight rows go up to 255 past the last: their numbers have to fit."""
+    call = binding.library().hsd_gemm_w4
+    for n in ((1 << 31) - 1, (1 << 31) - 255):
+        for r, k, group in ((1, 32, 32), (9, 128, 128)):
+            assert call(P, r, k, P, P, n, group, P, P, 1 << 40, None) == -8
