@@ -388,7 +388,7 @@ int hsd_kv_append_zeros(const void *qkv, int qkv_dtype, int rows, long long row_
  *   page_table device [batch, pages_per_seq] int32; keys on a page that is not in [0, n_pages) count as absent.  Memory of
  *              the pages behind a sequence's last key is not used, whatever it holds; keys and values that are there and not
  *              finite may make their heads' outputs NaN
- *   scale      finite
+ *   scale      finite, also times log2(e)
  *   workspace  device, 16-byte aligned, at least hsd_paged_attention_workspace_bytes(...) (0 = bad sizes); contents on entry are
  *              ignored, on exit unspecified
  * Results do not depend on earlier calls; how a sequence's keys are divided, and so the order of its fp32 sums, follows

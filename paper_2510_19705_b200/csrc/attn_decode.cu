@@ -816,7 +816,8 @@ extern "C" int hsd_paged_attention(const void *q, int batch, int n_q_heads, int 
                                    size_t workspace_bytes, void *out, void *stream) {
   using namespace hsd;
   if (!q || !page_table || !kv_lens || !out || !workspace || batch <= 0 || n_q_heads <= 0 || n_kv_heads <= 0 || n_q_heads % n_kv_heads) return HSD_E_INVALID_ARG;
-  if (!(scale == scale) || isinf(scale)) return HSD_E_INVALID_ARG;
+  const float scale2 = scale * 1.4426950408889634f;
+  if (!isfinite(scale2)) return HSD_E_INVALID_ARG;
   DecodeArgs a = {};
   const int status = pool_view(pool, n_kv_heads, head_dim, pages_per_seq, a.pool);
   if (status) return status;
@@ -825,7 +826,7 @@ extern "C" int hsd_paged_attention(const void *q, int batch, int n_q_heads, int 
   if (workspace_bytes < hsd_paged_attention_workspace_bytes(n_q_heads, n_kv_heads, head_dim)) return HSD_E_WORKSPACE_TOO_SMALL;
   a.q = q; a.out = out; a.page_table = page_table; a.kv_lens = kv_lens; a.joins = static_cast<int4 *>(workspace);
   a.parts = reinterpret_cast<float *>(a.joins + kGrid);
-  a.scale = scale * 1.4426950408889634f;
+  a.scale = scale2;
   a.batch = batch; a.nq = n_q_heads; a.nkv = n_kv_heads; a.pages_per_seq = pages_per_seq;
   a.group = n_q_heads / n_kv_heads;
   a.page_shift = -1;

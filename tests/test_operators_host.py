@@ -155,3 +155,8 @@ def test_gemm_w4_refuses_rows_past_32_bits():
     for n in ((1 << 31) - 1, (1 << 31) - 255):
         for r, k, group in ((1, 32, 32), (9, 128, 128)):
             assert call(P, r, k, P, P, n, group, P, P, 1 << 40, None) == -8
+
+
+@pytest.mark.parametrize("scale", [3e38, -3e38, 2.4e38])
+def test_attention_refuses_a_scale_that_is_infinite_in_powers_of_two(scale):
+    assert attention(scale=scale) == -1
