@@ -817,7 +817,7 @@ extern "C" int hsd_paged_attention(const void *q, int batch, int n_q_heads, int 
   using namespace hsd;
   if (!q || !page_table || !kv_lens || !out || !workspace || batch <= 0 || n_q_heads <= 0 || n_kv_heads <= 0 || n_q_heads % n_kv_heads) return HSD_E_INVALID_ARG;
   const float scale2 = scale * 1.4426950408889634f;
-  if (!isfinite(scale2)) return HSD_E_INVALID_ARG;
+  if (!isfinite(scale2) || !words(page_table, kv_lens)) return HSD_E_INVALID_ARG;
   DecodeArgs a = {};
   const int status = pool_view(pool, n_kv_heads, head_dim, pages_per_seq, a.pool);
   if (status) return status;

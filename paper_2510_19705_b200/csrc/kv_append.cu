@@ -150,6 +150,7 @@ int append(const void *qkv, int qkv_dtype, int rows, long long row_stride, int n
            const hsd_kv_pool *pool, void *q_out, bool zeros, cudaStream_t s) {
   if (!qkv || !kv_lens || !page_table || !rope || rows <= 0 || batch <= 0 || n_q_heads < 0 || n_positions <= 0) return HSD_E_INVALID_ARG;
   if ((n_q_heads > 0 && !q_out) || (qkv_dtype != HSD_F32 && qkv_dtype != HSD_BF16) || (!row_starts && rows != batch)) return HSD_E_INVALID_ARG;
+  if (!words(row_starts, kv_lens, page_table)) return HSD_E_INVALID_ARG;
   AppendArgs a = {};
   const int status = pool_view(pool, n_kv_heads, head_dim, pages_per_seq, a.pool);
   if (status) return status;

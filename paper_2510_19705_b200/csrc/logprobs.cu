@@ -537,6 +537,8 @@ extern "C" int hsd_token_logprobs(const void *logits, int dtype, int rows, int v
   if (dtype != HSD_F32 && dtype != HSD_BF16) return HSD_E_INVALID_ARG;
   if (top < 0 || top > kMaxTop || top > vocab || (top > 0 && (!out_top_tokens || !out_top_logprobs))) return HSD_E_INVALID_ARG;
   if (reinterpret_cast<uintptr_t>(logits) % (dtype == HSD_F32 ? 4 : 2)) return HSD_E_INVALID_ARG;
+  for (const void *x : {(const void *)tokens, (const void *)out_logprobs, (const void *)out_entropy, (const void *)out_ranks, (const void *)out_top_tokens, (const void *)out_top_logprobs})
+    if (reinterpret_cast<uintptr_t>(x) % 4) return HSD_E_INVALID_ARG;
   if (vocab > 0x7FFFFF00) return HSD_E_TOO_LARGE;
   LogprobArgs a = {logits, tokens, out_logprobs, out_entropy, out_ranks, out_top_tokens, out_top_logprobs, vocab, top};
   return dtype == HSD_F32 ? run<float>(a, rows, (cudaStream_t)stream) : run<__nv_bfloat16>(a, rows, (cudaStream_t)stream);

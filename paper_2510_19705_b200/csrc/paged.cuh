@@ -10,6 +10,11 @@ struct PoolView {
   int n_pages, page;
 };
 
+// Lists of 32-bit numbers stand where they can be read as such.
+static inline bool words(const void *a, const void *b, const void *c = nullptr) {
+  return ((reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b) | reinterpret_cast<uintptr_t>(c)) & 3) == 0;
+}
+
 // What both calls ask of a pool: 16-byte pieces of rows of head_dim values, sizes that 32-bit positions can name.
 static inline int pool_view(const hsd_kv_pool *p, int n_kv_heads, int head_dim, int pages_per_seq, PoolView &v) {
   if (!p || !p->k || !p->v || p->n_pages <= 0 || p->page_size <= 0 || pages_per_seq <= 0 || n_kv_heads <= 0) return HSD_E_INVALID_ARG;

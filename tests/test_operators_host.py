@@ -160,3 +160,14 @@ def test_gemm_w4_refuses_rows_past_32_bits():
 @pytest.mark.parametrize("scale", [3e38, -3e38, 2.4e38])
 def test_attention_refuses_a_scale_that_is_infinite_in_powers_of_two(scale):
     assert attention(scale=scale) == -1
+
+
+def test_lists_of_words_have_to_be_aligned():
+    for name in ("starts", "lens", "table"):
+        assert append(**{name: P + 2}) == -1, name
+    for name in ("lens", "table"):
+        assert attention(**{name: P + 1}) == -1, name
+    for name in ("tokens", "lp", "entropy", "ranks", "ids", "top_lp"):
+        d = dict(logits=P, dtype=1, rows=2, vocab=64, tokens=P, top=1, lp=P, entropy=P, ranks=P, ids=P, top_lp=P)
+        d[name] = P + 2
+        assert binding.library().hsd_token_logprobs(*d.values(), None) == -1, name
