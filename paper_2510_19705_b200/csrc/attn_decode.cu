@@ -206,6 +206,7 @@ template <int HD> __device__ __forceinline__ float *cta_part(float *parts, int c
 template <typename T, int HD> struct Feeder {
   using R = Ring<T, HD>;
   static constexpr int KEYS = Form<T, HD>::KEYS, PIECES = R::ROW / 16, AT_ONCE = 32 / PIECES;          // rows that the warp copies at once
+  static_assert(32 % KEYS == 0, "a tile lies in one window");
   const DecodeArgs &a;
   const Line &line;
   u32 ring;                                    // shared memory
@@ -241,11 +242,8 @@ template <typename T, int HD> struct Feeder {
   }
   // Place in the pools of a key of the tile, -1 without one.
   __device__ __forceinline__ long long place(int key, bool wanted) const {
-    const int pg = page_of(key), rel = pg - base;
-    // a tile has at most 32 pages, so they lie in this window and the next
-    int id = __shfl_sync(0xFFFFFFFFu, pages, rel & 31);
-    const int other = __shfl_sync(0xFFFFFFFFu, ahead_pages, rel & 31);
-    if (rel >= 32) id = other;
+    // a window's 32 pages are a multiple of 32 tokens, tiles are 8, 16 or 32 at multiples of their size: none lies in two windows
+    const int pg = page_of(key), id = __shfl_sync(0xFFFFFFFFu, pages, (pg - base) & 31);
     return wanted && key < len && id >= 0 && id < a.pool.n_pages ? id * a.pool.page_bytes + (key - pg * a.pool.page) * a.pool.token_bytes + head : -1;
   }
   __device__ __forceinline__ void copy(int stage) {
