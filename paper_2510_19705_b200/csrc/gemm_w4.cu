@@ -402,10 +402,16 @@ template <int GW> int run_line_rows(const W4Line &a, cudaStream_t s) {
 }
 int w4_tiles(int R) { return R <= 8 ? 1 : R <= 16 ? 2 : R <= 32 ? 4 : 8; }
 
-// Up to eight rows, one launch of loads straight into registers against the ring's three: 4096 x 4096 4.1 us (9.7 by the ring), 14336 x 4096 of
-// 1 / 8 rows 11.5 / 15.3 (13.1 / 15.0), 28672 x 4096 19.7 / 25.2 (22.3 / 22.8); with small groups, whose codes come in smaller pieces,
-// 32000 x 2048 20.6 (15.4).
-bool takes_small(int R, int N, int K, int group) { return R <= 8 && ((long long)N * K <= 60000000 || (group == 128 && R <= 4)); }
+// Up to eight rows: one launch of loads straight into registers, or the ring's three launches.  us of the one / the other, by the weights:
+//   groups of 32, whose codes come in pieces of 4 bytes: 8192 x 4096, 1 / 8 rows 11.9 / 13.2 and 13.7 / 13.9; 11008 x 4096 16.9 / 14.3 and 19.6 / 15.3
+//   groups of 64: 8192 x 8192 15.5 / 16.6 and 16.8 / 17.5; 20480 x 4096, 1 / 4 / 8 rows 17.6 / 17.9, 18.7 / 18.0, 21.6 / 18.3
+//   groups of 128: 8192 x 8192, 1 / 8 rows 13.5 / 16.1 and 15.8 / 16.8; 20480 x 4096, 1 / 4 / 8 rows 16.6 / 17.5, 17.1 / 17.6, 21.1 / 18.0;
+//     28672 x 4096, 1 / 4 rows 21.2 / 22.0 and 21.7 / 22.1; 128256 x 2048 45.8 / 39.7 and 47.1 / 40.1
+// (Below the limits the ring was at most 0.8 us ahead, at 4096 x 14336 with one row.)
+bool takes_small(int R, int N, int K, int group) {
+  const long long weights = (long long)N * K;
+  return R <= 8 && weights <= (group == 32 ? 40000000 : group == 128 && R <= 4 ? 120000000 : 70000000);
+}
 
 }  // namespace
 }  // namespace hsd
