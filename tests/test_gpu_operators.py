@@ -423,6 +423,14 @@ def test_append_gives_zeros_for_queries_of_skipped_rows(lib, dtype, rows, starts
         assert bool((q[skipped] == 0).all()) and torch.equal(q[sorted(found)], into[sorted(found)])
 
 
+@pytest.mark.parametrize("rows", [2501, 2502, 2503])
+def test_append_of_rows_that_are_not_whole_fours(lib, rows):
+    g = gen(rows)
+    k, v, table = cache(g, 3, 1, 32, 16, 70, BF16)
+    found = check_append(lib, randn(g, rows, 4, 32, dtype=BF16), k, v, table, [3, 0, 17], lib.rope_table(1100, 32), [0, 1000, 1903, rows])
+    assert len(found) == rows
+
+
 # ------------------------------------------------------------------------------------------------ 4-bit products
 def check_w4(lib, A, codes, scales, **more):
     got = lib.hsd_gemm_w4(A, codes, scales, **more)
@@ -479,6 +487,15 @@ def test_w4_keeps_what_is_not_finite_to_its_row(lib):
     rows, cols = [0, 2], [i for i in range(40) if i != 5]
     assert bool(got[1].isnan().all()) and not bool(got[rows][:, 5].isfinite().any())
     assert torch.equal(got[rows][:, cols], want[rows][:, cols])
+
+
+@pytest.mark.parametrize("rows,N,K,group", [(8, 28673, 4096, 128), (2, 32001, 4096, 128), (5, 32001, 2048, 32), (3, 40001, 2048, 64), (8, 40001, 2112, 64), (1, 33001, 1312, 32)])
+def test_w4_products_of_few_rows_and_large_matrices(lib, rows, N, K, group):
+    """Past the matrices whose few rows take one launch; groups that are not whole eights of a row."""
+    g = gen(N)
+    A, (codes, scales) = randn(g, rows, K, dtype=BF16), weights(g, N, K, group)
+    got = check_w4(lib, A, codes, scales)
+    assert torch.equal(lib.hsd_gemm_w4(A, codes, scales), got)
 
 
 # ------------------------------------------------------------------------------------------------ log probabilities
@@ -557,6 +574,24 @@ def test_logprobs_of_ties(lib, dtype, V):
 
 
 @pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("rows,V", [(300, 4099), (300, 32001), (300, 70001), (100, 262147), (1, 524291)])
+def test_logprobs_of_many_and_of_long_rows(lib, dtype, rows, V):
+    """A CTA a row, and CTAs of 512 threads alone and in clusters; odd rows lie off 16-byte boundaries."""
+    g = gen(V)
+    x = randn(g, rows, V, std=3.0, dtype=dtype)
+    if rows > 1:
+        x[1::6] = x[1::6].round()                                            # ties
+        x[2::6, V // 3:] = -float("inf")
+        x[3::6] = 2.0                                                        # more equals than candidates
+        x[4::12, : V - 7] = torch.finfo(dtype).min
+        x[5::12] = -float("inf")
+        x[5::12, ::V // 3] = 1.0                                             # three tokens
+    tokens = torch.randint(0, V, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    for top in (0, 5, 32):
+        check_logprobs(lib, x, tokens, top)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
 @pytest.mark.parametrize("V", [300, 32000])
 def test_logprobs_of_extreme_rows(lib, dtype, V):
     g = gen(V + 1)
@@ -632,6 +667,19 @@ def test_the_binding_refuses_shapes_and_types(lib):
     for c, s in ((codes[:, :32].contiguous(), scales), (codes, scales[:4])):
         with pytest.raises(ValueError):
             lib.hsd_gemm_w4(A, c, s)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_logprobs_of_the_largest_vocabulary(lib, dtype):
+    """Ids up to 2^31 - 257, whose steps of a thread's next pieces would pass 2^31."""
+    V = (1 << 31) - 256
+    x = torch.zeros(1, V, dtype=dtype, device="cuda")
+    x[0, V - 5] = 2.0
+    ref = -math.log(V - 1 + math.exp(2.0))
+    for t, rank, logit in ((5, 6, 0.0), (V - 20000, V - 19999, 0.0), (V - 300, V - 299, 0.0), (V - 5, 0, 2.0), (V - 1, V - 1, 0.0)):
+        lp, _, ranks, ids, _ = lib.hsd_token_logprobs(x, ints([t]), 3)
+        assert int(ranks) == rank and ids.tolist() == [[V - 5, 0, 1]]
+        assert abs(float(lp) - logit - ref) < 2e-5                          # 2^31 / (8 * 512) terms a thread, each rounded: 2^19 * 2^-24 at the very most is 0.03
 
 
 # ------------------------------------------------------------------------------------------------ together
