@@ -515,10 +515,12 @@ template <typename T, int THREADS, int U> int run_threads(const LogprobArgs &a, 
   hsd_count_launches(1);
   return hsd_launch_status();
 }
-// Many short rows take a warp each if few alternatives are asked for: 3000 x 1461 bf16 with five 10.7 us (by 128 threads 19.6), 600 rows 6.4
-// (7.8), 300 rows 6.4 (5.3), but with 20 as long and with 32 twice as long, as the maxima of 32 lanes bound those badly.
+// Many short rows take a warp each if few alternatives are asked for: bf16 with five, 3000 x 500 / 1461 / 2048 7.5 / 11.1 / 10.6 us (by 128 threads
+// 17.0 / 20.4 / 20.2), 600 rows 4.9 / 6.6 / 6.4 (6.6 / 7.7 / 7.7; fp32 of 1461 6.1, 5.7), 300 rows 4.8 / 6.3 / 6.3 (4.9 / 5.1 / 5.1); with eight up to 0.7
+// more; but with 20 600 rows take 6.4 / 10.0 / 10.3 (7.3 / 8.5 / 8.5), as the maxima of 32 lanes bound those badly.
 // Rows that do not fill the GPU are divided into parts of 2048 tokens or more.  Long ones take CTAs of 512 threads with eight pieces at once:
-// 700 x 131072 fp32 85 us (of 256 threads with four 117, divided among four such 111), but 576 x 32000 bf16 30 (17).
+// 700 x 131072 fp32 76 us (of 256 threads with four 109, divided among two / four such 93 / 100), 400 x 131072 bf16 36.7 (37.7), 300 x 70001 fp32 30.7 (28.7),
+// but 576 x 32000 bf16 25.7 (16.1).
 template <typename T> int run(const LogprobArgs &a, int rows, cudaStream_t s) {
   if (a.V <= 2048 && a.top <= 8 && rows >= 600) return run_threads<T, 32, 4>(a, rows, 1, s);
   if (a.V <= 4096) return run_threads<T, 128, 4>(a, rows, 1, s);
