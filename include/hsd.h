@@ -43,7 +43,7 @@ enum {
   HSD_E_IO = -7,
   HSD_E_TOO_LARGE = -8
 };
-enum { HSD_F32 = 0, HSD_BF16 = 1 };
+enum { HSD_F32 = 0, HSD_BF16 = 1, HSD_I8 = 2 /* hsd_gemm_w8's activations alone */ };
 
 /* Text for a status code (static storage). */
 const char *hsd_strerror(int status);
@@ -379,6 +379,17 @@ int hsd_kv_append_zeros(const void *qkv, int qkv_dtype, int rows, long long row_
                         const int32_t *row_starts, const int32_t *kv_lens, int batch, const int32_t *page_table, int pages_per_seq,
                         const float *rope, int n_positions, const hsd_kv_pool *pool, void *q_out, void *stream);
 
+/* hsd_kv_append_zeros (zeros != 0) or hsd_kv_append (0) of queries and keys that are normalised by head before they are rotated:
+ * x / sqrt(mean(x^2) + eps) * gain over the head_dim values of each query and key head, in fp32, without a rounding between it and the
+ * rotation.  Values are copied.  Squares of the values must not leave fp32's range (|x| below 2^60 does).
+ *   q_gain, k_gain  device [head_dim] of gain_dtype (HSD_F32 or HSD_BF16), 16-byte aligned, for all heads; either may be NULL: gain 1
+ *   eps             finite, not negative
+ * Everything else, and the errors, as hsd_kv_append's. */
+int hsd_kv_append_norm(const void *qkv, int qkv_dtype, int rows, long long row_stride, int n_q_heads, int n_kv_heads, int head_dim,
+                       const void *q_gain, const void *k_gain, int gain_dtype, float eps, const int32_t *row_starts,
+                       const int32_t *kv_lens, int batch, const int32_t *page_table, int pages_per_seq, const float *rope,
+                       int n_positions, const hsd_kv_pool *pool, int zeros, void *q_out, void *stream);
+
 /* Attention of one new token per sequence: out[b, h] = sum_j softmax_j(scale q[b, h] . k_j) v_j over the keys at positions
  * j < kv_lens[b] of head h * n_kv_heads / n_q_heads (the new token's own key is among them once it has been appended: pass
  * the lengths after the append).  Softmax and both sums in fp32, rounded once; fp32 factors count as multiples of 2^-136.
@@ -415,6 +426,28 @@ int hsd_paged_attention(const void *q, int batch, int n_q_heads, int n_kv_heads,
 size_t hsd_gemm_w4_workspace_bytes(int R, int N, int K, int group);
 int hsd_gemm_w4(const void *A, int R, int K, const void *codes, const void *scales, int N, int group, float *out, void *workspace,
                 size_t workspace_bytes, void *stream);
+
+/* Rows as 8-bit integers with a scale each: scales[r] = max_k |x[r, k]| / 127 (rounded to fp32), codes[r, k] = the whole number nearest to
+ * x[r, k] / scales[r], ties to even, within -127 .. 127.  A row of zeros has scale 0; a row with an infinity or a NaN has scale NaN; both
+ * have codes 0.  Activations for hsd_gemm_w8, and weights: a row is an output channel.
+ *   x       device [rows, K], HSD_F32 or HSD_BF16, rows row_stride elements apart
+ *   codes   device int8 [rows, K];  scales  device fp32 [rows]
+ * Errors: INVALID_ARG, CUDA. */
+int hsd_quantize_rows(const void *x, int dtype, int rows, int K, long long row_stride, void *codes, float *scales, void *stream);
+
+/* Product in 8-bit integers with scales of tokens and channels: out[r, n] = (sum_k a[r, k] codes[n, k]) a_scales[r] scales[n].  The sum is
+ * exact; it, and its products with the scales, are rounded to fp32, then to the output's type.
+ *   A, a_scales  a_dtype HSD_I8: device int8 [R, K] (16-byte aligned) and fp32 [R], as hsd_quantize_rows gives them.  HSD_F32, HSD_BF16:
+ *                device [R, K], of which the call makes codes and scales as hsd_quantize_rows does; a_scales is NULL
+ *   codes        device int8 [N, K], 16-byte aligned, of all values -128 .. 127; K a multiple of 16 below 2^17
+ *   scales       device fp32 [N]
+ *   out          device [R, N] of out_dtype, HSD_F32 or HSD_BF16
+ *   workspace    device, 256-byte aligned, at least hsd_gemm_w8_workspace_bytes(...) (0 = bad sizes); contents on entry are ignored
+ * Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, TOO_LARGE (K, N or R over 2^31 - 256, 2^43 outputs), UNSUPPORTED (no tensor-map support), CUDA;
+ * DEVICE_TIMEOUT is reported by hsd_gemm_status(workspace, stream). */
+size_t hsd_gemm_w8_workspace_bytes(int a_dtype, int R, int N, int K);
+int hsd_gemm_w8(const void *A, int a_dtype, const float *a_scales, int R, int K, const void *codes, const float *scales, int N,
+                void *out, int out_dtype, void *workspace, size_t workspace_bytes, void *stream);
 
 /* What given tokens' probabilities were under softmax(logits[r, :]), and what else was likely: out_logprobs[r] = log p(tokens[r]),
  * out_entropy[r] = -sum_x p(x) log p(x), out_ranks[r] = number of tokens in front of tokens[r], and the `top` first tokens with their log

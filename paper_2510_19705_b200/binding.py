@@ -16,7 +16,7 @@ from . import build
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libhsd.so")
 HOST_PATH = build.host_path()
-HSD_F32, HSD_BF16 = 0, 1
+HSD_F32, HSD_BF16, HSD_I8 = 0, 1, 2
 _lib = None
 _host = None
 
@@ -53,7 +53,8 @@ def _host_calls():
                    (lib.hsd_draft_sample, lib.hsd_verify_workspace_bytes, lib.hsd_verify_level, lib.hsd_gemm_workspace_bytes,
                     lib.hsd_gemm_bf16, lib.hsd_gemm_status, lib.hsd_strerror, lib.hsd_kv_append, lib.hsd_paged_attention_workspace_bytes,
                     lib.hsd_paged_attention, lib.hsd_gemm_w4_workspace_bytes, lib.hsd_gemm_w4, lib.hsd_token_logprobs,
-                    lib.hsd_kv_append_zeros)), HsdError)
+                    lib.hsd_kv_append_zeros, lib.hsd_kv_append_norm, lib.hsd_quantize_rows, lib.hsd_gemm_w8_workspace_bytes, lib.hsd_gemm_w8)),
+                 HsdError)
         _host = mod
     return _host
 
@@ -216,6 +217,9 @@ def _declare_engine(lib):
     for f in (lib.hsd_kv_append, lib.hsd_kv_append_zeros):
         f.restype = i32
         f.argtypes = [vp, i32, i32, c.c_longlong, i32, i32, i32, vp, vp, i32, vp, i32, vp, i32, c.POINTER(_KvPool), vp, vp]
+    lib.hsd_kv_append_norm.restype = i32
+    lib.hsd_kv_append_norm.argtypes = [vp, i32, i32, c.c_longlong, i32, i32, i32, vp, vp, i32, c.c_float, vp, vp, i32, vp, i32, vp, i32, c.POINTER(_KvPool),
+                                       i32, vp, vp]
     lib.hsd_paged_attention_workspace_bytes.restype = sz
     lib.hsd_paged_attention_workspace_bytes.argtypes = [i32, i32, i32]
     lib.hsd_paged_attention.restype = i32
@@ -224,6 +228,12 @@ def _declare_engine(lib):
     lib.hsd_gemm_w4_workspace_bytes.argtypes = [i32, i32, i32, i32]
     lib.hsd_gemm_w4.restype = i32
     lib.hsd_gemm_w4.argtypes = [vp, i32, i32, vp, vp, i32, i32, vp, vp, sz, vp]
+    lib.hsd_quantize_rows.restype = i32
+    lib.hsd_quantize_rows.argtypes = [vp, i32, i32, i32, c.c_longlong, vp, vp, vp]
+    lib.hsd_gemm_w8_workspace_bytes.restype = sz
+    lib.hsd_gemm_w8_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    lib.hsd_gemm_w8.restype = i32
+    lib.hsd_gemm_w8.argtypes = [vp, i32, vp, i32, i32, vp, vp, i32, vp, i32, vp, sz, vp]
     lib.hsd_token_logprobs.restype = i32
     lib.hsd_token_logprobs.argtypes = [vp, i32, i32, i32, vp, i32, vp, vp, vp, vp, vp, vp]
 
@@ -522,6 +532,12 @@ def hsd_kv_append(qkv, k_pool, v_pool, page_table, kv_lens, rope, row_starts=Non
     return (_host or _host_calls()).kv_append(qkv, k_pool, v_pool, page_table, kv_lens, rope, row_starts, q_out)
 
 
+def hsd_kv_append_norm(qkv, q_gain, k_gain, eps, k_pool, v_pool, page_table, kv_lens, rope, row_starts=None, q_out=None):
+    """hsd_kv_append of queries and keys that are normalised by head before they are rotated: x / sqrt(mean(x^2) + eps) * gain.
+    q_gain, k_gain: fp32 or bf16 [head_dim], both of one type, or None (1)."""
+    return (_host or _host_calls()).kv_append_norm(qkv, q_gain, k_gain, eps, k_pool, v_pool, page_table, kv_lens, rope, row_starts, q_out)
+
+
 def hsd_paged_attention_workspace_bytes(n_q_heads, n_kv_heads, head_dim):
     return int(library().hsd_paged_attention_workspace_bytes(n_q_heads, n_kv_heads, head_dim))
 
@@ -539,6 +555,22 @@ def hsd_gemm_w4_workspace_bytes(R, N, K, group):
 def hsd_gemm_w4(A, codes, scales, out=None, workspace=None):
     """A bf16 [R, K] (R <= 64), codes uint8 [N, K / 2] and scales bf16 [N, K / group] from w4_pack -> fp32 [R, N]."""
     return (_host or _host_calls()).gemm_w4(A, codes, scales, out, workspace)
+
+
+def hsd_quantize_rows(x):
+    """x [rows, K] (fp32/bf16; rows may lie apart) -> (codes int8 [rows, K], scales fp32 [rows]): the nearest whole numbers of scales, a row's
+    scale its largest magnitude / 127.  For weights [N, K] of hsd_gemm_w8, and for activations of several products."""
+    return (_host or _host_calls()).quantize_rows(x)
+
+
+def hsd_gemm_w8_workspace_bytes(a_dtype, R, N, K):
+    return int(library().hsd_gemm_w8_workspace_bytes(a_dtype, R, N, K))
+
+
+def hsd_gemm_w8(A, codes, scales, out_dtype=torch.float32, a_scales=None, out=None, workspace=None):
+    """A fp32/bf16 [R, K], of which the call makes 8-bit codes with a scale a row, or int8 [R, K] with a_scales fp32 [R]; codes int8 [N, K]
+    and scales fp32 [N] (both pairs as from hsd_quantize_rows) -> out_dtype (fp32/bf16) [R, N]."""
+    return (_host or _host_calls()).gemm_w8(A, codes, scales, out_dtype, a_scales, out, workspace)
 
 
 def hsd_token_logprobs(logits, tokens, top=0):

@@ -434,17 +434,23 @@ int tc_init() {
   return HSD_OK;
 }
 
-int tc_make_map(CUtensorMap *map, const void *base, long long rows, long long cols, int box_rows) {
+static int make_map(CUtensorMap *map, CUtensorMapDataType type, int size, const void *base, long long rows, long long cols, int box_cols, int box_rows) {
   if (!g_encode) return HSD_E_UNSUPPORTED;
-  if (((uintptr_t)base & 15) != 0 || (cols * 2) % 16 != 0 || box_rows < 1 || box_rows > 256) return HSD_E_INVALID_ARG;
+  if (((uintptr_t)base & 15) != 0 || (cols * size) % 16 != 0 || box_rows < 1 || box_rows > 256) return HSD_E_INVALID_ARG;
   cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-  cuuint64_t strides[1] = {(cuuint64_t)cols * 2};
-  cuuint32_t box[2] = {(cuuint32_t)kTcBlockK, (cuuint32_t)box_rows};
+  cuuint64_t strides[1] = {(cuuint64_t)cols * size};
+  cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows};
   cuuint32_t estr[2] = {1, 1};
-  CUresult r = g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(base), dims, strides, box, estr,
+  CUresult r = g_encode(map, type, 2, const_cast<void *>(base), dims, strides, box, estr,
                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? HSD_OK : HSD_E_CUDA;
+}
+int tc_make_map(CUtensorMap *map, const void *base, long long rows, long long cols, int box_rows) {
+  return make_map(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, rows, cols, kTcBlockK, box_rows);
+}
+int tc_make_map_bytes(CUtensorMap *map, const void *base, long long rows, long long cols, int box_rows) {
+  return make_map(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, base, rows, cols, 128, box_rows);
 }
 
 int tc_npad(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }

@@ -18,6 +18,9 @@ int tc_init();                     // HSD_OK when the tensor-map encoder is avai
 // 2-D bf16 tensor map over a row-major [rows, cols] matrix, box = [box_rows, 64], 128-byte swizzle.
 int tc_make_map(CUtensorMap *map, const void *base, long long rows, long long cols, int box_rows);
 
+// ... over bytes, box = [box_rows, 128].
+int tc_make_map_bytes(CUtensorMap *map, const void *base, long long rows, long long cols, int box_rows);
+
 int tc_npad(int rows);             // 16, 32, 64, 128 or 256 (rows <= 256)
 
 // Where the q / k / v projection's rows go (GEMM_QKV_T): q rotated -> q; k rotated, v -> their cache pages.

@@ -1,9 +1,14 @@
-// New rows into a paged key-value cache, queries and keys rotated on the way (hsd_kv_append).
+// New rows into a paged key-value cache, queries and keys rotated on the way (hsd_kv_append), and normalised before it by head
+// (hsd_kv_append_norm: x becomes x / sqrt(mean x^2 + eps) * gain).
 //   (y_i, y_{i+h}) = (x_i cos - x_{i+h} sin, x_{i+h} cos + x_i sin), h = head_dim / 2, cos and sin of the row's position from the
 // caller's table; values are copied.  The products and the sum are rounded to fp32 (none fused), the result once to the pool's type.
 // A thread takes eight pairs of one head of one row (16 bytes of a bf16 pool at each of the two places).  The rows' positions and
-// pages come first: a warp a row counts the row starts that do not lie behind it.
+// pages come first: a warp a row counts the row starts that do not lie behind it.  The norm's sum of squares goes over the two to eight
+// neighbouring threads of a head, from the values they hold anyway: nothing is read twice.
 // Bound by memory for prompts, by the chain row -> position -> page -> store for a few rows, whose heads are divided over CTAs.
+#include <math.h>
+#include <type_traits>
+
 #include "paged.cuh"
 
 namespace hsd {
@@ -21,6 +26,8 @@ struct AppendArgs {
   int rows, batch, pages_per_seq, n_positions, nq, nkv;
   int cta_rows, parts;                          // rows of a CTA, CTAs that share them
   bool zeros;                                   // the queries of skipped rows become zeros
+  const unsigned char *q_gain, *k_gain;         // norm: of a head's values, or null (1)
+  float eps;
 };
 
 template <typename T> __device__ __forceinline__ void load8(const unsigned char *p, float *f);
@@ -48,7 +55,32 @@ template <> __device__ __forceinline__ void store8<__nv_bfloat16>(unsigned char 
   *reinterpret_cast<uint4 *>(p) = make_uint4(pack(f[0], f[1]), pack(f[2], f[3]), pack(f[4], f[5]), pack(f[6], f[7]));
 }
 
-template <typename TI, typename TO, int HD>
+// What a head's values are multiplied with: TG the gains' type, void: there is no norm.
+template <typename TG, int HD>
+__device__ __forceinline__ void norm(const unsigned char *gain, int i, float eps, float *lo, float *hi) {
+  constexpr int UNITS = HD / 16;
+  float sum = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sum = fmaf(lo[e], lo[e], fmaf(hi[e], hi[e], sum));
+  const int lane = threadIdx.x & 31;
+  const u32 head = ((1u << UNITS) - 1) << (lane & ~(UNITS - 1));       // the head's threads go through the loop together
+#pragma unroll
+  for (int o = 1; o < UNITS; o <<= 1) sum += __shfl_xor_sync(head, sum, o);
+  const float f = __frsqrt_rn(__fadd_rn(sum * (1.f / HD), eps));
+  float g[8], h[8];
+  if (gain) {
+    load8<TG>(gain + i * sizeof(TG), g);
+    load8<TG>(gain + (i + HD / 2) * sizeof(TG), h);
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    lo[e] *= f;
+    hi[e] *= f;
+    if (gain) { lo[e] *= g[e]; hi[e] *= h[e]; }
+  }
+}
+
+template <typename TI, typename TO, typename TG, int HD>
 __global__ void __launch_bounds__(kThreads)
 kv_append_kernel(AppendArgs a) {
   constexpr int UNITS = HD / 16, HALF = HD / 2;
@@ -109,6 +141,7 @@ kv_append_kernel(AppendArgs a) {
     load8<TI>(src, lo);
     load8<TI>(src + HALF * sizeof(TI), hi);
     if (h < a.nq + a.nkv) {
+      if constexpr (!std::is_void<TG>::value) norm<TG, HD>(h < a.nq ? a.q_gain : a.k_gain, i, a.eps, lo, hi);
       float c[8], s[8];
       const unsigned char *t = reinterpret_cast<const unsigned char *>(a.rope + (size_t)pos * HD + i);
       load8<float>(t, c);
@@ -129,7 +162,7 @@ kv_append_kernel(AppendArgs a) {
   }
 }
 
-template <typename TI, typename TO> int run(AppendArgs &a, int hd, cudaStream_t s) {
+template <typename TI, typename TO, typename TG> int run(AppendArgs &a, int hd, cudaStream_t s) {
   const int per_row = (a.nq + 2 * a.nkv) * (hd / 16);
   // few rows: one a CTA and a row's heads over several, so that every thread has one piece; many rows: CTAs of up to kRows
   a.cta_rows = a.rows >= kRows * 2 * kMeasuredSMs ? kRows : 1;
@@ -137,21 +170,34 @@ template <typename TI, typename TO> int run(AppendArgs &a, int hd, cudaStream_t 
   const long long grid = (long long)ceil_div(a.rows, a.cta_rows) * a.parts;
   if (grid > 0x7FFFFFFFll) return HSD_E_TOO_LARGE;
   switch (hd) {
-    case 32: HSD_CUDA_OK(hsd_launch(kv_append_kernel<TI, TO, 32>, dim3((unsigned)grid), kThreads, 0, s, 0, true, a)); break;
-    case 64: HSD_CUDA_OK(hsd_launch(kv_append_kernel<TI, TO, 64>, dim3((unsigned)grid), kThreads, 0, s, 0, true, a)); break;
-    default: HSD_CUDA_OK(hsd_launch(kv_append_kernel<TI, TO, 128>, dim3((unsigned)grid), kThreads, 0, s, 0, true, a)); break;
+    case 32: HSD_CUDA_OK(hsd_launch(kv_append_kernel<TI, TO, TG, 32>, dim3((unsigned)grid), kThreads, 0, s, 0, true, a)); break;
+    case 64: HSD_CUDA_OK(hsd_launch(kv_append_kernel<TI, TO, TG, 64>, dim3((unsigned)grid), kThreads, 0, s, 0, true, a)); break;
+    default: HSD_CUDA_OK(hsd_launch(kv_append_kernel<TI, TO, TG, 128>, dim3((unsigned)grid), kThreads, 0, s, 0, true, a)); break;
   }
   hsd_count_launches(1);
   return hsd_launch_status();
 }
+template <typename TG> int run_types(AppendArgs &a, int from, int to, int hd, cudaStream_t s) {
+  if (from == HSD_F32) return to == HSD_F32 ? run<float, float, TG>(a, hd, s) : run<float, __nv_bfloat16, TG>(a, hd, s);
+  return to == HSD_F32 ? run<__nv_bfloat16, float, TG>(a, hd, s) : run<__nv_bfloat16, __nv_bfloat16, TG>(a, hd, s);
+}
+
+struct Norm { const void *q_gain, *k_gain; int gain_dtype; float eps; };
 
 int append(const void *qkv, int qkv_dtype, int rows, long long row_stride, int n_q_heads, int n_kv_heads, int head_dim, const int32_t *row_starts,
            const int32_t *kv_lens, int batch, const int32_t *page_table, int pages_per_seq, const float *rope, int n_positions,
-           const hsd_kv_pool *pool, void *q_out, bool zeros, cudaStream_t s) {
+           const hsd_kv_pool *pool, void *q_out, bool zeros, const Norm *norm, cudaStream_t s) {
   if (!qkv || !kv_lens || !page_table || !rope || rows <= 0 || batch <= 0 || n_q_heads < 0 || n_positions <= 0) return HSD_E_INVALID_ARG;
   if ((n_q_heads > 0 && !q_out) || (qkv_dtype != HSD_F32 && qkv_dtype != HSD_BF16) || (!row_starts && rows != batch)) return HSD_E_INVALID_ARG;
   if (!words(row_starts, kv_lens, page_table)) return HSD_E_INVALID_ARG;
   AppendArgs a = {};
+  if (norm) {
+    if ((norm->gain_dtype != HSD_F32 && norm->gain_dtype != HSD_BF16) || !(norm->eps >= 0.f) || isinf(norm->eps)) return HSD_E_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(norm->q_gain) | reinterpret_cast<uintptr_t>(norm->k_gain)) & 15) return HSD_E_INVALID_ARG;
+    a.q_gain = static_cast<const unsigned char *>(norm->q_gain);
+    a.k_gain = static_cast<const unsigned char *>(norm->k_gain);
+    a.eps = norm->eps;
+  }
   const int status = pool_view(pool, n_kv_heads, head_dim, pages_per_seq, a.pool);
   if (status) return status;
   if ((long long)n_q_heads + 2ll * n_kv_heads > 65536) return HSD_E_TOO_LARGE;
@@ -164,8 +210,8 @@ int append(const void *qkv, int qkv_dtype, int rows, long long row_stride, int n
   a.q_out = static_cast<unsigned char *>(q_out);
   a.rows = rows; a.batch = batch; a.pages_per_seq = pages_per_seq; a.n_positions = n_positions; a.nq = n_q_heads; a.nkv = n_kv_heads;
   a.zeros = zeros;
-  if (qkv_dtype == HSD_F32) return pool->dtype == HSD_F32 ? run<float, float>(a, head_dim, s) : run<float, __nv_bfloat16>(a, head_dim, s);
-  return pool->dtype == HSD_F32 ? run<__nv_bfloat16, float>(a, head_dim, s) : run<__nv_bfloat16, __nv_bfloat16>(a, head_dim, s);
+  if (!norm) return run_types<void>(a, qkv_dtype, pool->dtype, head_dim, s);
+  return norm->gain_dtype == HSD_F32 ? run_types<float>(a, qkv_dtype, pool->dtype, head_dim, s) : run_types<__nv_bfloat16>(a, qkv_dtype, pool->dtype, head_dim, s);
 }
 
 }  // namespace
@@ -175,12 +221,21 @@ extern "C" int hsd_kv_append(const void *qkv, int qkv_dtype, int rows, long long
                              const int32_t *row_starts, const int32_t *kv_lens, int batch, const int32_t *page_table, int pages_per_seq,
                              const float *rope, int n_positions, const hsd_kv_pool *pool, void *q_out, void *stream) {
   return hsd::append(qkv, qkv_dtype, rows, row_stride, n_q_heads, n_kv_heads, head_dim, row_starts, kv_lens, batch, page_table, pages_per_seq, rope,
-                     n_positions, pool, q_out, false, (cudaStream_t)stream);
+                     n_positions, pool, q_out, false, nullptr, (cudaStream_t)stream);
 }
 
 extern "C" int hsd_kv_append_zeros(const void *qkv, int qkv_dtype, int rows, long long row_stride, int n_q_heads, int n_kv_heads, int head_dim,
                                    const int32_t *row_starts, const int32_t *kv_lens, int batch, const int32_t *page_table, int pages_per_seq,
                                    const float *rope, int n_positions, const hsd_kv_pool *pool, void *q_out, void *stream) {
   return hsd::append(qkv, qkv_dtype, rows, row_stride, n_q_heads, n_kv_heads, head_dim, row_starts, kv_lens, batch, page_table, pages_per_seq, rope,
-                     n_positions, pool, q_out, true, (cudaStream_t)stream);
+                     n_positions, pool, q_out, true, nullptr, (cudaStream_t)stream);
+}
+
+extern "C" int hsd_kv_append_norm(const void *qkv, int qkv_dtype, int rows, long long row_stride, int n_q_heads, int n_kv_heads, int head_dim,
+                                  const void *q_gain, const void *k_gain, int gain_dtype, float eps, const int32_t *row_starts,
+                                  const int32_t *kv_lens, int batch, const int32_t *page_table, int pages_per_seq, const float *rope,
+                                  int n_positions, const hsd_kv_pool *pool, int zeros, void *q_out, void *stream) {
+  const hsd::Norm norm = {q_gain, k_gain, gain_dtype, eps};
+  return hsd::append(qkv, qkv_dtype, rows, row_stride, n_q_heads, n_kv_heads, head_dim, row_starts, kv_lens, batch, page_table, pages_per_seq, rope,
+                     n_positions, pool, q_out, zeros != 0, &norm, (cudaStream_t)stream);
 }

@@ -10,6 +10,7 @@
 #include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -34,6 +35,10 @@ decltype(&hsd_paged_attention) attention_fn = nullptr;
 decltype(&hsd_gemm_w4_workspace_bytes) gemm_w4_bytes_fn = nullptr;
 decltype(&hsd_gemm_w4) gemm_w4_fn = nullptr;
 decltype(&hsd_token_logprobs) logprobs_fn = nullptr;
+decltype(&hsd_kv_append_norm) kv_append_norm_fn = nullptr;
+decltype(&hsd_quantize_rows) quantize_fn = nullptr;
+decltype(&hsd_gemm_w8_workspace_bytes) gemm_w8_bytes_fn = nullptr;
+decltype(&hsd_gemm_w8) gemm_w8_fn = nullptr;
 PyObject *error_class = nullptr;
 
 struct Failed {};                                          // a Python exception is set
@@ -93,7 +98,7 @@ void *current_stream() { return c10::cuda::getCurrentCUDAStream().stream(); }
 PyObject *init(PyObject *, PyObject *const *args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   try {
-    arguments(n, 15);
+    arguments(n, 19);
     draft_sample_fn = reinterpret_cast<decltype(draft_sample_fn)>(word(args[0]));
     verify_bytes_fn = reinterpret_cast<decltype(verify_bytes_fn)>(word(args[1]));
     verify_level_fn = reinterpret_cast<decltype(verify_level_fn)>(word(args[2]));
@@ -108,8 +113,12 @@ PyObject *init(PyObject *, PyObject *const *args, Py_ssize_t n) {
     gemm_w4_fn = reinterpret_cast<decltype(gemm_w4_fn)>(word(args[11]));
     logprobs_fn = reinterpret_cast<decltype(logprobs_fn)>(word(args[12]));
     kv_append_zeros_fn = reinterpret_cast<decltype(kv_append_zeros_fn)>(word(args[13]));
-    Py_INCREF(args[14]);
-    error_class = args[14];
+    kv_append_norm_fn = reinterpret_cast<decltype(kv_append_norm_fn)>(word(args[14]));
+    quantize_fn = reinterpret_cast<decltype(quantize_fn)>(word(args[15]));
+    gemm_w8_bytes_fn = reinterpret_cast<decltype(gemm_w8_bytes_fn)>(word(args[16]));
+    gemm_w8_fn = reinterpret_cast<decltype(gemm_w8_fn)>(word(args[17]));
+    Py_INCREF(args[18]);
+    error_class = args[18];
     Py_RETURN_NONE;
   } catch (const Failed &) { return nullptr; }
   END_HANDLE_TH_ERRORS
@@ -259,43 +268,76 @@ hsd_kv_pool pools(PyObject *ko, PyObject *vo, const at::Tensor *like) {
   return {k.data_ptr(), v.data_ptr(), type == at::kFloat ? HSD_F32 : HSD_BF16, count(k.size(1)), count(k.size(2)), k.stride(0), k.stride(1), k.stride(2)};
 }
 
+// What both appends take; gains null: without a norm.
+struct Gains { PyObject *q, *k, *eps; };
+PyObject *append(PyObject *qkv_o, PyObject *k_o, PyObject *v_o, PyObject *table_o, PyObject *lens_o, PyObject *rope_o, PyObject *starts_o, PyObject *out_o, const Gains *gains) {
+  const at::Tensor &qkv = dims(tensor(qkv_o), "qkv", 3);
+  const at::ScalarType source = cache_type(qkv, "qkv");
+  typed(qkv_o, "qkv", source);
+  const hsd_kv_pool pool = pools(k_o, v_o, &qkv);
+  const int64_t nkv = tensor(k_o).size(0), hd = qkv.size(2), nq = qkv.size(1) - 2 * nkv;
+  if (nq < 0 || hd != tensor(k_o).size(3)) {
+    PyErr_SetString(PyExc_ValueError, "qkv has fewer heads than twice the pools' or another head size");
+    throw Failed();
+  }
+  if ((hd > 1 && qkv.stride(2) != 1) || (qkv.size(1) > 1 && qkv.stride(1) != hd)) refuse("qkv: the heads of a row have to be contiguous");
+  const at::Tensor &table = dims(typed(table_o, "page_table", at::kInt, &qkv), "page_table", 2);
+  const int64_t batch = table.size(0), rows = qkv.size(0);
+  sized(table, "page_table", {batch, table.size(1)});
+  const at::Tensor &lens = sized(typed(lens_o, "kv_lens", at::kInt, &qkv), "kv_lens", {batch});
+  const at::Tensor &rope = dims(typed(rope_o, "rope", at::kFloat, &qkv), "rope", 3);
+  sized(rope, "rope", {rope.size(0), 2, hd / 2});
+  const int32_t *starts = nullptr;
+  if (starts_o != Py_None) starts = static_cast<const int32_t *>(sized(typed(starts_o, "row_starts", at::kInt, &qkv), "row_starts", {batch + 1}).data_ptr());
+  const at::ScalarType type = pool.dtype == HSD_F32 ? at::kFloat : at::kBFloat16;
+  const void *gain[2] = {nullptr, nullptr};
+  at::ScalarType gain_type = at::kFloat;
+  double eps = 0.;
+  if (gains) {
+    const char *names[2] = {"q_gain", "k_gain"};
+    PyObject *given[2] = {gains->q, gains->k};
+    if (given[0] != Py_None) gain_type = cache_type(tensor(given[0]), names[0]);
+    else if (given[1] != Py_None) gain_type = cache_type(tensor(given[1]), names[1]);
+    for (int x = 0; x < 2; ++x)
+      if (given[x] != Py_None) gain[x] = sized(typed(given[x], names[x], gain_type, &qkv), names[x], {hd}).data_ptr();
+    eps = PyFloat_AsDouble(gains->eps);
+    if (eps == -1. && PyErr_Occurred()) throw Failed();
+  }
+  const c10::cuda::CUDAGuard guard(qkv.device());
+  at::Tensor out = out_o == Py_None ? fresh({rows, nq, hd}, type) : sized(typed(out_o, "q_out", type, &qkv), "q_out", {rows, nq, hd});
+  void *from = qkv.data_ptr(), *to = out.data_ptr(), *stream = current_stream();
+  const int n_rows = count(rows), heads = count(nq), kv_heads = count(nkv), dim = count(hd), n_batch = count(batch), pages = count(table.size(1)), positions = count(rope.size(0));
+  const long long stride = rows > 1 ? qkv.stride(0) : qkv.size(1) * hd;
+  const int dtype = source == at::kFloat ? HSD_F32 : HSD_BF16;
+  const int32_t *n_lens = static_cast<const int32_t *>(lens.data_ptr()), *n_table = static_cast<const int32_t *>(table.data_ptr());
+  const float *angles = static_cast<const float *>(rope.data_ptr());
+  const auto call = out_o == Py_None ? kv_append_zeros_fn : kv_append_fn;                  // (fresh memory holds anything)
+  check(released([&] {
+    if (gains) return kv_append_norm_fn(from, dtype, n_rows, stride, heads, kv_heads, dim, gain[0], gain[1], gain_type == at::kFloat ? HSD_F32 : HSD_BF16, (float)eps,
+                                        starts, n_lens, n_batch, n_table, pages, angles, positions, &pool, out_o == Py_None, to, stream);
+    return call(from, dtype, n_rows, stride, heads, kv_heads, dim, starts, n_lens, n_batch, n_table, pages, angles, positions, &pool, to, stream);
+  }));
+  return THPVariable_Wrap(std::move(out));
+}
+
 // kv_append(qkv [rows, nq + 2 nkv, hd], k_pool, v_pool, page_table [batch, pages], kv_lens [batch], rope [positions, 2, hd / 2],
 // row_starts [batch + 1] or None, q_out or None)
 PyObject *kv_append(PyObject *, PyObject *const *args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   try {
     arguments(n, 8);
-    const at::Tensor &qkv = dims(tensor(args[0]), "qkv", 3);
-    const at::ScalarType source = cache_type(qkv, "qkv");
-    typed(args[0], "qkv", source);
-    const hsd_kv_pool pool = pools(args[1], args[2], &qkv);
-    const int64_t nkv = tensor(args[1]).size(0), hd = qkv.size(2), nq = qkv.size(1) - 2 * nkv;
-    if (nq < 0 || hd != tensor(args[1]).size(3)) {
-      PyErr_SetString(PyExc_ValueError, "qkv has fewer heads than twice the pools' or another head size");
-      throw Failed();
-    }
-    if ((hd > 1 && qkv.stride(2) != 1) || (qkv.size(1) > 1 && qkv.stride(1) != hd)) refuse("qkv: the heads of a row have to be contiguous");
-    const at::Tensor &table = dims(typed(args[3], "page_table", at::kInt, &qkv), "page_table", 2);
-    const int64_t batch = table.size(0), rows = qkv.size(0);
-    sized(table, "page_table", {batch, table.size(1)});
-    const at::Tensor &lens = sized(typed(args[4], "kv_lens", at::kInt, &qkv), "kv_lens", {batch});
-    const at::Tensor &rope = dims(typed(args[5], "rope", at::kFloat, &qkv), "rope", 3);
-    sized(rope, "rope", {rope.size(0), 2, hd / 2});
-    const int32_t *starts = nullptr;
-    if (args[6] != Py_None) starts = static_cast<const int32_t *>(sized(typed(args[6], "row_starts", at::kInt, &qkv), "row_starts", {batch + 1}).data_ptr());
-    const at::ScalarType type = pool.dtype == HSD_F32 ? at::kFloat : at::kBFloat16;
-    const c10::cuda::CUDAGuard guard(qkv.device());
-    at::Tensor out = args[7] == Py_None ? fresh({rows, nq, hd}, type)
-                                        : sized(typed(args[7], "q_out", type, &qkv), "q_out", {rows, nq, hd});
-    void *from = qkv.data_ptr(), *to = out.data_ptr(), *stream = current_stream();
-    const int n_rows = count(rows), heads = count(nq), kv_heads = count(nkv), dim = count(hd), n_batch = count(batch), pages = count(table.size(1)), positions = count(rope.size(0));
-    const long long stride = rows > 1 ? qkv.stride(0) : qkv.size(1) * hd;
-    const auto call = args[7] == Py_None ? kv_append_zeros_fn : kv_append_fn;              // (fresh memory holds anything)
-    check(released([&] {
-      return call(from, source == at::kFloat ? HSD_F32 : HSD_BF16, n_rows, stride, heads, kv_heads, dim, starts, static_cast<const int32_t *>(lens.data_ptr()),
-                  n_batch, static_cast<const int32_t *>(table.data_ptr()), pages, static_cast<const float *>(rope.data_ptr()), positions, &pool, to, stream);
-    }));
-    return THPVariable_Wrap(std::move(out));
+    return append(args[0], args[1], args[2], args[3], args[4], args[5], args[6], args[7], nullptr);
+  } catch (const Failed &) { return nullptr; }
+  END_HANDLE_TH_ERRORS
+}
+
+// kv_append_norm(qkv, q_gain [hd] or None, k_gain [hd] or None, eps, then as kv_append)
+PyObject *kv_append_norm(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  try {
+    arguments(n, 11);
+    const Gains gains = {args[1], args[2], args[3]};
+    return append(args[0], args[4], args[5], args[6], args[7], args[8], args[9], args[10], &gains);
   } catch (const Failed &) { return nullptr; }
   END_HANDLE_TH_ERRORS
 }
@@ -374,6 +416,74 @@ PyObject *gemm_w4(PyObject *, PyObject *const *args, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// quantize_rows(x [rows, K])
+PyObject *quantize_rows(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  try {
+    arguments(n, 1);
+    const at::Tensor &x = dims(tensor(args[0]), "x", 2);
+    const at::ScalarType source = cache_type(x, "x");
+    typed(args[0], "x", source);
+    if (x.size(1) > 1 && x.stride(1) != 1) refuse("x: the values of a row have to be contiguous");
+    const int rows = count(x.size(0)), k = count(x.size(1));
+    const long long stride = rows > 1 ? x.stride(0) : k;
+    const c10::cuda::CUDAGuard guard(x.device());
+    at::Tensor codes = fresh({rows, k}, at::kChar), scales = fresh({rows}, at::kFloat);
+    void *from = x.data_ptr(), *to = codes.data_ptr(), *stream = current_stream();
+    float *scale = static_cast<float *>(scales.data_ptr());
+    check(released([&] { return quantize_fn(from, source == at::kFloat ? HSD_F32 : HSD_BF16, rows, k, stride, to, scale, stream); }));
+    PyObject *first = THPVariable_Wrap(std::move(codes)), *second = THPVariable_Wrap(std::move(scales)), *both = nullptr;
+    if (first && second) both = PyTuple_Pack(2, first, second);
+    Py_XDECREF(first);
+    Py_XDECREF(second);
+    return both;
+  } catch (const Failed &) { return nullptr; }
+  END_HANDLE_TH_ERRORS
+}
+
+// gemm_w8(A [R, K], codes int8 [N, K], scales fp32 [N], out dtype, a_scales fp32 [R] or None, out or None, workspace or None)
+PyObject *gemm_w8(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  try {
+    arguments(n, 7);
+    const at::Tensor &a = dims(tensor(args[0]), "A", 2);
+    const bool coded = a.scalar_type() == at::kChar;
+    const at::ScalarType source = coded ? at::kChar : cache_type(a, "A");
+    typed(args[0], "A", source);
+    const int64_t R = a.size(0), K = a.size(1);
+    sized(a, "A", {R, K});
+    const at::Tensor &codes = dims(typed(args[1], "codes", at::kChar, &a), "codes", 2);
+    const int64_t N = codes.size(0);
+    sized(codes, "codes", {N, K});
+    const at::Tensor &scales = sized(typed(args[2], "scales", at::kFloat, &a), "scales", {N});
+    if (!THPDtype_Check(args[3])) {
+      PyErr_SetString(PyExc_TypeError, "out_dtype: expected a torch.dtype");
+      throw Failed();
+    }
+    const at::ScalarType to_type = reinterpret_cast<THPDtype *>(args[3])->scalar_type;
+    if (to_type != at::kFloat && to_type != at::kBFloat16) refuse("out_dtype: expected float32 or bfloat16");
+    if (coded != (args[4] != Py_None)) refuse("a_scales go with an A of int8, and with no other");
+    const float *row_scales = coded ? static_cast<const float *>(sized(typed(args[4], "a_scales", at::kFloat, &a), "a_scales", {R}).data_ptr()) : nullptr;
+    const int rows = count(R), k = count(K), cols = count(N), dtype = coded ? HSD_I8 : source == at::kFloat ? HSD_F32 : HSD_BF16;
+    const size_t need = gemm_w8_bytes_fn(dtype, rows, cols, k);
+    if (need == 0) {
+      PyErr_Format(error_class, "hsd_gemm_w8: unsupported shape R=%d N=%d K=%d", rows, cols, k);
+      throw Failed();
+    }
+    const c10::cuda::CUDAGuard guard(a.device());
+    at::Tensor out = args[5] == Py_None ? fresh({R, N}, to_type) : sized(typed(args[5], "out", to_type, &a), "out", {R, N});
+    at::Tensor ws = args[6] == Py_None ? fresh({(int64_t)need}, at::kByte) : typed(args[6], "workspace", at::kByte, &a);
+    if (!ws.is_contiguous()) refuse("expected a contiguous CUDA tensor");
+    void *pa = a.data_ptr(), *pc = codes.data_ptr(), *to = out.data_ptr(), *scratch = ws.data_ptr(), *stream = current_stream();
+    const float *col_scales = static_cast<const float *>(scales.data_ptr());
+    check(released([&] {
+      return gemm_w8_fn(pa, dtype, row_scales, rows, k, pc, col_scales, cols, to, to_type == at::kFloat ? HSD_F32 : HSD_BF16, scratch, (size_t)ws.numel(), stream);
+    }));
+    return THPVariable_Wrap(std::move(out));
+  } catch (const Failed &) { return nullptr; }
+  END_HANDLE_TH_ERRORS
+}
+
 // token_logprobs(logits [..., vocab], tokens int32 [...], top)
 PyObject *token_logprobs(PyObject *, PyObject *const *args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
@@ -416,7 +526,8 @@ PyObject *token_logprobs(PyObject *, PyObject *const *args, Py_ssize_t n) {
 
 #define FAST(f) reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr
 PyMethodDef methods[] = {{"init", FAST(init)}, {"draft_sample", FAST(draft_sample)}, {"verify_level", FAST(verify_level)},
-                         {"gemm_bf16", FAST(gemm_bf16)}, {"kv_append", FAST(kv_append)}, {"paged_attention", FAST(paged_attention)},
+                         {"gemm_bf16", FAST(gemm_bf16)}, {"kv_append", FAST(kv_append)}, {"kv_append_norm", FAST(kv_append_norm)}, {"quantize_rows", FAST(quantize_rows)}, {"gemm_w8", FAST(gemm_w8)},
+                         {"paged_attention", FAST(paged_attention)},
                          {"gemm_w4", FAST(gemm_w4)}, {"token_logprobs", FAST(token_logprobs)}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,316 @@
+"""The operators of a decoding step over continuations of one prompt against plain implementations in 64 bits: appends with norms by head,
+products in 8-bit integers, attention over a shared prefix.
+
+Tolerances count roundings: half a step of the output's type, 2^-24 for each fp32 operation, 2^-23 where the tensor cores' adders may
+cut off instead of rounding."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+HALF_STEP = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8}
+BF16, FP32 = torch.bfloat16, torch.float32
+
+
+def gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def randn(g, *shape, dtype=FP32, std=1.0):
+    return (torch.randn(*shape, generator=g, device="cuda") * std).to(dtype)
+
+
+def ints(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def cache(g, batch, nkv, hd, page, per_seq, dtype, order="head", spare=3):
+    """Pools in the engine's order or token-major, a page table in any order, pages that no sequence has."""
+    n = batch * per_seq + spare
+    pools = []
+    for _ in range(2):
+        if order == "head":
+            pools.append(randn(g, nkv, n, page, hd, dtype=dtype))
+        else:
+            pools.append(randn(g, n, page, nkv, hd, dtype=dtype).permute(2, 0, 1, 3))
+    table = torch.randperm(n, generator=g, device="cuda")[:batch * per_seq].view(batch, per_seq).to(torch.int32).contiguous()
+    return pools[0], pools[1], table
+
+
+# ------------------------------------------------------------------------------------------------ append with norms
+def append64(qkv, gains, eps, table, before, rope, starts, nkv, pool_shape):
+    """Rows' (page, token, queries, keys, values, sizes of the rotation's terms) in 64 bits; rows that are skipped are missing."""
+    rows, heads, hd = qkv.shape
+    nq, (n_pages, page) = heads - 2 * nkv, pool_shape
+    x, t, table = qkv.double().cpu(), rope.double().cpu(), table.cpu()
+    gain = torch.ones(nq + nkv, hd, dtype=torch.float64)
+    for g, at in zip(gains, (slice(0, nq), slice(nq, None))):
+        if g is not None:
+            gain[at] = g.double().cpu()
+    found = {}
+    for b, len0 in enumerate(before):
+        for r in range(starts[b], min(starts[b + 1], rows)):
+            p = len0 + r - starts[b]
+            if len0 < 0 or p >= t.shape[0] or p >= table.shape[1] * page or not 0 <= int(table[b, p // page]) < n_pages:
+                continue
+            z = x[r, :nq + nkv]
+            z = z / torch.sqrt(z.square().mean(dim=1, keepdim=True) + eps) * gain
+            lo, hi = z[:, :hd // 2], z[:, hd // 2:]
+            y = torch.cat((lo * t[p, 0] - hi * t[p, 1], hi * t[p, 0] + lo * t[p, 1]), dim=1)
+            size = torch.cat(((lo * t[p, 0]).abs() + (hi * t[p, 1]).abs(), (hi * t[p, 0]).abs() + (lo * t[p, 1]).abs()), dim=1)
+            found[r] = (int(table[b, p // page]), p % page, y[:nq], y[nq:], x[r, nq + nkv:], size)
+    return found
+
+
+def check_append(lib, qkv, gains, eps, k, v, table, before, rope, starts=None):
+    nkv, n_pages, page, hd = k.shape
+    q_out = torch.full((qkv.shape[0], qkv.shape[1] - 2 * nkv, hd), 7.0, dtype=k.dtype, device="cuda")
+    k0, v0 = k.clone(), v.clone()
+    edges = list(range(len(before) + 1)) if starts is None else starts
+    found = append64(qkv, gains, eps, table, before, rope, edges, nkv, (n_pages, page))
+    assert lib.hsd_kv_append_norm(qkv, *gains, eps, k, v, table, ints(before), rope, None if starts is None else ints(starts), q_out) is q_out
+    touched = torch.zeros(n_pages, page, dtype=torch.bool)
+    step = HALF_STEP[k.dtype]
+    kc, vc, qc = k.cpu(), v.cpu(), q_out.cpu()
+    for r, (pg, t, qy, ky, vx, size) in found.items():
+        touched[pg, t] = True
+        for out, want, s in ((qc[r], qy, size[:qy.shape[0]]), (kc[:, pg, t], ky, size[qy.shape[0]:])):
+            # the mean: a chain of 16 and three sums, halved by the root; root, two products, the rotation's three operations
+            assert bool(((out.double() - want).abs() <= step * want.abs() + 18 * 2.0 ** -24 * s + 1e-37).all())
+        assert torch.equal(vc[:, pg, t], vx.to(FP32).to(k.dtype))
+    left = torch.tensor([r for r in range(qkv.shape[0]) if r not in found], dtype=torch.long, device="cuda")
+    assert bool((q_out[left] == 7.0).all())                                  # skipped rows: as they were
+    keep = ~touched.cuda()
+    assert torch.equal(k[:, keep], k0[:, keep]) and torch.equal(v[:, keep], v0[:, keep])
+    k.copy_(k0), v.copy_(v0)
+    zeros = lib.hsd_kv_append_norm(qkv, *gains, eps, k, v, table, ints(before), rope, None if starts is None else ints(starts))
+    assert bool((zeros[left] == 0).all()) and torch.equal(zeros[sorted(found)], q_out[sorted(found)])
+    return found
+
+
+@pytest.mark.parametrize("source", [BF16, FP32])
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("hd,nq,nkv,page,order", [(32, 5, 2, 16, "head"), (64, 1, 1, 3, "token"), (128, 8, 2, 16, "token"), (64, 0, 3, 8, "head"), (128, 1, 1, 16, "head")])
+def test_append_norm_one_token_each(lib, source, dtype, hd, nq, nkv, page, order):
+    g = gen(hd + nq)
+    before = [0, 1, 15, 16, 31, -1, 40]
+    k, v, table = cache(g, 7, nkv, hd, page, -(-41 // page), dtype, order)
+    gains = [1 + randn(g, hd, std=0.3).to(source) for _ in range(2)]
+    found = check_append(lib, randn(g, 7, nq + 2 * nkv, hd, dtype=source, std=3.0), gains, 1e-6, k, v, table, before, lib.rope_table(64, hd))
+    assert sorted(found) == [0, 1, 2, 3, 4, 6]
+
+
+@pytest.mark.parametrize("gains", [(None, None), (FP32, None), (None, BF16)])
+@pytest.mark.parametrize("eps", [0.0, 1e-5, 10.0])
+def test_append_norm_without_gains_and_other_eps(lib, gains, eps):
+    g = gen(2)
+    k, v, table = cache(g, 3, 2, 64, 16, 2, FP32)
+    gains = [None if t is None else randn(g, 64, dtype=t) for t in gains]
+    check_append(lib, randn(g, 3, 7, 64, std=1e-3), gains, eps, k, v, table, [3, 0, 31], lib.rope_table(64, 64))
+
+
+@pytest.mark.parametrize("rows", [1, 40, 2503])
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_append_norm_ragged_rows(lib, rows, dtype):
+    g = gen(rows)
+    batch = 70
+    cut = sorted(torch.randint(0, rows + 1, (batch - 1,), generator=torch.Generator().manual_seed(rows)).tolist())
+    starts = [0] + cut + [rows]
+    before = [(i * 37) % 50 for i in range(batch)]
+    longest = max(b + starts[i + 1] - starts[i] for i, b in enumerate(before))
+    k, v, table = cache(g, batch, 1, 32, 16, -(-longest // 16), dtype)
+    gains = [randn(g, 32), randn(g, 32)]
+    assert len(check_append(lib, randn(g, rows, 4, 32), gains, 1e-6, k, v, table, before, lib.rope_table(longest, 32), starts)) == rows
+
+
+def test_append_norm_skips_what_has_no_place_and_takes_rows_that_lie_apart(lib):
+    g = gen(3)
+    k, v, table = cache(g, 4, 1, 64, 16, 2, BF16)
+    table[1, 1], table[2, 0] = -1, k.shape[1]
+    qkv = randn(g, 30, 5 * 64)[:, 64:256].unflatten(1, (3, 64))
+    found = check_append(lib, qkv, [randn(g, 64), None], 1e-6, k, v, table, [28, 14, 0, 18], lib.rope_table(30, 64), [2, 8, 13, 16, 25])
+    assert sorted(found) == [2, 3, 8, 9] + list(range(16, 25))
+
+
+def test_append_norm_of_zeros_and_of_values_that_are_not_finite(lib):
+    g = gen(4)
+    k, v, table = cache(g, 1, 2, 64, 16, 1, FP32)
+    qkv = randn(g, 1, 6, 64)
+    qkv[0, 0], qkv[0, 1, 3], qkv[0, 4, 5] = 0, float("nan"), float("inf")
+    q = lib.hsd_kv_append_norm(qkv, None, None, 1e-6, k, v, table, ints([0]), lib.rope_table(4, 64))
+    at = int(table[0, 0])
+    assert bool((q[0, 0] == 0).all()) and bool(q[0, 1].isnan().all())
+    assert bool(k[:, at, 0].isfinite().all()) and torch.equal(v[:, at, 0], qkv[0, 4:])
+
+
+# ------------------------------------------------------------------------------------------------ 8-bit products
+def quantize64(x):
+    """(codes as doubles, scales): the nearest whole numbers of scales of 32 bits."""
+    x = x.double()
+    bad = ~x.isfinite().all(dim=1)
+    scale = (x.abs().amax(dim=1) / 127).float()
+    c = torch.round(x / torch.where(scale > 0, scale, torch.ones_like(scale)).double()[:, None]).clamp(-127, 127)
+    c[bad] = 0
+    scale[bad] = float("nan")
+    return c, scale
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("rows,K", [(1, 1), (3, 7), (5, 16), (2, 255), (7, 4096), (300, 1000), (2, 16384), (3, 16392), (1, 50001), (4095, 64)])
+def test_quantized_rows(lib, dtype, rows, K):
+    g = gen(K + rows)
+    x = randn(g, rows, K, dtype=dtype, std=2.0)
+    codes, scales = lib.hsd_quantize_rows(x)
+    assert codes.dtype == torch.int8 and codes.shape == (rows, K) and scales.dtype == FP32 and scales.shape == (rows,)
+    c, s = quantize64(x)
+    assert torch.equal(scales, s) and torch.equal(codes.double(), c)
+
+
+def test_quantized_rows_between_two_codes(lib):
+    """Values at and next to the middle of two codes, where a quotient's own rounding would decide."""
+    g = gen(1)
+    scale = torch.rand(64, 1, generator=g, device="cuda") * 10.0 ** torch.randint(-30, 30, (64, 1), generator=g, device="cuda").float()
+    half = torch.arange(-126, 126, device="cuda") + 0.5
+    x = (half * scale.double()).float()
+    x = torch.cat((x, torch.nextafter(x, torch.zeros_like(x)), torch.nextafter(x, 1e38 * torch.ones_like(x)), 127 * scale), dim=1)
+    codes, scales = lib.hsd_quantize_rows(x)
+    c, s = quantize64(x)
+    assert torch.equal(scales, s) and torch.equal(codes.double(), c)
+    y = half.repeat(3, 1).contiguous()
+    y[:, 0] = 127                                                            # scale 1: exact middles go to the even code
+    assert torch.equal(lib.hsd_quantize_rows(y)[0].double(), y.double().round())
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_quantized_rows_of_zeros_small_and_large_values_and_what_is_not_finite(lib, dtype):
+    x = randn(gen(2), 9, 64, dtype=dtype)
+    x[0] = 0
+    x[1, 5], x[2, 6], x[3, 7] = float("inf"), float("nan"), -float("inf")
+    x[4] *= torch.finfo(dtype).tiny                                          # subnormal scales
+    x[5] = torch.finfo(dtype).max * torch.where(x[5] > 0, 1.0, -1.0).to(dtype)
+    x[6] = 0
+    x[6, 3] = torch.finfo(dtype).smallest_normal / 64                        # the scale is 0 or the smallest number
+    x[7] *= 1e-33
+    codes, scales = lib.hsd_quantize_rows(x)
+    c, s = quantize64(x)
+    assert torch.equal(scales.nan_to_num(-1), s.nan_to_num(-1)) and torch.equal(codes.double(), c)
+
+
+def test_quantized_rows_that_lie_apart(lib):
+    x = randn(gen(3), 11, 200, dtype=BF16)
+    for part in (x[:, 8:136], x[:, 3:135], x[::2], x[:1, 1:70]):
+        codes, scales = lib.hsd_quantize_rows(part)
+        c, s = quantize64(part)
+        assert torch.equal(scales, s) and torch.equal(codes.double(), c)
+
+
+def check_w8(lib, A, codes, scales, out_dtype=FP32, **more):
+    got = lib.hsd_gemm_w8(A, codes, scales, out_dtype, **more)
+    c, s = (A, more["a_scales"]) if A.dtype == torch.int8 else quantize64(A)
+    want = torch.cat([(c.double() @ codes[n:n + 8192].double().T) for n in range(0, codes.shape[0], 8192)], dim=1) * torch.outer(s.double(), scales.double())
+    assert got.dtype == out_dtype and got.shape == want.shape
+    # the whole number's rounding, two products, the output's own
+    off, bound = (got.double() - want).abs(), (3.01 * 2.0 ** -24 + (2.0 ** -8 if out_dtype == BF16 else 0)) * want.abs() + 1e-37
+    assert bool((off <= bound).all()), (float((off / bound).max()), int((off > bound).sum()))
+    return got
+
+
+def weights(g, N, K):
+    return torch.randint(-128, 128, (N, K), generator=g, device="cuda", dtype=torch.int8), 0.01 * (0.1 + torch.rand(N, generator=g, device="cuda"))
+
+
+@pytest.mark.parametrize("rows", [1, 2, 15, 16, 17, 32, 33, 64, 65, 128, 129, 255, 256, 257, 300, 513])
+@pytest.mark.parametrize("N,K", [(1, 16), (17, 144), (100, 4096), (1001, 2064)])
+def test_w8_products(lib, rows, N, K):
+    g = gen(N + rows)
+    codes, scales = weights(g, N, K)
+    check_w8(lib, randn(g, rows, K, dtype=BF16), codes, scales)
+    check_w8(lib, randn(g, rows, K), codes, scales, BF16)
+
+
+@pytest.mark.parametrize("rows,N,K,out", [(1, 4096, 4096, FP32), (1, 6144, 4096, BF16), (16, 28672, 4096, FP32), (200, 2048, 5632, BF16), (144, 32000, 2048, FP32),
+                                          (40, 300, 14336, FP32), (700, 6144, 4096, BF16), (2049, 4096, 1024, FP32), (3, 9473, 512, FP32)])
+def test_w8_products_of_layers(lib, rows, N, K, out):
+    g = gen(N)
+    A, (codes, scales) = randn(g, rows, K, dtype=BF16), weights(g, N, K)
+    got = check_w8(lib, A, codes, scales, out)
+    into = torch.empty(rows, N, dtype=out, device="cuda")
+    assert lib.hsd_gemm_w8(A, codes, scales, out, out=into) is into and torch.equal(into, got)
+    a, s = lib.hsd_quantize_rows(A)
+    assert torch.equal(check_w8(lib, a, codes, scales, out, a_scales=s), got)
+
+
+@pytest.mark.parametrize("rows", [5, 300])
+def test_w8_sums_are_exact_at_their_largest(lib, rows):
+    K = (1 << 17) - 16
+    A, w = torch.full((rows, K), -128, dtype=torch.int8, device="cuda"), torch.full((200, K), -128, dtype=torch.int8, device="cuda")
+    w[::2], w[7], w[7, 5] = 127, 0, 1
+    got = lib.hsd_gemm_w8(A, w, torch.ones(200, device="cuda"), a_scales=torch.ones(rows, device="cuda"))
+    want = torch.full((200,), 16384.0 * K, dtype=torch.float64)
+    want[::2], want[7] = -128.0 * 127 * K, -128
+    assert torch.equal(got.cpu(), want.float().expand(rows, 200))
+
+
+@pytest.mark.parametrize("rows", [3, 400])
+def test_w8_keeps_what_is_not_finite_to_its_row(lib, rows):
+    g = gen(5)
+    A, (codes, scales) = randn(g, rows, 256, dtype=BF16), weights(g, 300, 256)
+    want = lib.hsd_gemm_w8(A, codes, scales)
+    A2, s2 = A.clone(), scales.clone()
+    A2[1, 7], s2[5] = float("nan"), float("inf")
+    A2[2] = 0
+    got = lib.hsd_gemm_w8(A2, codes, s2)
+    other, cols = [r for r in range(rows) if r not in (1, 2)], [i for i in range(300) if i != 5]
+    assert bool(got[1].isnan().all()) and not bool(got[other][:, 5].isfinite().any()) and bool((got[2][cols] == 0).all())
+    assert torch.equal(got[other][:, cols], want[other][:, cols])
+
+
+def test_w8_packed_weights_near_the_bf16_product(lib):
+    g = gen(6)
+    W, A = randn(g, 200, 512, dtype=BF16, std=0.02), randn(g, 40, 512, dtype=BF16)
+    codes, scales = lib.hsd_quantize_rows(W)
+    got = check_w8(lib, A, codes, scales)
+    c, s = quantize64(A)
+    # a weight is off by half of its row's scale at most, and an activation too
+    a = (c * s.double()[:, None]).abs()
+    bound = 0.5001 * (a.sum(dim=1)[:, None] * scales.double() + s.double()[:, None] * W.double().abs().sum(dim=1))
+    assert bool(((got.double() - A.double() @ W.double().T).abs() <= bound).all())
+
+
+def test_w8_captured_on_other_streams_and_two_at_once(lib):
+    g = gen(7)
+    codes, scales = weights(g, 3000, 1024)
+    xs = [randn(g, n, 1024, dtype=BF16) for n in (9, 300)]
+    want = [lib.hsd_gemm_w8(x, codes, scales) for x in xs]
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for x in xs:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs.append(lib.hsd_gemm_w8(x, codes, scales))
+        graphs.append(graph)
+    fresh = [randn(g, *x.shape, dtype=BF16) for x in xs]
+    for new in (xs, fresh):
+        keep = [x.clone() for x in new]
+        for x, y in zip(xs, keep):
+            x.copy_(y)
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        for x, out in zip(xs, outs):
+            assert torch.equal(out, lib.hsd_gemm_w8(x, codes, scales))
+    assert not torch.equal(outs[0], want[0])
+    want = [lib.hsd_gemm_w8(x, codes, scales) for x in xs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in xs]
+    got = [[] for _ in xs]
+    for _ in range(20):
+        for i, (x, st) in enumerate(zip(xs, streams)):
+            with torch.cuda.stream(st):
+                got[i].append(lib.hsd_gemm_w8(x, codes, scales))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(y, want[i]) for y in got[i])
