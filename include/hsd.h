@@ -411,6 +411,32 @@ int hsd_paged_attention(const void *q, int batch, int n_q_heads, int n_kv_heads,
                         const int32_t *page_table, int pages_per_seq, const int32_t *kv_lens, float scale, void *workspace,
                         size_t workspace_bytes, void *out, void *stream);
 
+/* Attention of a batch whose sequences share a prefix (samples of one prompt, drafts of them being verified), a few new tokens of each:
+ * out[r, h] = sum_j softmax_j(scale q[r, h] . k_j) v_j.  Of sequence b's n rows the i-th sees the positions j < kv_lens[b] - n + 1 + i (the
+ * new tokens' own keys are among them once they have been appended: pass the lengths after the append): those below P = *prefix_len
+ * on the prefix's pages, which are read once for the whole batch, the others on the sequence's own.  Softmax and sums in fp32, rounded once.
+ *   q, out         device [rows, n_q_heads, head_dim] in the pool's type, 16-byte aligned; n_q_heads a multiple of n_kv_heads
+ *   page_table     device [batch, pages_per_seq] int32: position p of a sequence in page page_table[b * pages_per_seq + p / page_size], as
+ *                  for the other calls; entries of whole pages below P are not read.  kv_lens device [batch] int32 counts the prefix too.  0 or
+ *                  less: the rows' outputs are zeros; more than the table (and the prefix) has room for: its room
+ *   row_starts     device [batch + 1] int32, not descending: rows row_starts[b] .. row_starts[b+1]-1 are sequence b's; NULL: rows == batch, a
+ *                  row each.  Rows in front of the first and from row_starts[batch] on: zeros (zeros != 0), or left as they were
+ *   prefix_pages   device [n_prefix_pages] int32: pages of the positions 0 .. P - 1;  prefix_len device [1] int32 (0 or less: no prefix;
+ *                  more than the pages have room for: their room).  P need not be whole pages; the last page of the list may be a copy
+ *   scale          finite, also times log2(e)
+ *   workspace      device, 256-byte aligned, at least hsd_prefix_attention_workspace_bytes(...) (0 = bad sizes); contents on entry are ignored
+ * Keys on a page that is not in [0, n_pages) count as absent; memory behind a sequence's or the prefix's last key is not used, whatever it
+ * holds; keys and values that are there and not finite may make their heads' outputs NaN.  Lists are read by the kernels only, so a captured
+ * call follows their changes.  How keys are divided, and so the order of the fp32 sums, follows the lengths of the whole batch.
+ * Errors: INVALID_ARG, UNSUPPORTED (head_dim not in {32, 64, 128}), TOO_LARGE (batch over 4096, over 65536 query heads, rows * n_q_heads over
+ * 2^26, (rows * n_q_heads / n_kv_heads + 8 batch + 8) * positions over 2^37), WORKSPACE_TOO_SMALL, CUDA; DEVICE_TIMEOUT is reported by
+ * hsd_gemm_status(workspace, stream). */
+size_t hsd_prefix_attention_workspace_bytes(int rows, int n_q_heads, int n_kv_heads, int head_dim);
+int hsd_prefix_attention(const void *q, int rows, int n_q_heads, int n_kv_heads, int head_dim, const hsd_kv_pool *pool,
+                         const int32_t *page_table, int pages_per_seq, const int32_t *kv_lens, const int32_t *row_starts, int batch,
+                         const int32_t *prefix_pages, int n_prefix_pages, const int32_t *prefix_len, float scale, void *workspace,
+                         size_t workspace_bytes, int zeros, void *out, void *stream);
+
 /* hsd_gemm_bf16 with 4-bit weights, for few rows: out[r, n] = sum_k A[r, k] (codes[n, k] - 8) scales[n, k / group].  Products exact,
  * sums in fp32 in a fixed order; a group's are added before they are scaled, so |A| has to be below 2^118.  For up to eight rows, up to 16
  * of large matrices and 32 with groups of 128: past those hsd_gemm_bf16 takes less time on the unpacked weights (28672 x 4096: 25 against 40 us with 16 rows, 57 against 44

@@ -53,8 +53,8 @@ def _host_calls():
                    (lib.hsd_draft_sample, lib.hsd_verify_workspace_bytes, lib.hsd_verify_level, lib.hsd_gemm_workspace_bytes,
                     lib.hsd_gemm_bf16, lib.hsd_gemm_status, lib.hsd_strerror, lib.hsd_kv_append, lib.hsd_paged_attention_workspace_bytes,
                     lib.hsd_paged_attention, lib.hsd_gemm_w4_workspace_bytes, lib.hsd_gemm_w4, lib.hsd_token_logprobs,
-                    lib.hsd_kv_append_zeros, lib.hsd_kv_append_norm, lib.hsd_quantize_rows, lib.hsd_gemm_w8_workspace_bytes, lib.hsd_gemm_w8)),
-                 HsdError)
+                    lib.hsd_kv_append_zeros, lib.hsd_kv_append_norm, lib.hsd_quantize_rows, lib.hsd_gemm_w8_workspace_bytes, lib.hsd_gemm_w8,
+                    lib.hsd_prefix_attention_workspace_bytes, lib.hsd_prefix_attention)), HsdError)
         _host = mod
     return _host
 
@@ -224,6 +224,10 @@ def _declare_engine(lib):
     lib.hsd_paged_attention_workspace_bytes.argtypes = [i32, i32, i32]
     lib.hsd_paged_attention.restype = i32
     lib.hsd_paged_attention.argtypes = [vp, i32, i32, i32, i32, c.POINTER(_KvPool), vp, i32, vp, c.c_float, vp, sz, vp, vp]
+    lib.hsd_prefix_attention_workspace_bytes.restype = sz
+    lib.hsd_prefix_attention_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    lib.hsd_prefix_attention.restype = i32
+    lib.hsd_prefix_attention.argtypes = [vp, i32, i32, i32, i32, c.POINTER(_KvPool), vp, i32, vp, vp, i32, vp, i32, vp, c.c_float, vp, sz, i32, vp, vp]
     lib.hsd_gemm_w4_workspace_bytes.restype = sz
     lib.hsd_gemm_w4_workspace_bytes.argtypes = [i32, i32, i32, i32]
     lib.hsd_gemm_w4.restype = i32
@@ -546,6 +550,18 @@ def hsd_paged_attention(q, k_pool, v_pool, page_table, kv_lens, scale=None, work
     """Attention of one token per sequence, q [batch, n_q, head_dim], over the keys at positions below kv_lens int32 [batch] of the
     pools (as hsd_kv_append's) -> [batch, n_q, head_dim] in their type.  scale None: head_dim ** -0.5."""
     return (_host or _host_calls()).paged_attention(q, k_pool, v_pool, page_table, kv_lens, scale, workspace, out)
+
+
+def hsd_prefix_attention_workspace_bytes(rows, n_q_heads, n_kv_heads, head_dim):
+    return int(library().hsd_prefix_attention_workspace_bytes(rows, n_q_heads, n_kv_heads, head_dim))
+
+
+def hsd_prefix_attention(q, k_pool, v_pool, page_table, kv_lens, prefix_pages, prefix_len, row_starts=None, scale=None, workspace=None, out=None):
+    """Attention of a few tokens per sequence, q [rows, n_q, head_dim], whose sequences share their first prefix_len (int32 [1]) positions, on
+    prefix_pages int32 [pages]: read once for all.  The others lie on page_table int32 [batch, pages], kv_lens int32 [batch] counts both;
+    row_starts int32 [batch + 1], or None: a row each.  -> [rows, n_q, head_dim] in the pools' type; rows without a sequence are zeros, or
+    what `out` held if it is given.  scale None: head_dim ** -0.5."""
+    return (_host or _host_calls()).prefix_attention(q, k_pool, v_pool, page_table, kv_lens, prefix_pages, prefix_len, row_starts, scale, workspace, out)
 
 
 def hsd_gemm_w4_workspace_bytes(R, N, K, group):

@@ -16,9 +16,7 @@
 // 234.)  What lies below TF32's smallest number, 2^-136, is lost.
 // The tensor cores' adders cut off: a chain of products loses up to 2^-23 of its sum a product (1.2e-4 of the output over 20000 keys
 // a sequence when the chain was a stretch).  So no chain is longer than a tile; tiles' products are added in fp32, rounded to nearest.
-#include <math.h>
-
-#include "paged.cuh"
+#include "attn_tiles.cuh"
 
 namespace hsd {
 namespace {
@@ -40,70 +38,8 @@ struct DecodeArgs {
   int group, chunk, chunks;                    // query heads of a key head; of them at once; times
 };
 
-// Keys of a tile (8 KB of keys and values, 4 KB for heads of 32) and query heads of one pass over them at most.
-template <typename T, int HD> struct Form {
-  static constexpr int KEYS = (HD == 128 ? 16 : 32) / ((int)sizeof(T) / 2), HEADS = sizeof(T) == 4 ? 8 : 16;
-};
-template <typename T, int HD> struct Ring {
-  static constexpr int ROW = HD * (int)sizeof(T), HALF = Form<T, HD>::KEYS * ROW, STAGE = 2 * HALF;    // keys, then values
-  static constexpr int STAGES = 24576 / STAGE, BYTES = STAGE * STAGES;
-};
-
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ void copy16(u32 to, const void *from, bool there) {       // zeros where there is nothing to read
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-__device__ __forceinline__ void mma(float *c, const u32 *a, u32 b0, u32 b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ void mma_tf32(float *c, const u32 *a, u32 b0, u32 b1) {
-  asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-// x = part[0] + part[1] + part[2], all of it: the first 11 bits, the next 11, the last two (four operations; NaN stays NaN, as do infinities).
-__device__ __forceinline__ void split3(float x, u32 *part) {
-  part[0] = __float_as_uint(x) & 0xFFFFE000u;
-  const float rest = x - __uint_as_float(part[0]);
-  part[1] = __float_as_uint(rest) & 0xFFFFE000u;
-  part[2] = __float_as_uint(rest - __uint_as_float(part[1]));
-}
-// x = high + mid to a last place: rounded to 11 bits, what is left rounded to 11 bits.  (For few numbers: the conversion has a quarter of the
-// rate.)  What rounding would make infinite is cut off.
-__device__ __forceinline__ void split2(float x, u32 &high, u32 &mid) {
-  asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(high) : "f"(x));
-  if (fabsf(x) > 3.4e38f) high = __float_as_uint(x) & 0xFFFFE000u;
-  asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(mid) : "f"(x - __uint_as_float(high)));
-}
-__device__ __forceinline__ float4 lds4(u32 at) {
-  float4 v;
-  asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
-  return v;
-}
-__device__ __forceinline__ void ldsm4(u32 *r, u32 at) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
-}
-__device__ __forceinline__ void ldsm4t(u32 *r, u32 at) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
-}
-// Byte of 16-byte piece c of row r of a tile: permuted so that the pieces a quarter warp reads together lie in different banks.
-template <typename T, int HD> __device__ __forceinline__ u32 piece(int r, int c) {
-  if constexpr (sizeof(T) == 4) return r * (HD * 4) + ((c ^ ((r & 1) << 2) ^ (r & 6)) << 4);
-  else if constexpr (HD == 32) return r * 64 + ((c ^ ((r >> 1) & 3)) << 4);
-  else return r * (HD * 2) + ((c ^ (r & 7)) << 4);
-}
-
 // The line of tiles: sequence b has as many for each of `items` (key head, chunk of query heads); before[b]: tiles of the
 // sequences in front of b, per item; lens[b]: keys.
-__device__ __forceinline__ long long divide(long long a, long long b) {          // (32 bits do nearly always, in a fourth of the time)
-  return ((a | b) >> 31) == 0 ? (long long)((u32)a / (u32)b) : a / b;
-}
 struct Line {
   const int *before, *lens;
   int batch, items, stretches;
@@ -300,282 +236,13 @@ template <typename T, int HD> struct Feeder {
   }
 };
 
-// ---------------------------------------------------------------------------- bf16
-// Two weights (at most 1) as three bf16 parts of each, all of their 24 bits.
-__device__ __forceinline__ void split3(float x, float y, u32 *part) {
-#pragma unroll
-  for (int e = 0; e < 3; ++e) {
-    const __nv_bfloat162 z = __floats2bfloat162_rn(x, y);
-    part[e] = *reinterpret_cast<const u32 *>(&z);
-    x -= __low2float(z);
-    y -= __high2float(z);
-  }
-}
-template <int HD, int H> struct Bf16Tile {     // H: 8 or 16 rows with queries
-  using T = __nv_bfloat16;
-  static constexpr int YS = H / 8, PRODUCTS = YS == 1 ? 2 : 3;         // with the values
-  u32 qf[HD / 16][4];
-  float o[HD / 8][2 * YS], m[2], l[2];
-  int lane;
-
-  // Rows of the tile: the chunk's query heads; rows without one are zeros.
-  __device__ __forceinline__ void begin(const DecodeArgs &a, int b, int item) {
-    const int h = item / a.chunks, c = item % a.chunks, heads = min(a.chunk, a.group - c * a.chunk);
-    const T *q = static_cast<const T *>(a.q) + ((size_t)b * a.nq + (size_t)h * a.group + c * a.chunk) * HD;
-    const int r = lane >> 2, col = (lane & 3) * 2;
-#pragma unroll
-    for (int k = 0; k < HD / 16; ++k)
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const int row = r + (x & 1) * 8;
-        qf[k][x] = (x & 1) < YS && row < heads ? __ldg(reinterpret_cast<const u32 *>(q + row * HD + k * 16 + col + (x >> 1) * 8)) : 0u;
-      }
-#pragma unroll
-    for (int n = 0; n < HD / 8; ++n)
-#pragma unroll
-      for (int x = 0; x < 2 * YS; ++x) o[n][x] = 0.f;
-    m[0] = m[1] = -INFINITY;
-    l[0] = l[1] = 0.f;
-  }
-  __device__ __forceinline__ void tile(const DecodeArgs &a, u32 at, u32 there) {
-    constexpr int KB = Form<T, HD>::KEYS / 16;                         // blocks of 16 keys
-    float s[2 * KB][4];
-#pragma unroll
-    for (int n = 0; n < 2 * KB; ++n)
-#pragma unroll
-      for (int x = 0; x < 4; ++x) s[n][x] = 0.f;
-    const int kr = (lane & 7) + ((lane >> 4) << 3), kc = (lane >> 3) & 1;
-#pragma unroll
-    for (int k = 0; k < HD / 16; ++k)
-#pragma unroll
-      for (int b = 0; b < KB; ++b) {
-        u32 f[4];
-        ldsm4(f, at + piece<T, HD>(b * 16 + kr, 2 * k + kc));
-        mma(s[2 * b], qf[k], f[0], f[1]);
-        mma(s[2 * b + 1], qf[k], f[2], f[3]);
-      }
-    const int col = (lane & 3) * 2;
-    float mx[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-    for (int n = 0; n < 2 * KB; ++n)
-#pragma unroll
-      for (int x = 0; x < 2 * YS; ++x) {
-        s[n][x] = (there >> (n * 8 + col + (x & 1))) & 1 ? s[n][x] * a.scale : -INFINITY;
-        mx[x >> 1] = fmaxf(mx[x >> 1], s[n][x]);
-      }
-    u32 w[KB][PRODUCTS][4];
-    float f[2] = {1.f, 1.f};
-    bool grown = false;
-#pragma unroll
-    for (int y = 0; y < YS; ++y) {
-      mx[y] = fmaxf(mx[y], __shfl_xor_sync(0xFFFFFFFFu, mx[y], 1));
-      mx[y] = fmaxf(mx[y], __shfl_xor_sync(0xFFFFFFFFu, mx[y], 2));
-      const float n = fmaxf(m[y], mx[y]), ref = n > -INFINITY ? n : 0.f;
-      f[y] = ex2(m[y] - ref);
-      grown |= n > m[y];
-      m[y] = n;
-      l[y] *= f[y];
-#pragma unroll
-      for (int n2 = 0; n2 < 2 * KB; ++n2) {
-        const float p0 = ex2(s[n2][2 * y] - ref), p1 = ex2(s[n2][2 * y + 1] - ref);
-        l[y] += p0 + p1;
-        u32 part[3];
-        split3(p0, p1, part);
-        if constexpr (YS == 1) {               // rows 8 to 15: the middle parts
-          w[n2 / 2][0][n2 % 2 * 2] = part[0]; w[n2 / 2][0][n2 % 2 * 2 + 1] = part[1];
-          w[n2 / 2][1][n2 % 2 * 2] = part[2]; w[n2 / 2][1][n2 % 2 * 2 + 1] = 0;
-        } else {
-#pragma unroll
-          for (int e = 0; e < 3; ++e) w[n2 / 2][e][n2 % 2 * 2 + y] = part[e];
-        }
-      }
-    }
-    if (__any_sync(0xFFFFFFFFu, grown)) {
-#pragma unroll
-      for (int n = 0; n < HD / 8; ++n)
-#pragma unroll
-        for (int x = 0; x < 2 * YS; ++x) o[n][x] *= f[x >> 1];
-    }
-    const u32 v = at + Ring<T, HD>::HALF;
-    const int vr = lane & 15, vc = lane >> 4;
-#pragma unroll
-    for (int n = 0; n < HD / 16; ++n) {
-      float d[2][4];                           // of this tile alone
-#pragma unroll
-      for (int x = 0; x < 4; ++x) d[0][x] = d[1][x] = 0.f;
-#pragma unroll
-      for (int b = 0; b < KB; ++b) {
-        u32 x[4];
-        ldsm4t(x, v + piece<T, HD>(b * 16 + vr, 2 * n + vc));
-#pragma unroll
-        for (int e = PRODUCTS - 1; e >= 0; --e) {                      // the small ones first
-          mma(d[0], w[b][e], x[0], x[1]);
-          mma(d[1], w[b][e], x[2], x[3]);
-        }
-      }
-#pragma unroll
-      for (int x = 0; x < 2 * YS; ++x) {
-        o[2 * n][x] += YS == 1 ? d[0][x] + d[0][2 + x] : d[0][x];
-        o[2 * n + 1][x] += YS == 1 ? d[1][x] + d[1][2 + x] : d[1][x];
-      }
-    }
-  }
-  __device__ __forceinline__ void end(const DecodeArgs &a, int b, int item, bool whole, float *part) {
-    const int h = item / a.chunks, c = item % a.chunks, heads = min(a.chunk, a.group - c * a.chunk), col = (lane & 3) * 2;
-    T *out = static_cast<T *>(a.out) + ((size_t)b * a.nq + (size_t)h * a.group + c * a.chunk) * HD;
-#pragma unroll
-    for (int y = 0; y < YS; ++y) {
-      l[y] += __shfl_xor_sync(0xFFFFFFFFu, l[y], 1);
-      l[y] += __shfl_xor_sync(0xFFFFFFFFu, l[y], 2);
-      const int row = (lane >> 2) + 8 * y;
-      if (row >= heads) continue;
-      if (whole) {
-        const float inv = l[y] != 0.f ? 1.f / l[y] : 0.f;
-#pragma unroll
-        for (int n = 0; n < HD / 8; ++n)
-          *reinterpret_cast<__nv_bfloat162 *>(out + row * HD + n * 8 + col) = __floats2bfloat162_rn(o[n][2 * y] * inv, o[n][2 * y + 1] * inv);
-      } else {
-#pragma unroll
-        for (int n = 0; n < HD / 8; ++n) *reinterpret_cast<float2 *>(part + row * HD + n * 8 + col) = make_float2(o[n][2 * y], o[n][2 * y + 1]);
-        if ((lane & 3) == 0) *reinterpret_cast<float2 *>(part + a.chunk * HD + row * 2) = make_float2(m[y], l[y]);
-      }
-    }
-  }
-};
-
-// ---------------------------------------------------------------------------- fp32
-// A lane's four values of a 16-byte piece are its k = j and j + 4 of two steps (keys) or its columns of four tiles (values): any order
-// of k will do that both factors have, and of columns that the output is written in.
-template <int HD> struct Fp32Tile {
-  using T = float;
-  u32 q[HD / 8][4];                            // rows 0 to 7 of the tile: the queries' high parts, rows 8 to 15: the rest
-  float o[HD / 8][2], m, l;
-  int lane;
-
-  __device__ __forceinline__ void begin(const DecodeArgs &a, int b, int item) {
-    const int h = item / a.chunks, c = item % a.chunks, heads = min(a.chunk, a.group - c * a.chunk), r = lane >> 2, j = lane & 3;
-    const float *from = static_cast<const float *>(a.q) + ((size_t)b * a.nq + (size_t)h * a.group + c * a.chunk + r) * HD;
-#pragma unroll
-    for (int i = 0; i < HD / 16; ++i) {
-      const float4 x = r < heads ? __ldg(reinterpret_cast<const float4 *>(from + i * 16 + j * 4)) : make_float4(0.f, 0.f, 0.f, 0.f);
-      split2(x.x, q[2 * i][0], q[2 * i][1]);
-      split2(x.y, q[2 * i][2], q[2 * i][3]);
-      split2(x.z, q[2 * i + 1][0], q[2 * i + 1][1]);
-      split2(x.w, q[2 * i + 1][2], q[2 * i + 1][3]);
-    }
-#pragma unroll
-    for (int n = 0; n < HD / 8; ++n) o[n][0] = o[n][1] = 0.f;
-    m = -INFINITY;
-    l = 0.f;
-  }
-  __device__ __forceinline__ void tile(const DecodeArgs &a, u32 at, u32 there) {
-    constexpr int KB = Form<T, HD>::KEYS / 8;                          // blocks of 8 keys
-    const int r = lane >> 2, j = lane & 3;
-    float p[KB][2], mx = -INFINITY;
-#pragma unroll
-    for (int b = 0; b < KB; ++b) {
-      float s[3][2][4];                        // of each part of the keys; two chains of each
-#pragma unroll
-      for (int e = 0; e < 3; ++e)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) s[e][0][x] = s[e][1][x] = 0.f;
-#pragma unroll
-      for (int i = 0; i < HD / 16; ++i) {
-        const float4 k = lds4(at + piece<T, HD>(b * 8 + r, i * 4 + j));
-        const float x[4] = {k.x, k.y, k.z, k.w};
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          u32 k0[3], k1[3];
-          split3(x[2 * y], k0);
-          split3(x[2 * y + 1], k1);
-#pragma unroll
-          for (int e = 0; e < 3; ++e) mma_tf32(s[e][y], q[2 * i + y], k0[e], k1[e]);
-        }
-      }
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        float sum = 0.f;                       // the small ones first
-#pragma unroll
-        for (int e = 2; e >= 0; --e) sum += (s[e][0][2 + x] + s[e][1][2 + x]) + (s[e][0][x] + s[e][1][x]);
-        p[b][x] = (there >> (b * 8 + 2 * j + x)) & 1 ? sum * a.scale : -INFINITY;
-        mx = fmaxf(mx, p[b][x]);
-      }
-    }
-    mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 1));
-    mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 2));
-    const float n = fmaxf(m, mx), ref = n > -INFINITY ? n : 0.f, f = ex2(m - ref);
-    const bool grown = n > m;
-    m = n;
-    l *= f;
-    if (__any_sync(0xFFFFFFFFu, grown)) {
-#pragma unroll
-      for (int i = 0; i < HD / 8; ++i) { o[i][0] *= f; o[i][1] *= f; }
-    }
-    u32 w[KB][4];                              // k = j: key 2 j; k = j + 4: key 2 j + 1
-#pragma unroll
-    for (int b = 0; b < KB; ++b) {
-      const float p0 = ex2(p[b][0] - ref), p1 = ex2(p[b][1] - ref);
-      l += p0 + p1;
-      split2(p0, w[b][0], w[b][1]);
-      split2(p1, w[b][2], w[b][3]);
-    }
-    const u32 v = at + Ring<T, HD>::HALF;
-#pragma unroll
-    for (int i = 0; i < HD / 32; ++i) {
-      float d[4][4];                           // of this tile alone
-#pragma unroll
-      for (int c = 0; c < 4; ++c)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) d[c][x] = 0.f;
-#pragma unroll
-      for (int b = 0; b < KB; ++b) {
-        const float4 v0 = lds4(v + piece<T, HD>(b * 8 + 2 * j, i * 8 + r)), v1 = lds4(v + piece<T, HD>(b * 8 + 2 * j + 1, i * 8 + r));
-        const float x[4] = {v0.x, v0.y, v0.z, v0.w}, y[4] = {v1.x, v1.y, v1.z, v1.w};
-        u32 x3[4][3], y3[4][3];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          split3(x[c], x3[c]);
-          split3(y[c], y3[c]);
-        }
-#pragma unroll
-        for (int e = 2; e >= 0; --e)
-#pragma unroll
-          for (int c = 0; c < 4; ++c) mma_tf32(d[c], w[b], x3[c][e], y3[c][e]);
-      }
-#pragma unroll
-      for (int c = 0; c < 4; ++c)
-#pragma unroll
-        for (int x = 0; x < 2; ++x) o[4 * i + c][x] += d[c][x] + d[c][2 + x];
-    }
-  }
-  __device__ __forceinline__ void end(const DecodeArgs &a, int b, int item, bool whole, float *part) {
-    const int h = item / a.chunks, c = item % a.chunks, r = lane >> 2, j = lane & 3;
-    l += __shfl_xor_sync(0xFFFFFFFFu, l, 1);
-    l += __shfl_xor_sync(0xFFFFFFFFu, l, 2);
-    if (r >= min(a.chunk, a.group - c * a.chunk)) return;
-    float *to = (whole ? static_cast<float *>(a.out) + ((size_t)b * a.nq + (size_t)h * a.group + c * a.chunk) * HD : part) + r * HD;
-    const float inv = !whole ? 1.f : l != 0.f ? 1.f / l : 0.f;
-#pragma unroll
-    for (int i = 0; i < HD / 32; ++i)
-#pragma unroll
-      for (int x = 0; x < 2; ++x)              // column n of tile 4 i + c stands for 32 i + 4 n + c
-#pragma unroll
-        for (int y = 0; y < 2; ++y)
-          *reinterpret_cast<float2 *>(to + i * 32 + j * 8 + x * 4 + y * 2) = make_float2(o[4 * i + 2 * y][x] * inv, o[4 * i + 2 * y + 1][x] * inv);
-    if (!whole && j == 0) *reinterpret_cast<float2 *>(part + a.chunk * HD + r * 2) = make_float2(m, l);
-  }
-};
-
-template <typename T, int HD, int H> struct TileOf { using type = Bf16Tile<HD, H>; };
-template <int HD> struct TileOf<float, HD, 8> { using type = Fp32Tile<HD>; };
 template <typename T, int HD> constexpr int smem_bytes(int batch) {
   return kWarps * Ring<T, HD>::BYTES + kWarps * Ring<T, HD>::STAGES * 4 + kWarps * 4 + (2 * batch + 1) * 4;
 }
 
-__device__ __forceinline__ void store4(float *to, float4 v) { *reinterpret_cast<float4 *>(to) = v; }
-__device__ __forceinline__ void store4(__nv_bfloat16 *to, float4 v) {
-  reinterpret_cast<__nv_bfloat162 *>(to)[0] = __floats2bfloat162_rn(v.x, v.y);
-  reinterpret_cast<__nv_bfloat162 *>(to)[1] = __floats2bfloat162_rn(v.z, v.w);
+// Row of q and the output that an item's first query head has.
+__device__ __forceinline__ size_t first_row(const DecodeArgs &a, int b, int item) {
+  return (size_t)b * a.nq + (size_t)(item / a.chunks) * a.group + item % a.chunks * a.chunk;
 }
 
 // What a warp's stretch leaves to its CTA.
@@ -620,14 +287,19 @@ attn_decode_kernel(DecodeArgs a) {
       if (fill < n) feed.copy(fill);
       copies_end();
     }
-    t.begin(a, at.b, at.item);
+    auto begin = [&] {                         // rows of the tile: the chunk's query heads
+      const int c = at.item % a.chunks, heads = min(a.chunk, a.group - c * a.chunk), r = lane >> 2;
+      const T *q = static_cast<const T *>(a.q) + first_row(a, at.b, at.item) * HD + r * HD;
+      t.begin(r < heads ? q : nullptr, r + 8 < heads ? q + 8 * HD : nullptr);
+    };
+    begin();
     for (long long i = 0; i < n; ++i) {
       copies_wait<S - 2>();
       __syncwarp();
       if (i + S - 1 < n) feed.copy(fill);
       copies_end();
       if (++fill == S) fill = 0;
-      t.tile(a, feed.ring + stage * R::STAGE, masks[stage]);
+      t.tile(a.scale, feed.ring + stage * R::STAGE, masks[stage], masks[stage]);
       if (++stage == S) stage = 0;
       const bool last = at.tile + 1 == at.tiles;
       if (last || i + 1 == n) {
@@ -641,11 +313,11 @@ attn_decode_kernel(DecodeArgs a) {
           left_here |= kHead;
           part = part_at<HD>(a.parts, a.chunk, me);
         }
-        t.end(a, at.b, at.item, part == nullptr, part);
+        t.end(part ? nullptr : static_cast<T *>(a.out) + first_row(a, at.b, at.item) * HD, part, a.chunk, min(a.chunk, a.group - at.item % a.chunks * a.chunk));
       }
       if (i + 1 < n) {
         at.next(line);
-        if (last) { first = 0; t.begin(a, at.b, at.item); }
+        if (last) { first = 0; begin(); }
       }
     }
     if (warp == 0 && lane == 0) {              // the item that this CTA begins inside of, told by the second CTA that has a part of it

@@ -39,6 +39,8 @@ decltype(&hsd_kv_append_norm) kv_append_norm_fn = nullptr;
 decltype(&hsd_quantize_rows) quantize_fn = nullptr;
 decltype(&hsd_gemm_w8_workspace_bytes) gemm_w8_bytes_fn = nullptr;
 decltype(&hsd_gemm_w8) gemm_w8_fn = nullptr;
+decltype(&hsd_prefix_attention_workspace_bytes) prefix_bytes_fn = nullptr;
+decltype(&hsd_prefix_attention) prefix_fn = nullptr;
 PyObject *error_class = nullptr;
 
 struct Failed {};                                          // a Python exception is set
@@ -98,7 +100,7 @@ void *current_stream() { return c10::cuda::getCurrentCUDAStream().stream(); }
 PyObject *init(PyObject *, PyObject *const *args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   try {
-    arguments(n, 19);
+    arguments(n, 21);
     draft_sample_fn = reinterpret_cast<decltype(draft_sample_fn)>(word(args[0]));
     verify_bytes_fn = reinterpret_cast<decltype(verify_bytes_fn)>(word(args[1]));
     verify_level_fn = reinterpret_cast<decltype(verify_level_fn)>(word(args[2]));
@@ -117,8 +119,10 @@ PyObject *init(PyObject *, PyObject *const *args, Py_ssize_t n) {
     quantize_fn = reinterpret_cast<decltype(quantize_fn)>(word(args[15]));
     gemm_w8_bytes_fn = reinterpret_cast<decltype(gemm_w8_bytes_fn)>(word(args[16]));
     gemm_w8_fn = reinterpret_cast<decltype(gemm_w8_fn)>(word(args[17]));
-    Py_INCREF(args[18]);
-    error_class = args[18];
+    prefix_bytes_fn = reinterpret_cast<decltype(prefix_bytes_fn)>(word(args[18]));
+    prefix_fn = reinterpret_cast<decltype(prefix_fn)>(word(args[19]));
+    Py_INCREF(args[20]);
+    error_class = args[20];
     Py_RETURN_NONE;
   } catch (const Failed &) { return nullptr; }
   END_HANDLE_TH_ERRORS
@@ -380,6 +384,53 @@ PyObject *paged_attention(PyObject *, PyObject *const *args, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// prefix_attention(q [rows, nq, hd], k_pool, v_pool, page_table [batch, pages], kv_lens [batch], prefix_pages [n], prefix_len [1],
+// row_starts [batch + 1] or None, scale or None, workspace or None, out or None)
+PyObject *prefix_attention(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  try {
+    arguments(n, 11);
+    const at::Tensor &q = dims(tensor(args[0]), "q", 3);
+    const hsd_kv_pool pool = pools(args[1], args[2], &q);
+    const at::Tensor &k = tensor(args[1]);
+    const int64_t rows = q.size(0), nq = q.size(1), hd = q.size(2);
+    sized(typed(args[0], "q", k.scalar_type(), &k), "q", {rows, nq, k.size(3)});
+    const at::Tensor &table = dims(typed(args[3], "page_table", at::kInt, &q), "page_table", 2);
+    const int64_t batch = table.size(0);
+    sized(table, "page_table", {batch, table.size(1)});
+    const at::Tensor &lens = sized(typed(args[4], "kv_lens", at::kInt, &q), "kv_lens", {batch});
+    const at::Tensor &prefix = dims(typed(args[5], "prefix_pages", at::kInt, &q), "prefix_pages", 1);
+    sized(prefix, "prefix_pages", {prefix.size(0)});
+    const at::Tensor &length = sized(typed(args[6], "prefix_len", at::kInt, &q), "prefix_len", {1});
+    const int32_t *starts = nullptr;
+    if (args[7] != Py_None) starts = static_cast<const int32_t *>(sized(typed(args[7], "row_starts", at::kInt, &q), "row_starts", {batch + 1}).data_ptr());
+    double scale = 1. / std::sqrt((double)hd);
+    if (args[8] != Py_None) {
+      scale = PyFloat_AsDouble(args[8]);
+      if (scale == -1. && PyErr_Occurred()) throw Failed();
+    }
+    const int n_rows = count(rows), heads = count(nq), kv_heads = count(k.size(0)), dim = count(hd), n_batch = count(batch), pages = count(table.size(1)), front = count(prefix.size(0));
+    const size_t need = prefix_bytes_fn(n_rows, heads, kv_heads, dim);
+    if (need == 0) {
+      PyErr_Format(error_class, "hsd_prefix_attention: unsupported sizes: %d rows, %d queries, %d keys of %d", n_rows, heads, kv_heads, dim);
+      throw Failed();
+    }
+    const c10::cuda::CUDAGuard guard(q.device());
+    at::Tensor ws = args[9] == Py_None ? fresh({(int64_t)need}, at::kByte) : typed(args[9], "workspace", at::kByte, &q);
+    if (!ws.is_contiguous()) refuse("expected a contiguous CUDA tensor");
+    at::Tensor out = args[10] == Py_None ? fresh({rows, nq, hd}, q.scalar_type()) : sized(typed(args[10], "out", q.scalar_type(), &q), "out", {rows, nq, hd});
+    void *from = q.data_ptr(), *to = out.data_ptr(), *scratch = ws.data_ptr(), *stream = current_stream();
+    const bool own = args[10] == Py_None;                                                  // (fresh memory holds anything)
+    check(released([&] {
+      return prefix_fn(from, n_rows, heads, kv_heads, dim, &pool, static_cast<const int32_t *>(table.data_ptr()), pages, static_cast<const int32_t *>(lens.data_ptr()), starts,
+                       n_batch, static_cast<const int32_t *>(prefix.data_ptr()), front, static_cast<const int32_t *>(length.data_ptr()), (float)scale, scratch, (size_t)ws.numel(),
+                       own, to, stream);
+    }));
+    return THPVariable_Wrap(std::move(out));
+  } catch (const Failed &) { return nullptr; }
+  END_HANDLE_TH_ERRORS
+}
+
 // gemm_w4(A bf16 [R, K], codes uint8 [N, K / 2], scales bf16 [N, K / group], out or None, workspace or None)
 PyObject *gemm_w4(PyObject *, PyObject *const *args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
@@ -526,7 +577,7 @@ PyObject *token_logprobs(PyObject *, PyObject *const *args, Py_ssize_t n) {
 
 #define FAST(f) reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr
 PyMethodDef methods[] = {{"init", FAST(init)}, {"draft_sample", FAST(draft_sample)}, {"verify_level", FAST(verify_level)},
-                         {"gemm_bf16", FAST(gemm_bf16)}, {"kv_append", FAST(kv_append)}, {"kv_append_norm", FAST(kv_append_norm)}, {"quantize_rows", FAST(quantize_rows)}, {"gemm_w8", FAST(gemm_w8)},
+                         {"gemm_bf16", FAST(gemm_bf16)}, {"kv_append", FAST(kv_append)}, {"kv_append_norm", FAST(kv_append_norm)}, {"quantize_rows", FAST(quantize_rows)}, {"gemm_w8", FAST(gemm_w8)}, {"prefix_attention", FAST(prefix_attention)},
                          {"paged_attention", FAST(paged_attention)},
                          {"gemm_w4", FAST(gemm_w4)}, {"token_logprobs", FAST(token_logprobs)}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

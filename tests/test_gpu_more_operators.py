@@ -314,3 +314,232 @@ def test_w8_captured_on_other_streams_and_two_at_once(lib):
     torch.cuda.synchronize()
     for i in range(2):
         assert all(torch.equal(y, want[i]) for y in got[i])
+
+
+# ------------------------------------------------------------------------------------------------ attention over a shared prefix
+def counts_of(starts, batch):
+    return [(b, b + 1) for b in range(batch)] if starts is None else list(zip(starts[:-1], starts[1:]))
+
+
+def prefix64(q, k_pool, v_pool, table, lens, pages, P, starts, scale):
+    """(out, sum of weights times |v|, the largest sum of |q||k|), all in 64 bits; rows without a sequence are NaN."""
+    rows, nq, hd = q.shape
+    nkv, n_pages, page, _ = k_pool.shape
+    out, size, most = (torch.full((rows, nq, n), float("nan"), dtype=torch.float64) for n in (hd, hd, 1))
+    P = min(max(P, 0), len(pages) * page)
+    room = table.shape[1] * page
+    kc, vc, qc = k_pool.double().cpu(), v_pool.double().cpu(), q.double().cpu()
+    for b, (r0, r1) in enumerate(counts_of(starts, len(lens))):
+        n = min(max(lens[b], 0), max(room, P))
+        where = [(int(pages[p // page]) if p < P else int(table[b, p // page]) if p < room else -1, p % page, p) for p in range(n)]
+        where = [x for x in where if 0 <= x[0] < n_pages]
+        for r in range(r0, min(r1, rows)):
+            limit = n - (r1 - r0) + 1 + r - r0
+            seen = [x for x in where if x[2] < limit]
+            out[r], size[r], most[r] = 0, 0, 0
+            if not seen:
+                continue
+            a, t, _ = (torch.tensor(x) for x in zip(*seen))
+            for h in range(nq):
+                k, v, x = kc[h * nkv // nq][a, t], vc[h * nkv // nq][a, t], qc[r, h]
+                w = torch.softmax(k @ x * scale, dim=0)
+                out[r, h], size[r, h], most[r, h] = w @ v, w @ v.abs(), (k.abs() @ x.abs()).max() * abs(scale)
+    return out, size, most
+
+
+def check_prefix(lib, q, k, v, table, lens, pages, P, starts=None, scale=None):
+    rows, nq, hd = q.shape
+    args = (q, k, v, table, ints(lens), pages, ints([P]), None if starts is None else ints(starts), scale)
+    got = lib.hsd_prefix_attention(*args)
+    want, size, most = prefix64(q, k, v, table.cpu(), lens, pages.cpu(), P, starts, hd ** -0.5 if scale is None else scale)
+    none = want[:, 0, 0].isnan()
+    # as in the attention by sequence: a score's sum and its exponential; tiles added one after the other; bf16 weights of 16 bits, and
+    # chains of up to 2048 keys in the tensor cores' adders, two products for every 16 keys
+    weight = (hd + 4) * 2.0 ** -23 * most + 2.0 ** -21 + (max(max(lens), P) / 8 + 64) * 2.0 ** -24 + (2.0 ** -16 if q.dtype == BF16 else 0)
+    chain = 256 * 2.0 ** -23 if q.dtype == BF16 else 0
+    bound = HALF_STEP[q.dtype] * want.abs() + (2 * weight + chain) * size + 1e-37
+    off = (got.double().cpu() - want).abs()
+    assert bool((off <= bound)[~none].all()), (float((off / bound)[~none].max()), int((off > bound)[~none].sum()))
+    assert bool((got.cpu()[none] == 0).all())
+    into = torch.full_like(q, 7.0)
+    assert lib.hsd_prefix_attention(*args, out=into) is into
+    assert torch.equal(into[~none.cuda()], got[~none.cuda()]) and bool((into[none.cuda()] == 7.0).all())      # sums in a fixed order
+    return got
+
+
+def prefix_cache(g, batch, nkv, hd, page, P, own, dtype, order="head"):
+    """A table whose whole pages below P are no pages at all, and the prefix's pages."""
+    per_seq = -(-(P + own) // page)
+    k, v, table = cache(g, batch, nkv, hd, page, per_seq, dtype, order, spare=-(-P // page) + 2)
+    used = set(table.flatten().tolist())
+    free = [p for p in range(k.shape[1]) if p not in used]
+    table[:, :P // page] = -7
+    pages = ints(free[:max(1, -(-P // page))][::-1])
+    return k, v, table, pages
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("hd", [32, 64, 128])
+@pytest.mark.parametrize("nq,nkv", [(1, 1), (8, 2), (7, 1), (40, 2)])
+@pytest.mark.parametrize("P", [1, 16, 45, 200])
+def test_prefix_attention_of_one_row_each(lib, dtype, hd, nq, nkv, P):
+    g = gen(hd + nq + P)
+    k, v, table, pages = prefix_cache(g, 7, nkv, hd, 16, P, 60, dtype)
+    lens = [P + 1, P, P + 17, 0, P + 60, -1, max(1, P - 3)]
+    check_prefix(lib, randn(g, 7, nq, hd, dtype=dtype, std=1.5), k, v, table, lens, pages, P)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("hd", [32, 64, 128])
+@pytest.mark.parametrize("P", [33, 300])
+def test_prefix_attention_of_several_rows(lib, dtype, hd, P):
+    """One to many rows a sequence, sequences without rows, shorter than their rows, rows in front of the first and behind the last."""
+    g = gen(hd + P)
+    n = [1, 9, 0, 4, 40, 3, 2]
+    starts = [2]
+    for x in n:
+        starts.append(starts[-1] + x)
+    k, v, table, pages = prefix_cache(g, 7, 2, hd, 16, P, 70, dtype)
+    lens = [P + 5, P + 9, P + 3, P + 2, P + 70, 2, P - 1]
+    check_prefix(lib, randn(g, starts[-1] + 3, 6, hd, dtype=dtype), k, v, table, lens, pages, P, starts)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("page,order", [(1, "head"), (3, "token"), (8, "token"), (24, "head"), (64, "token"), (128, "head")])
+def test_prefix_attention_over_pages_of_any_size(lib, dtype, page, order):
+    g = gen(page)
+    for P in (5, 131):
+        k, v, table, pages = prefix_cache(g, 30, 2, 64, page, P, 40, dtype, order)
+        lens = [P + 1 + (i * 7) % 40 for i in range(30)]
+        check_prefix(lib, randn(g, 30, 8, 64, dtype=dtype), k, v, table, lens, pages, P)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("batch,nq,nkv,P,own", [(1, 4, 1, 9001, 40), (2, 8, 8, 5000, 300), (40, 8, 2, 3001, 20), (70, 4, 1, 2500, 90), (300, 2, 1, 1500, 5)])
+def test_prefix_attention_is_joined_where_it_is_divided(lib, dtype, batch, nq, nkv, P, own):
+    g = gen(P)
+    k, v, table, pages = prefix_cache(g, batch, nkv, 128, 16, P, own, dtype)
+    lens = [P + 1 + (i * 13) % own for i in range(batch)]
+    check_prefix(lib, randn(g, batch, nq, 128, dtype=dtype, std=2.0), k, v, table, lens, pages, P)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_prefix_attention_without_a_prefix_and_with_more_than_its_pages(lib, dtype):
+    g = gen(3)
+    k, v, table, pages = prefix_cache(g, 20, 1, 64, 16, 32, 50, dtype)
+    q = randn(g, 20, 4, 64, dtype=dtype)
+    table[:, :2] = table[:, 2:4]
+    for P in (0, -5):
+        got = check_prefix(lib, q, k, v, table, [i * 4 for i in range(20)], pages, P)
+        assert bool((got[0] == 0).all())
+    check_prefix(lib, q, k, v, table, [40 + i for i in range(20)], pages, 1000)           # 32 positions of the prefix
+    long = ints(torch.arange(10).repeat(2).tolist())                                     # a prefix past the sequences' room
+    check_prefix(lib, q, k, v, table, [200 + 9 * i for i in range(20)], long, 290)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_prefix_attention_reads_nothing_that_is_not_there(lib, dtype):
+    g = gen(5)
+    P, batch = 75, 36
+    k, v, table, pages = prefix_cache(g, batch, 2, 64, 16, P, 40, dtype)
+    lens = [P + 1 + i for i in range(34)] + [0, 70]
+    q = randn(g, batch, 8, 64, dtype=dtype)
+    args = (table, ints(lens), pages, ints([P]))
+    want = lib.hsd_prefix_attention(q, k, v, *args)
+    for bad in (float("nan"), float("inf"), torch.finfo(dtype).min):
+        k2, v2 = torch.full_like(k, bad), torch.full_like(v, bad)
+        for i, n in enumerate(lens):
+            for p in range(n):
+                at = int(pages[p // 16]) if p < P else int(table[i, p // 16])
+                k2[:, at, p % 16], v2[:, at, p % 16] = k[:, at, p % 16], v[:, at, p % 16]
+        for p in range(P):
+            k2[:, pages[p // 16], p % 16], v2[:, pages[p // 16], p % 16] = k[:, pages[p // 16], p % 16], v[:, pages[p // 16], p % 16]
+        assert torch.equal(want, lib.hsd_prefix_attention(q, k2, v2, *args))
+    pages[1], pages[3], table[0, 5], table[3, 4] = -1, k.shape[1], 1 << 30, -5            # pages that are none: absent
+    check_prefix(lib, q, k, v, table, lens, pages, P)
+    pages[:] = -1
+    check_prefix(lib, q, k, v, table, lens, pages, P)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("scale", [0.0, -0.3, 4.0])
+def test_prefix_attention_scales(lib, dtype, scale):
+    g = gen(7)
+    k, v, table, pages = prefix_cache(g, 40, 1, 64, 16, 400, 30, dtype)
+    check_prefix(lib, randn(g, 40, 4, 64, dtype=dtype), k, v, table, [401 + i % 30 for i in range(40)], pages, 400, scale=scale)
+
+
+@pytest.mark.parametrize("rows", [3, 50])
+def test_prefix_attention_keeps_nan_to_its_rows(lib, rows):
+    g = gen(8)
+    for dtype in (BF16, FP32):
+        k, v, table, pages = prefix_cache(g, rows, 1, 64, 16, 600, 20, dtype)
+        q = randn(g, rows, 2, 64, dtype=dtype)
+        q[0, 1, 3] = float("nan")
+        v[0, table[1, 600 // 16], 600 % 16, 0] = float("inf")
+        got = lib.hsd_prefix_attention(q, k, v, table, ints([605] * rows), pages, ints([600]))
+        assert bool(got[0, 1].isnan().all()) and bool(got[0, 0].isfinite().all()) and bool(got[2:].isfinite().all())
+        assert not bool(got[1, :, 0].isfinite().any()) and bool(got[1, :, 1:].isfinite().all())
+
+
+@pytest.mark.parametrize("rows", [3, 60])
+def test_prefix_attention_follows_its_lists_when_replayed_and_on_other_streams(lib, rows):
+    g = gen(11)
+    k, v, table, pages = prefix_cache(g, rows, 2, 64, 16, 1000, 100, BF16)
+    q, lens, P = randn(g, rows, 8, 64, dtype=BF16), ints([0] * rows), ints([0])
+    starts = ints(list(range(rows + 1)))
+    other_q = randn(g, rows, 8, 64, dtype=BF16)
+    lib.hsd_prefix_attention(q, k, v, table, lens, pages, P, starts)
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for x in (q, other_q):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs.append(lib.hsd_prefix_attention(x, k, v, table, lens, pages, P, starts))
+        graphs.append(graph)
+    for prefix, shift in ((1000, 0), (992, 1), (3, 0), (0, 0)):
+        values = [prefix + 1 + (i * 17) % 90 for i in range(rows)]
+        lens.copy_(ints(values))
+        P.copy_(ints([prefix]))
+        starts.copy_(ints([max(0, i - shift) for i in range(rows + 1)]))
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        for x, out in zip((q, other_q), outs):
+            assert torch.equal(out, lib.hsd_prefix_attention(x, k, v, table, ints(values), pages, ints([prefix]), starts.clone()))
+    lens, P = ints([1001 + i for i in range(rows)]), ints([1000])
+    want = [lib.hsd_prefix_attention(x, k, v, table, lens, pages, P) for x in (q, other_q)]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], [[], []]
+    for _ in range(20):
+        for i, (x, s) in enumerate(zip((q, other_q), streams)):
+            with torch.cuda.stream(s):
+                got[i].append(lib.hsd_prefix_attention(x, k, v, table, lens, pages, P))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(y, want[i]) for y in got[i])
+
+
+def test_prefix_attention_of_one_table_is_the_attention_by_sequence(lib):
+    """Tables that name the prefix's pages themselves: what hsd_paged_attention gives, to the rounding of the sums."""
+    g = gen(12)
+    for dtype in (BF16, FP32):
+        P, batch = 512, 33
+        k, v, table, pages = prefix_cache(g, batch, 2, 128, 16, P, 64, dtype)
+        table[:, :P // 16] = pages
+        lens, q = ints([P + 1 + i for i in range(batch)]), randn(g, batch, 8, 128, dtype=dtype)
+        a, b = lib.hsd_prefix_attention(q, k, v, table, lens, pages, ints([P])), lib.hsd_paged_attention(q, k, v, table, lens)
+        size = v.abs().max()
+        assert bool(((a.double() - b.double()).abs() <= 2 * HALF_STEP[dtype] * b.double().abs() + 2.0 ** -15 * size).all())
+
+
+def test_prefix_attention_far_into_a_large_pool(lib):
+    """Places past 2^31 elements and 2^32 bytes of a pool."""
+    g = gen(13)
+    n_pages = (1 << 31) // (16 * 128) + 40
+    k, v = (torch.empty(1, n_pages, 16, 128, dtype=BF16, device="cuda") for _ in range(2))
+    pages = ints([n_pages - 1, 3, n_pages - 30])
+    table = ints([[-1, -1, n_pages - 2, n_pages - 3], [-1, -1, 7, n_pages - 5]] * 12)
+    for p in pages.tolist() + table[table >= 0].flatten().tolist():
+        k[0, p], v[0, p] = randn(g, 16, 128, dtype=BF16), randn(g, 16, 128, dtype=BF16)
+    check_prefix(lib, randn(g, 24, 4, 128, dtype=BF16), k, v, table, [45 + i % 19 for i in range(24)], pages, 44)
