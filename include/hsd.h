@@ -417,8 +417,9 @@ int hsd_paged_attention(const void *q, int batch, int n_q_heads, int n_kv_heads,
  * on the prefix's pages, which are read once for the whole batch, the others on the sequence's own.  Softmax and sums in fp32, rounded once.
  *   q, out         device [rows, n_q_heads, head_dim] in the pool's type, 16-byte aligned; n_q_heads a multiple of n_kv_heads
  *   page_table     device [batch, pages_per_seq] int32: position p of a sequence in page page_table[b * pages_per_seq + p / page_size], as
- *                  for the other calls; entries of whole pages below P are not read.  kv_lens device [batch] int32 counts the prefix too.  0 or
- *                  less: the rows' outputs are zeros; more than the table (and the prefix) has room for: its room
+ *                  for the other calls; entries of whole pages below P are not read.  kv_lens device [batch] int32 counts the prefix too; more than
+ *                  the table (and the prefix) has room for: its room.  A sequence that has not the whole prefix, kv_lens[b] - n + 1 < P (a
+ *                  padded one of length 0, say), or no key: its rows' outputs are zeros
  *   row_starts     device [batch + 1] int32, not descending: rows row_starts[b] .. row_starts[b+1]-1 are sequence b's; NULL: rows == batch, a
  *                  row each.  Rows in front of the first and from row_starts[batch] on: zeros (zeros != 0), or left as they were
  *   prefix_pages   device [n_prefix_pages] int32: pages of the positions 0 .. P - 1;  prefix_len device [1] int32 (0 or less: no prefix;
@@ -426,8 +427,8 @@ int hsd_paged_attention(const void *q, int batch, int n_q_heads, int n_kv_heads,
  *   scale          finite, also times log2(e)
  *   workspace      device, 256-byte aligned, at least hsd_prefix_attention_workspace_bytes(...) (0 = bad sizes); contents on entry are ignored
  * Keys on a page that is not in [0, n_pages) count as absent; memory behind a sequence's or the prefix's last key is not used, whatever it
- * holds; keys and values that are there and not finite may make their heads' outputs NaN.  Lists are read by the kernels only, so a captured
- * call follows their changes.  How keys are divided, and so the order of the fp32 sums, follows the lengths of the whole batch.
+ * holds; what is there and not finite may make the outputs NaN of the heads and rows that see it, and of no others.  Lists are read by the
+ * kernels only, so a captured call follows their changes.  How keys are divided, and so the order of the fp32 sums, follows the lengths of the whole batch.
  * Errors: INVALID_ARG, UNSUPPORTED (head_dim not in {32, 64, 128}), TOO_LARGE (batch over 4096, over 65536 query heads, rows * n_q_heads over
  * 2^26, (rows * n_q_heads / n_kv_heads + 8 batch + 8) * positions over 2^37), WORKSPACE_TOO_SMALL, CUDA; DEVICE_TIMEOUT is reported by
  * hsd_gemm_status(workspace, stream). */

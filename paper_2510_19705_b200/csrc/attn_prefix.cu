@@ -17,6 +17,7 @@ constexpr int kWarps = 8, kThreads = kWarps * 32;
 constexpr int kGrid = kMeasuredSMs;            // CTAs at most: fixed, as the workspace's size depends on it
 constexpr int kMaxBatch = 4096;                // its tiles' prefix sums lie in shared memory
 constexpr int kMostChunk = 16;                 // queries of an item
+constexpr int kAll = 0x7FFFFFFF;               // rows that are none see all positions
 
 struct PrefixArgs {
   const void *q;
@@ -42,8 +43,6 @@ struct Lens {
     room = (int)((long long)a.pages_per_seq * a.pool.page);
   }
   __device__ __forceinline__ int of(const PrefixArgs &a, int b) const { return min(max(a.kv_lens[b], 0), max(room, prefix)); }
-  // a sequence's keys end here (its own keys: from the prefix's end on)
-  __device__ __forceinline__ int end(const PrefixArgs &a, int b) const { return min(of(a, b), room); }
 };
 __device__ __forceinline__ int2 rows_of(const PrefixArgs &a, int b) {          // first row and one past the last
   if (!a.row_starts) return make_int2(b, b + 1);
@@ -60,10 +59,12 @@ __device__ __forceinline__ int seq_of(const PrefixArgs &a, int r) {            /
   }
   return lo >= 0 && r < a.row_starts[lo + 1] ? lo : lo < 0 ? -1 : a.batch;
 }
-// Positions that a row sees: those below its own and itself.
-__device__ __forceinline__ int limit_of(const PrefixArgs &a, const Lens &l, int r, int b) {
-  const int2 of = rows_of(a, b);
-  return l.of(a, b) - (of.y - of.x) + 1 + (r - of.x);
+// What a sequence's rows see: the first of them the positions below `first` (each one behind it one more), own keys up to `end`.  A sequence
+// that does not have the whole prefix has no keys: first < 0.
+struct Seen { int first, end; };
+__device__ __forceinline__ Seen seen_by(const PrefixArgs &a, const Lens &l, int b, int2 rows) {
+  const int len = l.of(a, b), first = len - (rows.y - rows.x) + 1;
+  return first < l.prefix || rows.x == rows.y ? Seen{-1, 0} : Seen{first, min(len, l.room)};
 }
 
 // The line of tiles.  Sequence 0 is the prefix, b + 1 the own keys of sequence b: tiles from `front` on (the own keys begin inside a tile).
@@ -91,8 +92,8 @@ __device__ __forceinline__ Line make_line(const PrefixArgs &a, bool prefix, int 
     if (s == 0) {
       if (prefix) { end = lens.prefix; n = (end + KEYS - 1) / KEYS * ceil_div(a.rows * a.group, a.chunk); }
     } else if (s < seqs) {
-      end = lens.end(a, s - 1);
       const int2 r = rows_of(a, s - 1);
+      end = seen_by(a, lens, s - 1, r).end;
       if (end > lens.prefix) n = ((end + KEYS - 1) / KEYS - front) * ceil_div((r.y - r.x) * a.group, a.chunk);
     }
     int upto = n;
@@ -170,7 +171,6 @@ struct Queries {
     v0 = (p.item - head * chunks) * a.chunk;
     n = min(a.chunk, (r.y - r.x) * a.group - v0);
   }
-  __device__ __forceinline__ int row(const PrefixArgs &a, int i) const { return row0 + (v0 + i) / a.group; }
   __device__ __forceinline__ size_t at(const PrefixArgs &a, int i) const {      // row and head of q and the output
     const int v = v0 + i, r = v / a.group;
     return (size_t)(row0 + r) * a.nq + head * a.group + (v - r * a.group);
@@ -285,6 +285,26 @@ template <typename T, int HD> constexpr int smem_bytes(int batch) {
 }
 __device__ __forceinline__ u32 below(int n) { return n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1; }
 
+// Of a tile that some rows see less of than others: whether one of the values that not all rows see (bits of `partly`) is not finite.
+template <typename T, int HD> __device__ __forceinline__ bool not_finite(u32 values, u32 partly, int lane) {
+  constexpr int PIECES = Ring<T, HD>::ROW / 16;
+  bool bad = false;
+  for (int i = lane; i < Form<T, HD>::KEYS * PIECES; i += 32) {
+    if (!((partly >> (i / PIECES)) & 1)) continue;
+    const float4 v = lds4(values + piece<T, HD>(i / PIECES, i % PIECES));
+    const u32 w[4] = {__float_as_uint(v.x), __float_as_uint(v.y), __float_as_uint(v.z), __float_as_uint(v.w)};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) bad |= (w[e] & 0x7F800000u) == 0x7F800000u || (sizeof(T) == 2 && (w[e] & 0x7F80u) == 0x7F80u);
+  }
+  return __any_sync(0xFFFFFFFFu, bad);
+}
+template <typename T, int HD> __device__ __forceinline__ void zero_values(u32 values, int from, int lane) {
+  constexpr int PIECES = Ring<T, HD>::ROW / 16;
+  for (int i = from * PIECES + lane; i < Form<T, HD>::KEYS * PIECES; i += 32)
+    sts4(values + piece<T, HD>(i / PIECES, i % PIECES), make_float4(0.f, 0.f, 0.f, 0.f));
+  __syncwarp();
+}
+
 enum { kHead = 1, kEnd = 2, kThrough = 4 };    // a part of an item from in front of a stretch that ends in it; of one that runs on behind it; from in front too
 
 template <typename T, int HD, int H>
@@ -326,23 +346,19 @@ prefix_lane_kernel(PrefixArgs a, bool prefix) {
       copies_end();
     }
     Queries qs;
-    int lim[2];                                // positions that the lane's rows see
+    int lim[2], least;                         // positions that the lane's rows see (rows that are none: all); all rows
     auto begin = [&] {
       qs.of(a, at, line.nkv);
+      const int sees = at.s > 0 ? seen_by(a, lens, at.s - 1, rows_of(a, at.s - 1)).first : line.prefix;
       const T *q[2];
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
         const int i = (lane >> 2) + 8 * y;
-        q[y] = nullptr;
-        lim[y] = 0;
-        if (y < H / 8 && i < qs.n) {
-          const int r = qs.row(a, i), b = at.s > 0 ? at.s - 1 : seq_of(a, r);
-          if (b >= 0 && b < a.batch) {
-            q[y] = static_cast<const T *>(a.q) + qs.at(a, i) * HD;
-            lim[y] = limit_of(a, lens, r, b);
-          }
-        }
+        const bool real = y < H / 8 && i < qs.n;
+        q[y] = real ? static_cast<const T *>(a.q) + qs.at(a, i) * HD : nullptr;
+        lim[y] = real && at.s > 0 ? sees + (qs.v0 + i) / a.group : kAll;
       }
+      least = __reduce_min_sync(0xFFFFFFFFu, min(lim[0], lim[1]));
       t.begin(q[0], q[1]);
     };
     begin();
@@ -353,8 +369,36 @@ prefix_lane_kernel(PrefixArgs a, bool prefix) {
       copies_end();
       if (++fill == S) fill = 0;
       const int key0 = at.first_key(line);
-      const u32 there = masks[stage];
-      t.tile(a.scale, feed.ring + stage * R::STAGE, there & below(lim[0] - key0), there & below(lim[1] - key0));
+      const u32 there = masks[stage], where = feed.ring + stage * R::STAGE;
+      u32 th[2] = {there, there};
+      int longest[2] = {-1, -1};
+      bool in_turn = false;
+      if (key0 + KEYS > least) {
+        th[0] &= below(lim[0] - key0);         // (rows that are none see all)
+        th[1] &= below(lim[1] - key0);
+        const u32 partly = there & ~__reduce_and_sync(0xFFFFFFFFu, th[0] & th[1]);
+        // A weight of 0 times a value that is not finite would be NaN in a row that does not see it.  Where there is one, rows go one limit
+        // after the other, the longest first, with the values behind it made zeros, and the other rows' sums are put back.
+        in_turn = partly && not_finite<T, HD>(where + R::HALF, partly, lane);
+      }
+      if (!in_turn) {
+        t.tile(a.scale, where, th[0], th[1]);
+      } else {
+        volatile float old[decltype(t)::SUMS];                         // (in local memory: hardly ever used)
+#pragma unroll
+        for (int y = 0; y < 2; ++y) longest[y] = lim[y] == kAll ? -1 : min(max(lim[y] - key0, 0), KEYS);
+        for (;;) {
+          const int most = __reduce_max_sync(0xFFFFFFFFu, max(longest[0], longest[1]));
+          if (most < 0) break;
+          zero_values<T, HD>(where + R::HALF, most, lane);
+          t.save(old);
+          t.tile(a.scale, where, longest[0] == most ? th[0] : 0u, longest[1] == most ? th[1] : 0u);
+          t.restore(old, longest[0] != most, longest[1] != most);
+#pragma unroll
+          for (int y = 0; y < 2; ++y)
+            if (longest[y] == most) longest[y] = -1;
+        }
+      }
       if (++stage == S) stage = 0;
       const bool last = at.tile + 1 == at.tiles;
       if (last || i + 1 == n) {
@@ -478,7 +522,8 @@ prefix_join_kernel(PrefixArgs a) {
     if (a.zeros && group == 0) store4(out + col, make_float4(0.f, 0.f, 0.f, 0.f));
     return;
   }
-  const bool has[2] = {lens.prefix > 0, lens.end(a, b) > lens.prefix};
+  const Seen sees = seen_by(a, lens, b, rows_of(a, b));
+  const bool has[2] = {sees.first >= 0 && lens.prefix > 0, sees.end > lens.prefix};
   const size_t at[2] = {blockIdx.x, (size_t)a.rows * a.nq + blockIdx.x};
   int4 more[2];
   int n[2];

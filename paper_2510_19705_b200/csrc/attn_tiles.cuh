@@ -54,6 +54,9 @@ __device__ __forceinline__ float4 lds4(u32 at) {
   asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
   return v;
 }
+__device__ __forceinline__ void sts4(u32 at, float4 v) {
+  asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(at), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+}
 __device__ __forceinline__ void ldsm4(u32 *r, u32 at) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
 }
@@ -188,6 +191,16 @@ template <int HD, int H> struct Bf16Tile {     // H: 8 or 16 rows with queries
         o[2 * n + 1][x] += YS == 1 ? d[1][x] + d[1][2 + x] : d[1][x];
       }
     }
+  }
+  static constexpr int SUMS = HD / 8 * 2 * YS;
+  __device__ __forceinline__ void save(volatile float *to) const {
+#pragma unroll
+    for (int i = 0; i < SUMS; ++i) to[i] = o[i / (2 * YS)][i % (2 * YS)];
+  }
+  __device__ __forceinline__ void restore(const volatile float *from, bool row0, bool row1) {          // of the lane's rows that say so
+#pragma unroll
+    for (int i = 0; i < SUMS; ++i)
+      if (i % (2 * YS) / 2 ? row1 : row0) o[i / (2 * YS)][i % (2 * YS)] = from[i];
   }
   __device__ __forceinline__ void total() {     // the sum of a row's weights, which four lanes have a share of each
 #pragma unroll
@@ -334,6 +347,16 @@ template <int HD> struct Fp32Tile {
 #pragma unroll
         for (int x = 0; x < 2; ++x) o[4 * i + c][x] += d[c][x] + d[c][2 + x];
     }
+  }
+  static constexpr int SUMS = HD / 8 * 2;
+  __device__ __forceinline__ void save(volatile float *to) const {
+#pragma unroll
+    for (int i = 0; i < SUMS; ++i) to[i] = o[i / 2][i % 2];
+  }
+  __device__ __forceinline__ void restore(const volatile float *from, bool row, bool) {
+#pragma unroll
+    for (int i = 0; i < SUMS; ++i)
+      if (row) o[i / 2][i % 2] = from[i];
   }
   __device__ __forceinline__ void total() {
     l += __shfl_xor_sync(0xFFFFFFFFu, l, 1);

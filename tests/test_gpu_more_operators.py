@@ -337,7 +337,7 @@ def prefix64(q, k_pool, v_pool, table, lens, pages, P, starts, scale):
             limit = n - (r1 - r0) + 1 + r - r0
             seen = [x for x in where if x[2] < limit]
             out[r], size[r], most[r] = 0, 0, 0
-            if not seen:
+            if not seen or n - (r1 - r0) + 1 < P:                            # without the whole prefix: zeros
                 continue
             a, t, _ = (torch.tensor(x) for x in zip(*seen))
             for h in range(nq):
@@ -480,6 +480,37 @@ def test_prefix_attention_keeps_nan_to_its_rows(lib, rows):
         got = lib.hsd_prefix_attention(q, k, v, table, ints([605] * rows), pages, ints([600]))
         assert bool(got[0, 1].isnan().all()) and bool(got[0, 0].isfinite().all()) and bool(got[2:].isfinite().all())
         assert not bool(got[1, :, 0].isfinite().any()) and bool(got[1, :, 1:].isfinite().all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("hd,page", [(32, 16), (64, 3), (128, 16)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_prefix_attention_keeps_new_keys_and_values_to_the_rows_that_see_them(lib, dtype, hd, page, bad):
+    """A new token's key or value that is not finite: rows in front of it do not see it."""
+    g, P, batch = gen(hd), 37, 12
+    n = [1 + i % 9 for i in range(batch)]
+    starts = [sum(n[:i]) for i in range(batch + 1)]
+    lens = [P + n[i] + 5 * i for i in range(batch)]
+    k, v, table, pages = prefix_cache(g, batch, 2, hd, page, P, 80, dtype)
+    q = randn(g, starts[-1], 8, hd, dtype=dtype)
+    args = (table, ints(lens), pages, ints([P]), ints(starts))
+    want = lib.hsd_prefix_attention(q, k, v, *args)
+    for pool in (k, v):
+        keep, blind = pool.clone(), []
+        for b in range(batch):
+            first = n[b] // 2                                               # rows from here on see a bad token, the last one two
+            for r in {first, n[b] - 1}:
+                at = lens[b] - n[b] + r
+                pool[:, table[b, at // page], at % page, hd // 3] = bad
+            blind += [starts[b] + r for r in range(first)]
+        got = lib.hsd_prefix_attention(q, k, v, *args)
+        assert torch.equal(got[blind], want[blind])
+        sees = [r for r in range(starts[-1]) if r not in blind]
+        if pool is v:
+            assert not bool(got[sees][:, :, hd // 3].isfinite().any())
+        elif bad != bad:
+            assert bool(got[sees].isnan().all())
+        pool.copy_(keep)
 
 
 @pytest.mark.parametrize("rows", [3, 60])
