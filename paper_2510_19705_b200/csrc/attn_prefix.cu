@@ -8,42 +8,17 @@
 // sets of 8 or 16; divided evenly over the warps of a grid of fixed size, whatever the lengths are.  Lengths, the prefix's too, are read
 // on the device.  A part of an item goes to the place of its rows (one for the prefix, one for the own keys) from the CTA in which the
 // item begins, and to a place of the CTA from those behind it.
+#include "attn_prefix.cuh"
 #include "attn_tiles.cuh"
 
 namespace hsd {
 namespace {
 
-constexpr int kWarps = 8, kThreads = kWarps * 32;
-constexpr int kGrid = kMeasuredSMs;            // CTAs at most: fixed, as the workspace's size depends on it
+constexpr int kWarps = 8, kThreads = kWarps * 32, kGrid = kPrefixGrid;
 constexpr int kMaxBatch = 4096;                // its tiles' prefix sums lie in shared memory
 constexpr int kMostChunk = 16;                 // queries of an item
 constexpr int kAll = 0x7FFFFFFF;               // rows that are none see all positions
 
-struct PrefixArgs {
-  const void *q;
-  void *out;
-  const int32_t *page_table, *kv_lens, *prefix_pages, *prefix_len, *row_starts;
-  float *first;                                // sums of each part [2][rows][heads][HD]: over the prefix, over own keys, of the CTA that begins the item
-  float2 *first_ml;                            // their m and l
-  int4 *more;                                  // where the parts of the CTAs behind it are: o's and ml's float in `rest`, floats between two CTAs, how many
-  float *rest;                                 // per CTA: a part that begins in front of it, chunk rows and their m and l
-  PoolView pool;
-  float scale;                                 // times log2(e)
-  int rows, batch, nq, nkv, pages_per_seq, prefix_pages_n, page_shift;   // log2 of the page size, or -1
-  int group, chunk;                            // query heads of a key head; queries of an item at most
-  bool zeros;                                  // rows without a sequence become zeros
-  int *status;                                 // set if a bounded wait gave up
-};
-
-// What the device's lists say, within what there is room for.
-struct Lens {
-  int prefix, room;                            // keys of the prefix; positions that a sequence's pages have room for
-  __device__ __forceinline__ void read(const PrefixArgs &a) {
-    prefix = (int)min((long long)max(*a.prefix_len, 0), (long long)a.prefix_pages_n * a.pool.page);
-    room = (int)((long long)a.pages_per_seq * a.pool.page);
-  }
-  __device__ __forceinline__ int of(const PrefixArgs &a, int b) const { return min(max(a.kv_lens[b], 0), max(room, prefix)); }
-};
 __device__ __forceinline__ int2 rows_of(const PrefixArgs &a, int b) {          // first row and one past the last
   if (!a.row_starts) return make_int2(b, b + 1);
   const int r0 = min(max(a.row_starts[b], 0), a.rows);
@@ -309,7 +284,7 @@ enum { kHead = 1, kEnd = 2, kThrough = 4 };    // a part of an item from in fron
 
 template <typename T, int HD, int H>
 __global__ void __launch_bounds__(kThreads, 1)
-prefix_lane_kernel(PrefixArgs a, bool prefix) {
+prefix_lane_kernel(PrefixArgs a, bool prefix) {        // prefix false: the kernel in front sums over the prefix
   using R = Ring<T, HD>;
   constexpr int S = R::STAGES, KEYS = Form<T, HD>::KEYS;
   static_assert(H * (HD + 2) * 4 <= R::BYTES, "a warp's last part takes its ring's place");
@@ -320,9 +295,10 @@ prefix_lane_kernel(PrefixArgs a, bool prefix) {
   unsigned char *rest_smem = smem + kWarps * R::BYTES;
   u32 *masks = reinterpret_cast<u32 *>(rest_smem) + warp * S;
   int *warp_sum = reinterpret_cast<int *>(rest_smem) + kWarps * S, *before = warp_sum + kWarps, *ends = before + a.batch + 2;
-  chain_wait();
+  // behind the call's own kernel, which began when all kernels in front of it were complete, the start need not wait
+  if (prefix) chain_wait();
   chain_next();
-  if (cta == 0 && threadIdx.x == 0) *a.status = 0;
+  if (prefix && cta == 0 && threadIdx.x == 0) *a.status = 0;
   const Line line = make_line<KEYS>(a, prefix, before, ends, warp_sum);
   Lens lens;
   lens.read(a);
@@ -500,6 +476,7 @@ prefix_lane_kernel(PrefixArgs a, bool prefix) {
       }
     }
   }
+  if (!prefix) chain_wait();                   // the join waits for this kernel alone
 }
 
 // Adds a row and head's parts, a CTA each: those over the prefix, then those over the own keys, in order.
@@ -590,28 +567,28 @@ prefix_join_kernel(PrefixArgs a) {
   store4(out + col, make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
 }
 
-template <typename T, int HD, int H> int run(const PrefixArgs &a, cudaStream_t s) {
+template <typename T, int HD, int H> int run(const PrefixArgs &a, bool tc, cudaStream_t s) {
   static std::atomic<u64> done{0};
   const int status = hsd_smem_limit((const void *)prefix_lane_kernel<T, HD, H>, smem_bytes<T, HD>(kMaxBatch), done);
   if (status) return status;
-  HSD_CUDA_OK(hsd_launch(prefix_lane_kernel<T, HD, H>, dim3(kGrid), kThreads, smem_bytes<T, HD>(a.batch), s, 0, true, a, true));
+  HSD_CUDA_OK(hsd_launch(prefix_lane_kernel<T, HD, H>, dim3(kGrid), kThreads, smem_bytes<T, HD>(a.batch), s, 0, true, a, !tc));
   HSD_CUDA_OK(hsd_launch(prefix_join_kernel<T, HD>, dim3(a.rows * a.nq), kJoinThreads, 0, s, 0, true, a));
   hsd_count_launches(2);
   return hsd_launch_status();
 }
-template <typename T, int HD> int run_chunk(PrefixArgs &a, cudaStream_t s) {
+template <typename T, int HD> int run_chunk(PrefixArgs &a, bool tc, cudaStream_t s) {
   // queries of an item: eight, or sixteen where a sequence's rows have more
   const long long per_seq = (long long)ceil_div(a.rows, a.batch) * a.group;
-  if constexpr (sizeof(T) == 2) if (per_seq > 8) { a.chunk = 16; return run<T, HD, 16>(a, s); }
+  if constexpr (sizeof(T) == 2) if (per_seq > 8) { a.chunk = 16; return run<T, HD, 16>(a, tc, s); }
   a.chunk = 8;
-  return run<T, HD, 8>(a, s);
+  return run<T, HD, 8>(a, tc, s);
 }
-template <typename T> int run_hd(PrefixArgs &a, int hd, cudaStream_t s) {
-  return hd == 32 ? run_chunk<T, 32>(a, s) : hd == 64 ? run_chunk<T, 64>(a, s) : run_chunk<T, 128>(a, s);
+template <typename T> int run_hd(PrefixArgs &a, int hd, bool tc, cudaStream_t s) {
+  return hd == 32 ? run_chunk<T, 32>(a, tc, s) : hd == 64 ? run_chunk<T, 64>(a, tc, s) : run_chunk<T, 128>(a, tc, s);
 }
 
 size_t align16(size_t n) { return (n + 15) / 16 * 16; }
-struct Layout { size_t first, first_ml, more, rest, total; };                // the status word in front
+struct Layout { size_t first, first_ml, more, rest, total; int tc_rest; };   // the status word in front
 Layout layout(int rows, int n_q_heads, int hd) {
   const size_t n = 2 * (size_t)rows * n_q_heads;
   Layout l;
@@ -619,7 +596,8 @@ Layout layout(int rows, int n_q_heads, int hd) {
   l.first_ml = l.first + n * hd * 4;
   l.more = align16(l.first_ml + n * 8);
   l.rest = l.more + n * 16;
-  l.total = l.rest + (size_t)kGrid * (kWarps + 1) * kMostChunk * (hd + 2) * 4;
+  l.tc_rest = kGrid * (kWarps + 1) * kMostChunk * (hd + 2);
+  l.total = l.rest + ((size_t)l.tc_rest + prefix_tc_floats(hd)) * 4;
   return l;
 }
 
@@ -666,5 +644,13 @@ extern "C" int hsd_prefix_attention(const void *q, int rows, int n_q_heads, int 
   a.page_shift = -1;
   for (int i = 0; i < 31; ++i)
     if (pool->page_size == 1 << i) a.page_shift = i;
-  return pool->dtype == HSD_F32 ? run_hd<float>(a, head_dim, (cudaStream_t)stream) : run_hd<__nv_bfloat16>(a, head_dim, (cudaStream_t)stream);
+  a.tc_rest = l.tc_rest;
+  cudaStream_t s = (cudaStream_t)stream;
+  bool tc = false;
+  if (prefix_tc_takes(a, pool->dtype, head_dim)) {
+    int launched = HSD_OK;
+    tc = launch_prefix_tc(a, head_dim, s, launched);
+    if (launched) return launched;
+  }
+  return pool->dtype == HSD_F32 ? run_hd<float>(a, head_dim, tc, s) : run_hd<__nv_bfloat16>(a, head_dim, tc, s);
 }

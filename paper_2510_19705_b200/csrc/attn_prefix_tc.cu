@@ -1,0 +1,474 @@
+// Sums over a shared prefix for all rows of a batch, on tcgen05 with scores, weights and outputs in tensor memory (hsd_prefix_attention).
+//
+// An item is one key head and up to 2 x 128 queries (rows times the head's group, tiles A and B) over all keys of the prefix, in tiles of
+// 64 keys; the items' tiles stand in one line, which is divided evenly over a CTA an SM, whatever the prefix's length is (it is read on the
+// device).  Per key tile and query tile
+//   S[128 x 64]   = Q K^T                      both operands in shared memory
+//   P             = exp2(S c - m), thread = query, as bf16 hi + lo halves that overwrite S (a weight keeps 16 bits and more)
+//   O[128 x hd]  += P_hi V + P_lo V            A operand from tensor memory, V as it lies in the cache (MN-major)
+// Two query tiles share every K and V tile; S has two buffers, so that the scores of the next key tile are ready when the weights of this one
+// are.  m moves only when a row's maximum has passed it by 8; then O is rescaled.
+// The tensor cores' adders cut off: a chain of products loses up to 2^-23 of its sum a product.  So a chain is not longer than kChain key
+// tiles (256 products of 16 keys' halves: 3e-5 at most, 2^-7 of a bf16 half step): then O is added in fp32 to the item's place in the
+// workspace, where each thread finds its own row again.
+// 320 threads: warps 0-3 / 4-7 = softmax of tile A / B, warp 8 = loader (TMA out of the pages, a lane a piece of a page), warp 9 = MMA
+// issue.  Every wait is bounded, and no waiter can be passed by (a parity wait sees a completion only until the next one): k_full and v_full
+// have their next loads behind k_free / v_free, which the issuer's commits complete; those their next MMAs behind the loader's tiles; s_full
+// and pv_done theirs behind p_ready of the tile's four softmax warps; o_done its next chain behind p_ready of a tile that they begin after
+// they have read O; q_ready its next queries behind o_done; p_ready its next weights behind the scores.
+#include <algorithm>
+#include "attn_prefix.cuh"
+#include "gemm_tc.cuh"
+#include "tc_ptx.cuh"
+
+namespace hsd {
+namespace {
+
+using namespace ptx;
+
+constexpr int kThreads = 320, kLoaderWarp = 8, kMmaWarp = 9;
+constexpr int TK = 64, kSet = 256;                       // keys of a tile; queries of an item at most
+constexpr int kQBlk = 128 * 128, kBlk = TK * 128;        // [128 queries][64 bf16] and [64 keys][64 bf16] blocks, 128-byte swizzle
+constexpr int kStages = 4, kMasks = 8;                   // (a mask outlives its keys' stage by two tiles at most)
+constexpr int kChain = 32;                               // key tiles of a chain
+
+template <int HD> struct Cfg {
+  static constexpr int NB = HD / 64;                     // 64-column blocks
+  static constexpr int kQTile = NB * kQBlk, kTile = NB * kBlk;
+  static constexpr int kOffK = 2 * kQTile, kOffV = kOffK + kStages * kTile, kOffMask = kOffV + kStages * kTile, kOffBar = kOffMask + kMasks * 8;
+  static constexpr int kSmem = kOffBar + 256 + 1024;
+};
+struct TcArgs {
+  CUtensorMap k, v;
+  PrefixArgs p;
+  int box;                                               // tokens of a copy
+  int sets, per_set;                                     // items of a key head; queries of each
+  float scale;                                           // positive; q is negated for a negative one
+  uint32_t sign;
+};
+
+constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_lo_k(uint32_t addr) { return ((addr & 0x3FFFFu) >> 4) | (1u << 16); }
+__device__ __forceinline__ uint32_t desc_lo_mn(uint32_t addr) { return ((addr & 0x3FFFFu) >> 4) | ((uint32_t)(kBlk >> 4) << 16); }
+__device__ __forceinline__ void umma_ss(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tmov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(acc), "r"(kDescHi) : "memory");
+}
+__device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\tmov.b64 db, {%2, %5};\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(idesc), "r"(acc), "r"(kDescHi) : "memory");
+}
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ void tmem_st8u(uint32_t taddr, const unsigned *r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+               ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, int w, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+               ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar) : "memory");
+}
+
+// What a CTA has of the line: pieces of items, one after the other.
+struct Pieces {
+  int at, to, tiles, per, sets;                          // tiles of the line; of an item; of a CTA; items of a key head
+  int head, set, t0, n;                                  // the piece: its item, first tile, tiles
+  int item;
+  __device__ __forceinline__ Pieces(const TcArgs &a, int prefix) {
+    tiles = (prefix + TK - 1) / TK;
+    sets = a.sets;
+    const int total = tiles * sets * a.p.nkv;
+    per = max((total + (int)gridDim.x - 1) / (int)gridDim.x, 1);
+    at = min((int)blockIdx.x * per, total);
+    to = min(at + per, total);
+    n = 0;
+  }
+  __device__ __forceinline__ bool next() {
+    at += n;
+    if (at >= to) return false;
+    item = at / tiles;
+    head = item / sets;
+    set = item - head * sets;
+    t0 = at - item * tiles;
+    n = min(tiles - t0, to - at);
+    return true;
+  }
+  __device__ __forceinline__ int ctas_behind() const {   // that have a part of the piece's item
+    return ((item + 1) * tiles - 1) / per - (int)blockIdx.x;
+  }
+};
+
+template <int HD>
+__global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_constant__ TcArgs a) {
+  using C = Cfg<HD>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  __shared__ uint32_t tmem_slot;
+  __shared__ int sh_abort;
+  volatile int *abort_flag = &sh_abort;
+  const uint32_t s0 = smem_u32(smem), b0 = s0 + C::kOffBar;
+  volatile uint64_t *masks = reinterpret_cast<volatile uint64_t *>(smem + C::kOffMask);
+  auto k_full = [&](int b) { return b0 + 8u * b; };
+  auto k_free = [&](int b) { return b0 + 8u * (4 + b); };
+  auto v_full = [&](int b) { return b0 + 8u * (8 + b); };
+  auto v_free = [&](int b) { return b0 + 8u * (12 + b); };
+  auto s_full = [&](int x, int b) { return b0 + 8u * (16 + 2 * x + b); };
+  auto p_ready = [&](int x, int b) { return b0 + 8u * (20 + 2 * x + b); };
+  auto pv_done = [&](int x) { return b0 + 8u * (24 + x); };
+  auto o_done = [&](int x) { return b0 + 8u * (26 + x); };           // a chain's last product
+  auto q_ready = [&](int x) { return b0 + 8u * (28 + x); };
+  const uint32_t v_land = b0 + 8u * 30;
+  const int warp = warp_index(), lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    for (int b = 0; b < kStages; ++b) { mbar_init(k_full(b), 1); mbar_init(k_free(b), 1); mbar_init(v_full(b), 1); mbar_init(v_free(b), 1); }
+    for (int x = 0; x < 2; ++x) {
+      mbar_init(s_full(x, 0), 1); mbar_init(s_full(x, 1), 1); mbar_init(p_ready(x, 0), 4); mbar_init(p_ready(x, 1), 4);
+      mbar_init(pv_done(x), 1); mbar_init(o_done(x), 1); mbar_init(q_ready(x), 4);
+    }
+    mbar_init(v_land, 1);
+    sh_abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == kMmaWarp) tmem_alloc(smem_u32(&tmem_slot), 512);
+  chain_wait();
+  chain_next();
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.p.status = 0;
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  Lens lens;
+  lens.read(a.p);
+  const int queries = a.p.rows * a.p.group;
+  auto tS = [&](int x) { return tmem + (uint32_t)(x * 128); };
+  auto tO = [&](int x) { return tmem + 256u + (uint32_t)(x * HD); };
+  Pieces piece(a, lens.prefix);
+
+  if (warp == kLoaderWarp) {
+    // ------------------------------------------------------------------ loader: lane i has the i-th piece of a tile's keys
+    const int box = a.box, copies = TK / box, page = a.p.pool.page;
+    bool ok = true;
+    int kt = 0, tails = 0;                                           // tiles so far
+    auto wait = [&](uint32_t bar, uint32_t parity) { ok = mbar_wait_warp(bar, parity, abort_flag); return ok; };
+    auto page_id = [&](int key) {                                    // n_pages, which reads as zeros, where there is none
+      const int id = lane < copies && key < lens.prefix ? a.p.prefix_pages[key / page] : -1;
+      return id >= 0 && id < a.p.pool.n_pages ? id : a.p.pool.n_pages;
+    };
+    while (ok && piece.next()) {
+      int key = piece.t0 * TK + lane * box, id = page_id(key);
+      for (int j = 0; j < piece.n; ++j, ++kt) {
+        const int b = kt % kStages, k0 = (piece.t0 + j) * TK, in_page = key % page;
+        const uint32_t ph = (uint32_t)((kt / kStages) & 1);
+        const uint32_t there = __ballot_sync(0xFFFFFFFFu, id < a.p.pool.n_pages);
+        const int id_now = id;
+        key += TK;
+        if (j + 1 < piece.n) id = page_id(key);                      // the next tile's, before the waits
+        uint64_t mask = ~0ull;
+        const bool tail = k0 + TK > lens.prefix;
+        if (there != (copies == 32 ? ~0u : (1u << copies) - 1) || tail) {
+          mask = 0;
+          for (int i = 0; i < copies; ++i)
+            if ((there >> i) & 1) mask |= (box == 64 ? ~0ull : (1ull << box) - 1) << (i * box);
+          if (tail) mask &= (1ull << (lens.prefix - k0)) - 1;
+        }
+        if (!wait(k_free(b), ph ^ 1u)) break;
+        if (lane == 0) {
+          masks[kt % kMasks] = mask;
+          mbar_expect_tx(k_full(b), C::kTile);
+        }
+        __syncwarp();
+        if (lane < copies) {
+#pragma unroll
+          for (int i = 0; i < C::NB; ++i)
+            tma_load_4d(s0 + C::kOffK + b * C::kTile + i * kBlk + lane * box * 128, &a.k, i * 64, in_page, id_now, piece.head, k_full(b));
+        }
+        if (!wait(v_free(b), ph ^ 1u)) break;
+        const uint32_t lands = tail ? v_land : v_full(b);
+        if (lane == 0) mbar_expect_tx(lands, C::kTile);
+        __syncwarp();
+        if (lane < copies) {
+#pragma unroll
+          for (int i = 0; i < C::NB; ++i)
+            tma_load_4d(s0 + C::kOffV + b * C::kTile + i * kBlk + lane * box * 128, &a.v, i * 64, in_page, id_now, piece.head, lands);
+        }
+        if (tail) {                                                  // values behind the prefix's end must be finite (P is 0 there)
+          if (!wait(v_land, (uint32_t)(tails++ & 1))) break;
+          const int r0 = lens.prefix - k0;
+          for (int i = r0 * 8 * C::NB + lane; i < TK * 8 * C::NB; i += 32) {
+            const int r = i / (8 * C::NB), c = i % (8 * C::NB);      // whole rows: the swizzle permutes within a row
+            *reinterpret_cast<uint4 *>(smem + C::kOffV + b * C::kTile + (c >> 3) * kBlk + r * 128 + ((c & 7) << 4)) = make_uint4(0u, 0u, 0u, 0u);
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(v_full(b));
+        }
+      }
+    }
+    if (!ok) {                                                       // copies in flight land before the shared memory goes away
+      const unsigned long long t0 = globaltimer_ns();
+      while (globaltimer_ns() - t0 < 200000ull) {}
+    }
+  } else if (warp == kMmaWarp) {
+    // ------------------------------------------------------------------ MMA issue
+    const bool issuer = elect_one();
+    const uint32_t id1 = umma_idesc_bf16(TK), id2 = umma_idesc_bf16(HD) | (1u << 16);      // bit 16: B is MN-major
+    bool ok = true;
+    int kt = 0, st[2] = {0, 0}, pieces[2] = {0, 0};                  // key tiles, each query tile's key tiles and pieces so far
+    while (ok && piece.next()) {
+      const int nq = min(a.per_set, queries - piece.set * a.per_set), n = piece.n;
+      const bool has_b = nq > 128;
+      auto issue_s = [&](int x, int j) {                             // (the issuer only)
+        const int b = (kt + j) % kStages, c = st[x] + j;
+        const uint32_t qb = desc_lo_k(s0 + x * C::kQTile), kb = desc_lo_k(s0 + C::kOffK + b * C::kTile), d = tS(x) + (uint32_t)((c & 1) * TK);
+#pragma unroll
+        for (int ks = 0; ks < HD / 16; ++ks)
+          umma_ss(d, qb + (ks >> 2) * (kQBlk / 16) + (ks & 3) * 2, kb + (ks >> 2) * (kBlk / 16) + (ks & 3) * 2, id1, ks > 0 ? 1u : 0u);
+        umma_commit(s_full(x, c & 1));
+      };
+      auto k_wait = [&](int j) { return mbar_wait_warp(k_full((kt + j) % kStages), (uint32_t)(((kt + j) / kStages) & 1), abort_flag); };
+      ok = mbar_wait_warp(q_ready(0), (uint32_t)(pieces[0]++ & 1), abort_flag);
+      if (ok && has_b) ok = mbar_wait_warp(q_ready(1), (uint32_t)(pieces[1]++ & 1), abort_flag);
+      for (int j = 0; j < min(2, n) && ok; ++j) {                    // the first two key tiles' scores
+        ok = k_wait(j);
+        if (!ok) break;
+        tc_fence_after();
+        if (issuer) {
+          issue_s(0, j);
+          if (has_b) issue_s(1, j);
+          umma_commit(k_free((kt + j) % kStages));
+        }
+      }
+      for (int j = 0; j < n && ok; ++j) {
+        const int b = (kt + j) % kStages;
+        const uint32_t vb = desc_lo_mn(s0 + C::kOffV + b * C::kTile);
+        ok = mbar_wait_warp(v_full(b), (uint32_t)(((kt + j) / kStages) & 1), abort_flag);
+        if (ok && j + 2 < n) ok = k_wait(j + 2);
+        for (int x = 0; x < (has_b ? 2 : 1) && ok; ++x) {
+          const int c = st[x] + j;
+          ok = mbar_wait_warp(p_ready(x, c & 1), (uint32_t)((c >> 1) & 1), abort_flag);
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t d = tO(x), p = tS(x) + (uint32_t)((c & 1) * TK);
+          if (issuer) {
+#pragma unroll
+            for (int ks = 0; ks < TK / 16; ++ks) umma_ts(d, p + ks * 16, vb + ks * 128, id2, ks > 0 || j % kChain > 0 ? 1u : 0u);
+#pragma unroll
+            for (int ks = 0; ks < TK / 16; ++ks) umma_ts(d, p + ks * 16 + 8, vb + ks * 128, id2, 1u);
+            umma_commit(pv_done(x));
+            if (j + 1 == n || (j + 1) % kChain == 0) umma_commit(o_done(x));
+            if (j + 2 < n) issue_s(x, j + 2);                        // over P(j), after the products that read it
+          }
+        }
+        if (ok && issuer) {
+          umma_commit(v_free(b));
+          if (j + 2 < n) umma_commit(k_free((kt + j + 2) % kStages));
+        }
+      }
+      kt += n;
+      st[0] += n;
+      if (has_b) st[1] += n;
+    }
+  } else {
+    // ------------------------------------------------------------------ softmax of query tile x: thread = query
+    const int x = warp >> 2, row = (warp & 3) * 32 + lane;
+    const uint32_t lq = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t O = tO(x) + lq;
+    const float sc = a.scale;
+    const size_t cta_floats = (size_t)kSet * (HD + 2);
+    bool ok = true;
+    int kt = 0, st = 0, chains = 0;                                  // key tiles, this query tile's key tiles and chains so far
+    auto wait = [&](uint32_t bar, uint32_t parity) {                 // lane 0 waits, the warp takes one decision
+      if (lane == 0) ok = mbar_wait(bar, parity, abort_flag);
+      ok = __shfl_sync(0xFFFFFFFFu, ok ? 1 : 0, 0) != 0;
+      if (ok) tc_fence_after();
+      return ok;
+    };
+    while (ok && piece.next()) {
+      const int q0 = piece.set * a.per_set, nq = min(a.per_set, queries - q0), n = piece.n;
+      if (x * 128 >= nq) { kt += n; continue; }
+      const bool real = x * 128 + row < nq, busy = x * 128 + (warp & 3) * 32 < nq;        // (a warp without queries only keeps up)
+      const int v = q0 + x * 128 + row, r = v / a.p.group;
+      const size_t at = (size_t)r * a.p.nq + piece.head * a.p.group + (v - r * a.p.group);
+      {
+        // Q: K-major, 128-byte swizzle; rows past the queries are zero.  (The products with the last piece's are over: o_done.)
+        const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(a.p.q) + at * HD);
+        uint4 w[HD / 8];
+#pragma unroll
+        for (int c = 0; c < HD / 8; ++c) w[c] = real ? __ldg(src + c) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int c = 0; c < HD / 8; ++c)
+          *reinterpret_cast<uint4 *>(smem + x * C::kQTile + (c >> 3) * kQBlk + (row >> 3) * 1024 + (row & 7) * 128 + (((c & 7) ^ (row & 7)) << 4)) =
+              make_uint4(w[c].x ^ a.sign, w[c].y ^ a.sign, w[c].z ^ a.sign, w[c].w ^ a.sign);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(q_ready(x));
+      }
+      // the part's place: the item's, or the CTA's if the item begins in front of it
+      float *to = piece.t0 == 0 ? a.p.first + at * HD : a.p.rest + a.p.tc_rest + blockIdx.x * cta_floats + (size_t)(x * 128 + row) * HD;
+      float m_ref = -INFINITY, l = 0.f, m_added = -INFINITY;         // m_added: of the sums that were added to the place
+      // A chain's end: its sums to the place.
+      auto add = [&](bool first) {
+        const float f = m_added > -INFINITY ? ex2((m_added - m_ref) * sc) : 1.f;
+#pragma unroll 1
+        for (int c0 = 0; c0 < HD; c0 += 32) {
+          float o[32];
+          tmem_ld16(O + (uint32_t)c0, o);
+          tmem_ld16(O + (uint32_t)(c0 + 16), o + 16);
+          float4 old[8];
+          if (!first && real) {
+#pragma unroll
+            for (int c = 0; c < 8; ++c) old[c] = *reinterpret_cast<const float4 *>(to + c0 + 4 * c);
+          }
+          tmem_ld_wait();
+          if (!real) continue;
+#pragma unroll
+          for (int c = 0; c < 8; ++c) {
+            float4 y = make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
+            if (!first) y = make_float4(fmaf(old[c].x, f, y.x), fmaf(old[c].y, f, y.y), fmaf(old[c].z, f, y.z), fmaf(old[c].w, f, y.w));
+            *reinterpret_cast<float4 *>(to + c0 + 4 * c) = y;
+          }
+        }
+        m_added = m_ref;
+      };
+      for (int j = 0; j < n; ++j, ++kt, ++st) {
+        if (j > 0 && j % kChain == 0) {
+          if (!wait(o_done(x), (uint32_t)(chains++ & 1))) break;
+          if (busy) add(j == kChain);
+        }
+        const uint32_t S = tS(x) + lq + (uint32_t)((st & 1) * TK);
+        if (!wait(s_full(x, st & 1), (uint32_t)((st >> 1) & 1))) break;
+        if (busy) {
+          float sv[TK];
+#pragma unroll
+          for (int c = 0; c < TK; c += 16) tmem_ld16(S + (uint32_t)c, sv + c);
+          const uint64_t mask = masks[kt % kMasks];
+          tmem_ld_wait();
+          if (mask != ~0ull) {
+            const uint32_t lo = (uint32_t)mask, hi = (uint32_t)(mask >> 32);
+#pragma unroll
+            for (int c = 0; c < TK; ++c)
+              if (!(((c < 32 ? lo : hi) >> (c & 31)) & 1)) sv[c] = -INFINITY;
+          }
+          float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int c = 0; c < TK; ++c) mx4[c & 3] = fmaxf(mx4[c & 3], sv[c]);
+          const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
+          // the reference moves only when a row's maximum has passed it by more than 8 in log2 units
+          const bool grow = (mx - m_ref) * sc > 8.f || (m_ref == -INFINITY && mx > -INFINITY);
+          if (__any_sync(0xFFFFFFFFu, grow)) {
+            const float m_new = grow ? mx : m_ref;
+            const float f = m_ref > -INFINITY ? ex2((m_ref - m_new) * sc) : 1.f;       // (sums without a key are zeros)
+            if (j % kChain > 0) {
+              // O holds the previous tile's products (those of the tile before that were complete when S(j) was)
+              if (!wait(pv_done(x), (uint32_t)((st - 1) & 1))) break;
+#pragma unroll 1
+              for (int c = 0; c < HD; c += 16) {
+                float o[16];
+                tmem_ld16(O + (uint32_t)c, o);
+                tmem_ld_wait();
+                unsigned w[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) w[e] = __float_as_uint(o[e] * f);
+                tmem_st16u(O + (uint32_t)c, w);
+              }
+            }
+            l *= f;
+            m_ref = m_new;
+          }
+          const float mneg = m_ref > -INFINITY ? -m_ref * sc : 0.f;
+          float2 l2a = make_float2(0.f, 0.f), l2b = l2a;
+          const float2 sc2 = make_float2(sc, sc), mneg2 = make_float2(mneg, mneg);
+#pragma unroll
+          for (int c = 0; c < TK; c += 16) {                         // weights over their own scores: per 16 keys 8 columns of hi, 8 of lo
+            unsigned hi[8], lo[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float2 t = __ffma2_rn(make_float2(sv[c + 2 * e], sv[c + 2 * e + 1]), sc2, mneg2);
+              const float2 p = make_float2(ex2(t.x), ex2(t.y));
+              if (e & 1) l2b = __fadd2_rn(l2b, p);
+              else l2a = __fadd2_rn(l2a, p);
+              const __nv_bfloat162 h2 = __floats2bfloat162_rn(p.x, p.y);
+              hi[e] = *reinterpret_cast<const unsigned *>(&h2);
+              const float2 rest = __ffma2_rn(make_float2(__uint_as_float(hi[e] << 16), __uint_as_float(hi[e] & 0xFFFF0000u)), make_float2(-1.f, -1.f), p);
+              const __nv_bfloat162 lw = __floats2bfloat162_rn(rest.x, rest.y);
+              lo[e] = *reinterpret_cast<const unsigned *>(&lw);
+            }
+            tmem_st8u(S + (uint32_t)c, hi);
+            tmem_st8u(S + (uint32_t)(c + 8), lo);
+          }
+          l += (l2a.x + l2a.y) + (l2b.x + l2b.y);
+          tmem_st_wait();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_ready(x, st & 1));
+      }
+      if (!ok || !wait(o_done(x), (uint32_t)(chains++ & 1))) break;
+      if (busy) add(n <= kChain);
+      if (real) {
+        const float2 ml = make_float2(m_ref > -INFINITY ? m_ref * sc : -INFINITY, l);
+        const size_t mine = a.p.tc_rest + blockIdx.x * cta_floats;
+        if (piece.t0 == 0) {
+          a.p.first_ml[at] = ml;
+          a.p.more[at] = make_int4((int)(mine + cta_floats + (size_t)(x * 128 + row) * HD), (int)(mine + cta_floats + (size_t)kSet * HD + 2 * (x * 128 + row)),
+                                   (int)cta_floats, piece.ctas_behind());
+        } else {
+          *reinterpret_cast<float2 *>(a.p.rest + mine + (size_t)kSet * HD + 2 * (x * 128 + row)) = ml;
+        }
+      }
+      tc_fence_before();                                             // (O is read: the next piece's products come behind its weights)
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == kMmaWarp) tmem_dealloc(tmem, 512);
+  if (threadIdx.x == 0 && *abort_flag) atomicExch(a.p.status, 1);
+}
+
+template <int HD> int launch_t(const TcArgs &a, cudaStream_t s) {
+  static std::atomic<u64> limits{0};
+  const int limit = hsd_smem_limit((const void *)prefix_tc_kernel<HD>, Cfg<HD>::kSmem, limits);
+  if (limit) return limit;
+  HSD_CUDA_OK(hsd_launch(prefix_tc_kernel<HD>, dim3(kPrefixGrid), kThreads, Cfg<HD>::kSmem, s, 0, true, a));
+  hsd_count_launches(1);
+  return hsd_launch_status();
+}
+
+}  // namespace
+
+bool prefix_tc_takes(const PrefixArgs &a, int dtype, int hd) {
+  const long long queries = (long long)a.rows * a.group, tiles = ((long long)a.prefix_pages_n * a.pool.page + TK - 1) / TK;
+  return dtype == HSD_BF16 && (hd == 64 || hd == 128) && a.pool.page % 8 == 0 && a.scale != 0.f && queries > 16 &&
+         (queries / 128 + 1) * a.nkv * tiles < (1ll << 30);
+}
+size_t prefix_tc_floats(int hd) { return hd == 32 ? 0 : (size_t)kPrefixGrid * kSet * (hd + 2); }
+
+bool launch_prefix_tc(const PrefixArgs &p, int hd, cudaStream_t s, int &status) {
+  if (tc_init()) return false;
+  TcArgs a;
+  a.p = p;
+  a.box = 8;
+  while (a.box < TK && p.pool.page % (2 * a.box) == 0) a.box *= 2;
+  const int queries = p.rows * p.group;
+  a.sets = ceil_div(queries, kSet);
+  a.per_set = ceil_div(queries, a.sets);
+  a.scale = p.scale < 0.f ? -p.scale : p.scale;
+  a.sign = p.scale < 0.f ? 0x80008000u : 0u;
+  const PoolView &v = p.pool;
+  if (tc_make_map_pool(&a.k, v.k, hd, v.page, v.n_pages, p.nkv, v.token_bytes, v.page_bytes, v.head_bytes, a.box) ||
+      tc_make_map_pool(&a.v, v.v, hd, v.page, v.n_pages, p.nkv, v.token_bytes, v.page_bytes, v.head_bytes, a.box)) return false;
+  status = hd == 64 ? launch_t<64>(a, s) : launch_t<128>(a, s);
+  return true;
+}
+
+}  // namespace hsd

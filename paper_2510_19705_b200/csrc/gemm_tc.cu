@@ -453,6 +453,17 @@ int tc_make_map_bytes(CUtensorMap *map, const void *base, long long rows, long l
   return make_map(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, base, rows, cols, 128, box_rows);
 }
 
+int tc_make_map_pool(CUtensorMap *map, const void *pool, int hd, int page, int n_pages, int heads, long long token_bytes, long long page_bytes,
+                     long long head_bytes, int box_tokens) {
+  if (!g_encode) return HSD_E_UNSUPPORTED;
+  cuuint64_t dims[4] = {(cuuint64_t)hd, (cuuint64_t)page, (cuuint64_t)n_pages, (cuuint64_t)heads};
+  cuuint64_t strides[3] = {(cuuint64_t)token_bytes, (cuuint64_t)page_bytes, (cuuint64_t)head_bytes};
+  cuuint32_t box[4] = {(cuuint32_t)kTcBlockK, (cuuint32_t)box_tokens, 1, 1}, estr[4] = {1, 1, 1, 1};
+  CUresult r = g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(pool), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? HSD_OK : HSD_E_CUDA;
+}
+
 int tc_npad(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
 
 namespace {

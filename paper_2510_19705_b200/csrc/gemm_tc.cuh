@@ -21,6 +21,11 @@ int tc_make_map(CUtensorMap *map, const void *base, long long rows, long long co
 // ... over bytes, box = [box_rows, 128].
 int tc_make_map_bytes(CUtensorMap *map, const void *base, long long rows, long long cols, int box_rows);
 
+// 4-D bf16 tensor map over pages [head][page][token][hd] with these strides, box = [1][1][box_tokens][64], 128-byte swizzle; a page out of
+// range is read as zeros.
+int tc_make_map_pool(CUtensorMap *map, const void *pool, int hd, int page, int n_pages, int heads, long long token_bytes, long long page_bytes,
+                     long long head_bytes, int box_tokens);
+
 int tc_npad(int rows);             // 16, 32, 64, 128 or 256 (rows <= 256)
 
 // Where the q / k / v projection's rows go (GEMM_QKV_T): q rotated -> q; k rotated, v -> their cache pages.
