@@ -479,92 +479,104 @@ prefix_lane_kernel(PrefixArgs a, bool prefix) {        // prefix false: the kern
   if (!prefix) chain_wait();                   // the join waits for this kernel alone
 }
 
-// Adds a row and head's parts, a CTA each: those over the prefix, then those over the own keys, in order.
-constexpr int kJoinThreads = 128, kMostParts = 2 * (kGrid + 1);
-template <typename T, int HD>
-__global__ void __launch_bounds__(kJoinThreads)
+// Adds a row and head's parts: those over the prefix, then those over the own keys.  A warp each, or, of few rows, eight warps each, which
+// take the parts in turn.  Bound by the trips to memory that depend on one another, so all that can be asked for without an answer is asked
+// for at once: first the lists, where the parts are, and the two first parts; then the others (rows and statistics), eight at a time.
+constexpr int kJoinWarps = 8, kAtOnce = 8;
+template <typename T, int HD, int W>
+__global__ void __launch_bounds__(kJoinWarps * 32)
 prefix_join_kernel(PrefixArgs a) {
-  constexpr int LANES = HD / 4, GROUPS = kJoinThreads / LANES;
-  __shared__ float weight[kMostParts];
-  __shared__ float4 sums[kJoinThreads];
-  __shared__ float top[kJoinThreads / 32], total[kJoinThreads / 32];
-  const int row = blockIdx.x / a.nq, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, group = threadIdx.x / LANES, col = threadIdx.x % LANES * 4;
-  T *out = static_cast<T *>(a.out) + (size_t)blockIdx.x * HD;
+  constexpr int COLS = HD / 32;
+  struct alignas(COLS * 4) Cols { float v[COLS]; };
+  __shared__ float sh_o[W > 1 ? kJoinWarps : 1][HD], sh_m[kJoinWarps], sh_l[kJoinWarps];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, w = W > 1 ? warp : 0;
+  const size_t at0 = W > 1 ? blockIdx.x : (size_t)blockIdx.x * kJoinWarps + warp, own = (size_t)a.rows * a.nq;
   chain_wait();
   chain_next();
+  if (at0 >= own) return;                      // (W == 1: the warps are for themselves)
+  const int row = (int)(at0 / a.nq);
+  T *out = static_cast<T *>(a.out) + at0 * HD + lane * COLS;
+  const int4 more0 = a.more[at0], more1 = a.more[own + at0];           // (of parts that are not there: anything, and not used)
+  const float2 ml0 = a.first_ml[at0], ml1 = a.first_ml[own + at0];
+  const Cols o0 = *reinterpret_cast<const Cols *>(a.first + at0 * HD + lane * COLS), o1 = *reinterpret_cast<const Cols *>(a.first + (own + at0) * HD + lane * COLS);
   Lens lens;
   lens.read(a);
   const int b = seq_of(a, row);
+  auto write = [&](const Cols &y) {
+#pragma unroll
+    for (int c = 0; c < COLS; ++c) {
+      if constexpr (sizeof(T) == 4) out[c] = y.v[c];
+      else out[c] = __float2bfloat16_rn(y.v[c]);
+    }
+  };
+  Cols sum = {};
   if (b < 0 || b >= a.batch) {
-    if (a.zeros && group == 0) store4(out + col, make_float4(0.f, 0.f, 0.f, 0.f));
+    if (a.zeros && w == 0) write(sum);
     return;
   }
   const Seen sees = seen_by(a, lens, b, rows_of(a, b));
-  const bool has[2] = {sees.first >= 0 && lens.prefix > 0, sees.end > lens.prefix};
-  const size_t at[2] = {blockIdx.x, (size_t)a.rows * a.nq + blockIdx.x};
-  int4 more[2];
-  int n[2];
+  const bool has0 = sees.first >= 0 && lens.prefix > 0, has1 = sees.end > lens.prefix;
+  float m = -INFINITY, l = 0.f;
+  auto take = [&](float2 ml, const Cols &o) {  // one more part
+    const float n = fmaxf(m, ml.x), ref = n > -INFINITY ? n : 0.f, f = ex2(m - ref), g = ex2(ml.x - ref);
+    l = fmaf(l, f, ml.y * g);
 #pragma unroll
-  for (int x = 0; x < 2; ++x) {
-    more[x] = has[x] ? a.more[at[x]] : make_int4(0, 0, 0, 0);
-    n[x] = has[x] ? 1 + more[x].w : 0;
-  }
-  auto part = [&](int p, const float2 *&ml) -> const float * {
-    const int x = p >= n[0], i = x ? p - n[0] : p;
-    if (i == 0) { ml = a.first_ml + at[x]; return a.first + at[x] * HD; }
-    ml = reinterpret_cast<const float2 *>(a.rest + more[x].y + (size_t)(i - 1) * more[x].z);
-    return a.rest + more[x].x + (size_t)(i - 1) * more[x].z;
+    for (int c = 0; c < COLS; ++c) sum.v[c] = fmaf(sum.v[c], f, o.v[c] * g);
+    m = n;
   };
-  const int parts = min(n[0] + n[1], kMostParts);
-  float m = -INFINITY;
-  float2 mine[(kMostParts + kJoinThreads - 1) / kJoinThreads];
-#pragma unroll
-  for (int k = 0; k < (kMostParts + kJoinThreads - 1) / kJoinThreads; ++k) {
-    const int p = threadIdx.x + k * kJoinThreads;
-    const float2 *ml;
-    mine[k] = make_float2(-INFINITY, 0.f);
-    if (p < parts) { part(p, ml); mine[k] = *ml; }
-    m = fmaxf(m, mine[k].x);
+  if (w == 0) {
+    if (has0) take(ml0, o0);
+    if (has1) take(ml1, o1);
   }
-  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-  if (lane == 0) top[warp] = m;
-  __syncthreads();
+#pragma unroll 1
+  for (int x = 0; x < 2; ++x) {
+    const int4 more = x == 0 ? more0 : more1;
+    const int n = (x == 0 ? has0 : has1) ? min(more.w, kGrid) : 0;
+#pragma unroll 1
+    for (int p0 = w; p0 < n; p0 += kAtOnce * W) {
+      const int p = p0 + lane * W;             // the lane's part's statistics
+      const float2 ml = lane < kAtOnce && p < n ? *reinterpret_cast<const float2 *>(a.rest + more.y + (size_t)p * more.z) : make_float2(-INFINITY, 0.f);
+      Cols o[kAtOnce];
+      const float *from = a.rest + more.x + (size_t)p0 * more.z + lane * COLS;
 #pragma unroll
-  for (int w = 0; w < kJoinThreads / 32; ++w) m = fmaxf(m, top[w]);
-  const float ref = m > -INFINITY ? m : 0.f;
-  float l = 0.f;
+      for (int k = 0; k < kAtOnce; ++k, from += W * more.z) {
+        o[k] = Cols{};
+        if (p0 + k * W < n) o[k] = *reinterpret_cast<const Cols *>(from);
+      }
+      float top = ml.x;
+      for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+      const float next = fmaxf(m, top), ref = next > -INFINITY ? next : 0.f, f = ex2(m - ref), g = ex2(ml.x - ref);
+      float more_l = ml.y * g;
+      for (int d = 16; d > 0; d >>= 1) more_l += __shfl_xor_sync(0xFFFFFFFFu, more_l, d);
+      l = fmaf(l, f, more_l);
 #pragma unroll
-  for (int k = 0; k < (kMostParts + kJoinThreads - 1) / kJoinThreads; ++k) {
-    const int p = threadIdx.x + k * kJoinThreads;
-    const float f = ex2(mine[k].x - ref);
-    l = fmaf(mine[k].y, f, l);
-    if (p < parts) weight[p] = f;
-  }
-  for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, o);
-  if (lane == 0) total[warp] = l;
-  __syncthreads();
-  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int p = group; p < parts; p += GROUPS) {
-    const float2 *ml;
-    const float *o = part(p, ml) + col;
-    const float2 x = *reinterpret_cast<const float2 *>(o), y = *reinterpret_cast<const float2 *>(o + 2);
-    const float f = weight[p];
-    sum.x = fmaf(x.x, f, sum.x); sum.y = fmaf(x.y, f, sum.y); sum.z = fmaf(y.x, f, sum.z); sum.w = fmaf(y.y, f, sum.w);
-  }
-  sums[threadIdx.x] = sum;
-  __syncthreads();
-  if (group > 0) return;
-  sum = sums[threadIdx.x];
-  for (int g = 1; g < GROUPS; ++g) {
-    const float4 x = sums[g * LANES + threadIdx.x];
-    sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
-  }
-  l = 0.f;
+      for (int c = 0; c < COLS; ++c) sum.v[c] *= f;
 #pragma unroll
-  for (int w = 0; w < kJoinThreads / 32; ++w) l += total[w];
+      for (int k = 0; k < kAtOnce; ++k) {
+        const float gk = __shfl_sync(0xFFFFFFFFu, g, k);
+#pragma unroll
+        for (int c = 0; c < COLS; ++c) sum.v[c] = fmaf(o[k].v[c], gk, sum.v[c]);
+      }
+      m = next;
+    }
+  }
+  if constexpr (W > 1) {
+#pragma unroll
+    for (int c = 0; c < COLS; ++c) sh_o[warp][lane * COLS + c] = sum.v[c];
+    if (lane == 0) { sh_m[warp] = m; sh_l[warp] = l; }
+    __syncthreads();
+    if (warp > 0) return;
+    for (int k = 1; k < W; ++k) {
+      Cols o;
+#pragma unroll
+      for (int c = 0; c < COLS; ++c) o.v[c] = sh_o[k][lane * COLS + c];
+      take(make_float2(sh_m[k], sh_l[k]), o);
+    }
+  }
   const float inv = l != 0.f ? 1.f / l : 0.f;
-  store4(out + col, make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
+#pragma unroll
+  for (int c = 0; c < COLS; ++c) sum.v[c] *= inv;
+  write(sum);
 }
 
 template <typename T, int HD, int H> int run(const PrefixArgs &a, bool tc, cudaStream_t s) {
@@ -572,7 +584,10 @@ template <typename T, int HD, int H> int run(const PrefixArgs &a, bool tc, cudaS
   const int status = hsd_smem_limit((const void *)prefix_lane_kernel<T, HD, H>, smem_bytes<T, HD>(kMaxBatch), done);
   if (status) return status;
   HSD_CUDA_OK(hsd_launch(prefix_lane_kernel<T, HD, H>, dim3(kGrid), kThreads, smem_bytes<T, HD>(a.batch), s, 0, true, a, !tc));
-  HSD_CUDA_OK(hsd_launch(prefix_join_kernel<T, HD>, dim3(a.rows * a.nq), kJoinThreads, 0, s, 0, true, a));
+  // eight warps a row and head while that leaves one CTA an SM at most
+  const int outputs = a.rows * a.nq;
+  if (outputs <= 2 * kGrid) HSD_CUDA_OK(hsd_launch(prefix_join_kernel<T, HD, kJoinWarps>, dim3(outputs), kJoinWarps * 32, 0, s, 0, true, a));
+  else HSD_CUDA_OK(hsd_launch(prefix_join_kernel<T, HD, 1>, dim3(ceil_div(outputs, kJoinWarps)), kJoinWarps * 32, 0, s, 0, true, a));
   hsd_count_launches(2);
   return hsd_launch_status();
 }
@@ -595,7 +610,7 @@ Layout layout(int rows, int n_q_heads, int hd) {
   l.first = 256;
   l.first_ml = l.first + n * hd * 4;
   l.more = align16(l.first_ml + n * 8);
-  l.rest = l.more + n * 16;
+  l.rest = (l.more + n * 16 + 255) / 256 * 256;
   l.tc_rest = kGrid * (kWarps + 1) * kMostChunk * (hd + 2);
   l.total = l.rest + ((size_t)l.tc_rest + prefix_tc_floats(hd)) * 4;
   return l;

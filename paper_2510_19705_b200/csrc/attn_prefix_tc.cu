@@ -11,9 +11,9 @@
 // The tensor cores' adders cut off: a chain of products loses up to 2^-23 of its sum a product.  So a chain is not longer than kChain key
 // tiles (256 products of 16 keys' halves: 3e-5 at most, 2^-7 of a bf16 half step): then O is added in fp32 to the item's place in the
 // workspace, where each thread finds its own row again.
-// 320 threads: warps 0-3 / 4-7 = softmax of tile A / B, warp 8 = loader (TMA out of the pages, a lane a piece of a page), warp 9 = MMA
-// issue.  Every wait is bounded, and no waiter can be passed by (a parity wait sees a completion only until the next one): k_full and v_full
-// have their next loads behind k_free / v_free, which the issuer's commits complete; those their next MMAs behind the loader's tiles; s_full
+// 352 threads: warps 0-3 / 4-7 = softmax of tile A / B, warp 8 = loader (TMA out of the pages, a lane a piece of a page), warps 9 / 10 = MMA
+// issue of tile A / B.  Every wait is bounded, and no waiter can be passed by (a parity wait sees a completion only until the next one): k_full and v_full
+// have their next loads behind k_free / v_free, which both issuers' commits complete; those their next MMAs behind the loader's tiles; s_full
 // and pv_done theirs behind p_ready of the tile's four softmax warps; o_done its next chain behind p_ready of a tile that they begin after
 // they have read O; q_ready its next queries behind o_done; p_ready its next weights behind the scores.
 #include <algorithm>
@@ -26,25 +26,24 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kThreads = 320, kLoaderWarp = 8, kMmaWarp = 9;
+constexpr int kThreads = 352, kLoaderWarp = 8, kMmaWarp = 9;             // (two MMA warps)
 constexpr int TK = 64, kSet = 256;                       // keys of a tile; queries of an item at most
 constexpr int kQBlk = 128 * 128, kBlk = TK * 128;        // [128 queries][64 bf16] and [64 keys][64 bf16] blocks, 128-byte swizzle
 constexpr int kStages = 4, kMasks = 8;                   // (a mask outlives its keys' stage by two tiles at most)
 constexpr int kChain = 32;                               // key tiles of a chain
+constexpr int kTurn = 32 * 20 * 4;                       // 32 rows x 16 columns (and 4 that keep banks apart) of a softmax warp on their way to memory
 
 template <int HD> struct Cfg {
   static constexpr int NB = HD / 64;                     // 64-column blocks
   static constexpr int kQTile = NB * kQBlk, kTile = NB * kBlk;
   static constexpr int kOffK = 2 * kQTile, kOffV = kOffK + kStages * kTile, kOffMask = kOffV + kStages * kTile, kOffBar = kOffMask + kMasks * 8;
-  static constexpr int kSmem = kOffBar + 256 + 1024;
+  static constexpr int kOffTurn = kOffBar + 384, kSmem = kOffTurn + 8 * kTurn + 1024;
 };
 struct TcArgs {
-  CUtensorMap k, v;
+  CUtensorMap k, v, q;
   PrefixArgs p;
-  int box;                                               // tokens of a copy
-  int sets, per_set;                                     // items of a key head; queries of each
-  float scale;                                           // positive; q is negated for a negative one
-  uint32_t sign;
+  int box;                                               // tokens of a copy of keys
+  int sets, per_set, per_tile;                           // items of a key head; rows (tokens) of each; of a query tile at most
 };
 
 constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
@@ -67,9 +66,23 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float y;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
 __device__ __forceinline__ void tmem_st8u(uint32_t taddr, const unsigned *r) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
                ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+               ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, int w, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
@@ -125,13 +138,14 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
   auto o_done = [&](int x) { return b0 + 8u * (26 + x); };           // a chain's last product
   auto q_ready = [&](int x) { return b0 + 8u * (28 + x); };
   const uint32_t v_land = b0 + 8u * 30;
+  auto q_free = [&](int x) { return b0 + 8u * (32 + x); };           // a piece's last scores
   const int warp = warp_index(), lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
-    for (int b = 0; b < kStages; ++b) { mbar_init(k_full(b), 1); mbar_init(k_free(b), 1); mbar_init(v_full(b), 1); mbar_init(v_free(b), 1); }
+    for (int b = 0; b < kStages; ++b) { mbar_init(k_full(b), 1); mbar_init(k_free(b), 2); mbar_init(v_full(b), 1); mbar_init(v_free(b), 2); }
     for (int x = 0; x < 2; ++x) {
       mbar_init(s_full(x, 0), 1); mbar_init(s_full(x, 1), 1); mbar_init(p_ready(x, 0), 4); mbar_init(p_ready(x, 1), 4);
-      mbar_init(pv_done(x), 1); mbar_init(o_done(x), 1); mbar_init(q_ready(x), 4);
+      mbar_init(pv_done(x), 1); mbar_init(o_done(x), 1); mbar_init(q_ready(x), 1); mbar_init(q_free(x), 1);
     }
     mbar_init(v_land, 1);
     sh_abort = 0;
@@ -147,7 +161,6 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
   const uint32_t tmem = tmem_slot;
   Lens lens;
   lens.read(a.p);
-  const int queries = a.p.rows * a.p.group;
   auto tS = [&](int x) { return tmem + (uint32_t)(x * 128); };
   auto tO = [&](int x) { return tmem + 256u + (uint32_t)(x * HD); };
   Pieces piece(a, lens.prefix);
@@ -156,7 +169,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
     // ------------------------------------------------------------------ loader: lane i has the i-th piece of a tile's keys
     const int box = a.box, copies = TK / box, page = a.p.pool.page;
     bool ok = true;
-    int kt = 0, tails = 0;                                           // tiles so far
+    int kt = 0, tails = 0, pieces[2] = {0, 0};                       // tiles, pieces of each query tile so far
     auto wait = [&](uint32_t bar, uint32_t parity) { ok = mbar_wait_warp(bar, parity, abort_flag); return ok; };
     auto page_id = [&](int key) {                                    // n_pages, which reads as zeros, where there is none
       const int id = lane < copies && key < lens.prefix ? a.p.prefix_pages[key / page] : -1;
@@ -164,6 +177,14 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
     };
     while (ok && piece.next()) {
       int key = piece.t0 * TK + lane * box, id = page_id(key);
+      const int row0 = piece.set * a.per_set, n_rows = min(a.per_set, a.p.rows - row0);
+      for (int x = 0; x < 2 && x * a.per_tile < n_rows && ok; ++x) { // queries, of the whole tile's rows: those behind the last are not used
+        if (!wait(q_free(x), (uint32_t)(pieces[x]++ & 1) ^ 1u)) break;
+        if (lane == 0) mbar_expect_tx(q_ready(x), (uint32_t)(a.per_tile * a.p.group * 128 * C::NB));
+        __syncwarp();
+        if (lane < C::NB) tma_load_3d(s0 + x * C::kQTile + lane * kQBlk, &a.q, lane * 64, piece.head * a.p.group, row0 + x * a.per_tile, q_ready(x));
+      }
+      if (!ok) break;
       for (int j = 0; j < piece.n; ++j, ++kt) {
         const int b = kt % kStages, k0 = (piece.t0 + j) * TK, in_page = key % page;
         const uint32_t ph = (uint32_t)((kt / kStages) & 1);
@@ -216,72 +237,65 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
       const unsigned long long t0 = globaltimer_ns();
       while (globaltimer_ns() - t0 < 200000ull) {}
     }
-  } else if (warp == kMmaWarp) {
-    // ------------------------------------------------------------------ MMA issue
+  } else if (warp >= kMmaWarp) {
+    // ------------------------------------------------------------------ MMA issue of query tile x: a warp each, as an issuing thread stands
+    // still while the pipe is full, and its waits and commits would leave the pipe empty
+    const int x = warp - kMmaWarp;
     const bool issuer = elect_one();
     const uint32_t id1 = umma_idesc_bf16(TK), id2 = umma_idesc_bf16(HD) | (1u << 16);      // bit 16: B is MN-major
     bool ok = true;
-    int kt = 0, st[2] = {0, 0}, pieces[2] = {0, 0};                  // key tiles, each query tile's key tiles and pieces so far
+    int kt = 0, st = 0, pieces = 0;                                  // key tiles, the query tile's key tiles and pieces so far
     while (ok && piece.next()) {
-      const int nq = min(a.per_set, queries - piece.set * a.per_set), n = piece.n;
-      const bool has_b = nq > 128;
-      auto issue_s = [&](int x, int j) {                             // (the issuer only)
-        const int b = (kt + j) % kStages, c = st[x] + j;
+      const int n_rows = min(a.per_set, a.p.rows - piece.set * a.per_set), n = piece.n;
+      if (x * a.per_tile >= n_rows) { kt += n; continue; }
+      const int frees = n_rows > a.per_tile ? 1 : 2;                 // (for the query tile that there is not)
+      auto issue_s = [&](int j) {                                    // (the issuer only)
+        const int b = (kt + j) % kStages, c = st + j;
         const uint32_t qb = desc_lo_k(s0 + x * C::kQTile), kb = desc_lo_k(s0 + C::kOffK + b * C::kTile), d = tS(x) + (uint32_t)((c & 1) * TK);
 #pragma unroll
         for (int ks = 0; ks < HD / 16; ++ks)
           umma_ss(d, qb + (ks >> 2) * (kQBlk / 16) + (ks & 3) * 2, kb + (ks >> 2) * (kBlk / 16) + (ks & 3) * 2, id1, ks > 0 ? 1u : 0u);
         umma_commit(s_full(x, c & 1));
+        for (int i = 0; i < frees; ++i) umma_commit(k_free(b));
+        if (j + 1 == n) umma_commit(q_free(x));
       };
       auto k_wait = [&](int j) { return mbar_wait_warp(k_full((kt + j) % kStages), (uint32_t)(((kt + j) / kStages) & 1), abort_flag); };
-      ok = mbar_wait_warp(q_ready(0), (uint32_t)(pieces[0]++ & 1), abort_flag);
-      if (ok && has_b) ok = mbar_wait_warp(q_ready(1), (uint32_t)(pieces[1]++ & 1), abort_flag);
+      ok = mbar_wait_warp(q_ready(x), (uint32_t)(pieces++ & 1), abort_flag);
       for (int j = 0; j < min(2, n) && ok; ++j) {                    // the first two key tiles' scores
         ok = k_wait(j);
         if (!ok) break;
         tc_fence_after();
-        if (issuer) {
-          issue_s(0, j);
-          if (has_b) issue_s(1, j);
-          umma_commit(k_free((kt + j) % kStages));
-        }
+        if (issuer) issue_s(j);
       }
       for (int j = 0; j < n && ok; ++j) {
-        const int b = (kt + j) % kStages;
+        const int b = (kt + j) % kStages, c = st + j;
         const uint32_t vb = desc_lo_mn(s0 + C::kOffV + b * C::kTile);
         ok = mbar_wait_warp(v_full(b), (uint32_t)(((kt + j) / kStages) & 1), abort_flag);
         if (ok && j + 2 < n) ok = k_wait(j + 2);
-        for (int x = 0; x < (has_b ? 2 : 1) && ok; ++x) {
-          const int c = st[x] + j;
-          ok = mbar_wait_warp(p_ready(x, c & 1), (uint32_t)((c >> 1) & 1), abort_flag);
-          if (!ok) break;
-          tc_fence_after();
-          const uint32_t d = tO(x), p = tS(x) + (uint32_t)((c & 1) * TK);
-          if (issuer) {
+        if (ok) ok = mbar_wait_warp(p_ready(x, c & 1), (uint32_t)((c >> 1) & 1), abort_flag);
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t d = tO(x), p = tS(x) + (uint32_t)((c & 1) * TK);
+        if (issuer) {
 #pragma unroll
-            for (int ks = 0; ks < TK / 16; ++ks) umma_ts(d, p + ks * 16, vb + ks * 128, id2, ks > 0 || j % kChain > 0 ? 1u : 0u);
+          for (int ks = 0; ks < TK / 16; ++ks) umma_ts(d, p + ks * 16, vb + ks * 128, id2, ks > 0 || j % kChain > 0 ? 1u : 0u);
 #pragma unroll
-            for (int ks = 0; ks < TK / 16; ++ks) umma_ts(d, p + ks * 16 + 8, vb + ks * 128, id2, 1u);
-            umma_commit(pv_done(x));
-            if (j + 1 == n || (j + 1) % kChain == 0) umma_commit(o_done(x));
-            if (j + 2 < n) issue_s(x, j + 2);                        // over P(j), after the products that read it
-          }
-        }
-        if (ok && issuer) {
-          umma_commit(v_free(b));
-          if (j + 2 < n) umma_commit(k_free((kt + j + 2) % kStages));
+          for (int ks = 0; ks < TK / 16; ++ks) umma_ts(d, p + ks * 16 + 8, vb + ks * 128, id2, 1u);
+          umma_commit(pv_done(x));
+          if (j + 1 == n || (j + 1) % kChain == 0) umma_commit(o_done(x));
+          for (int i = 0; i < frees; ++i) umma_commit(v_free(b));
+          if (j + 2 < n) issue_s(j + 2);                             // over P(j), after the products that read it
         }
       }
       kt += n;
-      st[0] += n;
-      if (has_b) st[1] += n;
+      st += n;
     }
   } else {
     // ------------------------------------------------------------------ softmax of query tile x: thread = query
     const int x = warp >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t lq = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t O = tO(x) + lq;
-    const float sc = a.scale;
+    const float sc = a.p.scale;
     const size_t cta_floats = (size_t)kSet * (HD + 2);
     bool ok = true;
     int kt = 0, st = 0, chains = 0;                                  // key tiles, this query tile's key tiles and chains so far
@@ -292,49 +306,59 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
       return ok;
     };
     while (ok && piece.next()) {
-      const int q0 = piece.set * a.per_set, nq = min(a.per_set, queries - q0), n = piece.n;
-      if (x * 128 >= nq) { kt += n; continue; }
-      const bool real = x * 128 + row < nq, busy = x * 128 + (warp & 3) * 32 < nq;        // (a warp without queries only keeps up)
-      const int v = q0 + x * 128 + row, r = v / a.p.group;
-      const size_t at = (size_t)r * a.p.nq + piece.head * a.p.group + (v - r * a.p.group);
-      {
-        // Q: K-major, 128-byte swizzle; rows past the queries are zero.  (The products with the last piece's are over: o_done.)
-        const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(a.p.q) + at * HD);
-        uint4 w[HD / 8];
-#pragma unroll
-        for (int c = 0; c < HD / 8; ++c) w[c] = real ? __ldg(src + c) : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-        for (int c = 0; c < HD / 8; ++c)
-          *reinterpret_cast<uint4 *>(smem + x * C::kQTile + (c >> 3) * kQBlk + (row >> 3) * 1024 + (row & 7) * 128 + (((c & 7) ^ (row & 7)) << 4)) =
-              make_uint4(w[c].x ^ a.sign, w[c].y ^ a.sign, w[c].z ^ a.sign, w[c].w ^ a.sign);
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) mbar_arrive(q_ready(x));
-      }
+      const int row0 = piece.set * a.per_set + x * a.per_tile, n = piece.n;
+      const int nq = min(min(a.per_set - x * a.per_tile, a.p.rows - row0), a.per_tile) * a.p.group;        // queries of the tile
+      if (nq <= 0) { kt += n; continue; }
+      const bool real = row < nq, busy = (warp & 3) * 32 < nq;       // (a warp without queries only keeps up)
+      const int tok = row / a.p.group;
+      const int at = (row0 + tok) * a.p.nq + piece.head * a.p.group + (row - tok * a.p.group);
       // the part's place: the item's, or the CTA's if the item begins in front of it
-      float *to = piece.t0 == 0 ? a.p.first + at * HD : a.p.rest + a.p.tc_rest + blockIdx.x * cta_floats + (size_t)(x * 128 + row) * HD;
+      float *const to = piece.t0 == 0 ? a.p.first : a.p.rest + a.p.tc_rest + blockIdx.x * cta_floats;
+      const int to_row = piece.t0 == 0 ? at : x * 128 + row, reals = min(nq - (warp & 3) * 32, 32);
+      bool next_ready = false;
       float m_ref = -INFINITY, l = 0.f, m_added = -INFINITY;         // m_added: of the sums that were added to the place
-      // A chain's end: its sums to the place.
+      // A chain's end: its sums to the place, by way of shared memory, so that a row's columns are written by neighbouring lanes.  (A short call
+      // runs this once, and waits for its instructions more than for anything: so they are few.)
+      float *block = reinterpret_cast<float *>(smem + C::kOffTurn + warp * kTurn);
       auto add = [&](bool first) {
         const float f = m_added > -INFINITY ? ex2((m_added - m_ref) * sc) : 1.f;
+        // no reference has moved, as a rule: added where they lie, without a trip there and back (a row's columns are always the same lane's,
+        // so the order is that of the chains)
+        const bool same = __all_sync(0xFFFFFFFFu, f == 1.f);
 #pragma unroll 1
-        for (int c0 = 0; c0 < HD; c0 += 32) {
-          float o[32];
+        for (int c0 = 0; c0 < HD; c0 += 16) {
+          float o[16];
           tmem_ld16(O + (uint32_t)c0, o);
-          tmem_ld16(O + (uint32_t)(c0 + 16), o + 16);
-          float4 old[8];
-          if (!first && real) {
-#pragma unroll
-            for (int c = 0; c < 8; ++c) old[c] = *reinterpret_cast<const float4 *>(to + c0 + 4 * c);
-          }
           tmem_ld_wait();
-          if (!real) continue;
 #pragma unroll
-          for (int c = 0; c < 8; ++c) {
-            float4 y = make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
-            if (!first) y = make_float4(fmaf(old[c].x, f, y.x), fmaf(old[c].y, f, y.y), fmaf(old[c].z, f, y.z), fmaf(old[c].w, f, y.w));
-            *reinterpret_cast<float4 *>(to + c0 + 4 * c) = y;
+          for (int c = 0; c < 16; c += 4) *reinterpret_cast<float4 *>(block + lane * 20 + c) = make_float4(o[c], o[c + 1], o[c + 2], o[c + 3]);
+          __syncwarp();
+#pragma unroll 1
+          for (int i0 = lane >> 4; i0 < 32; i0 += 16) {              // eight rows at a time: their shuffles and loads in flight together
+            float y[8];
+            float *p[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              p[k] = to + __shfl_sync(0xFFFFFFFFu, to_row, i0 + 2 * k) * (long long)HD + c0 + (lane & 15);
+              y[k] = block[(i0 + 2 * k) * 20 + (lane & 15)];
+            }
+            if (first) {
+#pragma unroll
+              for (int k = 0; k < 8; ++k)
+                if (i0 + 2 * k < reals) *p[k] = y[k];
+            } else if (same) {
+#pragma unroll
+              for (int k = 0; k < 8; ++k)
+                if (i0 + 2 * k < reals) asm volatile("red.global.add.f32 [%0], %1;" ::"l"(p[k]), "f"(y[k]) : "memory");
+            } else {
+#pragma unroll
+              for (int k = 0; k < 8; ++k) {
+                const float f_i = __shfl_sync(0xFFFFFFFFu, f, i0 + 2 * k);
+                if (i0 + 2 * k < reals) *p[k] = fmaf(*p[k], f_i, y[k]);
+              }
+            }
           }
+          __syncwarp();
         }
         m_added = m_ref;
       };
@@ -344,7 +368,9 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
           if (busy) add(j == kChain);
         }
         const uint32_t S = tS(x) + lq + (uint32_t)((st & 1) * TK);
-        if (!wait(s_full(x, st & 1), (uint32_t)((st >> 1) & 1))) break;
+        if (!next_ready && !wait(s_full(x, st & 1), (uint32_t)((st >> 1) & 1))) break;
+        tc_fence_after();
+        next_ready = false;
         if (busy) {
           float sv[TK];
 #pragma unroll
@@ -359,8 +385,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
           }
           float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-          for (int c = 0; c < TK; ++c) mx4[c & 3] = fmaxf(mx4[c & 3], sv[c]);
-          const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
+          for (int c = 0; c < TK; c += 2) mx4[(c >> 1) & 3] = max3(mx4[(c >> 1) & 3], sv[c], sv[c + 1]);
+          const float mx = max3(fmaxf(mx4[0], mx4[1]), mx4[2], mx4[3]);
           // the reference moves only when a row's maximum has passed it by more than 8 in log2 units
           const bool grow = (mx - m_ref) * sc > 8.f || (m_ref == -INFINITY && mx > -INFINITY);
           if (__any_sync(0xFFFFFFFFu, grow)) {
@@ -404,8 +430,11 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
             tmem_st8u(S + (uint32_t)c, hi);
             tmem_st8u(S + (uint32_t)(c + 8), lo);
           }
+          // the next tile's scores are there by now, as a rule: looked at here, the answer costs nothing
+          if (j + 1 < n) next_ready = mbar_test(s_full(x, (st + 1) & 1), (uint32_t)(((st + 1) >> 1) & 1));
           l += (l2a.x + l2a.y) + (l2b.x + l2b.y);
           tmem_st_wait();
+          next_ready = __all_sync(0xFFFFFFFFu, next_ready);
         }
         tc_fence_before();
         __syncwarp();
@@ -448,8 +477,8 @@ template <int HD> int launch_t(const TcArgs &a, cudaStream_t s) {
 
 bool prefix_tc_takes(const PrefixArgs &a, int dtype, int hd) {
   const long long queries = (long long)a.rows * a.group, tiles = ((long long)a.prefix_pages_n * a.pool.page + TK - 1) / TK;
-  return dtype == HSD_BF16 && (hd == 64 || hd == 128) && a.pool.page % 8 == 0 && a.scale != 0.f && queries > 16 &&
-         (queries / 128 + 1) * a.nkv * tiles < (1ll << 30);
+  return dtype == HSD_BF16 && (hd == 64 || hd == 128) && a.pool.page % 8 == 0 && a.scale > 0.f && queries > 16 && a.group <= 64 &&
+         (a.rows / (128 / a.group) + 1) * a.nkv * tiles < (1ll << 30);
 }
 size_t prefix_tc_floats(int hd) { return hd == 32 ? 0 : (size_t)kPrefixGrid * kSet * (hd + 2); }
 
@@ -459,13 +488,12 @@ bool launch_prefix_tc(const PrefixArgs &p, int hd, cudaStream_t s, int &status) 
   a.p = p;
   a.box = 8;
   while (a.box < TK && p.pool.page % (2 * a.box) == 0) a.box *= 2;
-  const int queries = p.rows * p.group;
-  a.sets = ceil_div(queries, kSet);
-  a.per_set = ceil_div(queries, a.sets);
-  a.scale = p.scale < 0.f ? -p.scale : p.scale;
-  a.sign = p.scale < 0.f ? 0x80008000u : 0u;
+  a.per_tile = 128 / p.group;
+  a.sets = ceil_div(p.rows, 2 * a.per_tile);
+  a.per_set = ceil_div(p.rows, a.sets);
   const PoolView &v = p.pool;
-  if (tc_make_map_pool(&a.k, v.k, hd, v.page, v.n_pages, p.nkv, v.token_bytes, v.page_bytes, v.head_bytes, a.box) ||
+  if (tc_make_map_rows(&a.q, p.q, hd, p.nq, p.rows, p.group, a.per_tile) ||
+      tc_make_map_pool(&a.k, v.k, hd, v.page, v.n_pages, p.nkv, v.token_bytes, v.page_bytes, v.head_bytes, a.box) ||
       tc_make_map_pool(&a.v, v.v, hd, v.page, v.n_pages, p.nkv, v.token_bytes, v.page_bytes, v.head_bytes, a.box)) return false;
   status = hd == 64 ? launch_t<64>(a, s) : launch_t<128>(a, s);
   return true;

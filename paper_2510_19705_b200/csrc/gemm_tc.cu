@@ -464,6 +464,15 @@ int tc_make_map_pool(CUtensorMap *map, const void *pool, int hd, int page, int n
   return r == CUDA_SUCCESS ? HSD_OK : HSD_E_CUDA;
 }
 
+int tc_make_map_rows(CUtensorMap *map, const void *base, int hd, int heads, int rows, int box_heads, int box_rows) {
+  if (!g_encode) return HSD_E_UNSUPPORTED;
+  cuuint64_t dims[3] = {(cuuint64_t)hd, (cuuint64_t)heads, (cuuint64_t)rows}, strides[2] = {(cuuint64_t)hd * 2, (cuuint64_t)heads * hd * 2};
+  cuuint32_t box[3] = {(cuuint32_t)kTcBlockK, (cuuint32_t)box_heads, (cuuint32_t)box_rows}, estr[3] = {1, 1, 1};
+  CUresult r = g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? HSD_OK : HSD_E_CUDA;
+}
+
 int tc_npad(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
 
 namespace {

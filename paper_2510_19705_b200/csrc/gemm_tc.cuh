@@ -26,6 +26,9 @@ int tc_make_map_bytes(CUtensorMap *map, const void *base, long long rows, long l
 int tc_make_map_pool(CUtensorMap *map, const void *pool, int hd, int page, int n_pages, int heads, long long token_bytes, long long page_bytes,
                      long long head_bytes, int box_tokens);
 
+// 3-D bf16 tensor map over rows [row][head][hd], box = [box_rows][box_heads][64], 128-byte swizzle.
+int tc_make_map_rows(CUtensorMap *map, const void *base, int hd, int heads, int rows, int box_heads, int box_rows);
+
 int tc_npad(int rows);             // 16, 32, 64, 128 or 256 (rows <= 256)
 
 // Where the q / k / v projection's rows go (GEMM_QKV_T): q rotated -> q; k rotated, v -> their cache pages.
