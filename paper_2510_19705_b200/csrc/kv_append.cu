@@ -2,7 +2,7 @@
 // (hsd_kv_append_norm: x becomes x / sqrt(mean x^2 + eps) * gain).
 //   (y_i, y_{i+h}) = (x_i cos - x_{i+h} sin, x_{i+h} cos + x_i sin), h = head_dim / 2, cos and sin of the row's position from the
 // caller's table; values are copied.  The products and the sum are rounded to fp32 (none fused), the result once to the pool's type.
-// A thread takes eight pairs of one head of one row (16 bytes of a bf16 pool at each of the two places).  The rows' positions and
+// A thread takes eight pairs of one head after the other of one row (16 bytes of a bf16 pool at each of the two places).  The rows' positions and
 // pages come first: a warp a row counts the row starts that do not lie behind it.  The norm's sum of squares goes over the two to eight
 // neighbouring threads of a head, from the values they hold anyway: nothing is read twice.
 // Bound by memory for prompts, by the chain row -> position -> page -> store for a few rows, whose heads are divided over CTAs.
@@ -14,7 +14,7 @@
 namespace hsd {
 namespace {
 
-constexpr int kThreads = 256, kRows = 4;       // rows of a CTA at most (8191 rows of 48 heads of 128: 39 us, of 8 45, of 2 49)
+constexpr int kThreads = 256, kRows = 8;       // rows of a CTA at most
 
 struct AppendArgs {
   const unsigned char *qkv;
@@ -42,6 +42,27 @@ template <> __device__ __forceinline__ void load8<__nv_bfloat16>(const unsigned 
   f[4] = __uint_as_float(v.z << 16); f[5] = __uint_as_float(v.z & 0xFFFF0000u);
   f[6] = __uint_as_float(v.w << 16); f[7] = __uint_as_float(v.w & 0xFFFF0000u);
 }
+// Eight gains as they lie in memory (registers cost CTAs here).
+template <typename T> struct Gain8;
+template <> struct Gain8<float> {
+  float f[8];
+  __device__ __forceinline__ void load(const unsigned char *p) { load8<float>(p, f); }
+  __device__ __forceinline__ void ones() {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = 1.f;
+  }
+  __device__ __forceinline__ float get(int e) const { return f[e]; }
+};
+template <> struct Gain8<__nv_bfloat16> {
+  u32 w[4];
+  __device__ __forceinline__ void load(const unsigned char *p) {
+    const uint4 v = __ldg(reinterpret_cast<const uint4 *>(p));
+    w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+  }
+  __device__ __forceinline__ void ones() { w[0] = w[1] = w[2] = w[3] = 0x3F803F80u; }
+  __device__ __forceinline__ float get(int e) const { return __uint_as_float(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16); }
+};
+template <> struct Gain8<void> {};
 template <typename T> __device__ __forceinline__ void store8(unsigned char *p, const float *f);
 template <> __device__ __forceinline__ void store8<float>(unsigned char *p, const float *f) {
   reinterpret_cast<float4 *>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
@@ -55,36 +76,24 @@ template <> __device__ __forceinline__ void store8<__nv_bfloat16>(unsigned char 
   *reinterpret_cast<uint4 *>(p) = make_uint4(pack(f[0], f[1]), pack(f[2], f[3]), pack(f[4], f[5]), pack(f[6], f[7]));
 }
 
-// What a head's values are multiplied with: TG the gains' type, void: there is no norm.
-template <typename TG, int HD>
-__device__ __forceinline__ void norm(const unsigned char *gain, int i, float eps, float *lo, float *hi) {
+// 1 / sqrt(mean of a head's squares + eps), from the 16 values that each of its threads has.
+template <int HD>
+__device__ __forceinline__ float norm(float eps, const float *lo, const float *hi) {
   constexpr int UNITS = HD / 16;
   float sum = 0.f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) sum = fmaf(lo[e], lo[e], fmaf(hi[e], hi[e], sum));
-  const int lane = threadIdx.x & 31;
-  const u32 head = ((1u << UNITS) - 1) << (lane & ~(UNITS - 1));       // the head's threads go through the loop together
+  const u32 head = ((1u << UNITS) - 1) << (threadIdx.x & 31 & ~(UNITS - 1));       // the head's threads go through the loop together
 #pragma unroll
   for (int o = 1; o < UNITS; o <<= 1) sum += __shfl_xor_sync(head, sum, o);
-  const float f = __frsqrt_rn(__fadd_rn(sum * (1.f / HD), eps));
-  float g[8], h[8];
-  if (gain) {
-    load8<TG>(gain + i * sizeof(TG), g);
-    load8<TG>(gain + (i + HD / 2) * sizeof(TG), h);
-  }
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    lo[e] *= f;
-    hi[e] *= f;
-    if (gain) { lo[e] *= g[e]; hi[e] *= h[e]; }
-  }
+  return __frsqrt_rn(__fadd_rn(sum * (1.f / HD), eps));
 }
 
 template <typename TI, typename TO, typename TG, int HD>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 4)         // (with the norm: 8191 rows of 48 heads of 128 41 us; three CTAs an SM 50, five, which spill, 49)
 kv_append_kernel(AppendArgs a) {
   constexpr int UNITS = HD / 16, HALF = HD / 2;
-  static_assert(kRows == 4, "rows of a piece are found by three comparisons");
+  static_assert(kThreads % kRows == 0 && kThreads / kRows % UNITS == 0, "a row has whole heads' threads");
   __shared__ int sh_pos[kRows];                 // -1: the row is skipped
   __shared__ long long sh_at[kRows];            // its place in a head of the pools, in bytes
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -123,49 +132,79 @@ kv_append_kernel(AppendArgs a) {
     }
   }
   __syncthreads();
-  const int per_row = (a.nq + 2 * a.nkv) * UNITS;
-  for (int u = part * kThreads + threadIdx.x; u < n_rows * per_row; u += a.parts * kThreads) {
-    const int row = (u >= per_row) + (u >= 2 * per_row) + (u >= 3 * per_row), x = u - row * per_row;
-    const int h = x / UNITS, i = x % UNITS * 8, pos = sh_pos[row];
-    if (pos < 0) {
-      if (a.zeros && h < a.nq) {
-        const float zero[8] = {};
-        unsigned char *to = a.q_out + (((size_t)(r0 + row) * a.nq + h) * HD + i) * sizeof(TO);
-        store8<TO>(to, zero);
-        store8<TO>(to + HALF * sizeof(TO), zero);
-      }
-      continue;
+  // A thread has the same 16 places of one head after the other of a row: angles and gains stay in its registers.
+  constexpr bool NORM = !std::is_void<TG>::value;
+  const int row_threads = kThreads / a.cta_rows, row = threadIdx.x / row_threads, x = part * row_threads + threadIdx.x % row_threads;
+  if (row >= n_rows) return;
+  const int heads = a.nq + 2 * a.nkv, turned = a.nq + a.nkv, i = x % UNITS * 8, step = a.parts * row_threads / UNITS, pos = sh_pos[row];
+  if (pos < 0) {
+    if (!a.zeros) return;
+    for (int h = x / UNITS; h < a.nq; h += step) {
+      const float zero[8] = {};
+      unsigned char *to = a.q_out + (((size_t)(r0 + row) * a.nq + h) * HD + i) * sizeof(TO);
+      store8<TO>(to, zero);
+      store8<TO>(to + HALF * sizeof(TO), zero);
     }
-    const unsigned char *src = a.qkv + (size_t)(r0 + row) * a.row_bytes + ((size_t)h * HD + i) * sizeof(TI);
-    float lo[8], hi[8];
-    load8<TI>(src, lo);
-    load8<TI>(src + HALF * sizeof(TI), hi);
-    if (h < a.nq + a.nkv) {
-      if constexpr (!std::is_void<TG>::value) norm<TG, HD>(h < a.nq ? a.q_gain : a.k_gain, i, a.eps, lo, hi);
-      float c[8], s[8];
-      const unsigned char *t = reinterpret_cast<const unsigned char *>(a.rope + (size_t)pos * HD + i);
-      load8<float>(t, c);
-      load8<float>(t + HALF * 4, s);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float x = lo[e], y = hi[e];
-        lo[e] = __fsub_rn(__fmul_rn(x, c[e]), __fmul_rn(y, s[e]));
-        hi[e] = __fadd_rn(__fmul_rn(y, c[e]), __fmul_rn(x, s[e]));
-      }
-    }
-    unsigned char *dst;
-    if (h < a.nq) dst = a.q_out + ((size_t)(r0 + row) * a.nq + h) * HD * sizeof(TO);
-    else if (h < a.nq + a.nkv) dst = a.pool.k + (h - a.nq) * a.pool.head_bytes + sh_at[row];
-    else dst = a.pool.v + (h - a.nq - a.nkv) * a.pool.head_bytes + sh_at[row];
-    store8<TO>(dst + i * sizeof(TO), lo);
-    store8<TO>(dst + (HALF + i) * sizeof(TO), hi);
+    return;
   }
+  const unsigned char *src = a.qkv + (size_t)(r0 + row) * a.row_bytes + i * sizeof(TI);
+  const long long at = sh_at[row];
+  float c[8], s[8];
+  Gain8<TG> g, g2;
+  const unsigned char *t = reinterpret_cast<const unsigned char *>(a.rope + (size_t)pos * HD + i);
+  load8<float>(t, c);
+  load8<float>(t + HALF * 4, s);
+  auto gains = [&](const unsigned char *from) {
+    if constexpr (NORM) {
+      g.ones();
+      g2.ones();
+      if (from) {
+        g.load(from + i * sizeof(TG));
+        g2.load(from + (i + HALF) * sizeof(TG));
+      }
+    }
+  };
+  // heads from .. to - 1, whose first has its place at dst, the others head_bytes apart
+  auto run = [&](int &h, int to, unsigned char *dst, long long head_bytes, bool turn) {
+    dst += h * head_bytes + i * sizeof(TO);
+#pragma unroll 1
+    for (; h < to; h += step, dst += step * head_bytes) {
+      float lo[8], hi[8];
+      load8<TI>(src + (size_t)h * HD * sizeof(TI), lo);
+      load8<TI>(src + ((size_t)h * HD + HALF) * sizeof(TI), hi);
+      if (turn) {
+        if constexpr (NORM) {
+          const float f = norm<HD>(a.eps, lo, hi);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            lo[e] = lo[e] * f * g.get(e);
+            hi[e] = hi[e] * f * g2.get(e);
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float x = lo[e], y = hi[e];
+          lo[e] = __fsub_rn(__fmul_rn(x, c[e]), __fmul_rn(y, s[e]));
+          hi[e] = __fadd_rn(__fmul_rn(y, c[e]), __fmul_rn(x, s[e]));
+        }
+      }
+      store8<TO>(dst, lo);
+      store8<TO>(dst + HALF * sizeof(TO), hi);
+    }
+  };
+  int h = x / UNITS;
+  gains(a.q_gain);
+  run(h, a.nq, a.q_out + (size_t)(r0 + row) * a.nq * HD * sizeof(TO), HD * sizeof(TO), true);
+  gains(a.k_gain);
+  run(h, turned, a.pool.k + at - a.nq * a.pool.head_bytes, a.pool.head_bytes, true);
+  run(h, heads, a.pool.v + at - turned * a.pool.head_bytes, a.pool.head_bytes, false);
 }
 
 template <typename TI, typename TO, typename TG> int run(AppendArgs &a, int hd, cudaStream_t s) {
   const int per_row = (a.nq + 2 * a.nkv) * (hd / 16);
   // few rows: one a CTA and a row's heads over several, so that every thread has one piece; many rows: CTAs of up to kRows
-  a.cta_rows = a.rows >= kRows * 2 * kMeasuredSMs ? kRows : 1;
+  // (8191 rows of 48 heads of 128, with the norm: eight rows a CTA 41 us, four 43)
+  a.cta_rows = a.rows >= kRows * 2 * kMeasuredSMs ? kRows : a.rows >= kRows * kMeasuredSMs ? kRows / 2 : 1;
   a.parts = a.cta_rows > 1 ? 1 : ceil_div(per_row, kThreads);
   const long long grid = (long long)ceil_div(a.rows, a.cta_rows) * a.parts;
   if (grid > 0x7FFFFFFFll) return HSD_E_TOO_LARGE;
