@@ -6,6 +6,11 @@
 //   S[128 x 64]   = Q K^T                      both operands in shared memory
 //   P             = exp2(S c - m), thread = query, as bf16 hi + lo halves that overwrite S (a weight keeps 16 bits and more)
 //   O[128 x hd]  += P_hi V + P_lo V            A operand from tensor memory, V as it lies in the cache (MN-major)
+// Bound by the softmax warps: 100 rows of 32 heads over 8 of 128 and 40000 keys 106 us, 1.6 of what the products take (a key tile 2240 cycles,
+// the products of its two query tiles 1545, of which P_lo 512).  Of those cycles the exponentials and the weights' halves are 1310, loads, maxima
+// and barriers the rest.  What did not help: sixteen softmax warps, two a row (3 % of the largest call, and a barrier that has no limit); a quarter of the
+// exponentials on the FMA pipe (2 % slower); the two query tiles' exponentials in turn (the same).  One issuing warp for both query tiles: 2900.
+// A short call waits for its instructions, first keys and the parts' way to memory: 64 rows over 8192 keys, seven key tiles a CTA, 27 us.
 // Two query tiles share every K and V tile; S has two buffers, so that the scores of the next key tile are ready when the weights of this one
 // are.  m moves only when a row's maximum has passed it by 8; then O is rescaled.
 // The tensor cores' adders cut off: a chain of products loses up to 2^-23 of its sum a product.  So a chain is not longer than kChain key
@@ -475,10 +480,16 @@ template <int HD> int launch_t(const TcArgs &a, cudaStream_t s) {
 
 }  // namespace
 
+// Whether the call's sums over the prefix go by this kernel or by the one whose warps take sets of 16 queries, whose start is shorter and which
+// reads the prefix again for each set: by queries times keys (as many as the list has room for: the length itself is not known here) times the
+// heads' columns.  us of the other / this one, 8 key heads of 128: 32 queries each over 512 keys 13.8 / 16.6, 4096 28.3 / 23.8, 32768 157 / 52;
+// 16 queries over 4096 19.2 / 23.2, 32768 84 / 51; 8 over 32768 46 / 51; 128 over 512 19.9 / 20.7.  2 of 64: 64 over 4096 13.4 / 16.3, 128
+// over 4096 19.4 / 16.8, 16 over 32768 18.7 / 21.3, 32 over 32768 27.6 / 21.6.
+constexpr long long kEnoughWork = 90000000;
 bool prefix_tc_takes(const PrefixArgs &a, int dtype, int hd) {
-  const long long queries = (long long)a.rows * a.group, tiles = ((long long)a.prefix_pages_n * a.pool.page + TK - 1) / TK;
-  return dtype == HSD_BF16 && (hd == 64 || hd == 128) && a.pool.page % 8 == 0 && a.scale > 0.f && queries > 16 && a.group <= 64 &&
-         (a.rows / (128 / a.group) + 1) * a.nkv * tiles < (1ll << 30);
+  const long long queries = (long long)a.rows * a.group, keys = (long long)a.prefix_pages_n * a.pool.page, tiles = (keys + TK - 1) / TK;
+  return dtype == HSD_BF16 && (hd == 64 || hd == 128) && a.pool.page % 8 == 0 && a.scale > 0.f && a.group <= 64 && queries >= 16 &&
+         queries * a.nkv * hd >= kEnoughWork / keys && (a.rows / (128 / a.group) + 1) * a.nkv * tiles < (1ll << 30);
 }
 size_t prefix_tc_floats(int hd) { return hd == 32 ? 0 : (size_t)kPrefixGrid * kSet * (hd + 2); }
 

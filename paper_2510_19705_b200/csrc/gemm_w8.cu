@@ -5,9 +5,10 @@
 //
 // Weight rows lie on the MMA's M side in both kernels: a thread of the finish has one weight row, so that a warp stores 32 neighbours of
 // an output row at a time, whatever N is.
-// Few rows (w8_stream_kernel): bound by the weight stream.  A tile is up to 128 weight rows, its tokens (padded to whole 16s) are on
+// Few rows (w8_stream_kernel): bound by the weight stream (16 rows, 28672 x 4096: 22 us, 0.83 of the copy bandwidth).  A tile is up to 128 weight rows, its tokens (padded to whole 16s) are on
 // the N side; with few tiles K is divided over a cluster of CTAs, whose sums are added over distributed shared memory.
-// Many rows (w8_pair_kernel): bound by the tensor pipe.  Tiles of 256 weight rows x up to 256 tokens on CTA pairs (cta_group::2), as the
+// Many rows (w8_pair_kernel): bound by the tensor pipe (4095 rows, 14336 x 4096: 161 us, 2.98 POP/s, alone; 2.35 POP/s among others, under the
+// power cap, with the codes' 11 us).  Tiles of 256 weight rows x up to 256 tokens on CTA pairs (cta_group::2), as the
 // prompt GEMM's.
 // Both: 192 threads (TMA producer, MMA issuer, four finishing warps), k-blocks of 128 codes = one 128-byte swizzle row, every wait bounded
 // (a wait that gives up sets the workspace's status word); no waiter can be passed by, as in the bf16 kernels: full has its next loads
@@ -579,6 +580,8 @@ template <int NPAD, typename TO> int run_stream(const W8Args &a, int n_tiles, in
 }
 template <typename TO> int run(W8Args &a, const void *codes_a, const void *codes_w, int K, cudaStream_t s) {
   const int sms = sm_count();
+  // Up to 256 rows by the weight stream, us against the pairs': 2048 x 5632, 16 / 128 / 256 rows 7.4 / 9.5 / 12.8 against 12.6 / 14.8 / 22.5; 4096 x 4096
+  // 7.3 / 10.7 / 14.6 against 10.4 / 12.9 / 19.4; 32000 x 2048 13.9 / 18.9 / 27.6 against 16.3 / 20.4 / 28.1 (14336 x 4096: 24.0 against 22.7 with 256)
   if (a.R <= 256) {
     const int S = split_of(a.N, a.KB, sms), npad = tc_npad(a.R);
     a.tile_rows = tile_rows_of(a.N, S, sms);

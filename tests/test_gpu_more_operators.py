@@ -347,10 +347,11 @@ def prefix64(q, k_pool, v_pool, table, lens, pages, P, starts, scale):
     return out, size, most
 
 
-def check_prefix(lib, q, k, v, table, lens, pages, P, starts=None, scale=None):
+def check_prefix(lib, q, k, v, table, lens, pages, P, starts=None, scale=None, long=True):
+    """With the list of pages as it is and, for bf16 (`long`), with more of them behind the prefix's end: a call whose list has room for many
+    keys takes the tensor-memory kernel."""
     rows, nq, hd = q.shape
-    args = (q, k, v, table, ints(lens), pages, ints([P]), None if starts is None else ints(starts), scale)
-    got = lib.hsd_prefix_attention(*args)
+    nkv, page = k.shape[0], k.shape[2]
     want, size, most = prefix64(q, k, v, table.cpu(), lens, pages.cpu(), P, starts, hd ** -0.5 if scale is None else scale)
     none = want[:, 0, 0].isnan()
     # as in the attention by sequence: a score's sum and its exponential; tiles added one after the other; bf16 weights of 16 bits, and
@@ -358,12 +359,18 @@ def check_prefix(lib, q, k, v, table, lens, pages, P, starts=None, scale=None):
     weight = (hd + 4) * 2.0 ** -23 * most + 2.0 ** -21 + (max(max(lens), P) / 8 + 64) * 2.0 ** -24 + (2.0 ** -16 if q.dtype == BF16 else 0)
     chain = 256 * 2.0 ** -23 if q.dtype == BF16 else 0
     bound = HALF_STEP[q.dtype] * want.abs() + (2 * weight + chain) * size + 1e-37
-    off = (got.double().cpu() - want).abs()
-    assert bool((off <= bound)[~none].all()), (float((off / bound)[~none].max()), int((off > bound)[~none].sum()))
-    assert bool((got.cpu()[none] == 0).all())
-    into = torch.full_like(q, 7.0)
-    assert lib.hsd_prefix_attention(*args, out=into) is into
-    assert torch.equal(into[~none.cuda()], got[~none.cuda()]) and bool((into[none.cuda()] == 7.0).all())      # sums in a fixed order
+    lists = [pages]
+    if long and q.dtype == BF16:
+        lists.append(torch.cat((pages, torch.full((1 + 90000000 // (rows * nq // nkv * nkv * hd * page),), -1, dtype=torch.int32, device="cuda"))))
+    for these in lists:
+        args = (q, k, v, table, ints(lens), these, ints([P]), None if starts is None else ints(starts), scale)
+        got = lib.hsd_prefix_attention(*args)
+        off = (got.double().cpu() - want).abs()
+        assert bool((off <= bound)[~none].all()), (float((off / bound)[~none].max()), int((off > bound)[~none].sum()))
+        assert bool((got.cpu()[none] == 0).all())
+        into = torch.full_like(q, 7.0)
+        assert lib.hsd_prefix_attention(*args, out=into) is into
+        assert torch.equal(into[~none.cuda()], got[~none.cuda()]) and bool((into[none.cuda()] == 7.0).all())      # sums in a fixed order
     return got
 
 
@@ -432,7 +439,7 @@ def test_prefix_attention_without_a_prefix_and_with_more_than_its_pages(lib, dty
     for P in (0, -5):
         got = check_prefix(lib, q, k, v, table, [i * 4 for i in range(20)], pages, P)
         assert bool((got[0] == 0).all())
-    check_prefix(lib, q, k, v, table, [40 + i for i in range(20)], pages, 1000)           # 32 positions of the prefix
+    check_prefix(lib, q, k, v, table, [40 + i for i in range(20)], pages, 1000, long=False)           # 32 positions of the prefix
     long = ints(torch.arange(10).repeat(2).tolist())                                     # a prefix past the sequences' room
     check_prefix(lib, q, k, v, table, [200 + 9 * i for i in range(20)], long, 290)
 
@@ -574,3 +581,128 @@ def test_prefix_attention_far_into_a_large_pool(lib):
     for p in pages.tolist() + table[table >= 0].flatten().tolist():
         k[0, p], v[0, p] = randn(g, 16, 128, dtype=BF16), randn(g, 16, 128, dtype=BF16)
     check_prefix(lib, randn(g, 24, 4, 128, dtype=BF16), k, v, table, [45 + i % 19 for i in range(24)], pages, 44)
+
+
+@pytest.mark.parametrize("nq,nkv", [(32, 1), (14, 2), (80, 2), (64, 1), (65, 1)])
+@pytest.mark.parametrize("rows", [4, 19, 70])
+def test_prefix_attention_of_query_tiles_that_are_not_full(lib, rows, nq, nkv):
+    """Groups that divide a tile of 128 queries or do not, one query tile, two, an odd number of them; groups past a half of one."""
+    g = gen(rows + nq)
+    k, v, table, pages = prefix_cache(g, rows, nkv, 128, 16, 150, 20, BF16)
+    check_prefix(lib, randn(g, rows, nq, 128, dtype=BF16), k, v, table, [151 + i % 20 for i in range(rows)], pages, 150)
+
+
+def prefix_in_64_bits(q, k, v, pages, P, scale):
+    out, group, hd = torch.empty(q.shape, dtype=torch.float64, device="cuda"), q.shape[1] // k.shape[0], q.shape[2]
+    for h in range(k.shape[0]):
+        kh, vh = (x[h][pages.long()].reshape(-1, hd)[:P].double() for x in (k, v))
+        for r in range(0, q.shape[0], 100):
+            out[r:r + 100, h * group:(h + 1) * group] = torch.softmax(q[r:r + 100, h * group:(h + 1) * group].double() @ kh.T * scale, dim=-1) @ vh
+    return out
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("grows", [False, True])
+def test_prefix_attention_adds_long_chains_in_fp32(lib, hd, grows):
+    """Several chains a CTA.  Means of 1 and its neighbour lie about their middle, where a small loss rounds down what should be rounded up; and
+    scores that grow along the keys, so that a row's reference moves between the chains."""
+    g, rows, P = gen(hd), 500, 40000
+    k = randn(g, 1, P // 16, 16, hd, dtype=BF16)
+    v = (1 + 2.0 ** -7 * torch.randint(0, 2, k.shape, generator=g, device="cuda")).to(BF16)
+    q = randn(g, rows, 8, hd, dtype=BF16, std=0.3)
+    if grows:
+        k[0, :, :, 0] = torch.linspace(0, 20, P // 16, device="cuda")[:, None].to(BF16)
+        q[:, :, 0] = 30.0
+    pages = torch.randperm(P // 16, generator=g, device="cuda").to(torch.int32).contiguous()
+    if grows:
+        pages = torch.arange(P // 16, dtype=torch.int32, device="cuda")
+    scale = hd ** -0.5
+    got = lib.hsd_prefix_attention(q, k, v, ints([[0]]).expand(rows, 1).contiguous(), ints([P] * rows), pages, ints([P])).double()
+    want = prefix_in_64_bits(q, k, v, pages, P, scale)
+    # a chain: 256 products, of which each may cut off 2^-23; chains and parts: some twenty additions and the quotient; the weights' sum: a CTA's 4300
+    # keys in four turns, nearest (eight deviations of 2^-24 / sqrt(3)); a weight counts by the values' difference, 2^-7, alone
+    most = float((q.double().abs().amax(dim=(0, 1)) * k.double().abs().amax(dim=(0, 1, 2))).sum()) * scale
+    bound = 256 * 2.0 ** -23 + 24 * 2.0 ** -24 + 8 / 3 ** 0.5 * 1075 ** 0.5 * 2.0 ** -24 + 2.0 ** -7 * (2.0 ** -15 + (hd + 4) * 2.0 ** -22 * most)
+    assert bool(((got - want).abs() <= 2.0 ** -8 + bound * want).all()), float(((got - want).abs() - 2.0 ** -8).max())
+    again = lib.hsd_prefix_attention(q, k, v, ints([[0]]).expand(rows, 1).contiguous(), ints([P] * rows), pages, ints([P])).double()
+    assert torch.equal(got, again)
+
+
+# ------------------------------------------------------------------------------------------------ together
+class Layer:
+    """One attention layer of a decoder with 8-bit weights and norms of queries and keys, over continuations of one prompt."""
+    d, nq, nkv, hd, page = 512, 8, 2, 64, 16
+
+    def __init__(self, lib, seed, batch, P, own):
+        g = gen(seed)
+        self.lib, self.P = lib, P
+        heads = self.nq + 2 * self.nkv
+        self.qkv = lib.hsd_quantize_rows(randn(g, heads * self.hd, self.d, dtype=BF16, std=self.d ** -0.5))
+        self.out = lib.hsd_quantize_rows(randn(g, self.d, self.nq * self.hd, dtype=BF16, std=self.d ** -0.5))
+        self.gains = [1 + randn(g, self.hd, std=0.2).to(BF16) for _ in range(2)]
+        self.rope = lib.rope_table(P + own, self.hd)
+        self.k, self.v, self.table, self.pages = prefix_cache(g, batch, self.nkv, self.hd, self.page, P, own, BF16)
+        self.prefix = ints([P])
+        # room behind the prefix in the list, so that its sums go by tensor memory
+        self.pages = torch.cat((self.pages, torch.full((3000,), -1, dtype=torch.int32, device="cuda")))
+
+    def step(self, x, before, after, starts):
+        """x [rows, d] -> (rows of q, k and v, queries, attention, output)."""
+        lib = self.lib
+        qkv = lib.hsd_gemm_w8(x, *self.qkv)
+        q = lib.hsd_kv_append_norm(qkv.view(len(x), -1, self.hd), *self.gains, 1e-6, self.k, self.v, self.table, before, self.rope, starts)
+        att = lib.hsd_prefix_attention(q, self.k, self.v, self.table, after, self.pages, self.prefix, starts)
+        return qkv, q, att, lib.hsd_gemm_w8(att.view(len(x), -1), *self.out, BF16)
+
+
+def test_a_layer_of_continuations_of_one_prompt(lib):
+    """The calls of a step as they follow one another, each against 64 bits on what the one before gave; steps of one to three rows."""
+    batch, P = 24, 100
+    layer, lens = Layer(lib, 5, batch, P, 40), [P + i % 7 for i in range(batch)]
+    for turn in range(3):
+        n = [1 + (i + turn) % 3 for i in range(batch)]
+        starts = [sum(n[:i]) for i in range(batch + 1)]
+        x = randn(gen(turn), starts[-1], layer.d, dtype=BF16)
+        after = [a + b for a, b in zip(lens, n)]
+        keep = layer.k.clone(), layer.v.clone()
+        qkv, q, att, y = layer.step(x, ints(lens), ints(after), ints(starts))
+        assert torch.equal(qkv, check_w8(lib, x, *layer.qkv))
+        k1, v1 = layer.k.clone(), layer.v.clone()
+        layer.k.copy_(keep[0]), layer.v.copy_(keep[1])
+        found = append64(qkv.view(len(x), -1, layer.hd), layer.gains, 1e-6, layer.table, lens, layer.rope, starts, layer.nkv, (layer.k.shape[1], layer.page))
+        assert len(found) == len(x)
+        for r, (pg, t, qy, ky, vx, size) in found.items():
+            assert bool(((q[r].double().cpu() - qy).abs() <= 2.0 ** -8 * qy.abs() + 18 * 2.0 ** -24 * size[:layer.nq] + 1e-37).all())
+            layer.k[:, pg, t], layer.v[:, pg, t] = k1[:, pg, t], v1[:, pg, t]
+        assert torch.equal(layer.k, k1) and torch.equal(layer.v, v1)                      # nothing else was written
+        assert torch.equal(att, check_prefix(lib, q, layer.k, layer.v, layer.table, after, layer.pages, P, starts, long=False))
+        assert torch.equal(y, check_w8(lib, att.view(len(x), -1), *layer.out, BF16))
+        lens = after
+
+
+def test_a_captured_layer_follows_its_inputs_and_two_at_once(lib):
+    batch, P = 24, 100
+    layers = [Layer(lib, 6 + i, batch, P, 40) for i in range(2)]
+    xs = [randn(gen(i), batch, Layer.d, dtype=BF16) for i in range(2)]
+    before, after = ints([P] * batch), ints([P + 1] * batch)
+    for layer, x in zip(layers, xs):
+        layer.step(x, before, after, None)
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for layer, x in zip(layers, xs):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs.append(layer.step(x, before, after, None)[3])
+        graphs.append(graph)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for turn in range(6):
+        before.copy_(ints([P + turn] * batch)), after.copy_(ints([P + turn + 1] * batch))
+        for i, x in enumerate(xs):
+            x.copy_(randn(gen(10 + 2 * turn + i), batch, Layer.d, dtype=BF16))
+        torch.cuda.synchronize()
+        for graph, stream in zip(graphs, streams):
+            with torch.cuda.stream(stream):
+                graph.replay()
+        torch.cuda.synchronize()
+        for layer, x, out in zip(layers, xs, outs):
+            assert torch.equal(out, layer.step(x, before, after, None)[3])
