@@ -598,9 +598,12 @@ template <typename TO> int run(W8Args &a, const void *codes_a, const void *codes
       default: return run_stream<256, TO>(a, n_tiles, S, grid, s);
     }
   }
-  // tokens of a tile: as many as spread R evenly over the tiles it needs
-  a.m_tiles = ceil_div(a.R, 256);
-  a.tokens = ceil_div(ceil_div(a.R, a.m_tiles), 32) * 32;
+  // tokens of a tile: as many as spread R evenly over the rounds of the CTA pairs that tiles of 256 need (us against tiles of 256: 3375 rows of
+  // 362 x 12528 41 / 48, 512 of 4096 x 4096 14.1 / 20.8, 1000 of 6144 x 4096 26.5 / 32.3, 2000 of 1000 x 2000 12.6 / 17.3)
+  const int n_tiles = ceil_div(a.N, 2 * kTile), pairs = sms / 2, most = ceil_div(a.R, 256);
+  const long long rounds = ((long long)most * n_tiles + pairs - 1) / pairs;
+  a.tokens = ceil_div(ceil_div(a.R, (int)std::max<long long>(most, std::min<long long>(rounds * pairs / n_tiles, a.R))), 32) * 32;
+  a.m_tiles = ceil_div(a.R, a.tokens);
   a.tiles = a.m_tiles * ceil_div(a.N, 2 * kTile);
   int status = tc_make_map_bytes(&a.w, codes_w, a.N, K, kTile);
   if (!status) status = tc_make_map_bytes(&a.a, codes_a, a.R, K, a.tokens / 2);
