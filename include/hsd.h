@@ -459,7 +459,7 @@ int hsd_gemm_w4(const void *A, int R, int K, const void *codes, const void *scal
  * have codes 0.  Activations for hsd_gemm_w8, and weights: a row is an output channel.
  *   x       device [rows, K], HSD_F32 or HSD_BF16, rows row_stride elements apart
  *   codes   device int8 [rows, K];  scales  device fp32 [rows]
- * Errors: INVALID_ARG, CUDA. */
+ * Errors: INVALID_ARG, TOO_LARGE (K over 2^31 - 2^16), CUDA. */
 int hsd_quantize_rows(const void *x, int dtype, int rows, int K, long long row_stride, void *codes, float *scales, void *stream);
 
 /* Product in 8-bit integers with scales of tokens and channels: out[r, n] = (sum_k a[r, k] codes[n, k]) a_scales[r] scales[n].  The sum is

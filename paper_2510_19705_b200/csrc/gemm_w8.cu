@@ -625,6 +625,7 @@ extern "C" int hsd_quantize_rows(const void *x, int dtype, int rows, int K, long
   using namespace hsd;
   if (!x || !codes || !scales || rows <= 0 || K <= 0 || row_stride < K || (dtype != HSD_F32 && dtype != HSD_BF16)) return HSD_E_INVALID_ARG;
   if ((reinterpret_cast<uintptr_t>(x) & (dtype == HSD_F32 ? 3 : 1)) || !words(scales, nullptr)) return HSD_E_INVALID_ARG;
+  if (K > 0x7FFF0000) return HSD_E_TOO_LARGE;                 // (places past the row's end have to be numbers too)
   return quantize(x, dtype, rows, K, row_stride, codes, scales, (cudaStream_t)stream);
 }
 

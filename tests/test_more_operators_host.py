@@ -94,6 +94,10 @@ def test_quantize_rows_refuses_arguments(bad):
     assert quantize(**bad) == -1
 
 
+def test_quantize_rows_sizes():
+    assert quantize(K=(1 << 31) - 1, stride=1 << 31) == -8
+
+
 def test_the_binding_wants_cuda_tensors_of_the_right_types():
     f, b, i = torch.zeros(2, 8, 64), torch.zeros(2, 4, 16, 64, dtype=torch.bfloat16), torch.zeros(2, 3, dtype=torch.int32)
     calls = (lambda: binding.hsd_kv_append_norm(f, None, None, 1e-6, b, b, i, i[:, 0], f), lambda: binding.hsd_prefix_attention(f, b, b, i, i[:, 0], i[0], i[0, :1]),
