@@ -706,3 +706,93 @@ def test_a_captured_layer_follows_its_inputs_and_two_at_once(lib):
         torch.cuda.synchronize()
         for layer, x, out in zip(layers, xs, outs):
             assert torch.equal(out, layer.step(x, before, after, None)[3])
+
+
+# ------------------------------------------------------------------------------------------------ on tensor memory
+def with_room(pages, keys=400000):
+    """A list with room for many keys behind the prefix's end, so that the call's sums over the prefix go by tensor memory."""
+    return torch.cat((pages, torch.full((keys // 16,), -1, dtype=torch.int32, device="cuda")))
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_prefix_attention_on_tensor_memory_reads_nothing_that_is_not_there(lib, hd):
+    g, P, batch = gen(hd), 75, 36
+    k, v, table, pages = prefix_cache(g, batch, 2, hd, 16, P, 40, BF16)
+    lens = [P + 1 + i for i in range(34)] + [0, 70]
+    q = randn(g, batch, 8, hd, dtype=BF16)
+    args = (table, ints(lens), with_room(pages), ints([P]))
+    want = lib.hsd_prefix_attention(q, k, v, *args)
+    for bad in (float("nan"), float("inf"), torch.finfo(BF16).min):
+        k2, v2 = torch.full_like(k, bad), torch.full_like(v, bad)
+        for i, n in enumerate(lens):
+            for p in range(P, n):
+                at = int(table[i, p // 16])
+                k2[:, at, p % 16], v2[:, at, p % 16] = k[:, at, p % 16], v[:, at, p % 16]
+        for p in range(P):
+            k2[:, pages[p // 16], p % 16], v2[:, pages[p // 16], p % 16] = k[:, pages[p // 16], p % 16], v[:, pages[p // 16], p % 16]
+        assert torch.equal(want, lib.hsd_prefix_attention(q, k2, v2, *args))
+
+
+@pytest.mark.parametrize("rows", [50, 130])
+def test_prefix_attention_on_tensor_memory_keeps_nan_to_its_rows(lib, rows):
+    g = gen(rows)
+    k, v, table, pages = prefix_cache(g, rows, 1, 64, 16, 600, 20, BF16)
+    q = randn(g, rows, 2, 64, dtype=BF16)
+    q[0, 1, 3], q[rows - 1, 0, 9] = float("nan"), float("inf")
+    args = (table, ints([605] * rows), with_room(pages), ints([600]))
+    got = lib.hsd_prefix_attention(q, k, v, *args)
+    assert bool(got[0, 1].isnan().all()) and bool(got[0, 0].isfinite().all()) and bool(got[1:-1].isfinite().all()) and bool(got[-1, 0].isnan().all())
+    v[0, pages[7], 3, 11] = float("nan")                                    # seen by all rows
+    assert bool(lib.hsd_prefix_attention(q, k, v, *args)[:, :, 11].isnan().all())
+    v[0, pages[7], 3, 11], k[0, pages[9], 2, 5] = 0, float("nan")
+    assert bool(lib.hsd_prefix_attention(q, k, v, *args).isnan().all())
+
+
+def test_prefix_attention_on_tensor_memory_follows_its_lists_when_replayed_and_on_two_streams(lib):
+    g, rows = gen(14), 70
+    k, v, table, pages = prefix_cache(g, rows, 2, 128, 16, 5000, 100, BF16)
+    qs, lens, P = [randn(g, rows, 8, 128, dtype=BF16) for _ in range(2)], ints([0] * rows), ints([0])
+    room = with_room(pages)
+    lib.hsd_prefix_attention(qs[0], k, v, table, lens, room, P)
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for x in qs:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs.append(lib.hsd_prefix_attention(x, k, v, table, lens, room, P))
+        graphs.append(graph)
+    streams = [torch.cuda.Stream() for _ in qs]
+    for prefix in (5000, 4992, 64, 1, 0, 2049):
+        values = [prefix + 1 + (i * 17) % 90 for i in range(rows)] if prefix >= 4992 else [prefix] * rows
+        lens.copy_(ints(values)), P.copy_(ints([prefix]))
+        torch.cuda.synchronize()
+        for graph, stream in zip(graphs, streams):
+            with torch.cuda.stream(stream):
+                graph.replay()
+        torch.cuda.synchronize()
+        for x, out in zip(qs, outs):
+            assert torch.equal(out, lib.hsd_prefix_attention(x, k, v, table, ints(values), room, ints([prefix])))
+
+
+@pytest.mark.parametrize("order,page", [("head", 8), ("token", 24), ("token", 64), ("head", 256)])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_prefix_attention_on_tensor_memory_over_pages_of_any_eights(lib, order, page, hd):
+    g = gen(page)
+    for P in (63, 64, 65, 700):
+        k, v, table, pages = prefix_cache(g, 9, 2, hd, page, P, 30, BF16, order)
+        check_prefix(lib, randn(g, 9, 12, hd, dtype=BF16), k, v, table, [P + 1 + i for i in range(9)], pages, P)
+
+
+def test_prefix_attention_takes_a_batch_of_thousands(lib):
+    g, batch, P = gen(15), 4096, 7
+    for dtype in (BF16, FP32):
+        k, v, table = cache(g, batch, 1, 32, 4, 4, dtype)
+        pages = ints([batch * 4, batch * 4 + 1])
+        spare = [p for p in range(k.shape[1]) if p not in set(table.flatten().tolist())]
+        pages = ints(spare[:2])
+        lens, q = ints([P + 1 + i % 9 for i in range(batch)]), randn(g, batch, 1, 32, dtype=dtype)
+        for t in (k, v):                                                    # the prefix's last page is half each sequence's own
+            t[:, table[:, 1].long(), :3] = t[:, pages[1].long(), :3][:, None]
+        table[:, 0] = pages[0]
+        a, b = lib.hsd_prefix_attention(q, k, v, table, lens, pages, ints([P])), lib.hsd_paged_attention(q, k, v, table, lens)
+        assert bool(((a.double() - b.double()).abs() <= 2 * HALF_STEP[dtype] * b.double().abs() + 2.0 ** -18 * v.abs().max()).all())
