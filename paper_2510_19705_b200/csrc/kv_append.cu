@@ -203,8 +203,9 @@ kv_append_kernel(AppendArgs a) {
 template <typename TI, typename TO, typename TG> int run(AppendArgs &a, int hd, cudaStream_t s) {
   const int per_row = (a.nq + 2 * a.nkv) * (hd / 16);
   // few rows: one a CTA and a row's heads over several, so that every thread has one piece; many rows: CTAs of up to kRows
-  // (8191 rows of 48 heads of 128, with the norm: eight rows a CTA 41 us, four 43)
-  a.cta_rows = a.rows >= kRows * 2 * kMeasuredSMs ? kRows : a.rows >= kRows * kMeasuredSMs ? kRows / 2 : 1;
+  // (48 heads of 128: 8191 rows with the norm, eight rows a CTA 41 us, four 43; without, 1000 rows, four rows a CTA 6.9, one 9.6, 300 rows two 4.4,
+  // one, whose CTAs are more than fit at once, 5.3)
+  a.cta_rows = a.rows >= kRows * 2 * kMeasuredSMs ? kRows : a.rows >= kRows / 2 * kMeasuredSMs ? kRows / 2 : a.rows > kMeasuredSMs ? kRows / 4 : 1;
   a.parts = a.cta_rows > 1 ? 1 : ceil_div(per_row, kThreads);
   const long long grid = (long long)ceil_div(a.rows, a.cta_rows) * a.parts;
   if (grid > 0x7FFFFFFFll) return HSD_E_TOO_LARGE;
