@@ -15,12 +15,13 @@
 // are.  m moves only when a row's maximum has passed it by 8; then O is rescaled.
 // The tensor cores' adders cut off: a chain of products loses up to 2^-23 of its sum a product.  So a chain is not longer than kChain key
 // tiles (256 products of 16 keys' halves: 3e-5 at most, 2^-7 of a bf16 half step): then O is added in fp32 to the item's place in the
-// workspace, where each thread finds its own row again.
+// workspace, the same columns by the same lanes each time.
 // 352 threads: warps 0-3 / 4-7 = softmax of tile A / B, warp 8 = loader (TMA out of the pages, a lane a piece of a page), warps 9 / 10 = MMA
 // issue of tile A / B.  Every wait is bounded, and no waiter can be passed by (a parity wait sees a completion only until the next one): k_full and v_full
 // have their next loads behind k_free / v_free, which both issuers' commits complete; those their next MMAs behind the loader's tiles; s_full
 // and pv_done theirs behind p_ready of the tile's four softmax warps; o_done its next chain behind p_ready of a tile that they begin after
-// they have read O; q_ready its next queries behind o_done; p_ready its next weights behind the scores.
+// they have read O; q_ready its next queries behind q_free, which the commit behind a piece's last scores completes; p_ready its next weights
+// behind the scores.
 #include <algorithm>
 #include "attn_prefix.cuh"
 #include "gemm_tc.cuh"

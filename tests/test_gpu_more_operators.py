@@ -112,7 +112,7 @@ def test_append_norm_without_gains_and_other_eps(lib, gains, eps):
     check_append(lib, randn(g, 3, 7, 64, std=1e-3), gains, eps, k, v, table, [3, 0, 31], lib.rope_table(64, 64))
 
 
-@pytest.mark.parametrize("rows", [1, 40, 2503])
+@pytest.mark.parametrize("rows", [1, 40, 301, 701, 2503])
 @pytest.mark.parametrize("dtype", [BF16, FP32])
 def test_append_norm_ragged_rows(lib, rows, dtype):
     g = gen(rows)
