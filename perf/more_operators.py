@@ -20,27 +20,27 @@ EPS = 1e-6
 def listed():
     return [
         # four continuations of the 8B shape's prompt of 1024 tokens, a few tokens in: latency
-        dict(name="prefix 4 x 1024", op="prefix", dtype="bf16", batch=4, most=1, nq=32, nkv=8, hd=128, page=16, prefix=1024, own=40),
+        dict(name="prefix, 4 x 1024", op="prefix", dtype="bf16", batch=4, most=1, nq=32, nkv=8, hd=128, page=16, prefix=1024, own=40),
         # samples of one long prompt, hundreds of tokens each
-        dict(name="prefix 64 x 8192", op="prefix", dtype="bf16", batch=64, most=1, nq=32, nkv=8, hd=128, page=16, prefix=8192, own=500),
+        dict(name="prefix, 64 x 8192", op="prefix", dtype="bf16", batch=64, most=1, nq=32, nkv=8, hd=128, page=16, prefix=8192, own=500),
         # up to nine rows a sequence (eight drafts and one more) behind a prompt that ends inside a page
-        dict(name="prefix 16 x 9 rows 16395", op="prefix", dtype="bf16", batch=16, most=9, nq=32, nkv=8, hd=128, page=16, prefix=16395, own=300),
+        dict(name="prefix, 16 x 9 rows, 16395", op="prefix", dtype="bf16", batch=16, most=9, nq=32, nkv=8, hd=128, page=16, prefix=16395, own=300),
         # a hundred samples of a whole document
-        dict(name="prefix 100 x 40000", op="prefix", dtype="bf16", batch=100, most=1, nq=32, nkv=8, hd=128, page=32, prefix=40000, own=300),
+        dict(name="prefix, 100 x 40000", op="prefix", dtype="bf16", batch=100, most=1, nq=32, nkv=8, hd=128, page=32, prefix=40000, own=300),
         # a small fp32 model's heads
-        dict(name="prefix fp32 heads of 32", op="prefix", dtype="fp32", batch=12, most=3, nq=8, nkv=2, hd=32, page=16, prefix=700, own=100),
+        dict(name="prefix, fp32 heads of 32", op="prefix", dtype="fp32", batch=12, most=3, nq=8, nkv=2, hd=32, page=16, prefix=700, own=100),
         # a token of each of eight sequences: the projections' fp32 rows into a bf16 cache
-        dict(name="append 8 x 1", op="append", source="fp32", dtype="bf16", batch=8, rows=8, nq=32, nkv=8, hd=128, page=16, before=1024),
+        dict(name="append, 8 x 1", op="append", source="fp32", dtype="bf16", batch=8, rows=8, nq=32, nkv=8, hd=128, page=16, before=1024),
         # prompts of a batch, ragged, together
-        dict(name="append prompts of 7", op="append", source="bf16", dtype="bf16", batch=7, rows=8191, nq=32, nkv=8, hd=128, page=16, before=300),
+        dict(name="append, prompts of 7", op="append", source="bf16", dtype="bf16", batch=7, rows=8191, nq=32, nkv=8, hd=128, page=16, before=300),
         # one token through q, k and v of the 8B shape
-        dict(name="w8 1 x 6144 x 4096", op="w8", source="bf16", out="fp32", rows=1, N=6144, K=4096),
+        dict(name="w8, 1 x 6144 x 4096", op="w8", source="bf16", out="fp32", rows=1, N=6144, K=4096),
         # sixteen sequences through its gate and up
-        dict(name="w8 16 x 28672 x 4096", op="w8", source="bf16", out="fp32", rows=16, N=28672, K=4096),
+        dict(name="w8, 16 x 28672 x 4096", op="w8", source="bf16", out="fp32", rows=16, N=28672, K=4096),
         # drafts of a batch through the 1B shape's down projection, from fp32 rows
-        dict(name="w8 144 x 2048 x 5632", op="w8", source="fp32", out="fp32", rows=144, N=2048, K=5632),
+        dict(name="w8, 144 x 2048 x 5632", op="w8", source="fp32", out="fp32", rows=144, N=2048, K=5632),
         # a prompt through the 8B shape's gate, an odd number of tokens
-        dict(name="w8 4095 x 14336 x 4096", op="w8", source="bf16", out="bf16", rows=4095, N=14336, K=4096),
+        dict(name="w8, 4095 x 14336 x 4096", op="w8", source="bf16", out="bf16", rows=4095, N=14336, K=4096),
     ]
 
 
