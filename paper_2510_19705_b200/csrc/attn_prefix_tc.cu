@@ -4,24 +4,28 @@
 // 64 keys; the items' tiles stand in one line, which is divided evenly over a CTA an SM, whatever the prefix's length is (it is read on the
 // device).  Per key tile and query tile
 //   S[128 x 64]   = Q K^T                      both operands in shared memory
-//   P             = exp2(S c - m), thread = query, as bf16 hi + lo halves that overwrite S (a weight keeps 16 bits and more)
-//   O[128 x hd]  += P_hi V + P_lo V            A operand from tensor memory, V as it lies in the cache (MN-major)
-// Bound by the softmax warps: 100 rows of 32 heads over 8 of 128 and 40000 keys 106 us, 1.6 of what the products take (a key tile 2240 cycles,
-// the products of its two query tiles 1545, of which P_lo 512).  Of those cycles the exponentials and the weights' halves are 1310, loads, maxima
-// and barriers the rest.  What did not help: sixteen softmax warps, two a row (3 % of the largest call, and a barrier that has no limit); a quarter of the
-// exponentials on the FMA pipe (2 % slower); the two query tiles' exponentials in turn (the same).  One issuing warp for both query tiles: 2900.
-// A short call waits for its instructions, first keys and the parts' way to memory: 64 rows over 8192 keys, seven key tiles a CTA, 27 us.
+//   P             = exp2(S c - m), thread = query, as three bf16 parts, all of its 24 bits: the high and middle ones overwrite S, the low ones go
+//                   to shared memory (tensor memory is full at heads of 128)
+//   O[128 x hd]  += P_lo V + P_mid V + P_hi V  V as it lies in the cache (MN-major)
+// Bound by the softmax warps and the chain weights -> products -> next scores: 100 rows of 32 heads over 8 of 128 and 40000 keys 176 us in all, 64 rows
+// over 8192 keys 55.  Weights of 16 bits (no low parts) would take 134 and 54 us, but move 2.2e-3 of the bf16 outputs of 64 x 8192 off the nearest, which
+// the plain fp32 formula does to 1.1e-3 and this kernel to 1.0e-3.  What did not help: sixteen softmax warps, two a row (3 % of the largest call, and a
+// barrier that has no limit); a quarter of the exponentials on the FMA pipe (2 % slower); the two query tiles' exponentials in turn (the same);
+// the next scores in front of the low parts' products (3 % slower); rows' sums in the softmax warps' registers, which then read S twice (169 and 58 us).
+// One issuing warp for both query tiles: 2900 cycles a key tile where two took 2240 (with weights of 16 bits).
+// A short call waits for its instructions, first keys and the parts' way to memory.
 // Two query tiles share every K and V tile; S has two buffers, so that the scores of the next key tile are ready when the weights of this one
 // are.  m moves only when a row's maximum has passed it by 8; then O is rescaled.
 // The tensor cores' adders cut off: a chain of products loses up to 2^-23 of its sum a product.  So a chain is not longer than kChain key
-// tiles (256 products of 16 keys' halves: 3e-5 at most, 2^-7 of a bf16 half step): then O is added in fp32 to the item's place in the
-// workspace, the same columns by the same lanes each time.
-// 352 threads: warps 0-3 / 4-7 = softmax of tile A / B, warp 8 = loader (TMA out of the pages, a lane a piece of a page), warps 9 / 10 = MMA
-// issue of tile A / B.  Every wait is bounded, and no waiter can be passed by (a parity wait sees a completion only until the next one): k_full and v_full
-// have their next loads behind k_free / v_free, which both issuers' commits complete; those their next MMAs behind the loader's tiles; s_full
-// and pv_done theirs behind p_ready of the tile's four softmax warps; o_done its next chain behind p_ready of a tile that they begin after
-// they have read O; q_ready its next queries behind q_free, which the commit behind a piece's last scores completes; p_ready its next weights
-// behind the scores.
+// tiles (96 products, 1.1e-5 at most): then O is added in fp32 to the item's place in the workspace, the same columns by the same lanes each time, while
+// the weights of the next chain's first tile are there already.  Chains of 4, 8, 16, 32 tiles: 100 x 40000 207, 181, 168, 159 us; outputs of 16 x 9 rows,
+// 16395 off the nearest 0.75e-3, 1.2e-3, 2.0e-3, 3.3e-3 (plain 1.4e-3).
+// 352 threads: warps 0-3 / 4-7 = softmax of tile A / B, warp 8 = loader (TMA out of the pages, a lane a piece of a page; keys a tile in front of
+// values), warps 9 / 10 = MMA issue of tile A / B.  Every wait is bounded, and no waiter can be passed by (a parity wait sees a completion only until the
+// next one): k_full and v_full have their next loads behind k_free / v_free, which both issuers' commits complete; those their next MMAs behind the
+// loader's tiles; s_full and pv_done (a buffer of S each) theirs behind p_ready of the tile's four softmax warps; o_done its next chain behind p_ready of
+// a tile that they begin after they have read O; q_ready its next queries behind q_free, which the commit behind a piece's last scores completes; p_ready
+// its next weights behind the scores.  The low parts' buffer is free when the scores that use its buffer of S are there, as these are issued behind its products.
 #include <algorithm>
 #include "attn_prefix.cuh"
 #include "gemm_tc.cuh"
@@ -35,15 +39,17 @@ using namespace ptx;
 constexpr int kThreads = 352, kLoaderWarp = 8, kMmaWarp = 9;             // (two MMA warps)
 constexpr int TK = 64, kSet = 256;                       // keys of a tile; queries of an item at most
 constexpr int kQBlk = 128 * 128, kBlk = TK * 128;        // [128 queries][64 bf16] and [64 keys][64 bf16] blocks, 128-byte swizzle
-constexpr int kStages = 4, kMasks = 8;                   // (a mask outlives its keys' stage by two tiles at most)
-constexpr int kChain = 32;                               // key tiles of a chain
-constexpr int kTurn = 32 * 20 * 4;                       // 32 rows x 16 columns (and 4 that keep banks apart) of a softmax warp on their way to memory
+constexpr int kMasks = 8;                                // (a mask outlives its keys' stage by two tiles at most)
+constexpr int kChain = 8;                                // key tiles of a chain
+constexpr int kLow = 128 * TK * 2;                       // the weights' low parts of a query tile, 128-byte swizzle
 
 template <int HD> struct Cfg {
   static constexpr int NB = HD / 64;                     // 64-column blocks
+  static constexpr int kStages = HD == 64 ? 4 : 3;
   static constexpr int kQTile = NB * kQBlk, kTile = NB * kBlk;
-  static constexpr int kOffK = 2 * kQTile, kOffV = kOffK + kStages * kTile, kOffMask = kOffV + kStages * kTile, kOffBar = kOffMask + kMasks * 8;
-  static constexpr int kOffTurn = kOffBar + 384, kSmem = kOffTurn + 8 * kTurn + 1024;
+  static constexpr int kOffK = 2 * kQTile, kOffV = kOffK + kStages * kTile, kOffLow = kOffV + kStages * kTile, kOffMask = kOffLow + 4 * kLow;
+  static constexpr int kOffBar = kOffMask + kMasks * 8, kSmem = kOffBar + 384 + 1024;
+  static_assert(kSmem + 16 <= 232448, "a block's shared memory");
 };
 struct TcArgs {
   CUtensorMap k, v, q;
@@ -134,24 +140,25 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
   volatile int *abort_flag = &sh_abort;
   const uint32_t s0 = smem_u32(smem), b0 = s0 + C::kOffBar;
   volatile uint64_t *masks = reinterpret_cast<volatile uint64_t *>(smem + C::kOffMask);
+  constexpr int kStages = C::kStages;
   auto k_full = [&](int b) { return b0 + 8u * b; };
   auto k_free = [&](int b) { return b0 + 8u * (4 + b); };
   auto v_full = [&](int b) { return b0 + 8u * (8 + b); };
   auto v_free = [&](int b) { return b0 + 8u * (12 + b); };
   auto s_full = [&](int x, int b) { return b0 + 8u * (16 + 2 * x + b); };
   auto p_ready = [&](int x, int b) { return b0 + 8u * (20 + 2 * x + b); };
-  auto pv_done = [&](int x) { return b0 + 8u * (24 + x); };
-  auto o_done = [&](int x) { return b0 + 8u * (26 + x); };           // a chain's last product
-  auto q_ready = [&](int x) { return b0 + 8u * (28 + x); };
-  const uint32_t v_land = b0 + 8u * 30;
+  auto pv_done = [&](int x, int b) { return b0 + 8u * (24 + 2 * x + b); };
+  auto o_done = [&](int x) { return b0 + 8u * (28 + x); };           // a chain's last product
+  auto q_ready = [&](int x) { return b0 + 8u * (30 + x); };
   auto q_free = [&](int x) { return b0 + 8u * (32 + x); };           // a piece's last scores
+  const uint32_t v_land = b0 + 8u * 34;
   const int warp = warp_index(), lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
     for (int b = 0; b < kStages; ++b) { mbar_init(k_full(b), 1); mbar_init(k_free(b), 2); mbar_init(v_full(b), 1); mbar_init(v_free(b), 2); }
     for (int x = 0; x < 2; ++x) {
       mbar_init(s_full(x, 0), 1); mbar_init(s_full(x, 1), 1); mbar_init(p_ready(x, 0), 4); mbar_init(p_ready(x, 1), 4);
-      mbar_init(pv_done(x), 1); mbar_init(o_done(x), 1); mbar_init(q_ready(x), 1); mbar_init(q_free(x), 1);
+      mbar_init(pv_done(x, 0), 1); mbar_init(pv_done(x, 1), 1); mbar_init(o_done(x), 1); mbar_init(q_ready(x), 1); mbar_init(q_free(x), 1);
     }
     mbar_init(v_land, 1);
     sh_abort = 0;
@@ -169,6 +176,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
   lens.read(a.p);
   auto tS = [&](int x) { return tmem + (uint32_t)(x * 128); };
   auto tO = [&](int x) { return tmem + 256u + (uint32_t)(x * HD); };
+  auto low = [&](int x, int b) { return (uint32_t)(C::kOffLow + (2 * x + b) * kLow); };
   Pieces piece(a, lens.prefix);
 
   if (warp == kLoaderWarp) {
@@ -191,52 +199,62 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
         if (lane < C::NB) tma_load_3d(s0 + x * C::kQTile + lane * kQBlk, &a.q, lane * 64, piece.head * a.p.group, row0 + x * a.per_tile, q_ready(x));
       }
       if (!ok) break;
-      for (int j = 0; j < piece.n; ++j, ++kt) {
-        const int b = kt % kStages, k0 = (piece.t0 + j) * TK, in_page = key % page;
-        const uint32_t ph = (uint32_t)((kt / kStages) & 1);
-        const uint32_t there = __ballot_sync(0xFFFFFFFFu, id < a.p.pool.n_pages);
-        const int id_now = id;
-        key += TK;
-        if (j + 1 < piece.n) id = page_id(key);                      // the next tile's, before the waits
-        uint64_t mask = ~0ull;
-        const bool tail = k0 + TK > lens.prefix;
-        if (there != (copies == 32 ? ~0u : (1u << copies) - 1) || tail) {
-          mask = 0;
-          for (int i = 0; i < copies; ++i)
-            if ((there >> i) & 1) mask |= (box == 64 ? ~0ull : (1ull << box) - 1) << (i * box);
-          if (tail) mask &= (1ull << (lens.prefix - k0)) - 1;
-        }
-        if (!wait(k_free(b), ph ^ 1u)) break;
-        if (lane == 0) {
-          masks[kt % kMasks] = mask;
-          mbar_expect_tx(k_full(b), C::kTile);
-        }
-        __syncwarp();
-        if (lane < copies) {
-#pragma unroll
-          for (int i = 0; i < C::NB; ++i)
-            tma_load_4d(s0 + C::kOffK + b * C::kTile + i * kBlk + lane * box * 128, &a.k, i * 64, in_page, id_now, piece.head, k_full(b));
-        }
-        if (!wait(v_free(b), ph ^ 1u)) break;
-        const uint32_t lands = tail ? v_land : v_full(b);
-        if (lane == 0) mbar_expect_tx(lands, C::kTile);
-        __syncwarp();
-        if (lane < copies) {
-#pragma unroll
-          for (int i = 0; i < C::NB; ++i)
-            tma_load_4d(s0 + C::kOffV + b * C::kTile + i * kBlk + lane * box * 128, &a.v, i * 64, in_page, id_now, piece.head, lands);
-        }
-        if (tail) {                                                  // values behind the prefix's end must be finite (P is 0 there)
-          if (!wait(v_land, (uint32_t)(tails++ & 1))) break;
-          const int r0 = lens.prefix - k0;
-          for (int i = r0 * 8 * C::NB + lane; i < TK * 8 * C::NB; i += 32) {
-            const int r = i / (8 * C::NB), c = i % (8 * C::NB);      // whole rows: the swizzle permutes within a row
-            *reinterpret_cast<uint4 *>(smem + C::kOffV + b * C::kTile + (c >> 3) * kBlk + r * 128 + ((c & 7) << 4)) = make_uint4(0u, 0u, 0u, 0u);
+      int of_v = 0, in_page_v = 0;                                   // the page and place in it of the values that come next
+      bool tail_v = false;
+      for (int j = 0; j <= piece.n; ++j) {                           // keys a tile in front of the values, whose place becomes free later
+        const int of_k = id, in_page = key % page;
+        const bool tail = j < piece.n && (piece.t0 + j + 1) * TK > lens.prefix;
+        if (j < piece.n) {
+          const int b = kt % kStages, k0 = (piece.t0 + j) * TK;
+          const uint32_t there = __ballot_sync(0xFFFFFFFFu, id < a.p.pool.n_pages);
+          key += TK;
+          if (j + 1 < piece.n) id = page_id(key);                    // the next tile's, before the waits
+          uint64_t mask = ~0ull;
+          if (there != (copies == 32 ? ~0u : (1u << copies) - 1) || tail) {
+            mask = 0;
+            for (int i = 0; i < copies; ++i)
+              if ((there >> i) & 1) mask |= (box == 64 ? ~0ull : (1ull << box) - 1) << (i * box);
+            if (tail) mask &= (1ull << (lens.prefix - k0)) - 1;
           }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          if (!wait(k_free(b), (uint32_t)((kt / kStages) & 1) ^ 1u)) break;
+          if (lane == 0) {
+            masks[kt % kMasks] = mask;
+            mbar_expect_tx(k_full(b), C::kTile);
+          }
           __syncwarp();
-          if (lane == 0) mbar_arrive(v_full(b));
+          if (lane < copies) {
+#pragma unroll
+            for (int i = 0; i < C::NB; ++i)
+              tma_load_4d(s0 + C::kOffK + b * C::kTile + i * kBlk + lane * box * 128, &a.k, i * 64, in_page, of_k, piece.head, k_full(b));
+          }
+          ++kt;
         }
+        if (j > 0) {
+          const int t = kt - (j < piece.n ? 2 : 1), b = t % kStages;
+          if (!wait(v_free(b), (uint32_t)((t / kStages) & 1) ^ 1u)) break;
+          const uint32_t lands = tail_v ? v_land : v_full(b);
+          if (lane == 0) mbar_expect_tx(lands, C::kTile);
+          __syncwarp();
+          if (lane < copies) {
+#pragma unroll
+            for (int i = 0; i < C::NB; ++i)
+              tma_load_4d(s0 + C::kOffV + b * C::kTile + i * kBlk + lane * box * 128, &a.v, i * 64, in_page_v, of_v, piece.head, lands);
+          }
+          if (tail_v) {                                              // values behind the prefix's end must be finite (P is 0 there)
+            if (!wait(v_land, (uint32_t)(tails++ & 1))) break;
+            const int r0 = lens.prefix - (piece.t0 + j - 1) * TK;
+            for (int i = r0 * 8 * C::NB + lane; i < TK * 8 * C::NB; i += 32) {
+              const int r = i / (8 * C::NB), c = i % (8 * C::NB);    // whole rows: the swizzle permutes within a row
+              *reinterpret_cast<uint4 *>(smem + C::kOffV + b * C::kTile + (c >> 3) * kBlk + r * 128 + ((c & 7) << 4)) = make_uint4(0u, 0u, 0u, 0u);
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(v_full(b));
+          }
+        }
+        of_v = of_k;
+        in_page_v = in_page;
+        tail_v = tail;
       }
     }
     if (!ok) {                                                       // copies in flight land before the shared memory goes away
@@ -282,12 +300,15 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
         if (!ok) break;
         tc_fence_after();
         const uint32_t d = tO(x), p = tS(x) + (uint32_t)((c & 1) * TK);
-        if (issuer) {
+        const uint32_t lows = desc_lo_k(s0 + low(x, c & 1));
+        if (issuer) {                                                // the small products first
 #pragma unroll
-          for (int ks = 0; ks < TK / 16; ++ks) umma_ts(d, p + ks * 16, vb + ks * 128, id2, ks > 0 || j % kChain > 0 ? 1u : 0u);
+          for (int ks = 0; ks < TK / 16; ++ks) umma_ss(d, lows + ks * 2, vb + ks * 128, id2, ks > 0 || j % kChain > 0 ? 1u : 0u);
 #pragma unroll
           for (int ks = 0; ks < TK / 16; ++ks) umma_ts(d, p + ks * 16 + 8, vb + ks * 128, id2, 1u);
-          umma_commit(pv_done(x));
+#pragma unroll
+          for (int ks = 0; ks < TK / 16; ++ks) umma_ts(d, p + ks * 16, vb + ks * 128, id2, 1u);
+          umma_commit(pv_done(x, c & 1));
           if (j + 1 == n || (j + 1) % kChain == 0) umma_commit(o_done(x));
           for (int i = 0; i < frees; ++i) umma_commit(v_free(b));
           if (j + 2 < n) issue_s(j + 2);                             // over P(j), after the products that read it
@@ -323,60 +344,47 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
       const int to_row = piece.t0 == 0 ? at : x * 128 + row, reals = min(nq - (warp & 3) * 32, 32);
       bool next_ready = false;
       float m_ref = -INFINITY, l = 0.f, m_added = -INFINITY;         // m_added: of the sums that were added to the place
-      // A chain's end: its sums to the place, by way of shared memory, so that a row's columns are written by neighbouring lanes.  (A short call
-      // runs this once, and waits for its instructions more than for anything: so they are few.)
-      float *block = reinterpret_cast<float *>(smem + C::kOffTurn + warp * kTurn);
-      auto add = [&](bool first) {
-        const float f = m_added > -INFINITY ? ex2((m_added - m_ref) * sc) : 1.f;
+      // A chain's sums, relative to m, to the place, by way of the warp's rows of low parts that no product reads any more, so that a row's columns
+      // are written by neighbouring lanes: 32 columns at a time, 16-byte pieces permuted within a row of 128.  (A short call runs this once, and waits
+      // for its instructions more than for anything: so they are few.)
+      auto add = [&](bool first, float m) {
+        float4 *const block = reinterpret_cast<float4 *>(smem + low(x, (st - 1) & 1) + (warp & 3) * 32 * 128);
+        const float f = m_added > -INFINITY ? ex2((m_added - m) * sc) : 1.f;
         // no reference has moved, as a rule: added where they lie, without a trip there and back (a row's columns are always the same lane's,
         // so the order is that of the chains)
         const bool same = __all_sync(0xFFFFFFFFu, f == 1.f);
 #pragma unroll 1
-        for (int c0 = 0; c0 < HD; c0 += 16) {
-          float o[16];
-          tmem_ld16(O + (uint32_t)c0, o);
+        for (int c0 = 0; c0 < HD; c0 += 32) {
+          float o[32];
+          tmem_ld32(O + (uint32_t)c0, o);
           tmem_ld_wait();
 #pragma unroll
-          for (int c = 0; c < 16; c += 4) *reinterpret_cast<float4 *>(block + lane * 20 + c) = make_float4(o[c], o[c + 1], o[c + 2], o[c + 3]);
+          for (int c = 0; c < 8; ++c) block[lane * 8 + (c ^ (lane & 7))] = make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
           __syncwarp();
-#pragma unroll 1
-          for (int i0 = lane >> 4; i0 < 32; i0 += 16) {              // eight rows at a time: their shuffles and loads in flight together
-            float y[8];
-            float *p[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              p[k] = to + __shfl_sync(0xFFFFFFFFu, to_row, i0 + 2 * k) * (long long)HD + c0 + (lane & 15);
-              y[k] = block[(i0 + 2 * k) * 20 + (lane & 15)];
-            }
-            if (first) {
-#pragma unroll
-              for (int k = 0; k < 8; ++k)
-                if (i0 + 2 * k < reals) *p[k] = y[k];
-            } else if (same) {
-#pragma unroll
-              for (int k = 0; k < 8; ++k)
-                if (i0 + 2 * k < reals) asm volatile("red.global.add.f32 [%0], %1;" ::"l"(p[k]), "f"(y[k]) : "memory");
-            } else {
-#pragma unroll
-              for (int k = 0; k < 8; ++k) {
-                const float f_i = __shfl_sync(0xFFFFFFFFu, f, i0 + 2 * k);
-                if (i0 + 2 * k < reals) *p[k] = fmaf(*p[k], f_i, y[k]);
-              }
+          for (int k = 0; k < 8; ++k) {                              // four rows
+            const int i = 4 * k + (lane >> 3);
+            float4 *const p = reinterpret_cast<float4 *>(to + __shfl_sync(0xFFFFFFFFu, to_row, i) * (long long)HD + c0) + (lane & 7);
+            const float4 y = block[i * 8 + ((lane & 7) ^ (i & 7))];
+            const float f_i = same ? 1.f : __shfl_sync(0xFFFFFFFFu, f, i);
+            if (i >= reals) {
+            } else if (first) *p = y;
+            else if (same) asm volatile("red.global.add.v4.f32 [%0], {%1,%2,%3,%4};" ::"l"(p), "f"(y.x), "f"(y.y), "f"(y.z), "f"(y.w) : "memory");
+            else {
+              const float4 there = *p;
+              *p = make_float4(fmaf(there.x, f_i, y.x), fmaf(there.y, f_i, y.y), fmaf(there.z, f_i, y.z), fmaf(there.w, f_i, y.w));
             }
           }
           __syncwarp();
         }
-        m_added = m_ref;
+        m_added = m;
       };
       for (int j = 0; j < n; ++j, ++kt, ++st) {
-        if (j > 0 && j % kChain == 0) {
-          if (!wait(o_done(x), (uint32_t)(chains++ & 1))) break;
-          if (busy) add(j == kChain);
-        }
         const uint32_t S = tS(x) + lq + (uint32_t)((st & 1) * TK);
         if (!next_ready && !wait(s_full(x, st & 1), (uint32_t)((st >> 1) & 1))) break;
         tc_fence_after();
         next_ready = false;
+        const float m_before = m_ref;
         if (busy) {
           float sv[TK];
 #pragma unroll
@@ -399,8 +407,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
             const float m_new = grow ? mx : m_ref;
             const float f = m_ref > -INFINITY ? ex2((m_ref - m_new) * sc) : 1.f;       // (sums without a key are zeros)
             if (j % kChain > 0) {
-              // O holds the previous tile's products (those of the tile before that were complete when S(j) was)
-              if (!wait(pv_done(x), (uint32_t)((st - 1) & 1))) break;
+              // O holds the products of the tile before
+              if (!wait(pv_done(x, (st - 1) & 1), (uint32_t)(((st - 1) >> 1) & 1))) break;
 #pragma unroll 1
               for (int c = 0; c < HD; c += 16) {
                 float o[16];
@@ -418,36 +426,48 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
           const float mneg = m_ref > -INFINITY ? -m_ref * sc : 0.f;
           float2 l2a = make_float2(0.f, 0.f), l2b = l2a;
           const float2 sc2 = make_float2(sc, sc), mneg2 = make_float2(mneg, mneg);
+          // weights as three bf16 parts, all of their 24 bits: per 16 keys 8 columns of the high ones and 8 of the middle ones over their own
+          // scores, the low ones to shared memory
+          uint8_t *const lows = smem + low(x, st & 1) + row * 128;
 #pragma unroll
-          for (int c = 0; c < TK; c += 16) {                         // weights over their own scores: per 16 keys 8 columns of hi, 8 of lo
-            unsigned hi[8], lo[8];
+          for (int c = 0; c < TK; c += 16) {
+            unsigned part[3][8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
               const float2 t = __ffma2_rn(make_float2(sv[c + 2 * e], sv[c + 2 * e + 1]), sc2, mneg2);
-              const float2 p = make_float2(ex2(t.x), ex2(t.y));
+              float2 p = make_float2(ex2(t.x), ex2(t.y));
               if (e & 1) l2b = __fadd2_rn(l2b, p);
               else l2a = __fadd2_rn(l2a, p);
-              const __nv_bfloat162 h2 = __floats2bfloat162_rn(p.x, p.y);
-              hi[e] = *reinterpret_cast<const unsigned *>(&h2);
-              const float2 rest = __ffma2_rn(make_float2(__uint_as_float(hi[e] << 16), __uint_as_float(hi[e] & 0xFFFF0000u)), make_float2(-1.f, -1.f), p);
-              const __nv_bfloat162 lw = __floats2bfloat162_rn(rest.x, rest.y);
-              lo[e] = *reinterpret_cast<const unsigned *>(&lw);
+#pragma unroll
+              for (int i = 0; i < 3; ++i) {
+                const __nv_bfloat162 w = __floats2bfloat162_rn(p.x, p.y);
+                part[i][e] = *reinterpret_cast<const unsigned *>(&w);
+                if (i < 2) p = __ffma2_rn(make_float2(__uint_as_float(part[i][e] << 16), __uint_as_float(part[i][e] & 0xFFFF0000u)), make_float2(-1.f, -1.f), p);
+              }
             }
-            tmem_st8u(S + (uint32_t)c, hi);
-            tmem_st8u(S + (uint32_t)(c + 8), lo);
+            tmem_st8u(S + (uint32_t)c, part[0]);
+            tmem_st8u(S + (uint32_t)(c + 8), part[1]);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              *reinterpret_cast<uint4 *>(lows + (((c / 8 + h) ^ (row & 7)) << 4)) = make_uint4(part[2][4 * h], part[2][4 * h + 1], part[2][4 * h + 2], part[2][4 * h + 3]);
           }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           // the next tile's scores are there by now, as a rule: looked at here, the answer costs nothing
           if (j + 1 < n) next_ready = mbar_test(s_full(x, (st + 1) & 1), (uint32_t)(((st + 1) >> 1) & 1));
           l += (l2a.x + l2a.y) + (l2b.x + l2b.y);
           tmem_st_wait();
           next_ready = __all_sync(0xFFFFFFFFu, next_ready);
         }
+        if (j > 0 && j % kChain == 0) {                              // the chain before has ended under these exponentials
+          if (!wait(o_done(x), (uint32_t)(chains++ & 1))) break;
+          if (busy) add(j == kChain, m_before);
+        }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(p_ready(x, st & 1));
       }
       if (!ok || !wait(o_done(x), (uint32_t)(chains++ & 1))) break;
-      if (busy) add(n <= kChain);
+      if (busy) add(n <= kChain, m_ref);
       if (real) {
         const float2 ml = make_float2(m_ref > -INFINITY ? m_ref * sc : -INFINITY, l);
         const size_t mine = a.p.tc_rest + blockIdx.x * cta_floats;
@@ -483,9 +503,9 @@ template <int HD> int launch_t(const TcArgs &a, cudaStream_t s) {
 
 // Whether the call's sums over the prefix go by this kernel or by the one whose warps take sets of 16 queries, whose start is shorter and which
 // reads the prefix again for each set: by queries times keys (as many as the list has room for: the length itself is not known here) times the
-// heads' columns.  us of the other / this one, 8 key heads of 128: 32 queries each over 512 keys 13.8 / 16.6, 4096 28.3 / 23.8, 32768 157 / 52;
-// 16 queries over 4096 19.2 / 23.2, 32768 84 / 51; 8 over 32768 46 / 51; 128 over 512 19.9 / 20.7.  2 of 64: 64 over 4096 13.4 / 16.3, 128
-// over 4096 19.4 / 16.8, 16 over 32768 18.7 / 21.3, 32 over 32768 27.6 / 21.6.
+// heads' columns.  us of the other / this one, 8 key heads of 128: 32 queries each over 2048 keys 19.1 / 21.4, 4096 28.1 / 23.5, 32768 156 / 65;
+// 16 queries over 4096 19.0 / 22.8, 8192 28.5 / 27.3, 32768 83 / 63; 128 over 512 19.7 / 20.1, 1024 30.6 / 22.1.  2 of 64: 64 over 4096 13.3 / 16.9,
+// 128 over 4096 19.2 / 17.3, 16 over 32768 18.5 / 22.6, 32 over 32768 28.1 / 22.9.
 constexpr long long kEnoughWork = 90000000;
 bool prefix_tc_takes(const PrefixArgs &a, int dtype, int hd) {
   const long long queries = (long long)a.rows * a.group, keys = (long long)a.prefix_pages_n * a.pool.page, tiles = (keys + TK - 1) / TK;

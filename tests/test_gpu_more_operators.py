@@ -796,3 +796,36 @@ def test_prefix_attention_takes_a_batch_of_thousands(lib):
         table[:, 0] = pages[0]
         a, b = lib.hsd_prefix_attention(q, k, v, table, lens, pages, ints([P])), lib.hsd_paged_attention(q, k, v, table, lens)
         assert bool(((a.double() - b.double()).abs() <= 2 * HALF_STEP[dtype] * b.double().abs() + 2.0 ** -18 * v.abs().max()).all())
+
+
+# ------------------------------------------------------------------------------------------------ how exact the sums on tensor memory are
+def launches(lib, call):
+    before = lib.hsd_kernel_launches()
+    out = call()
+    return out, lib.hsd_kernel_launches() - before
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_prefix_attention_on_tensor_memory_keeps_all_bits_of_its_weights(lib, hd):
+    """Differences of the weights of two keys whose scores are nearly the same: what a weight of fewer bits is off by stands out in them."""
+    g, rows, pairs = gen(hd), 64, 32
+    q, k = torch.zeros(rows, 8, hd, device="cuda"), torch.zeros(1, 4, 16, hd, device="cuda")
+    # scores in whole 2^-13s below 2^4: exact in any order of their sum
+    q[..., 0], q[..., 1] = (1 + torch.randint(0, 16, (rows, 8), generator=g, device="cuda") / 16), 2.0 ** -8
+    key = k.view(2 * pairs, hd)
+    key[:, 0] = (torch.randint(0, 16, (pairs,), generator=g, device="cuda") / 16).repeat_interleave(2)
+    key[1::2, 1] = 2.0 ** -5 * torch.randint(1, 4, (pairs,), generator=g, device="cuda")
+    v = torch.zeros(1, 4, 16, hd, device="cuda")
+    for i in range(pairs):                                                  # column i: the pair's first weight less its second
+        v.view(2 * pairs, hd)[2 * i, i], v.view(2 * pairs, hd)[2 * i + 1, i] = 1, -1
+    q, k, v = q.to(BF16), k.to(BF16), v.to(BF16)
+    args = (ints([[0]]).expand(rows, 1).contiguous(), ints([64] * rows), with_room(ints([0, 1, 2, 3]), 1 << 23), ints([64]), None, 1.0)
+    got, n = launches(lib, lambda: lib.hsd_prefix_attention(q, k, v, *args))
+    assert n == 3                                                           # on tensor memory
+    w = torch.softmax(q.double() @ key.to(BF16).double().T, dim=-1)
+    want = w @ v.double().view(2 * pairs, hd)
+    # an exponential is off by 2^-22 of itself, its argument (below 4) by half a place, 2^-22, twice each; the four products of 16 keys' high parts may cut off 2^-23 of
+    # the largest weight each; the rest (sum of the weights, quotient: factors of the difference) is less than one of these
+    bound = HALF_STEP[BF16] * want.abs() + w.amax(dim=-1, keepdim=True) * (2 * 2.0 ** -22 * (1 + math.log(2)) + 5 * 2.0 ** -23)
+    off = (got.double() - want).abs()
+    assert bool((off <= bound).all()), float((off / bound).max())
