@@ -432,7 +432,7 @@ int hsd_paged_attention(const void *q, int batch, int n_q_heads, int n_kv_heads,
  * kernels only, so a captured call follows their changes.  How keys are divided, and so the order of the fp32 sums, follows the lengths of the whole batch.
  * Errors: INVALID_ARG, UNSUPPORTED (head_dim not in {32, 64, 128}), TOO_LARGE (batch over 4096, over 65536 query heads, rows * n_q_heads over
  * 2^26, (rows * n_q_heads / n_kv_heads + 8 batch + 8) * positions over 2^37), WORKSPACE_TOO_SMALL, CUDA; DEVICE_TIMEOUT is reported by
- * hsd_gemm_status(workspace, stream). */
+ * hsd_gemm_status(workspace, stream): the rows of sequences are NaN then. */
 size_t hsd_prefix_attention_workspace_bytes(int rows, int n_q_heads, int n_kv_heads, int head_dim);
 int hsd_prefix_attention(const void *q, int rows, int n_q_heads, int n_kv_heads, int head_dim, const hsd_kv_pool *pool,
                          const int32_t *page_table, int pages_per_seq, const int32_t *kv_lens, const int32_t *row_starts, int batch,

@@ -496,6 +496,7 @@ prefix_join_kernel(PrefixArgs a) {
   if (at0 >= own) return;                      // (W == 1: the warps are for themselves)
   const int row = (int)(at0 / a.nq);
   T *out = static_cast<T *>(a.out) + at0 * HD + lane * COLS;
+  const int gave_up = *a.status;               // (final: both kernels in front are complete)
   const int4 more0 = a.more[at0], more1 = a.more[own + at0];           // (of parts that are not there: anything, and not used)
   const float2 ml0 = a.first_ml[at0], ml1 = a.first_ml[own + at0];
   const Cols o0 = *reinterpret_cast<const Cols *>(a.first + at0 * HD + lane * COLS), o1 = *reinterpret_cast<const Cols *>(a.first + (own + at0) * HD + lane * COLS);
@@ -512,6 +513,12 @@ prefix_join_kernel(PrefixArgs a) {
   Cols sum = {};
   if (b < 0 || b >= a.batch) {
     if (a.zeros && w == 0) write(sum);
+    return;
+  }
+  if (gave_up) {                               // parts may be missing, and where they would be may be anything
+#pragma unroll
+    for (int c = 0; c < COLS; ++c) sum.v[c] = NAN;
+    if (w == 0) write(sum);
     return;
   }
   const Seen sees = seen_by(a, lens, b, rows_of(a, b));
