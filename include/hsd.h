@@ -472,7 +472,7 @@ int hsd_quantize_rows(const void *x, int dtype, int rows, int K, long long row_s
  *   out          device [R, N] of out_dtype, HSD_F32 or HSD_BF16
  *   workspace    device, 256-byte aligned, at least hsd_gemm_w8_workspace_bytes(...) (0 = bad sizes); contents on entry are ignored
  * Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, TOO_LARGE (K, N or R over 2^31 - 256, 2^43 outputs), UNSUPPORTED (no tensor-map support), CUDA;
- * DEVICE_TIMEOUT is reported by hsd_gemm_status(workspace, stream). */
+ * DEVICE_TIMEOUT is reported by hsd_gemm_status(workspace, stream): outputs that were not computed are NaN then. */
 size_t hsd_gemm_w8_workspace_bytes(int a_dtype, int R, int N, int K);
 int hsd_gemm_w8(const void *A, int a_dtype, const float *a_scales, int R, int K, const void *codes, const float *scales, int N,
                 void *out, int out_dtype, void *workspace, size_t workspace_bytes, void *stream);

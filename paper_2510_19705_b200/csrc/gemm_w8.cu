@@ -70,6 +70,11 @@ __device__ __forceinline__ int4 ld_cluster(uint32_t addr, uint32_t rank) {
   asm volatile("ld.shared::cluster.v4.s32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(map_to_rank(addr, rank)) : "memory");
   return v;
 }
+__device__ __forceinline__ int ld_cluster_word(uint32_t addr, uint32_t rank) {
+  int v;
+  asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(map_to_rank(addr, rank)) : "memory");
+  return v;
+}
 
 template <int NPAD, typename TO>
 __global__ void __launch_bounds__(kThreads, 1) w8_stream_kernel(const __grid_constant__ W8Args a, int n_tiles, int S) {
@@ -182,7 +187,14 @@ __global__ void __launch_bounds__(kThreads, 1) w8_stream_kernel(const __grid_con
       const float col = mine && S == 1 ? a.col_scales[n] : 0.f;
       if (lane == 0) ok = mbar_wait(accf_bar(ab), (uint32_t)((ti >> 1) & 1), abort_flag);
       ok = __shfl_sync(0xFFFFFFFFu, ok ? 1 : 0, 0) != 0;
-      if (!ok) break;
+      if (!ok) {                                // what was not computed is NaN (S > 1: below)
+        for (int t = tile; t < n_tiles && S == 1; t += step) {
+          const int n = t * a.tile_rows + m;
+          if (m >= a.tile_rows || n >= a.N) continue;
+          for (int r = 0; r < a.R; ++r) store(static_cast<TO *>(a.out) + (size_t)r * a.N + n, NAN);
+        }
+        break;
+      }
       tc_fence_after();
       const uint32_t from = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(ab * NPAD);
       int *part = reinterpret_cast<int *>(smem);                // S > 1: every load of the CTA has been consumed
@@ -207,10 +219,11 @@ __global__ void __launch_bounds__(kThreads, 1) w8_stream_kernel(const __grid_con
     // ------------------------------------------------------------------ sums across the cluster; each rank finishes its share
     __syncthreads();
     cluster_sync();
-    const bool ok = !*abort_flag;
+    bool ok = true;                             // of all CTAs, whose sums these are
+    for (int p = 0; p < S; ++p) ok &= ld_cluster_word(smem_u32(const_cast<int *>(abort_flag)), (uint32_t)p) == 0;
     // groups of four weight rows of a token; tiles have whole eights of rows
     const int fours = a.tile_rows / 4, total = a.R * fours, i1 = (int)((long long)total * (rank + 1) / S);
-    for (int i = (int)((long long)total * rank / S) + threadIdx.x; i < i1 && ok; i += kThreads) {
+    for (int i = (int)((long long)total * rank / S) + threadIdx.x; i < i1; i += kThreads) {
       const int r = i / fours, m = (i - r * fours) * 4, n = tile0 * a.tile_rows + m;
       int4 x[8];
 #pragma unroll
@@ -223,7 +236,7 @@ __global__ void __launch_bounds__(kThreads, 1) w8_stream_kernel(const __grid_con
       TO *out = static_cast<TO *>(a.out) + (size_t)r * a.N + n;
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (n + e < a.N) store(out + e, scaled(sum[e], row_scales[r], a.col_scales[n + e]));
+        if (n + e < a.N) store(out + e, ok ? scaled(sum[e], row_scales[r], a.col_scales[n + e]) : NAN);
     }
     __syncwarp();
     cluster_sync();                             // nobody leaves while its sums are being read
@@ -356,7 +369,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) w8_pair
       const float col = n < a.N ? a.col_scales[n] : 0.f;
       if (et == 0) wait_ok[ab] = mbar_wait(accf_bar(ab), (uint32_t)((ti >> 1) & 1), abort_flag) ? 1 : 0;
       asm volatile("bar.sync 1, 128;" ::: "memory");
-      if (!wait_ok[ab]) break;
+      if (!wait_ok[ab]) {                       // what was not computed is NaN
+        for (int x = t; x < a.tiles; x += pairs) {
+          const int n = x / a.m_tiles * 2 * kTile + (int)rank * kTile + q * 32 + lane, r0 = x % a.m_tiles * a.tokens, left = min(a.tokens, a.R - r0);
+          for (int r = 0; r < left && n < a.N; ++r) store(static_cast<TO *>(a.out) + (size_t)(r0 + r) * a.N + n, NAN);
+        }
+        break;
+      }
       tc_fence_after();
       const uint32_t from = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(ab * 256);
       const int left = min(a.tokens, a.R - r0);

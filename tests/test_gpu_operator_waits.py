@@ -57,3 +57,23 @@ def test_prefix_attention_whose_waits_run_out(lib, prefix, hd, rows, nq):
     args = (q, k, v, table, lens, pages, length)
     assert torch.equal(lib.hsd_prefix_attention(*args, workspace=ws), lib.hsd_prefix_attention(*args))
     assert binding.library().hsd_gemm_status(ws.data_ptr(), stream) == 0
+
+
+@pytest.fixture(scope="module")
+def w8(lib, tmp_path_factory):
+    lib.library()
+    so = native(tmp_path_factory, "w8_waits")
+    so.w8_without_data.argtypes = [vp, vp, i32, i32, vp, vp, i32, vp, i32, vp, vp]
+    return so
+
+
+# K by clusters of eight, four and two, by CTAs of their own with one tile and with several; CTA pairs with one tile and with several
+@pytest.mark.parametrize("R,N,K", [(3, 1000, 2048), (16, 2000, 2048), (200, 5000, 512), (1, 18000, 256), (250, 40000, 128), (300, 500, 256), (1000, 12000, 128)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_products_whose_waits_run_out(lib, w8, R, N, K, dtype):
+    a, w = (torch.ones(n, K, dtype=torch.int8, device="cuda") for n in (R, N))
+    rows, cols, status = torch.ones(R, device="cuda"), torch.ones(N, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    out, stream = torch.zeros(R, N, dtype=dtype, device="cuda"), torch.cuda.current_stream().cuda_stream
+    assert w8.w8_without_data(a.data_ptr(), rows.data_ptr(), R, K, w.data_ptr(), cols.data_ptr(), N, out.data_ptr(), 0 if dtype == torch.float32 else 1, status.data_ptr(), stream) == 0
+    torch.cuda.synchronize()
+    assert int(status) == 1 and bool(out.isnan().all())
