@@ -556,12 +556,13 @@ def hsd_prefix_attention_workspace_bytes(rows, n_q_heads, n_kv_heads, head_dim):
     return int(library().hsd_prefix_attention_workspace_bytes(rows, n_q_heads, n_kv_heads, head_dim))
 
 
-def hsd_prefix_attention(q, k_pool, v_pool, page_table, kv_lens, prefix_pages, prefix_len, row_starts=None, scale=None, workspace=None, out=None):
+def hsd_prefix_attention(q, k_pool, v_pool, page_table, kv_lens, prefix_pages, prefix_len, row_starts=None, scale=None, workspace=None, out=None, check=False):
     """Attention of a few tokens per sequence, q [rows, n_q, head_dim], whose sequences share their first prefix_len (int32 [1]) positions, on
     prefix_pages int32 [pages]: read once for all.  The others lie on page_table int32 [batch, pages], kv_lens int32 [batch] counts both;
     row_starts int32 [batch + 1], or None: a row each.  -> [rows, n_q, head_dim] in the pools' type; rows without a sequence are zeros, or
-    what `out` held if it is given.  scale None: head_dim ** -0.5."""
-    return (_host or _host_calls()).prefix_attention(q, k_pool, v_pool, page_table, kv_lens, prefix_pages, prefix_len, row_starts, scale, workspace, out)
+    what `out` held if it is given.  scale None: head_dim ** -0.5.  check (not while capturing): the stream is waited for, and a wait on the device that
+    gave up raises; without it the outputs are NaN then."""
+    return (_host or _host_calls()).prefix_attention(q, k_pool, v_pool, page_table, kv_lens, prefix_pages, prefix_len, row_starts, scale, workspace, out, check)
 
 
 def hsd_gemm_w4_workspace_bytes(R, N, K, group):
@@ -583,10 +584,11 @@ def hsd_gemm_w8_workspace_bytes(a_dtype, R, N, K):
     return int(library().hsd_gemm_w8_workspace_bytes(a_dtype, R, N, K))
 
 
-def hsd_gemm_w8(A, codes, scales, out_dtype=torch.float32, a_scales=None, out=None, workspace=None):
+def hsd_gemm_w8(A, codes, scales, out_dtype=torch.float32, a_scales=None, out=None, workspace=None, check=False):
     """A fp32/bf16 [R, K], of which the call makes 8-bit codes with a scale a row, or int8 [R, K] with a_scales fp32 [R]; codes int8 [N, K]
-    and scales fp32 [N] (both pairs as from hsd_quantize_rows) -> out_dtype (fp32/bf16) [R, N]."""
-    return (_host or _host_calls()).gemm_w8(A, codes, scales, out_dtype, a_scales, out, workspace)
+    and scales fp32 [N] (both pairs as from hsd_quantize_rows) -> out_dtype (fp32/bf16) [R, N].  check (not while capturing): the stream is waited for,
+    and a wait on the device that gave up raises; without it outputs that were not computed are NaN."""
+    return (_host or _host_calls()).gemm_w8(A, codes, scales, out_dtype, a_scales, out, workspace, check)
 
 
 def hsd_token_logprobs(logits, tokens, top=0):

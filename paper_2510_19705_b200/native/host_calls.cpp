@@ -179,6 +179,13 @@ PyObject *verify_level(PyObject *, PyObject *const *args, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// If the caller asks for it: the stream is waited for, a device-side wait that gave up is an error.
+void check_waits(PyObject *wanted, void *workspace, void *stream) {
+  const int yes = PyObject_IsTrue(wanted);
+  if (yes < 0) throw Failed();
+  if (yes) check(released([&] { return gemm_status_fn(workspace, stream); }));
+}
+
 // gemm_bf16(A [R, K], W [N, K], out or None, workspace or None, check)
 PyObject *gemm_bf16(PyObject *, PyObject *const *args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
@@ -200,9 +207,7 @@ PyObject *gemm_bf16(PyObject *, PyObject *const *args, Py_ssize_t n) {
     void *scratch = reinterpret_cast<void *>(base), *stream = current_stream();
     const int64_t left = ws.numel() - (int64_t)(base - start);
     check(released([&] { return gemm_fn(pa, R, K, pw, N, to, scratch, left < 0 ? 0 : (size_t)left, stream); }));
-    const int wanted = PyObject_IsTrue(args[4]);
-    if (wanted < 0) throw Failed();
-    if (wanted) check(released([&] { return gemm_status_fn(scratch, stream); }));
+    check_waits(args[4], scratch, stream);
     return THPVariable_Wrap(std::move(out));
   } catch (const Failed &) { return nullptr; }
   END_HANDLE_TH_ERRORS
@@ -385,11 +390,11 @@ PyObject *paged_attention(PyObject *, PyObject *const *args, Py_ssize_t n) {
 }
 
 // prefix_attention(q [rows, nq, hd], k_pool, v_pool, page_table [batch, pages], kv_lens [batch], prefix_pages [n], prefix_len [1],
-// row_starts [batch + 1] or None, scale or None, workspace or None, out or None)
+// row_starts [batch + 1] or None, scale or None, workspace or None, out or None, check)
 PyObject *prefix_attention(PyObject *, PyObject *const *args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   try {
-    arguments(n, 11);
+    arguments(n, 12);
     const at::Tensor &q = dims(tensor(args[0]), "q", 3);
     const hsd_kv_pool pool = pools(args[1], args[2], &q);
     const at::Tensor &k = tensor(args[1]);
@@ -426,6 +431,7 @@ PyObject *prefix_attention(PyObject *, PyObject *const *args, Py_ssize_t n) {
                        n_batch, static_cast<const int32_t *>(prefix.data_ptr()), front, static_cast<const int32_t *>(length.data_ptr()), (float)scale, scratch, (size_t)ws.numel(),
                        own, to, stream);
     }));
+    check_waits(args[11], scratch, stream);
     return THPVariable_Wrap(std::move(out));
   } catch (const Failed &) { return nullptr; }
   END_HANDLE_TH_ERRORS
@@ -492,11 +498,11 @@ PyObject *quantize_rows(PyObject *, PyObject *const *args, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-// gemm_w8(A [R, K], codes int8 [N, K], scales fp32 [N], out dtype, a_scales fp32 [R] or None, out or None, workspace or None)
+// gemm_w8(A [R, K], codes int8 [N, K], scales fp32 [N], out dtype, a_scales fp32 [R] or None, out or None, workspace or None, check)
 PyObject *gemm_w8(PyObject *, PyObject *const *args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   try {
-    arguments(n, 7);
+    arguments(n, 8);
     const at::Tensor &a = dims(tensor(args[0]), "A", 2);
     const bool coded = a.scalar_type() == at::kChar;
     const at::ScalarType source = coded ? at::kChar : cache_type(a, "A");
@@ -530,6 +536,7 @@ PyObject *gemm_w8(PyObject *, PyObject *const *args, Py_ssize_t n) {
     check(released([&] {
       return gemm_w8_fn(pa, dtype, row_scales, rows, k, pc, col_scales, cols, to, to_type == at::kFloat ? HSD_F32 : HSD_BF16, scratch, (size_t)ws.numel(), stream);
     }));
+    check_waits(args[7], scratch, stream);
     return THPVariable_Wrap(std::move(out));
   } catch (const Failed &) { return nullptr; }
   END_HANDLE_TH_ERRORS

@@ -77,3 +77,32 @@ def test_products_whose_waits_run_out(lib, w8, R, N, K, dtype):
     assert w8.w8_without_data(a.data_ptr(), rows.data_ptr(), R, K, w.data_ptr(), cols.data_ptr(), N, out.data_ptr(), 0 if dtype == torch.float32 else 1, status.data_ptr(), stream) == 0
     torch.cuda.synchronize()
     assert int(status) == 1 and bool(out.isnan().all())
+
+
+def test_calls_that_are_asked_to_report_waits_that_gave_up(lib):
+    """check=True on whole calls, and with a status call that answers with the error."""
+    g = torch.randn(40, 8, 64, device="cuda").to(torch.bfloat16)
+    k, v = (torch.randn(2, 4, 16, 64, device="cuda").to(torch.bfloat16) for _ in range(2))
+    prefix_args = (g, k, v, ints([[2, 3]] * 40), ints([20] * 40), ints([0, 1]), ints([17]))
+    codes, scales = lib.hsd_quantize_rows(torch.randn(100, 512, device="cuda"))
+    calls = (lambda **c: lib.hsd_prefix_attention(*prefix_args, **c), lambda **c: lib.hsd_gemm_w8(g.view(40, -1), codes, scales, **c))
+    for call in calls:
+        assert torch.equal(call(check=True), call())
+    asked = []
+    fake = ctypes.CFUNCTYPE(i32, vp, vp)(lambda workspace, stream: asked.append(workspace) or -5)
+    library = binding.library()
+    real, binding._host = library.hsd_gemm_status, None
+    try:
+        library.hsd_gemm_status = fake
+        binding._host_calls()
+        for i, call in enumerate(calls):
+            with pytest.raises(binding.HsdError, match="timed out"):
+                call(check=True)
+            assert len(asked) == i + 1 and asked[i] % 256 == 0
+            call()
+            assert len(asked) == i + 1                                      # not asked, not waited for
+    finally:
+        library.hsd_gemm_status, binding._host = real, None
+        binding._host_calls()
+    for call in calls:
+        call(check=True)
