@@ -423,6 +423,7 @@ int hsd_paged_attention(const void *q, int batch, int n_q_heads, int n_kv_heads,
  *                  padded one of length 0, say), or no key: its rows' outputs are zeros
  *   row_starts     device [batch + 1] int32, not descending: rows row_starts[b] .. row_starts[b+1]-1 are sequence b's; NULL: rows == batch, a
  *                  row each.  Rows in front of the first and from row_starts[batch] on: zeros (zeros != 0), or left as they were
+ *                  (a list may name more rows than the call has: they count as new tokens, as in an append)
  *   prefix_pages   device [n_prefix_pages] int32: pages of the positions 0 .. P - 1;  prefix_len device [1] int32 (0 or less: no prefix;
  *                  more than the pages have room for: their room).  P need not be whole pages; the last page of the list may be a copy
  *   scale          finite, also times log2(e)

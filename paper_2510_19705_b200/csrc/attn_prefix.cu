@@ -19,10 +19,12 @@ constexpr int kMaxBatch = 4096;                // its tiles' prefix sums lie in 
 constexpr int kMostChunk = 16;                 // queries of an item
 constexpr int kAll = 0x7FFFFFFF;               // rows that are none see all positions
 
-__device__ __forceinline__ int2 rows_of(const PrefixArgs &a, int b) {          // first row and one past the last
-  if (!a.row_starts) return make_int2(b, b + 1);
-  const int r0 = min(max(a.row_starts[b], 0), a.rows);
-  return make_int2(r0, min(max(a.row_starts[b + 1], r0), a.rows));
+// A sequence's rows: the first and one past the last that the call has; how many its list names, and how many of those are in front of the first.
+struct Rows { int x, y, n, front; };
+__device__ __forceinline__ Rows rows_of(const PrefixArgs &a, int b) {
+  if (!a.row_starts) return {b, b + 1, 1, 0};
+  const int s0 = a.row_starts[b], s1 = a.row_starts[b + 1], r0 = min(max(s0, 0), a.rows);
+  return {r0, min(max(s1, r0), a.rows), (int)min(max((long long)s1 - s0, 0ll), 0x7FFFFFFFll), s0 < 0 ? -s0 : 0};
 }
 __device__ __forceinline__ int seq_of(const PrefixArgs &a, int r) {            // -1, batch: rows without one
   if (!a.row_starts) return r;
@@ -37,9 +39,9 @@ __device__ __forceinline__ int seq_of(const PrefixArgs &a, int r) {            /
 // What a sequence's rows see: the first of them the positions below `first` (each one behind it one more), own keys up to `end`.  A sequence
 // that does not have the whole prefix has no keys: first < 0.
 struct Seen { int first, end; };
-__device__ __forceinline__ Seen seen_by(const PrefixArgs &a, const Lens &l, int b, int2 rows) {
-  const int len = l.of(a, b), first = len - (rows.y - rows.x) + 1;
-  return first < l.prefix || rows.x == rows.y ? Seen{-1, 0} : Seen{first, min(len, l.room)};
+__device__ __forceinline__ Seen seen_by(const PrefixArgs &a, const Lens &l, int b, const Rows &rows) {
+  const int len = l.of(a, b), first = len - rows.n + 1;
+  return first < l.prefix || rows.x == rows.y ? Seen{-1, 0} : Seen{first + rows.front, min(len, l.room)};
 }
 
 // The line of tiles.  Sequence 0 is the prefix, b + 1 the own keys of sequence b: tiles from `front` on (the own keys begin inside a tile).
@@ -67,7 +69,7 @@ __device__ __forceinline__ Line make_line(const PrefixArgs &a, bool prefix, int 
     if (s == 0) {
       if (prefix) { end = lens.prefix; n = (end + KEYS - 1) / KEYS * ceil_div(a.rows * a.group, a.chunk); }
     } else if (s < seqs) {
-      const int2 r = rows_of(a, s - 1);
+      const Rows r = rows_of(a, s - 1);
       end = seen_by(a, lens, s - 1, r).end;
       if (end > lens.prefix) n = ((end + KEYS - 1) / KEYS - front) * ceil_div((r.y - r.x) * a.group, a.chunk);
     }
@@ -140,7 +142,7 @@ struct Queries {
   template <int KEYS> __device__ __forceinline__ void of(const PrefixArgs &a, const Place<KEYS> &p, int nkv) {
     const int chunks = p.items / nkv;
     head = p.item / chunks;
-    int2 r = make_int2(0, a.rows);
+    Rows r = {0, a.rows, a.rows, 0};
     if (p.s > 0) r = rows_of(a, p.s - 1);
     row0 = r.x;
     v0 = (p.item - head * chunks) * a.chunk;

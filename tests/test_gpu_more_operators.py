@@ -829,3 +829,24 @@ def test_prefix_attention_on_tensor_memory_keeps_all_bits_of_its_weights(lib, hd
     bound = HALF_STEP[BF16] * want.abs() + w.amax(dim=-1, keepdim=True) * (2 * 2.0 ** -22 * (1 + math.log(2)) + 5 * 2.0 ** -23)
     off = (got.double() - want).abs()
     assert bool((off <= bound).all()), float((off / bound).max())
+
+
+# ------------------------------------------------------------------------------------------------ lists that name more rows than there are
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("cut", [1, 6, 11])
+def test_prefix_attention_of_a_list_that_names_more_rows(lib, dtype, cut):
+    """The rows that are there see what they would see in the whole call, as an append of the same list places them."""
+    g, P = gen(cut), 50
+    n = [2, 5, 9, 4]
+    starts = [sum(n[:i]) for i in range(5)]
+    k, v, table, pages = prefix_cache(g, 4, 2, 64, 16, P, 40, dtype)
+    lens = [P + 2, P + 20, P + 9, P + 30]
+    q = randn(g, starts[-1], 8, 64, dtype=dtype)
+    whole = check_prefix(lib, q, k, v, table, lens, pages, P, starts)
+    part = check_prefix(lib, q[:-cut].contiguous(), k, v, table, lens, pages, P, starts)
+    size = v.abs().max().double()
+    assert bool(((part.double() - whole[:-cut].double()).abs() <= 2 * HALF_STEP[dtype] * whole[:-cut].double().abs() + 2.0 ** -15 * size).all())
+    # rows in front of the call's first: the first three of a sequence
+    shifted = [s - 3 for s in starts]
+    late = lib.hsd_prefix_attention(q[3:].contiguous(), k, v, table, ints(lens), pages, ints([P]), ints(shifted))
+    assert bool(((late.double() - whole[3:].double()).abs() <= 2 * HALF_STEP[dtype] * whole[3:].double().abs() + 2.0 ** -15 * size).all())
