@@ -181,7 +181,8 @@ template <typename T, int HD> struct Feeder {
   __device__ __forceinline__ int load(const Place<KEYS> &p, int from) const {
     const int i = from + lane;
     if (p.s >= line.seqs || (long long)i * a.pool.page >= line.ends[p.s]) return -1;
-    return p.s > 0 ? a.page_table[(size_t)(p.s - 1) * a.pages_per_seq + i] : a.prefix_pages[i];
+    if (p.s == 0) return a.prefix_pages[i];
+    return ((long long)i + 1) * a.pool.page <= line.prefix ? -1 : a.page_table[(size_t)(p.s - 1) * a.pages_per_seq + i];   // (whole pages below: not read)
   }
   __device__ __forceinline__ void window_behind() {                    // of the one in `ahead`
     if (((long long)ahead_base + 32) * a.pool.page < line.ends[ahead.s]) ahead_base += 32;
