@@ -584,10 +584,11 @@ int split_of(int N, int KB, int sms) {
   while (S < (tiles <= 14 ? 8 : 4) && tiles * S * 2 <= sms && S * 2 <= KB) S *= 2;
   return S;
 }
+long long ceil_div64(long long a, long long b) { return (a + b - 1) / b; }       // (sizes end close to 2^31)
 // Rows of a tile: as many as spread N evenly over the rounds of the SMs, or of the clusters that run at once.
 int tile_rows_of(int N, int S, int sms) {
-  const int at_once = S == 2 ? 74 : S == 4 ? 32 : S == 8 ? 14 : sms, rounds = ceil_div(N, kTile * at_once);
-  return std::min(kTile, ceil_div(ceil_div(N, rounds * at_once), 8) * 8);
+  const long long at_once = S == 2 ? 74 : S == 4 ? 32 : S == 8 ? 14 : sms, rounds = ceil_div64(N, kTile * at_once);
+  return (int)std::min<long long>(kTile, ceil_div64(ceil_div64(N, rounds * at_once), 8) * 8);
 }
 template <int NPAD, typename TO> int run_stream(const W8Args &a, int n_tiles, int S, int grid, cudaStream_t s) {
   static std::atomic<u64> limits{0};
@@ -620,8 +621,8 @@ template <typename TO> int run(W8Args &a, const void *codes_a, const void *codes
   // tokens of a tile: as many as spread R evenly over the rounds of the CTA pairs that tiles of 256 need (us against tiles of 256: 3375 rows of
   // 362 x 12528 41 / 48, 512 of 4096 x 4096 14.1 / 20.8, 1000 of 6144 x 4096 26.5 / 32.3, 2000 of 1000 x 2000 12.6 / 17.3)
   const int n_tiles = ceil_div(a.N, 2 * kTile), pairs = sms / 2, most = ceil_div(a.R, 256);
-  const long long rounds = ((long long)most * n_tiles + pairs - 1) / pairs;
-  a.tokens = ceil_div(ceil_div(a.R, (int)std::max<long long>(most, std::min<long long>(rounds * pairs / n_tiles, a.R))), 32) * 32;
+  const long long rounds = ceil_div64((long long)most * n_tiles, pairs), in_them = std::max<long long>(most, std::min<long long>(rounds * pairs / n_tiles, a.R));
+  a.tokens = (int)ceil_div64(ceil_div64(a.R, in_them), 32) * 32;
   a.m_tiles = ceil_div(a.R, a.tokens);
   a.tiles = a.m_tiles * ceil_div(a.N, 2 * kTile);
   int status = tc_make_map_bytes(&a.w, codes_w, a.N, K, kTile);

@@ -850,3 +850,21 @@ def test_prefix_attention_of_a_list_that_names_more_rows(lib, dtype, cut):
     shifted = [s - 3 for s in starts]
     late = lib.hsd_prefix_attention(q[3:].contiguous(), k, v, table, ints(lens), pages, ints([P]), ints(shifted))
     assert bool(((late.double() - whole[3:].double()).abs() <= 2 * HALF_STEP[dtype] * whole[3:].double().abs() + 2.0 ** -15 * size).all())
+
+
+# ------------------------------------------------------------------------------------------------ sizes next to 2^31
+@pytest.mark.parametrize("R,N", [(1, (1 << 31) - 300), ((1 << 31) - 300, 1)])
+def test_products_of_sizes_next_to_their_limit(lib, R, N):
+    K, g = 16, gen(1)
+    a, w = (torch.ones(n, K, dtype=torch.int8, device="cuda") for n in (R, N))
+    rows, cols = torch.ones(R, device="cuda"), torch.ones(N, device="cuda")
+    for x in (a, w):
+        x[-1000:] = torch.randint(-128, 128, x[-1000:].shape, generator=g, device="cuda").to(torch.int8)
+    out = lib.hsd_gemm_w8(a, w, cols, BF16, a_scales=rows)
+    few = w if R == 1 else a                                                # the long one; the other has one row
+    one = (a if R == 1 else w).float()[0]
+    long, count = out.view(-1), few.shape[0]
+    assert torch.equal(long[-1000:], (few[-1000:].float() @ one).to(BF16))
+    first = one.sum().to(BF16)
+    for i in range(0, count - 1000, 1 << 28):
+        assert bool((long[i:min(i + (1 << 28), count - 1000)] == first).all())
