@@ -7,6 +7,7 @@
 // neighbouring threads of a head, from the values they hold anyway: nothing is read twice.
 // Bound by memory for prompts, by the chain row -> position -> page -> store for a few rows, whose heads are divided over CTAs.
 #include <math.h>
+#include <algorithm>
 #include <type_traits>
 
 #include "paged.cuh"
@@ -14,7 +15,8 @@
 namespace hsd {
 namespace {
 
-constexpr int kThreads = 256, kRows = 8;       // rows of a CTA at most
+constexpr int kThreads = 256, kCtasPerSm = 4;
+constexpr int kRows = 8;                       // rows of a CTA at most
 
 struct AppendArgs {
   const unsigned char *qkv;
@@ -90,7 +92,7 @@ __device__ __forceinline__ float norm(float eps, const float *lo, const float *h
 }
 
 template <typename TI, typename TO, typename TG, int HD>
-__global__ void __launch_bounds__(kThreads, 4)         // (with the norm: 8191 rows of 48 heads of 128 41 us; three CTAs an SM 50, five, which spill, 49)
+__global__ void __launch_bounds__(kThreads, kCtasPerSm)        // (with the norm: 8191 rows of 48 heads of 128 41 us; three CTAs an SM 50, five, which spill, 49)
 kv_append_kernel(AppendArgs a) {
   constexpr int UNITS = HD / 16, HALF = HD / 2;
   static_assert(kThreads % kRows == 0 && kThreads / kRows % UNITS == 0, "a row has whole heads' threads");
@@ -202,11 +204,12 @@ kv_append_kernel(AppendArgs a) {
 
 template <typename TI, typename TO, typename TG> int run(AppendArgs &a, int hd, cudaStream_t s) {
   const int per_row = (a.nq + 2 * a.nkv) * (hd / 16);
-  // few rows: one a CTA and a row's heads over several, so that every thread has one piece; many rows: CTAs of up to kRows
-  // (48 heads of 128: 8191 rows with the norm, eight rows a CTA 41 us, four 43; without, 1000 rows, four rows a CTA 6.9, one 9.6, 300 rows two 4.4,
-  // one, whose CTAs are more than fit at once, 5.3)
-  a.cta_rows = a.rows >= kRows * 2 * kMeasuredSMs ? kRows : a.rows >= kRows / 2 * kMeasuredSMs ? kRows / 2 : a.rows > kMeasuredSMs ? kRows / 4 : 1;
-  a.parts = a.cta_rows > 1 ? 1 : ceil_div(per_row, kThreads);
+  // As few rows a CTA as let all CTAs run at once, and few rows' heads divided over as many as do.  us against twice the rows a CTA: 48 heads of 128, 800
+  // rows, two a CTA 4.9 / 6.1, 1184 6.7 / 8.1, 2368, four 13.4 / 15.9, 8191, eight 37.5 (four 38.3); 144 heads, 592 rows, one 11.1 / 12.8, 1184, two 18.3 /
+  // 21.8, 2368, four 32.3 / 38.9; 200 rows, a row over two CTAs 4.9, over five, of which 592 run at once, 5.9.  With the norm likewise (1184 rows 7.7 / 9.5, 2368 14.5 / 17.7).
+  constexpr int at_once = kCtasPerSm * kMeasuredSMs;
+  a.cta_rows = a.rows <= at_once ? 1 : a.rows <= 2 * at_once ? 2 : a.rows <= 4 * at_once ? 4 : kRows;
+  a.parts = a.cta_rows > 1 ? 1 : std::max(1, std::min(ceil_div(per_row, kThreads), at_once / a.rows));
   const long long grid = (long long)ceil_div(a.rows, a.cta_rows) * a.parts;
   if (grid > 0x7FFFFFFFll) return HSD_E_TOO_LARGE;
   switch (hd) {

@@ -868,3 +868,30 @@ def test_products_of_sizes_next_to_their_limit(lib, R, N):
     first = one.sum().to(BF16)
     for i in range(0, count - 1000, 1 << 28):
         assert bool((long[i:min(i + (1 << 28), count - 1000)] == first).all())
+
+
+# ------------------------------------------------------------------------------------------------ appends where the rows of a CTA change
+@pytest.mark.parametrize("rows,nq,nkv", [(592, 3, 1), (593, 3, 1), (1184, 2, 1), (1185, 2, 1), (2368, 1, 1), (2369, 1, 1), (149, 130, 8), (296, 130, 8), (297, 130, 8), (593, 60, 20)])
+def test_appends_where_the_rows_of_a_cta_change(lib, rows, nq, nkv):
+    g, batch = gen(rows), 5
+    starts = [rows * i // batch for i in range(batch + 1)]
+    before = [3 * i for i in range(batch)]
+    longest = max(b + starts[i + 1] - starts[i] for i, b in enumerate(before))
+    k, v, table = cache(g, batch, nkv, 32, 16, -(-longest // 16), BF16)
+    qkv, rope = randn(g, rows, nq + 2 * nkv, 32, dtype=BF16), lib.rope_table(longest, 32)
+    assert len(check_append(lib, qkv, [randn(g, 32), randn(g, 32)], 1e-6, k, v, table, before, rope, starts)) == rows
+    # without norms: the same as in pieces of a sequence's rows, which a call of few rows takes otherwise
+    whole = lib.hsd_kv_append(qkv, k, v, table, ints(before), rope, ints(starts))
+    kept = k.clone(), v.clone()
+    k.zero_(), v.zero_()
+    for b in range(batch):
+        for r in range(starts[b], starts[b + 1], 100):
+            n = min(100, starts[b + 1] - r)
+            part = lib.hsd_kv_append(qkv[r:r + n], k, v, table[b:b + 1], ints([before[b] + r - starts[b]]), rope, ints([0, n]))
+            assert torch.equal(part, whole[r:r + n])
+    used = torch.zeros(k.shape[1], 16, dtype=torch.bool)
+    for b in range(batch):
+        for p in range(before[b], before[b] + starts[b + 1] - starts[b]):
+            used[int(table[b, p // 16]), p % 16] = True
+    used = used.cuda()
+    assert torch.equal(k[:, used], kept[0][:, used]) and torch.equal(v[:, used], kept[1][:, used])
