@@ -22,7 +22,8 @@
 // 16395 off the nearest 0.75e-3, 1.2e-3, 2.0e-3, 3.3e-3 (plain 1.4e-3).
 // 352 threads: warps 0-3 / 4-7 = softmax of tile A / B, warp 8 = loader (TMA out of the pages, a lane a piece of a page; keys a tile in front of
 // values), warps 9 / 10 = MMA issue of tile A / B.  Every wait is bounded, and no waiter can be passed by (a parity wait sees a completion only until the
-// next one): k_full and v_full have their next loads behind k_free / v_free, which both issuers' commits complete; those their next MMAs behind the
+// next one) or come so late that it takes the one before the last for its own: k_full and v_full have their next loads behind k_free / v_free, which both
+// issuers complete, in a piece without its query tile too, where an issuer waits for every key tile and lets it go; those their next MMAs behind the
 // loader's tiles; s_full and pv_done (a buffer of S each) theirs behind p_ready of the tile's four softmax warps; o_done its next chain behind p_ready of
 // a tile that they begin after they have read O; q_ready its next queries behind q_free, which the commit behind a piece's last scores completes; p_ready
 // its next weights behind the scores.  The low parts' buffer is free when the scores that use its buffer of S are there, as these are issued behind its products.
@@ -271,8 +272,17 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
     int kt = 0, st = 0, pieces = 0;                                  // key tiles, the query tile's key tiles and pieces so far
     while (ok && piece.next()) {
       const int n_rows = min(a.per_set, a.p.rows - piece.set * a.per_set), n = piece.n;
-      if (x * a.per_tile >= n_rows) { kt += n; continue; }
-      const int frees = n_rows > a.per_tile ? 1 : 2;                 // (for the query tile that there is not)
+      if (x * a.per_tile >= n_rows) {                                // a query tile that there is not lets keys and values go as they come
+        for (int j = 0; j < n && ok; ++j, ++kt) {
+          const int b = kt % kStages;
+          const uint32_t ph = (uint32_t)((kt / kStages) & 1);
+          ok = mbar_wait_warp(k_full(b), ph, abort_flag);
+          if (ok && lane == 0) mbar_arrive(k_free(b));
+          ok = ok && mbar_wait_warp(v_full(b), ph, abort_flag);
+          if (ok && lane == 0) mbar_arrive(v_free(b));
+        }
+        continue;
+      }
       auto issue_s = [&](int j) {                                    // (the issuer only)
         const int b = (kt + j) % kStages, c = st + j;
         const uint32_t qb = desc_lo_k(s0 + x * C::kQTile), kb = desc_lo_k(s0 + C::kOffK + b * C::kTile), d = tS(x) + (uint32_t)((c & 1) * TK);
@@ -280,7 +290,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
         for (int ks = 0; ks < HD / 16; ++ks)
           umma_ss(d, qb + (ks >> 2) * (kQBlk / 16) + (ks & 3) * 2, kb + (ks >> 2) * (kBlk / 16) + (ks & 3) * 2, id1, ks > 0 ? 1u : 0u);
         umma_commit(s_full(x, c & 1));
-        for (int i = 0; i < frees; ++i) umma_commit(k_free(b));
+        umma_commit(k_free(b));
         if (j + 1 == n) umma_commit(q_free(x));
       };
       auto k_wait = [&](int j) { return mbar_wait_warp(k_full((kt + j) % kStages), (uint32_t)(((kt + j) / kStages) & 1), abort_flag); };
@@ -310,7 +320,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
           for (int ks = 0; ks < TK / 16; ++ks) umma_ts(d, p + ks * 16, vb + ks * 128, id2, 1u);
           umma_commit(pv_done(x, c & 1));
           if (j + 1 == n || (j + 1) % kChain == 0) umma_commit(o_done(x));
-          for (int i = 0; i < frees; ++i) umma_commit(v_free(b));
+          umma_commit(v_free(b));
           if (j + 2 < n) issue_s(j + 2);                             // over P(j), after the products that read it
         }
       }

@@ -895,3 +895,23 @@ def test_appends_where_the_rows_of_a_cta_change(lib, rows, nq, nkv):
             used[int(table[b, p // 16]), p % 16] = True
     used = used.cuda()
     assert torch.equal(k[:, used], kept[0][:, used]) and torch.equal(v[:, used], kept[1][:, used])
+
+
+# ------------------------------------------------------------------------------------------------ CTAs that go from one query tile to two
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("rows,nq,nkv,P", [(65, 8, 2, 10000), (65, 640, 160, 700), (65, 600, 150, 130), (33, 512, 64, 1000)])
+def test_prefix_attention_of_sets_with_one_query_tile_and_with_two(lib, hd, rows, nq, nkv, P):
+    """Rows that make a set of two query tiles and one of one, for each key head: CTAs go from the end of the one to the other."""
+    g = gen(rows + nq + hd)
+    k, v = (randn(g, nkv, -(-P // 16), 16, hd, dtype=BF16) for _ in range(2))
+    q, pages = randn(g, rows, nq, hd, dtype=BF16), torch.randperm(-(-P // 16), generator=g, device="cuda").to(torch.int32)
+    args = (ints([[0]] * rows), ints([P] * rows), with_room(pages, 1 << 22), ints([P]))
+    got, n = launches(lib, lambda: lib.hsd_prefix_attention(q, k, v, *args))
+    assert n == 3
+    scale = hd ** -0.5
+    want, size = prefix_in_64_bits(q, k, v, pages, P, scale), prefix_in_64_bits(q, k, v.abs(), pages, P, scale)
+    most = float((q.double().abs().amax(dim=(0, 1)) * k.double().abs().amax(dim=(0, 1, 2))).sum()) * scale
+    weight = (hd + 4) * 2.0 ** -23 * most + 2.0 ** -21 + (P / 8 + 64) * 2.0 ** -24
+    assert bool(((got.double() - want).abs() <= HALF_STEP[BF16] * want.abs() + (2 * weight + 96 * 2.0 ** -23) * size).all())
+    for _ in range(10):
+        assert torch.equal(got, lib.hsd_prefix_attention(q, k, v, *args))
