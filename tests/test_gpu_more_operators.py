@@ -915,3 +915,32 @@ def test_prefix_attention_of_sets_with_one_query_tile_and_with_two(lib, hd, rows
     assert bool(((got.double() - want).abs() <= HALF_STEP[BF16] * want.abs() + (2 * weight + 96 * 2.0 ** -23) * size).all())
     for _ in range(10):
         assert torch.equal(got, lib.hsd_prefix_attention(q, k, v, *args))
+
+
+# ------------------------------------------------------------------------------------------------ which kernels a call takes
+def kernels_of(lib, dtype=BF16, hd=64, page=16, order="head", rows=40, nq=8, nkv=2, scale=None, room=True):
+    g = gen(1)
+    k, v, table, pages = prefix_cache(g, rows, nkv, hd, page, 100, 20, dtype, order)
+    args = (randn(g, rows, nq, hd, dtype=dtype), k, v, table, ints([101] * rows), with_room(pages, 1 << 24) if room else pages, ints([100]), None, scale)
+    return launches(lib, lambda: lib.hsd_prefix_attention(*args))[1]
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("call", [{}, dict(order="token"), dict(page=8), dict(page=24, order="token"), dict(page=24), dict(page=64, order="token"), dict(page=128), dict(page=256), dict(rows=4),
+                                  dict(nq=32, nkv=1), dict(nq=14, nkv=2), dict(nq=80, nkv=2), dict(nq=64, nkv=1), dict(nq=7, nkv=1, rows=70), dict(rows=300, nq=2, nkv=1), dict(scale=4.0)])
+def test_prefix_attention_takes_tensor_memory(lib, hd, call):
+    """The kernel for the prefix, the one for own keys, the join: what tests with room in the list of pages take for granted."""
+    assert kernels_of(lib, hd=hd, **call) == 3
+
+
+@pytest.mark.parametrize("call", [dict(room=False), dict(dtype=FP32), dict(hd=32), dict(page=3), dict(page=12), dict(scale=0.0), dict(scale=-0.3), dict(nq=65, nkv=1), dict(rows=3, nq=8, nkv=2)])
+def test_prefix_attention_takes_sets_of_queries(lib, call):
+    assert kernels_of(lib, **call) == 2
+
+
+def test_layers_and_long_chains_take_tensor_memory(lib):
+    layer = Layer(lib, 5, 24, 100, 40)
+    q = randn(gen(1), 24, layer.nq, layer.hd, dtype=BF16)
+    assert launches(lib, lambda: lib.hsd_prefix_attention(q, layer.k, layer.v, layer.table, ints([101] * 24), layer.pages, layer.prefix))[1] == 3
+    k, pages = randn(gen(2), 1, 2500, 16, 64, dtype=BF16), ints(list(range(2500)))
+    assert launches(lib, lambda: lib.hsd_prefix_attention(randn(gen(3), 500, 8, 64, dtype=BF16), k, k, ints([[0]] * 500), ints([40000] * 500), pages, ints([40000])))[1] == 3
