@@ -70,10 +70,13 @@ __device__ __forceinline__ int4 ld_cluster(uint32_t addr, uint32_t rank) {
   asm volatile("ld.shared::cluster.v4.s32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(map_to_rank(addr, rank)) : "memory");
   return v;
 }
-__device__ __forceinline__ int ld_cluster_word(uint32_t addr, uint32_t rank) {
-  int v;
-  asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(map_to_rank(addr, rank)) : "memory");
-  return v;
+// Weight row m of the tiles from `tile` on, which a wait that gave up left out.
+template <typename TO> __device__ __noinline__ void no_result(const W8Args &a, int tile, int end, int step, int m) {
+  for (; tile < end; tile += step) {
+    const int n = tile * a.tile_rows + m;
+    if (m >= a.tile_rows || n >= a.N) continue;
+    for (int r = 0; r < a.R; ++r) store(static_cast<TO *>(a.out) + (size_t)r * a.N + n, NAN);
+  }
 }
 
 template <int NPAD, typename TO>
@@ -179,7 +182,7 @@ __global__ void __launch_bounds__(kThreads, 1) w8_stream_kernel(const __grid_con
     chain_wait();
     for (int r = threadIdx.x - 64; r < a.R; r += 128) row_scales[r] = a.row_scales[r];
     asm volatile("bar.sync 1, 128;" ::: "memory");
-    int ti = 0;
+    int ti = 0, missing = n_tiles;
     bool ok = true;
     for (int tile = tile0; tile < n_tiles; tile += step, ++ti) {
       const int ab = ti & 1, n = tile * a.tile_rows + m;
@@ -187,14 +190,7 @@ __global__ void __launch_bounds__(kThreads, 1) w8_stream_kernel(const __grid_con
       const float col = mine && S == 1 ? a.col_scales[n] : 0.f;
       if (lane == 0) ok = mbar_wait(accf_bar(ab), (uint32_t)((ti >> 1) & 1), abort_flag);
       ok = __shfl_sync(0xFFFFFFFFu, ok ? 1 : 0, 0) != 0;
-      if (!ok) {                                // what was not computed is NaN (S > 1: below)
-        for (int t = tile; t < n_tiles && S == 1; t += step) {
-          const int n = t * a.tile_rows + m;
-          if (m >= a.tile_rows || n >= a.N) continue;
-          for (int r = 0; r < a.R; ++r) store(static_cast<TO *>(a.out) + (size_t)r * a.N + n, NAN);
-        }
-        break;
-      }
+      if (!ok) { missing = tile; break; }
       tc_fence_after();
       const uint32_t from = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(ab * NPAD);
       int *part = reinterpret_cast<int *>(smem);                // S > 1: every load of the CTA has been consumed
@@ -213,14 +209,13 @@ __global__ void __launch_bounds__(kThreads, 1) w8_stream_kernel(const __grid_con
       __syncwarp();
       if (lane == 0) mbar_arrive(acce_bar(ab));
     }
+    if (S == 1 && missing < n_tiles) no_result<TO>(a, missing, n_tiles, step, m);
   }
   __syncwarp();
   if (S > 1) {
     // ------------------------------------------------------------------ sums across the cluster; each rank finishes its share
     __syncthreads();
     cluster_sync();
-    bool ok = true;                             // of all CTAs, whose sums these are
-    for (int p = 0; p < S; ++p) ok &= ld_cluster_word(smem_u32(const_cast<int *>(abort_flag)), (uint32_t)p) == 0;
     // groups of four weight rows of a token; tiles have whole eights of rows
     const int fours = a.tile_rows / 4, total = a.R * fours, i1 = (int)((long long)total * (rank + 1) / S);
     for (int i = (int)((long long)total * rank / S) + threadIdx.x; i < i1; i += kThreads) {
@@ -236,10 +231,11 @@ __global__ void __launch_bounds__(kThreads, 1) w8_stream_kernel(const __grid_con
       TO *out = static_cast<TO *>(a.out) + (size_t)r * a.N + n;
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (n + e < a.N) store(out + e, ok ? scaled(sum[e], row_scales[r], a.col_scales[n + e]) : NAN);
+        if (n + e < a.N) store(out + e, scaled(sum[e], row_scales[r], a.col_scales[n + e]));
     }
     __syncwarp();
     cluster_sync();                             // nobody leaves while its sums are being read
+    if (*abort_flag && threadIdx.x < kTile) no_result<TO>(a, tile0, tile0 + 1, 1, threadIdx.x);        // over what the others made of them
   }
   tc_fence_before();
   __syncthreads();
