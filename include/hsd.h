@@ -414,8 +414,7 @@ int hsd_paged_attention(const void *q, int batch, int n_q_heads, int n_kv_heads,
 /* Attention of a batch whose sequences share a prefix (samples of one prompt, drafts of them being verified), a few new tokens of each:
  * out[r, h] = sum_j softmax_j(scale q[r, h] . k_j) v_j.  Of sequence b's n rows the i-th sees the positions j < kv_lens[b] - n + 1 + i (the
  * new tokens' own keys are among them once they have been appended: pass the lengths after the append): those below P = *prefix_len
- * on the prefix's pages, which are read once for the whole batch, the others on the sequence's own.  Softmax, weights and sums in fp32, rounded once;
- * products of up to 512 keys are added up by the tensor cores, which may cut off a sum's last place where fp32 rounds it.
+ * on the prefix's pages, which are read once for the whole batch, the others on the sequence's own.  Softmax and sums in fp32, rounded once.
  *   q, out         device [rows, n_q_heads, head_dim] in the pool's type, 16-byte aligned; n_q_heads a multiple of n_kv_heads
  *   page_table     device [batch, pages_per_seq] int32: position p of a sequence in page page_table[b * pages_per_seq + p / page_size], as
  *                  for the other calls; entries of whole pages below P are not read.  kv_lens device [batch] int32 counts the prefix too; more than
