@@ -12,9 +12,10 @@
 // products come first.  With weights of 16 bits and chains of up to 2048 keys 64 x 8192 rows and keys took 54 us instead of 59, 100 x 40000 134 instead of 181, but
 // 2.2e-3 and more of the bf16 outputs were not the nearest, against 1.1e-3 of the formula in fp32; now 0.35e-3.  (Three parts and chains of 512 keys,
 // added in the workspace: 56 and 177 us, 1.0e-3.)
-// Bound by the softmax warps and the way weights -> products -> sums -> next weights: at 100 x 40000 the tensor pipe is busy for 53 % of the time.  The scores of 32 of a tile's 64 keys stay in registers from the maximum on, the others are read twice: registers hold O (16 more
-// kept: 3 % slower, they spill).  What did not help: sixteen softmax warps, two a row (a barrier that has no limit); a quarter of the exponentials on
-// the FMA pipe; the two query tiles' exponentials in turn; the next scores in front of the low parts' products; parts cut off instead of rounded.
+// Bound by the softmax warps and the way weights -> products -> sums -> next weights: at 100 x 40000 the tensor pipe is busy for 53 % of the time.
+// The scores of 32 of a tile's 64 keys stay in registers from the maximum on, the others are read twice: registers hold O (16 more kept: 3 %
+// slower, they spill).  What did not help: sixteen softmax warps, two a row (a barrier that has no limit); a quarter of the exponentials on the FMA
+// pipe; the two query tiles' exponentials in turn; the next scores in front of the low parts' products; parts cut off instead of rounded.
 // One issuing warp for both query tiles was a quarter slower.
 // A short call waits for its instructions, first keys and the parts' way to memory.
 // Two query tiles share every K and V tile; S has two buffers, so that the scores of the next key tile are ready when the weights of this one
